@@ -487,6 +487,143 @@ int lmgc_op_attention_bf16(const uint16_t* d_q, const uint16_t* d_k, const uint1
                            uint16_t* d_o, int32_t B, int32_t Hq, int32_t Hkv, int32_t W,
                            int32_t hd, void* stream);
 
+/* ------------------------------------------- decoder steps in fewer bits */
+/*
+ * Operators of a decoder layer whose weights, activations and key/value cache
+ * are held in 4 and 8 bits.  A step of the decompression reads every weight
+ * and the whole key/value prefix (Sec. 4, "Compression"), so their bytes are
+ * its time.  Not part of lmgc_probs: a prior in fewer bits is another prior,
+ * and both ends of a container have to use the same one.
+ *
+ * Microscaled matrices (OCP Microscaling Formats).  Blocks of 32 consecutive
+ * columns of a row share a scale s = 2^(byte - 127); a value is s times an
+ * e4m3 (LMGC_MX_FP8, one byte) or e2m1 (LMGC_MX_FP4, two to a byte, the first
+ * in the low half) number.  The scale is the smallest power of two, 2^-127 at
+ * least, with |v| <= 448 s (6 s) for every v of the block, so nothing
+ * saturates; codes are v / s rounded to nearest even.  A block that holds a
+ * NaN or an infinity gets the scale byte 255 and reads as NaN as a whole.
+ * Rows layout: with Kp = cols rounded up to 128, codes [rows, Kp] bytes
+ * (FP8) or [rows, Kp / 2] (FP4), zero behind the last column; scales [rows,
+ * 16 ceil(cols / 512)] bytes, block j at byte 16 (j / 16) + 4 (j % 4) +
+ * (j % 16) / 4, zero behind the last block.
+ * Blocks layout (FP4 weights, rows rounded up to 16): the 32 columns
+ * 128 k + 32 g .. of row n are the 16 bytes at 1024 ((n / 16) (Kp / 128) + k)
+ * + 16 (n % 16 + 16 g); the scale word (4 bytes: columns 512 u + 128 i + 32 g
+ * .., i = 0..3) of row n is at 256 ((n / 16) ceil(cols / 512) + u) +
+ * 4 (n % 16 + 16 g).  Rows behind the last are zero.
+ * All buffers: device memory, 16-byte aligned, fully written by the calls.
+ */
+enum { LMGC_MX_FP8 = 0, LMGC_MX_FP4 = 1 };
+
+/* Bytes of codes and of scales of a matrix in the rows layout, and in the
+ * blocks layout (FP4); < 0: EINVAL (rows in [0, 2^31 - 1], cols in [1, 2^20]). */
+int64_t lmgc_mx_code_bytes(int32_t fmt, int64_t rows, int64_t cols);
+int64_t lmgc_mx_scale_bytes(int64_t rows, int64_t cols);
+int64_t lmgc_mx_block_code_bytes(int64_t rows, int64_t cols);
+int64_t lmgc_mx_block_scale_bytes(int64_t rows, int64_t cols);
+
+/*
+ * Quantise d_src [rows, cols] (dtype LMGC_DTYPE_F32 or _BF16, rows `ld`
+ * elements apart, any alignment of its elements) into the rows layout.
+ * GPU, async.  Errors: EINVAL.
+ */
+int lmgc_op_mx_quantize(const void* d_src, int32_t dtype, int64_t rows, int64_t cols, int64_t ld,
+                        int32_t fmt, uint8_t* d_codes, uint8_t* d_scales, void* stream);
+/* The values of a matrix in the rows layout as dtype [rows, cols], rows `ld`
+ * elements apart (float32: exact; bf16: rounded where its exponent ends).
+ * GPU, async.  Errors: EINVAL. */
+int lmgc_op_mx_dequantize(const uint8_t* d_codes, const uint8_t* d_scales, int32_t fmt,
+                          int64_t rows, int64_t cols, void* d_out, int32_t dtype, int64_t ld,
+                          void* stream);
+/* FP4 weights [N, K] from the rows layout into the blocks layout (once, when
+ * they are loaded; no in-place).  GPU, async.  Errors: EINVAL. */
+int lmgc_op_mx_block(const uint8_t* d_codes, const uint8_t* d_scales, int64_t N, int64_t K,
+                     uint8_t* d_block_codes, uint8_t* d_block_scales, void* stream);
+
+/*
+ * Residual add and RMSNorm with a microscaled output, the operand of the next
+ * product: t = h + x (rounded to h's type), d_out = t, y = t / sqrt(mean(t^2)
+ * + eps) * gain in float32, and y [M, d] quantised into the rows layout.
+ *   d_h [M, d] (h_dtype), d_x [M, d] (x_dtype; NULL: t = h), d_gain [d]
+ *   (g_dtype), d_out [M, d] of h_dtype: NULL, d_h itself, or a buffer that
+ *   overlaps nothing.  d % 32 == 0, d <= 16384, 0 <= M <= 2^31 - 1.
+ * Row m depends on row m alone.  GPU, async.  Errors: EINVAL, EUNSUPPORTED.
+ */
+int lmgc_op_add_norm_mx(const void* d_h, int32_t h_dtype, const void* d_x, int32_t x_dtype,
+                        const void* d_gain, int32_t g_dtype, float eps, int64_t M, int64_t d,
+                        int32_t fmt, void* d_out, uint8_t* d_codes, uint8_t* d_scales,
+                        void* stream);
+
+/*
+ * C[M, N] = A[M, K] B[N, K]^T + add with microscaled operands: A (a_fmt, rows
+ * layout: activations), B (FP4, blocks layout: weights).
+ *   kind LMGC_OP_STORE: C float32; LMGC_OP_STORE_BF16: C bf16.
+ *   d_add: float32 [M, N] or NULL; may be d_out where that is float32 (the
+ *   residual add of lmgc_op_gemm_bf16_blocked).
+ * Each element is one chain over rising k of the scaled 16x16x128 matrix
+ * instruction, so a row of C is a bitwise function of that row of A, of add
+ * and of B, not of M.  FP4 x FP4 sums as float32 sums; with FP8 in A the
+ * instruction drops product bits some 2^-18 below a step's largest (about
+ * 5e-6 of the result on normal data).
+ * 0 <= M <= 2^26, 0 < N, K <= 2^20.  GPU, async.  Errors: EINVAL.
+ */
+enum { LMGC_OP_STORE_BF16 = 3 };
+int lmgc_op_gemm_mx(const uint8_t* d_a, const uint8_t* d_a_scales, int32_t a_fmt,
+                    const uint8_t* d_b, const uint8_t* d_b_scales, const float* d_add, void* d_out,
+                    int32_t M, int32_t N, int32_t K, int32_t kind, void* stream);
+
+/*
+ * Key/value cache of one layer in 8 bits: B sequences, Hkv heads of hd (64 or
+ * 128) dims, `cap` tokens (a multiple of 64) each.  Blocks of 64 tokens of a
+ * head are e4m3 codes with one float32 scale, a power of two:
+ *   d_kc, d_vc: [B, Hkv, cap / 64, 64 hd] bytes; in a block key (t, d) is at
+ *     ((t/16) (hd/64) + d/64) 1024 + ((t%16) + 16 ((d%64)/16)) 16 + d%16 and
+ *     value (t, d) at (d/16) 1024 + ((d%16) + 16 ((t%16)/4)) 16 + 4 (t/16) + t%4
+ *   d_ks, d_vs: [B, Hkv, cap / 64] float32.
+ * Appending stores the T new tokens of each sequence at positions lens[b] ..;
+ * d_lens [B] (tokens there before) and d_counts [B] (how many of the T rows
+ * are tokens; NULL: T) are device memory, read when the call runs.  Rows t >=
+ * counts[b], and rows that pass cap, are left out; a sequence with lens[b]
+ * outside [0, cap) has none.  k, v: bf16 [B, Hkv, T, hd].
+ * A block's scale is the smallest power of two >= 2^-64 with |v| <= 448 scale
+ * over the tokens of the call, or the one it had if that is larger (and
+ * lens[b] lies inside the block: then it holds earlier tokens, whose codes
+ * are divided, and rounded again, when the scale grows).  A block that gets
+ * its first token is cleared behind the new ones.  A NaN or an infinity makes
+ * the block's scale NaN, until the block is begun anew.  So appending token by
+ * token and all at once differ at most by a second rounding of values that
+ * fall among the subnormals of the final scale.
+ * All pointers 16-byte aligned.  GPU, async; no workspace.  Errors: EINVAL,
+ * EUNSUPPORTED (hd).
+ */
+int lmgc_op_kv8_append(const uint16_t* d_k, const uint16_t* d_v, int32_t B, int32_t Hkv, int32_t T,
+                       int32_t hd, int32_t cap, const int32_t* d_lens, const int32_t* d_counts,
+                       uint8_t* d_kc, float* d_ks, uint8_t* d_vc, float* d_vs, void* stream);
+
+/*
+ * Attention of the T tokens just appended (same lens, counts: query t of
+ * sequence b is at position lens[b] + t) over the cache: softmax(q.k /
+ * sqrt(hd)) v over keys j <= position and, if window > 0, j > position -
+ * window or j < sinks (the sliding window with first tokens that stay
+ * visible).  Query head h reads key/value head h Hkv / Hq.  Every query sees
+ * at least itself.
+ *   d_q: bf16 [B, Hq, T, hd]; d_out: bf16 [B T, Hq hd]; the rows that hold no
+ *   token (as above) are left as they were.  window >= 0 (0: none), sinks >= 0.
+ *   d_ws: lmgc_kv8_workspace bytes, 16-byte aligned, its contents free; calls
+ *   that may run at the same time need one each.
+ * Masked keys count for nothing, whatever their block holds; a visible key of
+ * a block with a NaN scale gives NaN.  A query's result depends on the cache,
+ * on its position and on whether T Hq / Hkv <= 16, not on the other sequences
+ * or queries.
+ * GPU, async.  Errors: EINVAL, ESIZE, EUNSUPPORTED (hd).
+ */
+int64_t lmgc_kv8_workspace(int32_t B, int32_t Hq, int32_t Hkv, int32_t T, int32_t hd, int32_t cap);
+int lmgc_op_attention_kv8(const uint16_t* d_q, int32_t B, int32_t Hq, int32_t Hkv, int32_t T,
+                          int32_t hd, int32_t cap, const int32_t* d_lens, const int32_t* d_counts,
+                          const uint8_t* d_kc, const float* d_ks, const uint8_t* d_vc,
+                          const float* d_vs, int32_t window, int32_t sinks, uint16_t* d_out,
+                          void* d_ws, size_t ws_bytes, void* stream);
+
 /* ------------------------------------------------------------------ timing */
 /*
  * Per-kernel timing with HIP events recorded around each launch lmgc_probs

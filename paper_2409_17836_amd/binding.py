@@ -107,6 +107,20 @@ def lib():
         "lmgc_op_gemm_f32": (ctypes.c_int, [vp, vp, vp, i32, i32, i32, vp]),
         "lmgc_op_block_weights": (ctypes.c_int, [vp, vp, i32, i32, vp]),
         "lmgc_op_attention_bf16": (ctypes.c_int, [vp, vp, vp, vp, i32, i32, i32, i32, i32, vp]),
+        "lmgc_mx_code_bytes": (i64, [i32, i64, i64]),
+        "lmgc_mx_scale_bytes": (i64, [i64, i64]),
+        "lmgc_mx_block_code_bytes": (i64, [i64, i64]),
+        "lmgc_mx_block_scale_bytes": (i64, [i64, i64]),
+        "lmgc_op_mx_quantize": (ctypes.c_int, [vp, i32, i64, i64, i64, i32, vp, vp, vp]),
+        "lmgc_op_mx_dequantize": (ctypes.c_int, [vp, vp, i32, i64, i64, vp, i32, i64, vp]),
+        "lmgc_op_mx_block": (ctypes.c_int, [vp, vp, i64, i64, vp, vp, vp]),
+        "lmgc_op_add_norm_mx": (ctypes.c_int, [vp, i32, vp, i32, vp, i32, ctypes.c_float, i64, i64, i32,
+                                               vp, vp, vp, vp]),
+        "lmgc_op_gemm_mx": (ctypes.c_int, [vp, vp, i32, vp, vp, vp, vp, i32, i32, i32, i32, vp]),
+        "lmgc_op_kv8_append": (ctypes.c_int, [vp, vp, i32, i32, i32, i32, i32, vp, vp, vp, vp, vp, vp, vp]),
+        "lmgc_kv8_workspace": (i64, [i32, i32, i32, i32, i32, i32]),
+        "lmgc_op_attention_kv8": (ctypes.c_int, [vp, i32, i32, i32, i32, i32, i32, vp, vp, vp, vp, vp, vp,
+                                                 i32, i32, vp, vp, sz, vp]),
         "lmgc_timing_enable": (ctypes.c_int, [i32]),
         "lmgc_timing_kinds": (ctypes.c_int, [u32]),
         "lmgc_timing_read": (ctypes.c_int, [i32, P(ctypes.c_double), P(i64)]),
@@ -547,6 +561,187 @@ def op_attention_bf16(q, k, vt, o=None, stream=None):
     _check(lib().lmgc_op_attention_bf16(_ptr(q), _ptr(k), _ptr(vt), _ptr(o), B, Hq, Hkv, W, hd,
                                         _stream(stream)))
     return o
+
+
+# ------------------------------------------- decoder steps in fewer bits --
+MX_FORMATS = {"fp8": 0, "fp4": 1}
+
+
+def _size(n: int) -> int:
+    if n < 0:
+        _check(n)
+    return int(n)
+
+
+def _dtype(t) -> int:
+    """LMGC_DTYPE_* of a float32 or bfloat16 tensor."""
+    import torch
+    assert t.dtype in (torch.float32, torch.bfloat16), t.dtype
+    return 1 if t.dtype == torch.bfloat16 else 0
+
+
+def _mx_empty(rows, cols, fmt, codes, scales, device):
+    """Code and scale tensors of the rows layout: uint8 [rows, bytes of a row]."""
+    import torch
+    L, f = lib(), MX_FORMATS[fmt]
+    nc, ns = _size(L.lmgc_mx_code_bytes(f, 1, cols)), _size(L.lmgc_mx_scale_bytes(1, cols))
+    if codes is None:
+        codes = torch.empty((rows, nc), dtype=torch.uint8, device=device)
+    if scales is None:
+        scales = torch.empty((rows, ns), dtype=torch.uint8, device=device)
+    _mx_check(codes, scales, rows, cols, fmt)
+    return codes, scales
+
+
+def _mx_check(codes, scales, rows, cols, fmt):
+    import torch
+    L, f = lib(), MX_FORMATS[fmt]
+    assert codes.dtype == torch.uint8 and codes.is_contiguous()
+    assert scales.dtype == torch.uint8 and scales.is_contiguous()
+    assert codes.numel() == _size(L.lmgc_mx_code_bytes(f, rows, cols)), (tuple(codes.shape), rows, cols, fmt)
+    assert scales.numel() == _size(L.lmgc_mx_scale_bytes(rows, cols)), (tuple(scales.shape), rows, cols)
+
+
+def op_mx_quantize(x, fmt: str, codes=None, scales=None, stream=None):
+    """x [rows, cols] float32 or bf16 CUDA tensor (rows may be strided) ->
+    (codes uint8 [rows, Kp or Kp / 2], scales uint8 [rows, 16 ceil(cols / 512)]),
+    fmt "fp8" (e4m3) or "fp4" (e2m1)."""
+    rows, cols = x.shape
+    assert cols == 1 or x.stride(1) == 1
+    codes, scales = _mx_empty(rows, cols, fmt, codes, scales, x.device)
+    ld = x.stride(0) if rows > 1 else cols
+    _check(lib().lmgc_op_mx_quantize(_ptr(x), _dtype(x), rows, cols, ld, MX_FORMATS[fmt], _ptr(codes),
+                                     _ptr(scales), _stream(stream)))
+    return codes, scales
+
+
+def op_mx_dequantize(codes, scales, fmt: str, cols: int, dtype=None, out=None, stream=None):
+    """The values of a microscaled matrix: float32 (or dtype=torch.bfloat16) [rows, cols]."""
+    import torch
+    rows = codes.shape[0]
+    _mx_check(codes, scales, rows, cols, fmt)
+    if out is None:
+        out = torch.empty((rows, cols), dtype=dtype or torch.float32, device=codes.device)
+    assert tuple(out.shape) == (rows, cols) and (cols == 1 or out.stride(1) == 1)
+    ld = out.stride(0) if rows > 1 else cols
+    _check(lib().lmgc_op_mx_dequantize(_ptr(codes), _ptr(scales), MX_FORMATS[fmt], rows, cols, _ptr(out),
+                                       _dtype(out), ld, _stream(stream)))
+    return out
+
+
+def op_mx_block(codes, scales, cols: int, stream=None):
+    """4-bit weights from the rows layout -> (codes, scales) in blocks, flat uint8."""
+    import torch
+    rows = codes.shape[0]
+    _mx_check(codes, scales, rows, cols, "fp4")
+    bc = torch.empty(_size(lib().lmgc_mx_block_code_bytes(rows, cols)), dtype=torch.uint8, device=codes.device)
+    bs = torch.empty(_size(lib().lmgc_mx_block_scale_bytes(rows, cols)), dtype=torch.uint8, device=codes.device)
+    _check(lib().lmgc_op_mx_block(_ptr(codes), _ptr(scales), rows, cols, _ptr(bc), _ptr(bs), _stream(stream)))
+    return bc, bs
+
+
+def op_add_norm_mx(h, x, gain, eps: float, fmt: str, out=None, codes=None, scales=None, stream=None):
+    """t = h + x (x may be None), RMSNorm of t times gain, microscaled: h and x
+    [M, d] float32 or bf16 -> (codes, scales); t goes to `out` (h itself: in
+    place; None: not stored)."""
+    M, d = h.shape
+    assert h.is_contiguous() and gain.is_contiguous() and gain.numel() == d
+    assert x is None or (x.is_contiguous() and tuple(x.shape) == (M, d))
+    assert out is None or (out.is_contiguous() and tuple(out.shape) == (M, d) and out.dtype == h.dtype)
+    codes, scales = _mx_empty(M, d, fmt, codes, scales, h.device)
+    _check(lib().lmgc_op_add_norm_mx(_ptr(h), _dtype(h), _ptr(x), _dtype(x) if x is not None else 0, _ptr(gain),
+                                     _dtype(gain), float(eps), M, d, MX_FORMATS[fmt], _ptr(out), _ptr(codes),
+                                     _ptr(scales), _stream(stream)))
+    return codes, scales
+
+
+MX_KINDS = {"store": 0, "bf16": 3}
+
+
+def op_gemm_mx(a, a_scales, a_fmt: str, b, b_scales, N: int, K: int, kind: str = "store", add=None, out=None,
+               stream=None):
+    """a (rows layout, "fp8" or "fp4") times the 4-bit weights b [N, K] (blocks
+    layout), transposed -> [M, N] float32 ("store") or bf16 ("bf16"), plus the
+    float32 `add` [M, N] if given (out may be add)."""
+    import torch
+    M = a.shape[0]
+    _mx_check(a, a_scales, M, K, a_fmt)
+    L = lib()
+    assert b.dtype == torch.uint8 and b.is_contiguous() and b.numel() == _size(L.lmgc_mx_block_code_bytes(N, K))
+    assert b_scales.dtype == torch.uint8 and b_scales.is_contiguous()
+    assert b_scales.numel() == _size(L.lmgc_mx_block_scale_bytes(N, K))
+    dt = torch.bfloat16 if kind == "bf16" else torch.float32
+    if out is None:
+        out = torch.empty((M, N), dtype=dt, device=a.device)
+    assert out.dtype == dt and out.is_contiguous() and tuple(out.shape) == (M, N)
+    if add is not None:
+        assert add.dtype == torch.float32 and add.is_contiguous() and tuple(add.shape) == (M, N)
+    _check(L.lmgc_op_gemm_mx(_ptr(a), _ptr(a_scales), MX_FORMATS[a_fmt], _ptr(b), _ptr(b_scales), _ptr(add),
+                             _ptr(out), M, N, K, MX_KINDS[kind], _stream(stream)))
+    return out
+
+
+def kv8_cache(B: int, Hkv: int, cap: int, hd: int, device="cuda"):
+    """An empty 8-bit key/value cache of one layer: (key codes, key scales,
+    value codes, value scales)."""
+    import torch
+    assert cap % 64 == 0
+    return tuple(t for _ in range(2) for t in
+                 (torch.zeros((B, Hkv, cap // 64, 64 * hd), dtype=torch.uint8, device=device),
+                  torch.ones((B, Hkv, cap // 64), dtype=torch.float32, device=device)))
+
+
+def _kv8_check(cache, B, Hkv, hd):
+    import torch
+    kc, ks, vc, vs = cache
+    cap = 64 * kc.shape[2]
+    for c, s in ((kc, ks), (vc, vs)):
+        assert c.dtype == torch.uint8 and c.is_contiguous() and tuple(c.shape) == (B, Hkv, cap // 64, 64 * hd)
+        assert s.dtype == torch.float32 and s.is_contiguous() and tuple(s.shape) == (B, Hkv, cap // 64)
+    return kc, ks, vc, vs, cap
+
+
+def _kv8_lens(lens, counts, B):
+    import torch
+    for t in (lens, counts):
+        assert t is None or (t.dtype == torch.int32 and t.is_contiguous() and t.numel() == B)
+    assert lens is not None
+
+
+def op_kv8_append(cache, k, v, lens, counts=None, stream=None):
+    """Stores k, v (bf16 [B, Hkv, T, hd]) at positions lens[b] .. of each
+    sequence (lens, counts: CUDA int32 [B])."""
+    import torch
+    B, Hkv, T, hd = k.shape
+    kc, ks, vc, vs, cap = _kv8_check(cache, B, Hkv, hd)
+    assert k.dtype == v.dtype == torch.bfloat16 and k.is_contiguous() and v.is_contiguous() and v.shape == k.shape
+    _kv8_lens(lens, counts, B)
+    _check(lib().lmgc_op_kv8_append(_ptr(k), _ptr(v), B, Hkv, T, hd, cap, _ptr(lens), _ptr(counts), _ptr(kc),
+                                    _ptr(ks), _ptr(vc), _ptr(vs), _stream(stream)))
+
+
+def kv8_workspace(B: int, Hq: int, Hkv: int, T: int, hd: int, cap: int) -> int:
+    return _size(lib().lmgc_kv8_workspace(B, Hq, Hkv, T, hd, cap))
+
+
+def op_attention_kv8(q, cache, lens, counts=None, window: int = 0, sinks: int = 0, out=None, ws=None, stream=None):
+    """Attention of the T tokens just appended over the 8-bit cache: q bf16
+    [B, Hq, T, hd] -> bf16 [B T, Hq hd]."""
+    import torch
+    B, Hq, T, hd = q.shape
+    Hkv = cache[0].shape[1]
+    kc, ks, vc, vs, cap = _kv8_check(cache, B, Hkv, hd)
+    assert q.dtype == torch.bfloat16 and q.is_contiguous()
+    _kv8_lens(lens, counts, B)
+    if out is None:
+        out = torch.empty((B * T, Hq * hd), dtype=torch.bfloat16, device=q.device)
+    assert out.dtype == torch.bfloat16 and out.is_contiguous() and out.numel() == q.numel()
+    if ws is None:
+        ws = workspace(kv8_workspace(B, Hq, Hkv, T, hd, cap), q.device)
+    _check(lib().lmgc_op_attention_kv8(_ptr(q), B, Hq, Hkv, T, hd, cap, _ptr(lens), _ptr(counts), _ptr(kc), _ptr(ks),
+                                       _ptr(vc), _ptr(vs), int(window), int(sinks), _ptr(out), _ptr(ws), ws.numel(),
+                                       _stream(stream)))
+    return out
 
 
 # ----------------------------------------------------------------- timing --

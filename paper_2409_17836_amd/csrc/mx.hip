@@ -1,0 +1,253 @@
+// Microscaled operands of the 4- and 8-bit products: quantisation of rows,
+// the way back, the block layout of weights, and the residual add with
+// RMSNorm whose output is microscaled.  All are bound by the bytes they move.
+#include <algorithm>
+
+#include "mx.h"
+
+namespace lmgc {
+namespace {
+
+// ---------------------------------------------------------------- quantise
+// Unit: one row x 512 columns, a wave; lane l takes columns 8 l .. 8 l + 7.
+// VEC: rows are whole 16-byte pieces (base, ld and cols), so a lane reads its
+// columns in one or two loads.
+template <int FMT, typename T, bool VEC>
+__global__ __launch_bounds__(256) void mx_quantize_kernel(const T* __restrict__ src, int64_t rows, int cols, int64_t ld,
+                                                          uint8_t* __restrict__ codes, uint8_t* __restrict__ scales) {
+  const int kcols = (int)mx_cols(cols), ns = (int)mx_row_scales(cols), n512 = ns / 16;
+  const int lane = threadIdx.x & 63;
+  const int64_t units = rows * n512, stride = (int64_t)gridDim.x * 4;
+  for (int64_t u = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6); u < units; u += stride) {
+    const int64_t row = u / n512;
+    const int c = (int)(u - row * n512) * 64 + lane;
+    float v[8] = {};
+    const T* p = src + row * ld + 8 * (int64_t)c;
+    if (VEC) {
+      if (8 * c < cols) load8(p, v);
+    } else {
+#pragma unroll
+      for (int i = 0; i < 8; i++)
+        if (8 * c + i < cols) v[i] = load1(p + i);
+    }
+    mx_store8<FMT>(v, c, kcols, ns, codes + row * (FMT == LMGC_MX_FP8 ? kcols : kcols / 2), scales + row * ns);
+  }
+}
+
+// -------------------------------------------------------------- dequantise
+template <int FMT, typename T>
+__global__ __launch_bounds__(256) void mx_dequantize_kernel(const uint8_t* __restrict__ codes,
+                                                            const uint8_t* __restrict__ scales, int64_t rows, int cols,
+                                                            T* __restrict__ out, int64_t ld) {
+  const int kcols = (int)mx_cols(cols), ns = (int)mx_row_scales(cols), nc = (cols + 7) / 8;
+  const int64_t stride = (int64_t)gridDim.x * 256;
+  for (int64_t t = (int64_t)blockIdx.x * 256 + threadIdx.x; t < rows * nc; t += stride) {
+    const int64_t row = t / nc;
+    const int c = (int)(t - row * nc);
+    const float s = mx_scale(scales[row * ns + mx_scale_pos(c >> 2)]);
+    float v[8];
+    if constexpr (FMT == LMGC_MX_FP8) {
+      const mx_u32x2 w = *reinterpret_cast<const mx_u32x2*>(codes + row * kcols + 8 * c);
+#pragma unroll
+      for (int i = 0; i < 2; i++) {
+        v[4 * i] = __builtin_amdgcn_cvt_f32_fp8((int)w[i], 0);
+        v[4 * i + 1] = __builtin_amdgcn_cvt_f32_fp8((int)w[i], 1);
+        v[4 * i + 2] = __builtin_amdgcn_cvt_f32_fp8((int)w[i], 2);
+        v[4 * i + 3] = __builtin_amdgcn_cvt_f32_fp8((int)w[i], 3);
+      }
+    } else {
+      typedef float f32x2 __attribute__((ext_vector_type(2)));
+      const uint32_t w = *reinterpret_cast<const uint32_t*>(codes + row * (kcols / 2) + 4 * c);
+      const f32x2 a = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, 1.0f, 0), b = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, 1.0f, 1);
+      const f32x2 d = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, 1.0f, 2), e = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, 1.0f, 3);
+      v[0] = a[0], v[1] = a[1], v[2] = b[0], v[3] = b[1], v[4] = d[0], v[5] = d[1], v[6] = e[0], v[7] = e[1];
+    }
+    T* p = out + row * ld + 8 * (int64_t)c;
+#pragma unroll
+    for (int i = 0; i < 8; i++) {
+      if (8 * c + i >= cols) continue;
+      if constexpr (sizeof(T) == 2) p[i] = f32_to_bf16(v[i] * s);
+      else p[i] = v[i] * s;
+    }
+  }
+}
+
+// ------------------------------------------------------------------ blocks
+// Row-major 4-bit codes and scales -> blocks (common.h): thread t moves the
+// 16-byte piece (32 columns of a row) that is piece t of the blocks, and the
+// threads whose piece opens a 512-column group its word of scales.
+__global__ __launch_bounds__(256) void mx_block_kernel(const uint8_t* __restrict__ codes, const uint8_t* __restrict__ scales,
+                                                       int64_t N, int K, uint8_t* __restrict__ bcodes,
+                                                       uint8_t* __restrict__ bscales) {
+  const int nk = (int)(mx_cols(K) / 128), n512 = (int)(mx_row_scales(K) / 16);
+  const int64_t pieces = (N + 15) / 16 * nk * 64, stride = (int64_t)gridDim.x * 256;
+  for (int64_t t = (int64_t)blockIdx.x * 256 + threadIdx.x; t < pieces; t += stride) {
+    const int lane = (int)(t & 63), r = lane & 15, g = lane >> 4;
+    const int64_t blk = t >> 6, grp = blk / nk, n = grp * 16 + r;
+    const int k = (int)(blk - grp * nk);
+    mx_u32x4 v = {};
+    if (n < N) v = *reinterpret_cast<const mx_u32x4*>(codes + n * (nk * 64) + k * 64 + 16 * g);
+    *reinterpret_cast<mx_u32x4*>(bcodes + t * 16) = v;
+    if ((k & 3) == 0) {
+      const int s = k >> 2;
+      uint32_t w = 0;
+      if (n < N) w = *reinterpret_cast<const uint32_t*>(scales + n * (n512 * 16) + s * 16 + 4 * g);
+      *reinterpret_cast<uint32_t*>(bscales + (grp * n512 + s) * 256 + lane * 4) = w;
+    }
+  }
+}
+
+// -------------------------------------------------------- add and RMSNorm
+__device__ inline float wave_sum(float v) {
+#pragma unroll
+  for (int o = 32; o; o >>= 1) v += __shfl_xor(v, o, 64);
+  return v;
+}
+
+__device__ inline void store8(float* p, const float (&v)[8]) {
+  *reinterpret_cast<mx_f32x4*>(p) = mx_f32x4{v[0], v[1], v[2], v[3]};
+  *reinterpret_cast<mx_f32x4*>(p + 4) = mx_f32x4{v[4], v[5], v[6], v[7]};
+}
+__device__ inline void store8(uint16_t* p, const float (&v)[8]) {
+  mx_u32x4 w;
+#pragma unroll
+  for (int i = 0; i < 4; i++) w[i] = (uint32_t)f32_to_bf16(v[2 * i]) | ((uint32_t)f32_to_bf16(v[2 * i + 1]) << 16);
+  *reinterpret_cast<mx_u32x4*>(p) = w;
+}
+
+// A block per row; thread t keeps columns 8 (t + 256 i) .. + 7 in registers
+// between the sum of squares and the codes, so a row is read once.  The sum
+// that is normalised is the one that is stored.
+template <int FMT, typename TH, typename TX, typename TG, int NC>
+__global__ __launch_bounds__(256) void add_norm_mx_kernel(const TH* h, const TX* __restrict__ x,
+                                                          const TG* __restrict__ gain, float eps, int d,
+                                                          TH* out, uint8_t* __restrict__ codes,
+                                                          uint8_t* __restrict__ scales) {
+#pragma clang fp contract(off)
+  __shared__ float part[4];
+  const int64_t row = blockIdx.x;
+  const int t = threadIdx.x, nchunks = d / 8;
+  const int kcols = (int)mx_cols(d), ns = (int)mx_row_scales(d);
+  float v[NC][8];
+  float ss = 0.f;
+#pragma unroll
+  for (int i = 0; i < NC; i++) {
+    const int c = t + 256 * i;
+#pragma unroll
+    for (int e = 0; e < 8; e++) v[i][e] = 0.f;
+    if (c >= nchunks) continue;
+    load8(h + row * d + 8 * c, v[i]);
+    if (x) {
+      float w[8];
+      load8(x + row * d + 8 * c, w);
+#pragma unroll
+      for (int e = 0; e < 8; e++) {
+        v[i][e] += w[e];
+        if constexpr (sizeof(TH) == 2) v[i][e] = bf16_to_f32(f32_to_bf16(v[i][e]));
+      }
+    }
+    if (out) store8(out + row * d + 8 * c, v[i]);
+#pragma unroll
+    for (int e = 0; e < 8; e++) ss += v[i][e] * v[i][e];
+  }
+  ss = wave_sum(ss);
+  if ((t & 63) == 0) part[t >> 6] = ss;
+  __syncthreads();
+  ss = (part[0] + part[1]) + (part[2] + part[3]);
+  const float r = 1.0f / sqrtf(ss / (float)d + eps);
+#pragma unroll
+  for (int i = 0; i < NC; i++) {
+    const int c = t + 256 * i;
+    if (c < nchunks) {
+      float g[8];
+      load8(gain + 8 * c, g);
+#pragma unroll
+      for (int e = 0; e < 8; e++) v[i][e] = v[i][e] * r * g[e];
+    }
+    mx_store8<FMT>(v[i], c, kcols, ns, codes + row * (FMT == LMGC_MX_FP8 ? kcols : kcols / 2), scales + row * ns);
+  }
+}
+
+int grid_of(int64_t blocks) { return (int)std::max<int64_t>(1, std::min<int64_t>(blocks, 1 << 16)); }
+
+template <int FMT, typename T>
+void quantize(const T* src, int64_t rows, int cols, int64_t ld, uint8_t* codes, uint8_t* scales, hipStream_t s) {
+  const bool vec = cols % 8 == 0 && ld * sizeof(T) % 16 == 0 && ((uintptr_t)src & 15) == 0;
+  const int grid = grid_of((rows * (mx_row_scales(cols) / 16) + 3) / 4);
+  if (vec) mx_quantize_kernel<FMT, T, true><<<grid, 256, 0, s>>>(src, rows, cols, ld, codes, scales);
+  else mx_quantize_kernel<FMT, T, false><<<grid, 256, 0, s>>>(src, rows, cols, ld, codes, scales);
+}
+
+template <int FMT, typename TH, typename TX, typename TG>
+void add_norm(const void* h, const void* x, const void* gain, float eps, int64_t M, int d, void* out, uint8_t* codes,
+              uint8_t* scales, hipStream_t s) {
+  const int nc = (int)((mx_row_scales(d) * 4 + 255) / 256);  // 512-column groups, 64 threads each
+  auto go = [&](auto n) {
+    add_norm_mx_kernel<FMT, TH, TX, TG, decltype(n)::value><<<(unsigned)M, 256, 0, s>>>(
+        (const TH*)h, (const TX*)x, (const TG*)gain, eps, d, (TH*)out, codes, scales);
+  };
+  if (nc <= 1) go(std::integral_constant<int, 1>{});
+  else if (nc <= 2) go(std::integral_constant<int, 2>{});
+  else if (nc <= 4) go(std::integral_constant<int, 4>{});
+  else go(std::integral_constant<int, 8>{});
+}
+
+}  // namespace
+
+hipError_t launch_mx_quantize(const void* src, int dtype, int64_t rows, int cols, int64_t ld, int fmt, uint8_t* codes,
+                              uint8_t* scales, hipStream_t s) {
+  const bool bf = dtype == LMGC_DTYPE_BF16;
+  if (fmt == LMGC_MX_FP8) {
+    if (bf) quantize<LMGC_MX_FP8>((const uint16_t*)src, rows, cols, ld, codes, scales, s);
+    else quantize<LMGC_MX_FP8>((const float*)src, rows, cols, ld, codes, scales, s);
+  } else {
+    if (bf) quantize<LMGC_MX_FP4>((const uint16_t*)src, rows, cols, ld, codes, scales, s);
+    else quantize<LMGC_MX_FP4>((const float*)src, rows, cols, ld, codes, scales, s);
+  }
+  return hipGetLastError();
+}
+
+hipError_t launch_mx_dequantize(const uint8_t* codes, const uint8_t* scales, int fmt, int64_t rows, int cols, void* out,
+                                int dtype, int64_t ld, hipStream_t s) {
+  const int grid = grid_of((rows * ((cols + 7) / 8) + 255) / 256);
+  auto go = [&](auto f) {
+    constexpr int F = decltype(f)::value;
+    if (dtype == LMGC_DTYPE_BF16) mx_dequantize_kernel<F><<<grid, 256, 0, s>>>(codes, scales, rows, cols, (uint16_t*)out, ld);
+    else mx_dequantize_kernel<F><<<grid, 256, 0, s>>>(codes, scales, rows, cols, (float*)out, ld);
+  };
+  if (fmt == LMGC_MX_FP8) go(std::integral_constant<int, LMGC_MX_FP8>{});
+  else go(std::integral_constant<int, LMGC_MX_FP4>{});
+  return hipGetLastError();
+}
+
+hipError_t launch_mx_block(const uint8_t* codes, const uint8_t* scales, int64_t N, int K, uint8_t* bcodes,
+                           uint8_t* bscales, hipStream_t s) {
+  const int grid = grid_of(((N + 15) / 16 * (mx_cols(K) / 128) * 64 + 255) / 256);
+  mx_block_kernel<<<grid, 256, 0, s>>>(codes, scales, N, K, bcodes, bscales);
+  return hipGetLastError();
+}
+
+hipError_t launch_add_norm_mx(const void* h, int h_dtype, const void* x, int x_dtype, const void* gain, int g_dtype,
+                              float eps, int64_t M, int d, int fmt, void* out, uint8_t* codes, uint8_t* scales,
+                              hipStream_t s) {
+  auto go3 = [&](auto f, auto th, auto tx) {
+    using TH = decltype(th);
+    using TX = decltype(tx);
+    constexpr int F = decltype(f)::value;
+    if (g_dtype == LMGC_DTYPE_BF16) add_norm<F, TH, TX, uint16_t>(h, x, gain, eps, M, d, out, codes, scales, s);
+    else add_norm<F, TH, TX, float>(h, x, gain, eps, M, d, out, codes, scales, s);
+  };
+  auto go2 = [&](auto f, auto th) {
+    if (x_dtype == LMGC_DTYPE_BF16) go3(f, th, uint16_t{});
+    else go3(f, th, float{});
+  };
+  auto go1 = [&](auto f) {
+    if (h_dtype == LMGC_DTYPE_BF16) go2(f, uint16_t{});
+    else go2(f, float{});
+  };
+  if (fmt == LMGC_MX_FP8) go1(std::integral_constant<int, LMGC_MX_FP8>{});
+  else go1(std::integral_constant<int, LMGC_MX_FP4>{});
+  return hipGetLastError();
+}
+
+}  // namespace lmgc
