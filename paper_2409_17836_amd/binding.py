@@ -580,11 +580,34 @@ def _dtype(t) -> int:
     return 1 if t.dtype == torch.bfloat16 else 0
 
 
+def _on(t, stream):
+    """The stream to launch on (the current one unless given): the tensors'
+    device has to be the current device, as for every call of the library."""
+    import torch
+    dev = t.get_device()
+    if dev != torch.cuda.current_device():
+        raise ValueError(f"tensors on device {dev}, the current device is {torch.cuda.current_device()}")
+    return stream.cuda_stream if stream is not None else _raw_stream(dev)
+
+
+def _raw_stream(dev: int) -> int:
+    """The current stream's handle, without building a Stream object (2.6 us)
+    where torch offers that."""
+    import torch
+    get = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+    return get(dev) if get is not None else torch.cuda.current_stream(dev).cuda_stream
+
+
+def _mx_sizes(rows: int, cols: int, fmt: str) -> Tuple[int, int]:
+    """Bytes of a row's codes and scales (lmgc_mx_code_bytes, lmgc_mx_scale_bytes)."""
+    kp = -(-cols // 128) * 128
+    return kp if MX_FORMATS[fmt] == 0 else kp // 2, 16 * -(-cols // 512)
+
+
 def _mx_empty(rows, cols, fmt, codes, scales, device):
     """Code and scale tensors of the rows layout: uint8 [rows, bytes of a row]."""
     import torch
-    L, f = lib(), MX_FORMATS[fmt]
-    nc, ns = _size(L.lmgc_mx_code_bytes(f, 1, cols)), _size(L.lmgc_mx_scale_bytes(1, cols))
+    nc, ns = _mx_sizes(rows, cols, fmt)
     if codes is None:
         codes = torch.empty((rows, nc), dtype=torch.uint8, device=device)
     if scales is None:
@@ -595,11 +618,9 @@ def _mx_empty(rows, cols, fmt, codes, scales, device):
 
 def _mx_check(codes, scales, rows, cols, fmt):
     import torch
-    L, f = lib(), MX_FORMATS[fmt]
-    assert codes.dtype == torch.uint8 and codes.is_contiguous()
-    assert scales.dtype == torch.uint8 and scales.is_contiguous()
-    assert codes.numel() == _size(L.lmgc_mx_code_bytes(f, rows, cols)), (tuple(codes.shape), rows, cols, fmt)
-    assert scales.numel() == _size(L.lmgc_mx_scale_bytes(rows, cols)), (tuple(scales.shape), rows, cols)
+    nc, ns = _mx_sizes(rows, cols, fmt)
+    assert codes.dtype == torch.uint8 and codes.is_contiguous() and codes.numel() == rows * nc, (tuple(codes.shape), rows, cols, fmt)
+    assert scales.dtype == torch.uint8 and scales.is_contiguous() and scales.numel() == rows * ns, (tuple(scales.shape), rows, cols)
 
 
 def op_mx_quantize(x, fmt: str, codes=None, scales=None, stream=None):
@@ -611,7 +632,7 @@ def op_mx_quantize(x, fmt: str, codes=None, scales=None, stream=None):
     codes, scales = _mx_empty(rows, cols, fmt, codes, scales, x.device)
     ld = x.stride(0) if rows > 1 else cols
     _check(lib().lmgc_op_mx_quantize(_ptr(x), _dtype(x), rows, cols, ld, MX_FORMATS[fmt], _ptr(codes),
-                                     _ptr(scales), _stream(stream)))
+                                     _ptr(scales), _on(x, stream)))
     return codes, scales
 
 
@@ -625,7 +646,7 @@ def op_mx_dequantize(codes, scales, fmt: str, cols: int, dtype=None, out=None, s
     assert tuple(out.shape) == (rows, cols) and (cols == 1 or out.stride(1) == 1)
     ld = out.stride(0) if rows > 1 else cols
     _check(lib().lmgc_op_mx_dequantize(_ptr(codes), _ptr(scales), MX_FORMATS[fmt], rows, cols, _ptr(out),
-                                       _dtype(out), ld, _stream(stream)))
+                                       _dtype(out), ld, _on(codes, stream)))
     return out
 
 
@@ -636,7 +657,7 @@ def op_mx_block(codes, scales, cols: int, stream=None):
     _mx_check(codes, scales, rows, cols, "fp4")
     bc = torch.empty(_size(lib().lmgc_mx_block_code_bytes(rows, cols)), dtype=torch.uint8, device=codes.device)
     bs = torch.empty(_size(lib().lmgc_mx_block_scale_bytes(rows, cols)), dtype=torch.uint8, device=codes.device)
-    _check(lib().lmgc_op_mx_block(_ptr(codes), _ptr(scales), rows, cols, _ptr(bc), _ptr(bs), _stream(stream)))
+    _check(lib().lmgc_op_mx_block(_ptr(codes), _ptr(scales), rows, cols, _ptr(bc), _ptr(bs), _on(codes, stream)))
     return bc, bs
 
 
@@ -651,7 +672,7 @@ def op_add_norm_mx(h, x, gain, eps: float, fmt: str, out=None, codes=None, scale
     codes, scales = _mx_empty(M, d, fmt, codes, scales, h.device)
     _check(lib().lmgc_op_add_norm_mx(_ptr(h), _dtype(h), _ptr(x), _dtype(x) if x is not None else 0, _ptr(gain),
                                      _dtype(gain), float(eps), M, d, MX_FORMATS[fmt], _ptr(out), _ptr(codes),
-                                     _ptr(scales), _stream(stream)))
+                                     _ptr(scales), _on(h, stream)))
     return codes, scales
 
 
@@ -667,9 +688,10 @@ def op_gemm_mx(a, a_scales, a_fmt: str, b, b_scales, N: int, K: int, kind: str =
     M = a.shape[0]
     _mx_check(a, a_scales, M, K, a_fmt)
     L = lib()
-    assert b.dtype == torch.uint8 and b.is_contiguous() and b.numel() == _size(L.lmgc_mx_block_code_bytes(N, K))
-    assert b_scales.dtype == torch.uint8 and b_scales.is_contiguous()
-    assert b_scales.numel() == _size(L.lmgc_mx_block_scale_bytes(N, K))
+    nc, ns = _mx_sizes(N, K, "fp4")
+    n16 = -(-N // 16) * 16
+    assert b.dtype == torch.uint8 and b.is_contiguous() and b.numel() == n16 * nc
+    assert b_scales.dtype == torch.uint8 and b_scales.is_contiguous() and b_scales.numel() == n16 * ns
     dt = torch.bfloat16 if kind == "bf16" else torch.float32
     if out is None:
         out = torch.empty((M, N), dtype=dt, device=a.device)
@@ -677,7 +699,7 @@ def op_gemm_mx(a, a_scales, a_fmt: str, b, b_scales, N: int, K: int, kind: str =
     if add is not None:
         assert add.dtype == torch.float32 and add.is_contiguous() and tuple(add.shape) == (M, N)
     _check(L.lmgc_op_gemm_mx(_ptr(a), _ptr(a_scales), MX_FORMATS[a_fmt], _ptr(b), _ptr(b_scales), _ptr(add),
-                             _ptr(out), M, N, K, MX_KINDS[kind], _stream(stream)))
+                             _ptr(out), M, N, K, MX_KINDS[kind], _on(a, stream)))
     return out
 
 
@@ -717,7 +739,7 @@ def op_kv8_append(cache, k, v, lens, counts=None, stream=None):
     assert k.dtype == v.dtype == torch.bfloat16 and k.is_contiguous() and v.is_contiguous() and v.shape == k.shape
     _kv8_lens(lens, counts, B)
     _check(lib().lmgc_op_kv8_append(_ptr(k), _ptr(v), B, Hkv, T, hd, cap, _ptr(lens), _ptr(counts), _ptr(kc),
-                                    _ptr(ks), _ptr(vc), _ptr(vs), _stream(stream)))
+                                    _ptr(ks), _ptr(vc), _ptr(vs), _on(k, stream)))
 
 
 def kv8_workspace(B: int, Hq: int, Hkv: int, T: int, hd: int, cap: int) -> int:
@@ -740,7 +762,7 @@ def op_attention_kv8(q, cache, lens, counts=None, window: int = 0, sinks: int = 
         ws = workspace(kv8_workspace(B, Hq, Hkv, T, hd, cap), q.device)
     _check(lib().lmgc_op_attention_kv8(_ptr(q), B, Hq, Hkv, T, hd, cap, _ptr(lens), _ptr(counts), _ptr(kc), _ptr(ks),
                                        _ptr(vc), _ptr(vs), int(window), int(sinks), _ptr(out), _ptr(ws), ws.numel(),
-                                       _stream(stream)))
+                                       _on(q, stream)))
     return out
 
 

@@ -198,7 +198,8 @@ int lmgc_op_kv8_append(const uint16_t* d_k, const uint16_t* d_v, int32_t B, int3
 
 int64_t lmgc_kv8_workspace(int32_t B, int32_t Hq, int32_t Hkv, int32_t T, int32_t hd, int32_t cap) {
   clear_error();
-  if (B <= 0 || B > 16383 || Hkv <= 0 || Hq <= 0 || Hq > 65535 || Hq % Hkv || T <= 0 || T > (1 << 24) || cap <= 0 || cap > (1 << 24) || cap % 64)
+  if (B <= 0 || B > 16383 || Hkv <= 0 || Hq <= 0 || Hq > 65535 || Hq % Hkv || T <= 0 || T > (1 << 24) || cap <= 0 || cap > (1 << 24) || cap % 64 ||
+      (int64_t)T * (Hq / Hkv) > (1 << 30))
     return set_error(LMGC_EINVAL, "bad sizes");
   if (hd != 64 && hd != 128) return set_error(LMGC_EUNSUPPORTED, "need hd in {64, 128}");
   return kv8_workspace_bytes(B, Hq, Hkv, T, hd, cap);
@@ -212,6 +213,7 @@ int lmgc_op_attention_kv8(const uint16_t* d_q, int32_t B, int32_t Hq, int32_t Hk
   int rc = check_cache(B, Hkv, T, hd, cap, d_lens, d_kc, d_ks, d_vc, d_vs);
   if (rc) return rc;
   if (Hq <= 0 || Hq > 65535 || Hq % Hkv) return set_error(LMGC_EINVAL, "Hq must be a positive multiple of Hkv");
+  if ((int64_t)T * (Hq / Hkv) > (1 << 30)) return set_error(LMGC_EINVAL, "T Hq / Hkv above 2^30");
   if (window < 0 || sinks < 0) return set_error(LMGC_EINVAL, "window and sinks must be >= 0");
   if (!d_q || !d_out) return set_error(LMGC_EINVAL, "NULL device buffer");
   if (!aligned(d_q) || !aligned(d_out) || !aligned(d_ws) || ((uintptr_t)d_counts & 3))

@@ -7,6 +7,7 @@
 // whatever M, N and the tile, so a row's result depends on that row of A and
 // on B alone.
 #include <algorithm>
+#include <type_traits>
 
 #include "mx.h"
 
@@ -20,92 +21,422 @@ typedef float f32x4 __attribute__((ext_vector_type(4)));
 // Lane l = r + 16 g of the instruction: e2m1 operands: columns 32 g .. + 31
 // of row r; e4m3 operands: columns 16 g .. + 15 and 64 + 16 g .. + 15.  In
 // both the lane gives the scale of columns 32 g .. + 31.
-template <int FMT>
-__device__ inline i32x8 load_a(const uint8_t* row, int k, int g) {
-  i32x8 a = {};
-  if constexpr (FMT == LMGC_MX_FP8) {
-    const i32x4 lo = *reinterpret_cast<const i32x4*>(row + (int64_t)k * 128 + 16 * g);
-    const i32x4 hi = *reinterpret_cast<const i32x4*>(row + (int64_t)k * 128 + 64 + 16 * g);
+//
+// weights x activations: element e of the result is column 4 g + e of the
+// block, row r; KS: the stage's byte of the scale words
+template <int FMT, int KS>
+__device__ inline f32x4 mma(const i32x4& w4, const i32x8& a, f32x4 c, uint32_t sw, uint32_t sa) {
+  constexpr int blgp = FMT == LMGC_MX_FP8 ? 0 : 4;
+  const i32x8 w = {w4[0], w4[1], w4[2], w4[3], 0, 0, 0, 0};
+  return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(w, a, c, 4, blgp, KS, (int)sw, KS, (int)sa);
+}
+
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+typedef __attribute__((address_space(3))) char* lds_bytes_t;
+
+constexpr int kXcds = 8;
+
+// Two floats -> a packed bf16 pair, round to nearest even.
+__device__ inline uint32_t pack_bf16(float a, float b) {
+  typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+  const bf16x2 v = {(__bf16)a, (__bf16)b};
+  return __builtin_bit_cast(uint32_t, v);
+}
+
+// s_waitcnt vmcnt(n) alone (vmcnt bits 3:0 and 15:14)
+constexpr int vmcnt_imm(int n) { return (n & 15) | ((n >> 4) << 14) | 0xF70; }
+// mask that adds lgkmcnt(0) to it
+constexpr int kLgkm0 = 0xF0FF;
+
+// Buffer resource over `bytes` bytes at p (gfx9: stride 0, word 3
+// 0x00020000); a lane offset at or past them loads zero.  The scalar offset
+// is not part of that check.
+__device__ inline __amdgpu_buffer_rsrc_t buffer_of(const uint8_t* p, int bytes) {
+  return __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t*>(p), (short)0, bytes, 0x00020000);
+}
+
+// 16 bytes a lane from the buffer straight to LDS: lane l's piece lands at
+// lds + 16 l.
+__device__ inline void load_lds(__amdgpu_buffer_rsrc_t rsrc, lds_bytes_t lds, int voff, int soff) {
+  __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, (__attribute__((address_space(3))) void*)lds, 16, voff, soff, 0, 0);
+}
+
+// Rows of COLS float32 values in LDS (COLS + 4 apart) to the output: `rows`
+// rows of `nc` columns from element `at` on, N apart.
+template <int COLS>
+__device__ inline void store_rows(const float* src, int64_t at, int rows, int nc, int N, int lane, const float* add, void* out,
+                                  int bf16) {
+  constexpr int RS = COLS + 4;
+  if (bf16) {
+    constexpr int PER = 8, LPR = COLS / PER, RPI = 64 / LPR < 16 ? 64 / LPR : 16;  // values a lane, lanes a row, rows at once
+    const bool vec = (N & 7) == 0;
 #pragma unroll
-    for (int i = 0; i < 4; i++) {
-      a[i] = lo[i];
-      a[4 + i] = hi[i];
+    for (int q = 0; q < 16 / RPI; q++) {
+      const int row = q * RPI + lane / LPR, c = lane % LPR * PER;
+      if (row >= rows || c >= nc) continue;
+      f32x4 v[2] = {*reinterpret_cast<const f32x4*>(src + row * RS + c), *reinterpret_cast<const f32x4*>(src + row * RS + c + 4)};
+      const int64_t p = at + (int64_t)row * N + c;
+      if (vec) {
+        if (add) {
+          v[0] += *reinterpret_cast<const f32x4*>(add + p);
+          v[1] += *reinterpret_cast<const f32x4*>(add + p + 4);
+        }
+        const u32x4 w = {pack_bf16(v[0][0], v[0][1]), pack_bf16(v[0][2], v[0][3]), pack_bf16(v[1][0], v[1][1]),
+                         pack_bf16(v[1][2], v[1][3])};
+        *reinterpret_cast<u32x4*>((uint16_t*)out + p) = w;
+      } else {
+#pragma unroll
+        for (int e = 0; e < 8; e++)
+          if (c + e < nc) ((uint16_t*)out)[p + e] = f32_to_bf16(add ? v[e >> 2][e & 3] + add[p + e] : v[e >> 2][e & 3]);
+      }
     }
   } else {
-    const i32x4 lo = *reinterpret_cast<const i32x4*>(row + (int64_t)k * 64 + 16 * g);
+    constexpr int PER = 4, LPR = COLS / PER, RPI = 64 / LPR < 16 ? 64 / LPR : 16;
+    const bool vec = (N & 3) == 0;
 #pragma unroll
-    for (int i = 0; i < 4; i++) a[i] = lo[i];
-  }
-  return a;
-}
-
-template <int FMT>
-__device__ inline f32x4 mma(const i32x8& a, const i32x4& b4, f32x4 c, uint32_t sa, uint32_t sb) {
-  constexpr int cbsz = FMT == LMGC_MX_FP8 ? 0 : 4;
-  const i32x8 b = {b4[0], b4[1], b4[2], b4[3], 0, 0, 0, 0};
-  return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, b, c, cbsz, 4, 0, (int)sa, 0, (int)sb);
-}
-
-// A wave per 32 x 32 outputs, operands straight from memory.
-template <int FMT>
-__global__ __launch_bounds__(64) void gemm_mx_kernel(const uint8_t* __restrict__ A, const uint8_t* __restrict__ As,
-                                                     const uint8_t* __restrict__ B, const uint8_t* __restrict__ Bs,
-                                                     int M, int N, int K, const float* add, void* out, int bf16) {
-  const int lane = threadIdx.x, r = lane & 15, g = lane >> 4;
-  const int nk = (int)(mx_cols(K) / 128), ns = (int)mx_row_scales(K);
-  const int64_t lda = FMT == LMGC_MX_FP8 ? (int64_t)nk * 128 : (int64_t)nk * 64;
-  const int64_t m0 = (int64_t)blockIdx.y * 32;
-  const int n0 = blockIdx.x * 32, groups = (N + 15) / 16;
-  const uint8_t *pa[2], *psa[2], *pb[2], *psb[2];
+    for (int q = 0; q < 16 / RPI; q++) {
+      const int row = q * RPI + lane / LPR, c = lane % LPR * PER;
+      if (row >= rows || c >= nc) continue;
+      f32x4 v = *reinterpret_cast<const f32x4*>(src + row * RS + c);
+      const int64_t p = at + (int64_t)row * N + c;
+      if (vec) {
+        if (add) v += *reinterpret_cast<const f32x4*>(add + p);
+        *reinterpret_cast<f32x4*>((float*)out + p) = v;
+      } else {
 #pragma unroll
-  for (int i = 0; i < 2; i++) {
-    const int64_t m = min<int64_t>(m0 + 16 * i + r, M - 1);
-    pa[i] = A + m * lda;
-    psa[i] = As + m * ns + 4 * g;
-    const int64_t grp = min(n0 / 16 + i, groups - 1);
-    pb[i] = B + grp * nk * 1024 + lane * 16;
-    psb[i] = Bs + grp * (ns / 16) * 256 + lane * 4;
-  }
-  f32x4 acc[2][2] = {};
-  for (int k = 0; k < nk; k++) {
-    i32x8 a[2];
-    i32x4 b[2];
-    uint32_t sa[2], sb[2];
-#pragma unroll
-    for (int i = 0; i < 2; i++) {
-      a[i] = load_a<FMT>(pa[i], k, g);
-      b[i] = *reinterpret_cast<const i32x4*>(pb[i] + (int64_t)k * 1024);
-      sa[i] = *reinterpret_cast<const uint32_t*>(psa[i] + (k >> 2) * 16) >> (8 * (k & 3));
-      sb[i] = *reinterpret_cast<const uint32_t*>(psb[i] + (int64_t)(k >> 2) * 256) >> (8 * (k & 3));
+        for (int e = 0; e < 4; e++)
+          if (c + e < nc) ((float*)out)[p + e] = add ? v[e] + add[p + e] : v[e];
+      }
     }
+  }
+}
+
+// Tiles.  A workgroup of WM x WN waves computes BM x BN outputs, a wave BM /
+// WM x BN / WN of them as 16 x 16 blocks with the weights as the
+// instruction's first operand, so a lane ends up with four neighbouring
+// columns of one row.
+//
+// K advances in stages of 128 bytes of a row of A (one step of 128 columns in
+// e4m3, two in e2m1) through a ring of ST stages in LDS.  A load of A takes 8
+// rows x 128 bytes: whole cache lines (16 rows x 64 bytes, the lanes' own
+// order, moved 37 KB a microsecond and CU where this moves 90 to 117).  Chunk
+// c of row r lies at slot c ^ ((r >> 1) & 7) of its row, so that the 16 rows
+// that one cycle of an LDS read serves fall on 16 different quads of banks.
+// B's 1 KB blocks lie as they are, in the lanes' order.  Scales come in groups
+// of four steps, PS groups ahead, through a ring of their own.
+//
+// Step k: its operands are in registers.  Before the operands of the next
+// stage are read: wait for that stage's loads and for the wave's reads of
+// this one; barrier; load the stage ST further on into this one's place.
+// Then the operands of step k + 1 are read into a second set of registers
+// while step k is multiplied.  Past the last stage the loads go on with an
+// empty buffer: they move nothing, and the counts of loads in flight stay
+// constants.
+template <int FMT, int BM, int BN, int WM, int WN, int ST>
+struct Tile {
+  static constexpr int NW = WM * WN, PA = FMT == LMGC_MX_FP8 ? 2 : 1, KPS = 2 / PA;  // steps per stage
+  static constexpr int G = 4 / KPS;                                                   // stages per group of scales
+  static constexpr int LA = BM / 8, LB = BN / 16 * KPS, L = LA + LB;                  // pieces of a stage
+  static constexpr int LPA = (LA + NW - 1) / NW, LPB = LB / NW, LPW = LPA + LPB;      // loads of a stage, each wave
+  static constexpr int SA = (BM + 63) / 64, SB = (BN + 63) / 64, S = SA + SB;  // pieces of a group's scales
+  // with fewer pieces than waves, some waves load one again, so that all have
+  // the same loads in flight
+  static constexpr int SPA = (SA + NW - 1) / NW, SPB = (SB + NW - 1) / NW, SPW = SPA + SPB;
+  static constexpr int PS = (ST + G - 1) / G;  // the scales of a group are asked for before the operands of its stages
+  static constexpr int FM = BM / WM / 16, FN = BN / WN / 16;
+  static constexpr int kStage = L * 1024, kScale = S * 1024;
+  static constexpr int kLds = ST * kStage + (PS + 1) * kScale;
+  static_assert(LB % NW == 0 && kLds <= 160 * 1024, "stage does not fit");
+  // loads that may be in flight when stage G u + s + 1 is needed: those of
+  // the ST - 2 stages after it, and the scales asked for among them
+  static constexpr int in_flight(int s) {
+    int n = (ST - 2) * LPW;
+    for (int i = s - ST + 2; i <= s - 1; i++)
+      if (((i % G) + G) % G == 0) n += SPW;
+    return n;
+  }
+};
+
+template <int FMT, int BM, int BN, int WM, int WN, int ST>
+__global__ __launch_bounds__(WM * WN * 64, 1) void gemm_mx_tile_kernel(
+    const uint8_t* __restrict__ A, const uint8_t* __restrict__ As, const uint8_t* __restrict__ B,
+    const uint8_t* __restrict__ Bs, int M, int N, int nk, int ns, int ntm, int ntn, int gm, const float* add, void* out,
+    int bf16) {
+  using C = Tile<FMT, BM, BN, WM, WN, ST>;
+  __shared__ u32x4 smem[C::kLds / 16];
+  int tm, tn;
+  {
+    // XCD x (workgroups x, x + 8, ..) walks a contiguous range of the tiles,
+    // in groups of gm row tiles
+    const int per = gridDim.x / kXcds, t = ((int)blockIdx.x % kXcds) * per + (int)blockIdx.x / kXcds;
+    if (t >= ntm * ntn) return;
+    const int grp = t / (gm * ntn), first = grp * gm, gs = min(ntm - first, gm), r = t - grp * gm * ntn;
+    tm = __builtin_amdgcn_readfirstlane(first + r % gs);
+    tn = __builtin_amdgcn_readfirstlane(r / gs);
+  }
+  const int tid = threadIdx.x, lane = tid & 63, r = lane & 15, g = lane >> 4;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), wm = wave / WN, wn = wave % WN;
+  const int64_t m0 = (int64_t)tm * BM;
+  const int n0 = tn * BN, mrows = (int)min<int64_t>(BM, M - m0), groups = min(BN / 16, (N + 15) / 16 - n0 / 16);
+  const int lda = FMT == LMGC_MX_FP8 ? nk * 128 : nk * 64, nst = (nk + C::KPS - 1) / C::KPS;
+  const uint8_t *pa = A + m0 * lda, *psa = As + m0 * ns, *pb = B + (int64_t)(n0 / 16) * nk * 1024,
+                *psb = Bs + (int64_t)(n0 / 16) * ns * 16;
+  const __amdgpu_buffer_rsrc_t rsa = buffer_of(psa, mrows * ns), rsb = buffer_of(psb, groups * ns * 16);
+  const lds_bytes_t lds0 = (lds_bytes_t)(char*)smem;
+
+  // wave w loads pieces w LPA .. of A's part of a stage and w LPB .. of B's,
+  // and so with the scales of a group
+  int va[C::LPA], vb[C::LPB], vsa[C::SPA], vsb[C::SPB];
 #pragma unroll
-    for (int i = 0; i < 2; i++)
-#pragma unroll
-      for (int j = 0; j < 2; j++) acc[i][j] = mma<FMT>(a[i], b[j], acc[i][j], sa[i], sb[j]);
+  for (int i = 0; i < C::LPA; i++) {
+    const int row = min(wave * C::LPA + i, C::LA - 1) * 8 + (lane >> 3);
+    va[i] = row * lda + (((lane & 7) ^ ((row >> 1) & 7)) << 4);
   }
 #pragma unroll
-  for (int i = 0; i < 2; i++)
+  for (int i = 0; i < C::LPB; i++) {
+    const int q = wave * C::LPB + i;
+    vb[i] = (q / C::KPS * nk + q % C::KPS) * 1024 + lane * 16;
+  }
 #pragma unroll
-    for (int j = 0; j < 2; j++)
+  for (int i = 0; i < C::SPA; i++) vsa[i] = (min(wave * C::SPA + i, C::SA - 1) * 64 + lane) * ns;
+#pragma unroll
+  for (int i = 0; i < C::SPB; i++)
+    vsb[i] = (min(wave * C::SPB + i, C::SB - 1) * 4 + (lane >> 4)) * ns * 16 + (lane & 15) * 16;
+  auto load_stage = [&](int s, int slot) __attribute__((always_inline)) {
+    const lds_bytes_t at = lds0 + slot * C::kStage;
+    const __amdgpu_buffer_rsrc_t ra = buffer_of(pa, s < nst ? mrows * lda : 0), rb = buffer_of(pb, s < nst ? groups * nk * 1024 : 0);
+#pragma unroll
+    for (int i = 0; i < C::LPA; i++) load_lds(ra, at + min(wave * C::LPA + i, C::LA - 1) * 1024, va[i], s * 128);
+#pragma unroll
+    for (int i = 0; i < C::LPB; i++) load_lds(rb, at + (C::LA + wave * C::LPB + i) * 1024, vb[i], s * (C::KPS * 1024));
+  };
+  const int nu = ns / 16;
+  auto load_scales = [&](int u) __attribute__((always_inline)) {
+    const int uu = min(u, nu - 1);
+    const lds_bytes_t at = lds0 + ST * C::kStage + (u % (C::PS + 1)) * C::kScale;
+#pragma unroll
+    for (int i = 0; i < C::SPA; i++) load_lds(rsa, at + min(wave * C::SPA + i, C::SA - 1) * 1024, vsa[i], uu * 16);
+#pragma unroll
+    for (int i = 0; i < C::SPB; i++) load_lds(rsb, at + (C::SA + min(wave * C::SPB + i, C::SB - 1)) * 1024, vsb[i], uu * 256);
+  };
+
+  f32x4 acc[C::FM][C::FN] = {};
+  uint32_t sa[C::FM], sb[C::FN];
+  u32x4 a[C::FM][C::PA], b[2][C::FN];
+  auto sync = [&](auto s_tag) __attribute__((always_inline)) {
+    __builtin_amdgcn_sched_barrier(0);
+    __builtin_amdgcn_s_waitcnt(vmcnt_imm(C::in_flight(decltype(s_tag)::value)) & kLgkm0);
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_sched_barrier(0);
+  };
+  // chunk g of the lane's row; chunk 4 + g is 64 bytes away under the xor
+  const int arow = (r >> 3) * 64 + (r & 7) * 8 + (g ^ ((r >> 1) & 7));
+  // operands of step h of the stage at `slot`: the weights into set p, a row
+  // block of A
+  auto read_b = [&](int p, int slot, int h) __attribute__((always_inline)) {
+#pragma unroll
+    for (int j = 0; j < C::FN; j++) b[p][j] = smem[slot * (C::kStage / 16) + (C::LA + (wn * C::FN + j) * C::KPS + h) * 64 + lane];
+  };
+  auto read_a = [&](int i, int slot, int h) __attribute__((always_inline)) {
+#pragma unroll
+    for (int q = 0; q < C::PA; q++) a[i][q] = smem[slot * (C::kStage / 16) + (wm * C::FM + i) * 128 + (arow ^ (4 * (q + h)))];
+  };
+  auto scales_at = [&](int u) __attribute__((always_inline)) {
+    return (const char*)smem + ST * C::kStage + (u % (C::PS + 1)) * C::kScale;
+  };
+  auto read_sa = [&](int i, int u) __attribute__((always_inline)) {
+    sa[i] = *reinterpret_cast<const uint32_t*>(scales_at(u) + (wm * C::FM + i) * 256 + r * 16 + 4 * g);
+  };
+  auto read_sb = [&](uint32_t* to, int u) __attribute__((always_inline)) {
+#pragma unroll
+    for (int j = 0; j < C::FN; j++) to[j] = *reinterpret_cast<const uint32_t*>(scales_at(u) + C::SA * 1024 + (wn * C::FN + j) * 256 + lane * 4);
+  };
+  // what the stages before the first do: the loads alone
+#pragma unroll
+  for (int u = 0; u < C::PS; u++)
+    if (C::G * (u - C::PS) < -ST) load_scales(u);
+#pragma unroll
+  for (int i = -ST; i < -1; i++) {
+    if (i % C::G == 0) load_scales(i / C::G + C::PS);
+    load_stage(i + ST, i + ST);
+  }
+  sync(std::integral_constant<int, C::G - 1>{});
+  load_stage(ST - 1, ST - 1);
+  read_b(0, 0, 0);
+  read_sb(sb, 0);
+#pragma unroll
+  for (int i = 0; i < C::FM; i++) {
+    read_a(i, 0, 0);
+    read_sa(i, 0);
+  }
+  int slot = 0;  // of the stage of step k
+  // A step: rows of blocks 0 .. HALF - 1; then (if the next step opens a
+  // stage) the meeting of the waves; then the other rows, while the next
+  // step's weights are read into the other set and its rows of A into the
+  // registers of rows already multiplied.
+  constexpr int HALF = C::FM / 2;
+  auto step = [&](auto ks_tag, int k) __attribute__((always_inline)) {
+    constexpr int KS = decltype(ks_tag)::value, P = KS & 1, H = KS % C::KPS, SG = KS / C::KPS;
+    constexpr bool kNext = H == C::KPS - 1;
+    auto row = [&](int i) __attribute__((always_inline)) {
+      i32x8 av = {};
 #pragma unroll
       for (int e = 0; e < 4; e++) {
-        const int64_t m = m0 + 16 * i + 4 * g + e;
-        const int n = n0 + 16 * j + r;
-        if (m >= M || n >= N) continue;
-        float v = acc[i][j][e];
-        if (add) v += add[m * N + n];
-        if (bf16) ((uint16_t*)out)[m * N + n] = f32_to_bf16(v);
-        else ((float*)out)[m * N + n] = v;
+        av[e] = (int)a[i][0][e];
+        av[4 + e] = FMT == LMGC_MX_FP8 ? (int)a[i][C::PA - 1][e] : 0;
       }
+#pragma unroll
+      for (int j = 0; j < C::FN; j++) acc[i][j] = mma<FMT, KS>(__builtin_bit_cast(i32x4, b[P][j]), av, acc[i][j], sb[j], sa[i]);
+    };
+#pragma unroll
+    for (int i = 0; i < HALF; i++) row(i);
+    if constexpr (kNext) {
+      const int s = k / C::KPS;
+      sync(std::integral_constant<int, SG>{});
+      if (SG == 0) load_scales(s / C::G + C::PS);
+      load_stage(s + ST, slot);
+      slot = slot == ST - 1 ? 0 : slot + 1;
+    }
+    constexpr int HN = kNext ? 0 : H + 1;
+    read_b(P ^ 1, slot, HN);
+#pragma unroll
+    for (int i = 0; i < HALF; i++) {
+      read_a(i, slot, HN);
+      if (KS == 3) read_sa(i, (k >> 2) + 1);
+    }
+#pragma unroll
+    for (int i = HALF; i < C::FM; i++) {
+      row(i);
+      if (i == HALF) {
+        // the reads above between this row's products
+#pragma unroll
+        for (int j = 0; j < C::FN; j++) {
+          __builtin_amdgcn_sched_group_barrier(0x100, (C::FN + HALF * C::PA + C::FN - 1) / C::FN, 0);
+          __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+        }
+      }
+      __builtin_amdgcn_sched_barrier(0);
+      read_a(i, slot, HN);
+      if (KS == 3) read_sa(i, (k >> 2) + 1);
+    }
+    if (KS == 3) read_sb(sb, (k >> 2) + 1);
+  };
+  int k = 0;
+  for (; k + 4 <= nk; k += 4) {
+    step(std::integral_constant<int, 0>{}, k);
+    step(std::integral_constant<int, 1>{}, k + 1);
+    step(std::integral_constant<int, 2>{}, k + 2);
+    step(std::integral_constant<int, 3>{}, k + 3);
+  }
+  if (k < nk) {
+    step(std::integral_constant<int, 0>{}, k);
+    if (k + 1 < nk) {
+      step(std::integral_constant<int, 1>{}, k + 1);
+      if (k + 2 < nk) step(std::integral_constant<int, 2>{}, k + 2);
+    }
+  }
+
+  // Results through LDS, a row block of the wave (16 rows x 16 FN columns) at
+  // a time, so that memory sees whole lines (8 bytes of 16 rows at once, as
+  // the registers have them, made the stores a fifth of the large product's
+  // time).  Rows are 16 bytes longer than their values, against bank
+  // conflicts.
+  __builtin_amdgcn_s_waitcnt(vmcnt_imm(0) & kLgkm0);  // no load to LDS is in flight past this
+  __builtin_amdgcn_s_barrier();
+  asm volatile("" ::: "memory");
+  constexpr int COLS = C::FN * 16, RS = COLS + 4;  // floats of a row
+  static_assert(C::NW * 16 * RS * 4 <= C::kLds, "epilogue does not fit");
+  float* mine = reinterpret_cast<float*>(smem) + wave * 16 * RS;
+  const int nw = n0 + wn * COLS, nc = min(COLS, N - nw);  // the wave's columns
+#pragma unroll
+  for (int i = 0; i < C::FM; i++) {
+#pragma unroll
+    for (int j = 0; j < C::FN; j++) *reinterpret_cast<f32x4*>(mine + r * RS + 16 * j + 4 * g) = acc[i][j];
+    __builtin_amdgcn_s_waitcnt(0xC07F);  // lgkmcnt(0)
+    asm volatile("" ::: "memory");
+    const int ml0 = wm * (BM / WM) + 16 * i;
+    if (nc > 0 && ml0 < mrows) store_rows<COLS>(mine, (m0 + ml0) * N + nw, min(16, mrows - ml0), nc, N, lane, add, out, bf16);
+    asm volatile("" ::: "memory");
+  }
+}
+
+// Row tiles per group of the tile order: an XCD's 32 workgroups then cover
+// about as many bytes of A as of B (16384 x 12288 x 4096, e4m3: 573 us with 4,
+// 594 with 8, 604 with 16).
+constexpr int kGroupM = 4;
+
+template <int FMT, int BM, int BN, int WM, int WN, int ST>
+void launch_tile(const uint8_t* a, const uint8_t* as, const uint8_t* b, const uint8_t* bs, int M, int N, int K,
+                 const float* add, void* out, int bf16, hipStream_t s) {
+  const int nk = (int)(mx_cols(K) / 128), ns = (int)mx_row_scales(K);
+  const int ntm = (M + BM - 1) / BM, ntn = (N + BN - 1) / BN;
+  const int64_t grid = ((int64_t)ntm * ntn + kXcds - 1) / kXcds * kXcds;
+  gemm_mx_tile_kernel<FMT, BM, BN, WM, WN, ST><<<(unsigned)grid, WM * WN * 64, 0, s>>>(a, as, b, bs, M, N, nk, ns, ntm, ntn,
+                                                                                     kGroupM, add, out, bf16);
+}
+
+enum MxTile { k16x16, k32x128, k64x64, k128x128, k128x256, k256x256, kTiles };
+
+// The tile with the least modelled time: a fixed part, and for every round of
+// tiles over the 256 CUs a part per tile and one per step of 128 columns
+// (microseconds, fitted to launches from a graph with N x K of 768 x 768 to
+// 22016 x 4096 and 1 to 16384 rows).  At K = 4096, e4m3, the choice and what
+// the next tile would take:
+//   16 x 4096      16x16   5.8 us   64x64  7.5      1 x 22016   32x128 10.2   64x64 11.2
+//   256 x 4096     64x64   8.5      32x128 9.8      1000 x 4096 128x128 19.7  128x256 23.4
+//   2048 x 4096    128x256 28.2     128x128 35.4    16384 x 12288 256x256 585 128x256 630
+// 16x16 tiles run three to a CU and, past that, fetch the rows of A too often
+// (22016 columns: 13.4 us); 32x128 is for 32 rows at most.  256x256 is left to
+// e4m3: with e2m1 128x256 is as fast (16384 x 4096 x 11008: 364 and 365 us).
+MxTile pick_tile(int fmt, int64_t M, int64_t N, int K) {
+  struct Cost {
+    int bm, bn;
+    double fixed, tile, step;
+  };
+  static const Cost cost[2][kTiles] = {
+      {{16, 16, 2.0, 0.4, 0.100}, {32, 128, 2.0, 0.8, 0.200}, {64, 64, 2.0, 0.7, 0.146}, {128, 128, 2.0, 1.5, 0.400},
+       {128, 256, 2.0, 3.0, 0.555}, {256, 256, 3.0, 5.0, 1.070}},
+      {{16, 16, 2.0, 0.4, 0.071}, {32, 128, 2.0, 0.8, 0.152}, {64, 64, 2.0, 0.9, 0.145}, {128, 128, 2.0, 1.8, 0.310},
+       {128, 256, 2.0, 2.2, 0.425}, {256, 256, 0, 1e30, 0}}};
+  const int nk = (int)(mx_cols(K) / 128);
+  int best = k64x64;
+  double least = 1e300;
+  for (int t = 0; t < kTiles; t++) {
+    const Cost& c = cost[fmt == LMGC_MX_FP8 ? 0 : 1][t];
+    const int64_t tiles = (M + c.bm - 1) / c.bm * ((N + c.bn - 1) / c.bn);
+    if (t == k16x16 ? tiles > 3 * 256 : t == k32x128 && M > 32) continue;
+    const double rounds = t == k16x16 ? 1.0 : (double)((tiles + 255) / 256);
+    const double us = c.fixed + rounds * (c.tile + c.step * nk);
+    if (us < least) {
+      least = us;
+      best = t;
+    }
+  }
+  return (MxTile)best;
+}
+
+template <int FMT>
+void launch_fmt(const uint8_t* a, const uint8_t* as, const uint8_t* b, const uint8_t* bs, int M, int N, int K,
+                const float* add, void* out, int bf16, hipStream_t s) {
+  constexpr bool F8 = FMT == LMGC_MX_FP8;
+  switch (pick_tile(FMT, M, N, K)) {
+    case k16x16: return launch_tile<FMT, 16, 16, 1, 1, F8 ? 8 : 6>(a, as, b, bs, M, N, K, add, out, bf16, s);
+    case k32x128: return launch_tile<FMT, 32, 128, 1, 4, F8 ? 6 : 4>(a, as, b, bs, M, N, K, add, out, bf16, s);
+    case k64x64: return launch_tile<FMT, 64, 64, 2, 2, 4>(a, as, b, bs, M, N, K, add, out, bf16, s);
+    case k128x128: return launch_tile<FMT, 128, 128, 2, 2, F8 ? 4 : 3>(a, as, b, bs, M, N, K, add, out, bf16, s);
+    case k128x256: return launch_tile<FMT, 128, 256, 2, 4, F8 ? 4 : 2>(a, as, b, bs, M, N, K, add, out, bf16, s);
+    default:
+      if constexpr (F8) launch_tile<FMT, 256, 256, 4, 2, 3>(a, as, b, bs, M, N, K, add, out, bf16, s);
+  }
 }
 
 }  // namespace
 
 hipError_t launch_gemm_mx(const uint8_t* a, const uint8_t* as, int a_fmt, const uint8_t* b, const uint8_t* bs, int M,
                           int N, int K, const float* add, void* out, int bf16, hipStream_t s) {
-  const dim3 grid((N + 31) / 32, (M + 31) / 32);
-  if (a_fmt == LMGC_MX_FP8) gemm_mx_kernel<LMGC_MX_FP8><<<grid, 64, 0, s>>>(a, as, b, bs, M, N, K, add, out, bf16);
-  else gemm_mx_kernel<LMGC_MX_FP4><<<grid, 64, 0, s>>>(a, as, b, bs, M, N, K, add, out, bf16);
+  if (a_fmt == LMGC_MX_FP8) launch_fmt<LMGC_MX_FP8>(a, as, b, bs, M, N, K, add, out, bf16, s);
+  else launch_fmt<LMGC_MX_FP4>(a, as, b, bs, M, N, K, add, out, bf16, s);
   return hipGetLastError();
 }
 

@@ -272,12 +272,213 @@ __global__ __launch_bounds__(64) void attn_kv8_join_kernel(const float* __restri
     out[((int64_t)b * T + t) * (Hkv * G * HD) + hq * HD + lane + 64 * i] = f32_to_bf16(acc[i] / L);
 }
 
+// Prompts: a workgroup of eight waves takes 256 columns of one (sequence,
+// key/value head), each wave 32, and walks the cache in steps of 8 KB of keys
+// and of values (64 tokens of 128 dims, 128 of 64).  Each thread fetches 16
+// bytes of codes of both a step ahead, converts them and stores them as bf16
+// in the order of the matrix operands, so a conversion serves 256 columns and
+// the products read LDS a lane's 16 bytes in a row.  Keys run one step ahead
+// of values: the scores of step s + 1 are multiplied while the exponentials
+// of step s are taken.  The block scales cost nothing per score: the keys'
+// goes into the exponent's factor, the values' (a power of two) into its
+// summand, from which the row sums are freed once per block.
+template <int HD>
+__global__ __launch_bounds__(512, 2) void attn_kv8_prompt_kernel(
+    const uint16_t* __restrict__ q, const uint8_t* __restrict__ kc, const float* __restrict__ ks,
+    const uint8_t* __restrict__ vc, const float* __restrict__ vs, const int32_t* __restrict__ lens,
+    const int32_t* __restrict__ counts, int B, int Hkv, int G, int T, int cap, int ntile, Mask mask, float sl2,
+    uint16_t* __restrict__ out) {
+  constexpr int NC = HD / 64, ND = HD / 16, NB = 128 / HD, TB = NB * kBlk;  // blocks and tokens of a step
+  constexpr int KQ = HD / 32;                                               // 32-dim steps of a score
+  __shared__ u32x4 sk[2][1024], sv[2][1024];  // 16 KB each
+  const int npair = B * Hkv;
+  // pairs fastest: with a multiple of eight pairs all tiles of a pair run on
+  // one XCD and share its L2; the longest tiles first
+  const int pair = blockIdx.x % npair, c0 = (ntile - 1 - (int)blockIdx.x / npair) * 256;
+  const int b = pair / Hkv, kvh = pair % Hkv;
+  int len;
+  const int n = new_tokens(lens, counts, b, T, cap, len);
+  const int ncol = min(256, n * G - c0);
+  if (ncol <= 0) return;
+  const int tid = threadIdx.x, lane = tid & 63, col = lane & 15, g = lane >> 4;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int p0 = len + c0 / G, p1 = len + (c0 + ncol - 1) / G;
+  // the wave's columns (past the last: the last one's again)
+  const int w0 = min(c0 + wave * 32, c0 + ncol - 1), w1 = min(c0 + wave * 32 + 31, c0 + ncol - 1);
+  const bool works = wave * 32 < ncol;
+  const int q0 = len + w0 / G, q1 = len + w1 / G;
+  int pos[2];
+  bf16x8 qf[2][KQ];
+#pragma unroll
+  for (int i = 0; i < 2; i++) {
+    const int c = min(w0 + 16 * i + col, w1), t = c / G;
+    pos[i] = len + t;
+    const uint16_t* qp = q + (((int64_t)b * Hkv * G + kvh * G + c % G) * T + t) * HD + 16 * g;
+#pragma unroll
+    for (int x = 0; x < KQ; x++) qf[i][x] = *reinterpret_cast<const bf16x8*>(qp + 64 * (x >> 1) + 8 * (x & 1));
+  }
+  const int64_t blk0 = (int64_t)pair * (cap / kBlk);
+  const uint8_t *kp = kc + blk0 * (kBlk * HD), *vp = vc + blk0 * (kBlk * HD);
+  const int nsteps = p1 / TB + 1;
+  const int64_t bytes = (int64_t)cap * HD;
+  const int w_step = mask.window ? max(0, p0 - mask.window + 1) / TB : 0;  // first step that the window reaches
+  auto after = [&](int s) __attribute__((always_inline)) {
+    const int x = s + 1;
+    return x * TB >= mask.sinks && x < w_step ? w_step : x;
+  };
+  const u32x4 zero = {0, 0, 0, 0};
+  auto fetch = [&](const uint8_t* p, int s) __attribute__((always_inline)) {
+    const int64_t off = (int64_t)s * 8192 + tid * 16;
+    return s < nsteps && off < bytes ? *reinterpret_cast<const u32x4*>(p + off) : zero;
+  };
+  auto stash = [&](u32x4* to, u32x4 w) __attribute__((always_inline)) {
+    u32x4* at = to + (tid >> 6) * 128 + lane;
+    at[0] = __builtin_bit_cast(u32x4, fp8_bf16(w[0], w[1]));
+    at[64] = __builtin_bit_cast(u32x4, fp8_bf16(w[2], w[3]));
+  };
+  // scores of step s: token tile i of the step, column tile x
+  f32x4 sc[NB * 4][2], sn[NB * 4][2];
+  auto scores = [&](f32x4(&o)[NB * 4][2], const u32x4* k) __attribute__((always_inline)) {
+#pragma unroll
+    for (int i = 0; i < NB * 4; i++)
+#pragma unroll
+      for (int x = 0; x < KQ; x++) {
+        const bf16x8 kf = __builtin_bit_cast(bf16x8, k[(i * KQ + x) * 64 + lane]);
+#pragma unroll
+        for (int y = 0; y < 2; y++)
+          o[i][y] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, qf[y][x], x == 0 ? f32x4{} : o[i][y], 0, 0, 0);
+      }
+  };
+  f32x4 acc[ND][2] = {};
+  float m[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f};
+
+  int s = mask.window && mask.sinks == 0 ? w_step : 0;
+  int s1 = after(s);
+  u32x4 kr = fetch(kp, s), vr = fetch(vp, s);
+  stash(sk[0], kr);
+  stash(sv[0], vr);
+  kr = fetch(kp, s1);
+  vr = fetch(vp, s1);
+  __syncthreads();
+  scores(sc, sk[0]);
+  stash(sk[1], kr);
+  kr = fetch(kp, after(s1));
+  __syncthreads();
+  for (int it = 0; s < nsteps; it++) {
+    // here: sc the scores of s; sk[(it + 1) & 1] the keys of s1, kr the next
+    // ones; sv[it & 1] the values of s, vr those of s1
+    const int s2 = after(s1);
+    stash(sv[(it + 1) & 1], vr);
+    vr = fetch(vp, s2);
+    if (works) {
+      scores(sn, sk[(it + 1) & 1]);
+#pragma unroll
+      for (int h = 0; h < NB; h++) {
+        const int j0 = s * TB + h * kBlk;
+        if (j0 >= cap || !mask.any(q0, q1, j0, j0 + kBlk)) continue;
+        const float fk = ks[blk0 + j0 / kBlk] * sl2, fv = vs[blk0 + j0 / kBlk];
+        // log2 of the values' scale (a power of two; NaN stays NaN)
+        const float ev = fv == fv ? (float)((int)(__builtin_bit_cast(uint32_t, fv) >> 23) - 127) : fv;
+        const float unscale = fv == fv ? 1.0f / fv : 1.0f;
+        const bool whole = mask.all(q0, q1, j0, j0 + kBlk);
+        bf16x8 pf[2][2];
+#pragma unroll
+        for (int y = 0; y < 2; y++) {
+          float mx = -INFINITY;
+          if (!whole) {
+#pragma unroll
+            for (int i = 0; i < 4; i++)
+#pragma unroll
+              for (int r = 0; r < 4; r++)
+                if (!mask.sees(pos[y], j0 + 16 * i + 4 * g + r)) sc[4 * h + i][y][r] = -INFINITY;
+          }
+#pragma unroll
+          for (int i = 0; i < 4; i++)
+#pragma unroll
+            for (int r = 0; r < 4; r++) mx = fmaxf(mx, sc[4 * h + i][y][r]);
+          mx *= fk;
+          // a column's reference moves only when a score passes it by 2^8
+          if (__ballot(mx > m[y] + 8.0f)) {
+            mx = fmaxf(mx, __shfl_xor(mx, 16, 64));
+            mx = fmaxf(mx, __shfl_xor(mx, 32, 64));
+            if (mx > m[y] + 8.0f) {
+              const float a = __builtin_amdgcn_exp2f(m[y] - mx);
+              l[y] *= a;
+#pragma unroll
+              for (int i = 0; i < ND; i++) acc[i][y] *= a;
+              m[y] = mx;
+            }
+          }
+          const float sub = ev - (m[y] == -INFINITY ? 0.f : m[y]);
+          float sum = 0.f;
+#pragma unroll
+          for (int i = 0; i < 4; i++) {
+            float p[4];
+#pragma unroll
+            for (int r = 0; r < 4; r++) {
+              p[r] = __builtin_amdgcn_exp2f(fmaf(sc[4 * h + i][y][r], fk, sub));
+              if (!whole && sc[4 * h + i][y][r] == -INFINITY) p[r] = 0.f;
+            }
+            const bf16x2 a = {(__bf16)p[0], (__bf16)p[1]}, c = {(__bf16)p[2], (__bf16)p[3]}, one = {(__bf16)1.0f, (__bf16)1.0f};
+            sum = __builtin_amdgcn_fdot2_f32_bf16(a, one, sum, false);
+            sum = __builtin_amdgcn_fdot2_f32_bf16(c, one, sum, false);
+#pragma unroll
+            for (int r = 0; r < 2; r++) {
+              pf[y][i >> 1][(i & 1) * 4 + r] = a[r];
+              pf[y][i >> 1][(i & 1) * 4 + 2 + r] = c[r];
+            }
+          }
+          l[y] = fmaf(sum, unscale, l[y]);
+        }
+#pragma unroll
+        for (int i = 0; i < ND; i++)
+#pragma unroll
+          for (int x = 0; x < 2; x++) {
+            const bf16x8 vf = __builtin_bit_cast(bf16x8, sv[it & 1][((h * ND + i) * 2 + x) * 64 + lane]);
+#pragma unroll
+            for (int y = 0; y < 2; y++) acc[i][y] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, pf[y][x], acc[i][y], 0, 0, 0);
+          }
+      }
+#pragma unroll
+      for (int i = 0; i < NB * 4; i++)
+#pragma unroll
+        for (int y = 0; y < 2; y++) sc[i][y] = sn[i][y];
+    }
+    stash(sk[it & 1], kr);
+    kr = fetch(kp, after(s2));
+    __syncthreads();
+    s = s1;
+    s1 = s2;
+  }
+  if (!works) return;
+#pragma unroll
+  for (int y = 0; y < 2; y++) {
+    const int c = w0 + 16 * y + col;
+    float L = l[y];
+    L += __shfl_xor(L, 16, 64);
+    L += __shfl_xor(L, 32, 64);
+    if (c > w1) continue;
+    const float inv = 1.0f / L;
+    uint16_t* op = out + ((int64_t)b * T + c / G) * ((int64_t)Hkv * G * HD) + (kvh * G + c % G) * HD + 4 * g;
+#pragma unroll
+    for (int i = 0; i < ND; i++) {
+      mx_u32x2 w;
+#pragma unroll
+      for (int e = 0; e < 2; e++)
+        w[e] = (uint32_t)f32_to_bf16(acc[i][y][2 * e] * inv) | ((uint32_t)f32_to_bf16(acc[i][y][2 * e + 1] * inv) << 16);
+      *reinterpret_cast<mx_u32x2*>(op + 16 * i) = w;
+    }
+  }
+}
+
+// Columns up to which a (sequence, key/value head) takes the split form.
+constexpr int kSplitCols = 64;
+
 }  // namespace
 
 int64_t kv8_workspace_bytes(int B, int Hq, int Hkv, int T, int hd, int cap) {
-  (void)Hkv;
   const int64_t nsplit = (cap + kChunk - 1) / kChunk;
-  if (nsplit <= 1) return 0;
+  if (nsplit <= 1 || (int64_t)T * (Hq / Hkv) > kSplitCols) return 0;
   return (int64_t)B * Hq * T * nsplit * (hd + 2) * 4;
 }
 
@@ -300,6 +501,12 @@ hipError_t launch_attention_kv8(const uint16_t* q, int B, int Hq, int Hkv, int T
   float2* pml = (float2*)(po + (int64_t)B * Hq * T * nsplit * hd);
   auto go = [&](auto h) {
     constexpr int HD = decltype(h)::value;
+    if ((int64_t)T * G > kSplitCols) {
+      const int tiles = (int)(((int64_t)T * G + 255) / 256);
+      attn_kv8_prompt_kernel<HD><<<dim3((unsigned)tiles * B * Hkv), 512, 0, s>>>(q, kc, ks, vc, vs, lens, counts, B, Hkv, G, T,
+                                                                               cap, tiles, mask, sl2, out);
+      return;
+    }
     attn_kv8_split_kernel<HD><<<dim3(nsplit * ntile, Hkv, B), 256, 0, s>>>(q, kc, ks, vc, vs, lens, counts, Hkv, G, T, cap,
                                                                            nsplit, mask, sl2, po, pml, out);
     if (nsplit > 1)
