@@ -13,6 +13,7 @@
 #include <math.h>
 
 #include <algorithm>
+#include <type_traits>
 
 #include "mx.h"
 
@@ -46,6 +47,23 @@ __device__ inline int new_tokens(const int32_t* lens, const int32_t* counts, int
 // ------------------------------------------------------------------ append
 // A workgroup per (block of the cache that new tokens may fall into, key/value
 // head, sequence x {key, value}).
+//
+// A block that gets its first token is read once, 16 bytes a load, and written
+// once, 16 bytes of codes a lane, 1 KB in a row.  A key's 16 codes are 32
+// bytes of its row.  A value's are 16 tokens of one dim: a thread takes 4
+// tokens x 8 dims, packs the 4 tokens of each dim into the word they are in
+// the block, and the words meet in LDS.  A block that has tokens already is
+// the rare one (one per sequence and call): its new tokens are written byte by
+// byte, and the earlier codes are gone over only when the scale grows.
+__device__ inline uint32_t abs_max2(uint32_t a, uint32_t w) { return max(a, max(w & 0x7fffu, (w >> 16) & 0x7fffu)); }
+
+__device__ inline uint32_t block_max(uint32_t a, uint32_t* part) {
+  for (int o = 32; o; o >>= 1) a = max(a, (uint32_t)__shfl_xor((int)a, o, 64));
+  if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = a;
+  __syncthreads();
+  return max(max(part[0], part[1]), max(part[2], part[3]));
+}
+
 template <int HD>
 __global__ __launch_bounds__(256) void kv8_append_kernel(const uint16_t* __restrict__ kin, const uint16_t* __restrict__ vin,
                                                          int Hkv, int T, int cap, const int32_t* __restrict__ lens,
@@ -53,7 +71,8 @@ __global__ __launch_bounds__(256) void kv8_append_kernel(const uint16_t* __restr
                                                          float* __restrict__ ks, uint8_t* __restrict__ vc,
                                                          float* __restrict__ vs) {
   __shared__ uint32_t part[4];
-  const int b = blockIdx.z >> 1, is_v = blockIdx.z & 1, h = blockIdx.y;
+  __shared__ uint32_t words[kBlk * HD / 4];
+  const int b = blockIdx.z >> 1, is_v = blockIdx.z & 1, h = blockIdx.y, tid = threadIdx.x, lane = tid & 63;
   int len;
   const int n = new_tokens(lens, counts, b, T, cap, len);
   if (n <= 0) return;
@@ -64,34 +83,96 @@ __global__ __launch_bounds__(256) void kv8_append_kernel(const uint16_t* __restr
   const uint16_t* src = (is_v ? vin : kin) + (hb * T + (t0 - len)) * HD;  // row of token t0 (rows lo .. hi - 1 exist)
   uint8_t* codes = (is_v ? vc : kc) + (hb * (cap / kBlk) + blk) * (kBlk * HD);
   float* scale = (is_v ? vs : ks) + hb * (cap / kBlk) + blk;
-  uint32_t a = 0;
-  for (int i = threadIdx.x; i < (hi - lo) * HD; i += 256) a = max(a, abs_bits(load1(src + (int64_t)lo * HD + i)));
-  for (int o = 32; o; o >>= 1) a = max(a, (uint32_t)__shfl_xor((int)a, o, 64));
-  if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = a;
-  __syncthreads();
-  a = max(max(part[0], part[1]), max(part[2], part[3]));
-  const float s_old = lo ? *scale : 0.f;
-  float s_new = a >= 0x7f800000u ? __builtin_bit_cast(float, 0x7fc00000u)
-                                 : mx_scale(max(mx_scale_byte<LMGC_MX_FP8>(a), kMinScale));
-  const bool nan = s_new != s_new || s_old != s_old;
-  const float s = nan ? __builtin_bit_cast(float, 0x7fc00000u) : fmaxf(s_old, s_new);
-  const float inv = nan ? 1.0f : 1.0f / s, grow = nan ? 1.0f : s_old * inv;
-  __syncthreads();  // every thread has read the old scale
-  if (threadIdx.x == 0) *scale = s;
-  for (int i = threadIdx.x; i < kBlk * HD; i += 256) {
-    const int t = i / HD, d = i - t * HD;
-    uint8_t* p = codes + (is_v ? value_at(t, d) : key_at(t, d, HD));
-    float v;
-    if (t >= lo && t < hi) {
-      v = load1(src + (int64_t)t * HD + d) * inv;
-      if (nan) v = 0.f;
-    } else if (lo == 0) {
-      v = 0.f;  // a new block is cleared behind its tokens
-    } else {
-      if (t >= hi || grow == 1.0f) continue;
-      v = __builtin_amdgcn_cvt_f32_fp8((int)*p, 0) * grow;
+  // bf16 bits of a magnitude -> block scale (NaN for a NaN or an infinity)
+  auto scale_of = [](uint32_t a) __attribute__((always_inline)) {
+    return a >= 0x7f80u ? __builtin_bit_cast(float, 0x7fc00000u) : mx_scale(max(mx_scale_byte<LMGC_MX_FP8>(a << 16), kMinScale));
+  };
+  auto lo16 = [](uint32_t w) __attribute__((always_inline)) { return __builtin_bit_cast(float, w << 16); };
+  auto hi16 = [](uint32_t w) __attribute__((always_inline)) { return __builtin_bit_cast(float, w & 0xffff0000u); };
+  auto pack4 = [](float a, float b2, float c, float d) __attribute__((always_inline)) {
+    const int w = __builtin_amdgcn_cvt_pk_fp8_f32(a, b2, 0, false);
+    return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(c, d, w, true);
+  };
+  const u32x4 zero = {0, 0, 0, 0};
+  if (lo == 0 && !is_v) {
+    constexpr int NP = HD / 64, NC = HD / 64;  // pieces of a thread; chunks of 64 dims
+    u32x4 w[NP][2];
+    uint32_t a = 0;
+#pragma unroll
+    for (int i = 0; i < NP; i++) {
+      const int p = (tid >> 6) + 4 * i, t = 16 * (p / NC) + (lane & 15), d = 64 * (p % NC) + 16 * (lane >> 4);
+      const u32x4* q = reinterpret_cast<const u32x4*>(src + (int64_t)t * HD + d);
+      w[i][0] = t < hi ? q[0] : zero;
+      w[i][1] = t < hi ? q[1] : zero;
     }
-    *p = (uint8_t)__builtin_amdgcn_cvt_pk_fp8_f32(v, v, 0, false);
+#pragma unroll
+    for (int i = 0; i < NP; i++)
+#pragma unroll
+      for (int e = 0; e < 8; e++) a = abs_max2(a, w[i][e >> 2][e & 3]);
+    const float s = scale_of(block_max(a, part));
+    const bool nan = s != s;
+    const float inv = nan ? 0.f : 1.0f / s;
+    if (tid == 0) *scale = s;
+#pragma unroll
+    for (int i = 0; i < NP; i++) {
+      u32x4 o = zero;
+#pragma unroll
+      for (int e = 0; e < 4; e++) {
+        const uint32_t x = w[i][e >> 1][2 * (e & 1)], y = w[i][e >> 1][2 * (e & 1) + 1];
+        if (!nan) o[e] = pack4(lo16(x) * inv, hi16(x) * inv, lo16(y) * inv, hi16(y) * inv);
+      }
+      reinterpret_cast<u32x4*>(codes)[((tid >> 6) + 4 * i) * 64 + lane] = o;
+    }
+  } else if (lo == 0) {
+    const int quad = tid & 15, d0 = (tid >> 4) * 8;  // tokens 4 quad .. + 3, dims d0 .. + 7
+    u32x4 w[4];
+    uint32_t a = 0;
+#pragma unroll
+    for (int r = 0; r < 4; r++) {
+      const int t = 4 * quad + r;
+      w[r] = t < hi && d0 < HD ? *reinterpret_cast<const u32x4*>(src + (int64_t)t * HD + d0) : zero;
+#pragma unroll
+      for (int e = 0; e < 4; e++) a = abs_max2(a, w[r][e]);
+    }
+    const float s = scale_of(block_max(a, part));
+    const bool nan = s != s;
+    const float inv = nan ? 0.f : 1.0f / s;
+    if (tid == 0) *scale = s;
+    if (d0 < HD) {
+#pragma unroll
+      for (int e = 0; e < 8; e++) {
+        const int d = d0 + e;
+        float v[4];
+#pragma unroll
+        for (int r = 0; r < 4; r++) v[r] = (e & 1 ? hi16(w[r][e >> 1]) : lo16(w[r][e >> 1])) * inv;
+        words[(d >> 4) * 256 + ((d & 15) + 16 * (quad & 3)) * 4 + (quad >> 2)] = nan ? 0u : pack4(v[0], v[1], v[2], v[3]);
+      }
+    }
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < HD / 64; i++)
+      reinterpret_cast<u32x4*>(codes)[i * 256 + tid] = *reinterpret_cast<const u32x4*>(words + (i * 256 + tid) * 4);
+  } else {
+    uint32_t a = 0;
+    for (int i = tid; i < (hi - lo) * HD; i += 256) a = max(a, (uint32_t)src[(int64_t)lo * HD + i] & 0x7fffu);
+    const float s_old = *scale;
+    const float s_new = scale_of(block_max(a, part));  // (the barrier in it: every thread has read the old scale)
+    const bool nan = s_new != s_new || s_old != s_old;
+    const float s = nan ? __builtin_bit_cast(float, 0x7fc00000u) : fmaxf(s_old, s_new);
+    const float inv = 1.0f / s, grow = s_old * inv;
+    if (tid == 0) *scale = s;
+    if (!nan && s != s_old)
+      for (int i = tid; i < lo * HD; i += 256) {
+        const int t = i / HD, d = i - t * HD;
+        uint8_t* p = codes + (is_v ? value_at(t, d) : key_at(t, d, HD));
+        const float v = __builtin_amdgcn_cvt_f32_fp8((int)*p, 0) * grow;
+        *p = (uint8_t)__builtin_amdgcn_cvt_pk_fp8_f32(v, v, 0, false);
+      }
+    for (int i = tid; i < (hi - lo) * HD; i += 256) {
+      const int t = lo + i / HD, d = i % HD;
+      const float v = nan ? 0.f : bf16_to_f32(src[(int64_t)t * HD + d]) * inv;
+      codes[is_v ? value_at(t, d) : key_at(t, d, HD)] = (uint8_t)__builtin_amdgcn_cvt_pk_fp8_f32(v, v, 0, false);
+    }
   }
 }
 
@@ -119,39 +200,54 @@ __device__ inline bf16x8 fp8_bf16(uint32_t w0, uint32_t w1) {
   return bf16x8{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
 }
 
-constexpr int kChunk = 256;  // tokens of a split: one block for each of four waves
+// Columns: column c = t G + i of a (sequence, key/value head) is query head
+// kvh G + i of new token t.  A column's result is a function of the column's
+// query and of the cache, whatever columns, sequences and splits run with it:
+// blocks that a column does not see add exact zeros.
 
-// Column c = t G + g of a (sequence, key/value head): query head kvh G + g of
-// new token t.
-//
-// Grid: (splits x column tiles, Hkv, B); a workgroup computes 16 columns over
-// kChunk tokens, wave w over its block w.  S^T = K Q^T: lane (col, g) holds
-// the scores of its column and tokens 16 i + 4 g + r.
+// ---- few columns (kSplitCols at most)
+// Grid: (splits x tiles of 16 columns, Hkv, B), 512 threads.  A split is 256
+// KB of the cache; wave w takes its blocks w, w + 8, ..: S^T = K Q^T, so lane
+// (col, g) holds the scores of its column and tokens 16 i + 4 g + r of a
+// block, an online softmax, O^T += V^T P^T.  The waves' parts meet in LDS.
+constexpr int kSplitCols = 32;
+constexpr int kSplitBytes = 256 << 10;
+constexpr int kSplitWaves = 8;
+
+__host__ __device__ constexpr int split_tokens(int hd) { return kSplitBytes / (2 * hd); }
+
 template <int HD>
-__global__ __launch_bounds__(256) void attn_kv8_split_kernel(
+__global__ __launch_bounds__(kSplitWaves * 64, 4) void attn_kv8_split_kernel(
     const uint16_t* __restrict__ q, const uint8_t* __restrict__ kc, const float* __restrict__ ks,
     const uint8_t* __restrict__ vc, const float* __restrict__ vs, const int32_t* __restrict__ lens,
     const int32_t* __restrict__ counts, int Hkv, int G, int T, int cap, int nsplit, Mask mask, float sl2,
     float* __restrict__ part_o, float2* __restrict__ part_ml, uint16_t* __restrict__ out) {
-  constexpr int NC = HD / 64, ND = HD / 16;
-  __shared__ float so[4][16][HD + 4];
-  __shared__ float sm[4][16], sl[4][16];
+  constexpr int NC = HD / 64, ND = HD / 16, CH = split_tokens(HD), NW = kSplitWaves;
+  __shared__ float so[NW / 2][16][HD + 4];
+  __shared__ float sm[NW][16], sl[NW][16];
   const int split = blockIdx.x % nsplit, c0 = blockIdx.x / nsplit * 16, kvh = blockIdx.y, b = blockIdx.z;
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, col = lane & 15, g = lane >> 4;
+  const int tid = threadIdx.x, lane = tid & 63, col = lane & 15, g = lane >> 4;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   int len;
   const int n = new_tokens(lens, counts, b, T, cap, len);
   const int ncol = min(16, n * G - c0);
   if (ncol <= 0) return;
   const int p0 = len + c0 / G, p1 = len + (c0 + ncol - 1) / G;  // positions of the tile's queries
-  const int j0 = split * kChunk + wave * kBlk;
-  if (!mask.any(p0, p1, split * kChunk, split * kChunk + kChunk)) return;
+  if (!mask.any(p0, p1, split * CH, split * CH + CH)) return;
   const int c = c0 + min(col, ncol - 1), t = c / G, pos = len + t;
   const int64_t hb = (int64_t)b * Hkv + kvh, nblk = cap / kBlk;
+  const uint16_t* qp = q + (((int64_t)b * Hkv * G + kvh * G + c % G) * T + t) * HD + 16 * g;
+  bf16x8 qf[NC][2];
+#pragma unroll
+  for (int x = 0; x < NC; x++)
+#pragma unroll
+    for (int y = 0; y < 2; y++) qf[x][y] = *reinterpret_cast<const bf16x8*>(qp + 64 * x + 8 * y);
 
   float m = -INFINITY, l = 0.f;
   f32x4 o[ND] = {};
-  if (j0 < cap && mask.any(p0, p1, j0, j0 + kBlk)) {
-    const uint16_t* qp = q + (((int64_t)b * Hkv * G + kvh * G + c % G) * T + t) * HD;
+  const int jend = min(min(cap, split * CH + CH), p1 + 1);
+  for (int j0 = split * CH + wave * kBlk; j0 < jend; j0 += NW * kBlk) {
+    if (!mask.any(p0, p1, j0, j0 + kBlk)) continue;
     const int64_t blk = hb * nblk + j0 / kBlk;
     const u32x4* kp = reinterpret_cast<const u32x4*>(kc + blk * (kBlk * HD)) + lane;
     const u32x4* vp = reinterpret_cast<const u32x4*>(vc + blk * (kBlk * HD)) + lane;
@@ -162,30 +258,35 @@ __global__ __launch_bounds__(256) void attn_kv8_split_kernel(
       for (int x = 0; x < NC; x++) kr[i][x] = kp[(i * NC + x) * 64];
 #pragma unroll
     for (int i = 0; i < ND; i++) vr[i] = vp[i * 64];
-    const float sk = ks[blk] * sl2, sv = vs[blk];
+    const float fk = ks[blk] * sl2, fv = vs[blk];
     f32x4 s[4] = {};
 #pragma unroll
     for (int x = 0; x < NC; x++)
 #pragma unroll
-      for (int y = 0; y < 2; y++) {
-        const bf16x8 qf = *reinterpret_cast<const bf16x8*>(qp + 64 * x + 16 * g + 8 * y);
+      for (int y = 0; y < 2; y++)
 #pragma unroll
         for (int i = 0; i < 4; i++)
-          s[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fp8_bf16(kr[i][x][2 * y], kr[i][x][2 * y + 1]), qf, s[i], 0, 0, 0);
-      }
+          s[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fp8_bf16(kr[i][x][2 * y], kr[i][x][2 * y + 1]), qf[x][y], s[i], 0, 0, 0);
     const bool whole = mask.all(p0, p1, j0, j0 + kBlk);
     bool see[4][4];
+    float mx = -INFINITY;
 #pragma unroll
     for (int i = 0; i < 4; i++)
 #pragma unroll
       for (int r = 0; r < 4; r++) {
         see[i][r] = whole || mask.sees(pos, j0 + 16 * i + 4 * g + r);
-        s[i][r] = see[i][r] ? s[i][r] * sk : -INFINITY;
-        m = fmaxf(m, s[i][r]);
-        // (fmaxf drops a NaN; it comes back through the exponential)
+        s[i][r] = see[i][r] ? s[i][r] * fk : -INFINITY;
+        mx = fmaxf(mx, s[i][r]);  // (drops a NaN; it comes back through the exponential)
       }
-    m = fmaxf(m, __shfl_xor(m, 16, 64));
-    m = fmaxf(m, __shfl_xor(m, 32, 64));
+    mx = fmaxf(mx, __shfl_xor(mx, 16, 64));
+    mx = fmaxf(mx, __shfl_xor(mx, 32, 64));
+    if (mx > m) {
+      const float a = __builtin_amdgcn_exp2f(m - mx);
+      l *= a;
+#pragma unroll
+      for (int i = 0; i < ND; i++) o[i] *= a;
+      m = mx;
+    }
     const float ref = m == -INFINITY ? 0.f : m;
     bf16x8 pf[2];
 #pragma unroll
@@ -195,71 +296,93 @@ __global__ __launch_bounds__(256) void attn_kv8_split_kernel(
         // rounded to bf16 for the second product; the sum is of the rounded values
         const __bf16 p = (__bf16)__builtin_amdgcn_exp2f(s[i][r] - ref);
         l += (float)p;
-        pf[i >> 1][(i & 1) * 4 + r] = see[i][r] ? (__bf16)((float)p * sv) : (__bf16)0.f;
+        pf[i >> 1][(i & 1) * 4 + r] = see[i][r] ? (__bf16)((float)p * fv) : (__bf16)0.f;
       }
-    l += __shfl_xor(l, 16, 64);
-    l += __shfl_xor(l, 32, 64);
 #pragma unroll
     for (int i = 0; i < ND; i++)
 #pragma unroll
       for (int y = 0; y < 2; y++)
         o[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fp8_bf16(vr[i][2 * y], vr[i][2 * y + 1]), pf[y], o[i], 0, 0, 0);
   }
+  l += __shfl_xor(l, 16, 64);
+  l += __shfl_xor(l, 32, 64);
   if (g == 0) {
     sm[wave][col] = m;
     sl[wave][col] = l;
   }
-#pragma unroll
-  for (int i = 0; i < ND; i++) *reinterpret_cast<f32x4*>(&so[wave][col][16 * i + 4 * g]) = o[i];
   __syncthreads();
-  // whether this chunk is all that the tile's queries see
+  // waves without a token they see (m = -inf, l = 0) count for nothing
+  float M = sm[0][col];
+#pragma unroll
+  for (int w = 1; w < NW; w++) M = fmaxf(M, sm[w][col]);
+  float L = 0.f;
+  auto weight = [&](float mw, float lw) __attribute__((always_inline)) {
+    return mw == -INFINITY && lw == 0.f ? 0.f : __builtin_amdgcn_exp2f(mw - M);
+  };
+#pragma unroll
+  for (int w = 0; w < NW; w++) L += weight(sm[w][col], sl[w][col]) * sl[w][col];
+  const float a = weight(m, l);
+#pragma unroll
+  for (int i = 0; i < ND; i++) o[i] *= a;
+#pragma unroll
+  for (int half = NW / 2; half; half >>= 1) {
+    if (wave >= half && wave < 2 * half)
+#pragma unroll
+      for (int i = 0; i < ND; i++) *reinterpret_cast<f32x4*>(&so[wave - half][col][16 * i + 4 * g]) = o[i];
+    __syncthreads();
+    if (wave < half)
+#pragma unroll
+      for (int i = 0; i < ND; i++) o[i] += *reinterpret_cast<const f32x4*>(&so[wave][col][16 * i + 4 * g]);
+    __syncthreads();
+  }
+  if (wave != 0 || col >= ncol) return;
+  // whether this split is all that the tile's queries see
   bool only = true;
   for (int x = 0; x < nsplit; x++)
-    if (x != split && mask.any(p0, p1, x * kChunk, x * kChunk + kChunk)) only = false;
-  for (int i = tid; i < ncol * HD; i += 256) {
-    const int cc = i / HD, d = i - cc * HD;
-    const float M = fmaxf(fmaxf(sm[0][cc], sm[1][cc]), fmaxf(sm[2][cc], sm[3][cc]));
-    float acc = 0.f, L = 0.f;
+    if (x != split && mask.any(p0, p1, x * CH, x * CH + CH)) only = false;
+  if (only) {
+    const float inv = 1.0f / L;
+    uint16_t* op = out + ((int64_t)b * T + t) * ((int64_t)Hkv * G * HD) + (kvh * G + c % G) * HD + 4 * g;
 #pragma unroll
-    for (int w = 0; w < 4; w++) {
-      const float a = sm[w][cc] == -INFINITY && sl[w][cc] == 0.f ? 0.f : __builtin_amdgcn_exp2f(sm[w][cc] - M);
-      acc += a * so[w][cc][d];
-      L += a * sl[w][cc];
+    for (int i = 0; i < ND; i++) {
+      mx_u32x2 w;
+#pragma unroll
+      for (int e = 0; e < 2; e++)
+        w[e] = (uint32_t)f32_to_bf16(o[i][2 * e] * inv) | ((uint32_t)f32_to_bf16(o[i][2 * e + 1] * inv) << 16);
+      *reinterpret_cast<mx_u32x2*>(op + 16 * i) = w;
     }
-    const int64_t row = (hb * T) * G + c0 + cc;
-    if (only) {
-      const int ct = (c0 + cc) / G, hq = kvh * G + (c0 + cc) % G;
-      out[((int64_t)b * T + ct) * (Hkv * G * HD) + hq * HD + d] = f32_to_bf16(acc / L);
-    } else {
-      part_o[(row * nsplit + split) * HD + d] = acc;
-      if (d == 0) part_ml[row * nsplit + split] = make_float2(M, L);
-    }
+  } else {
+    const int64_t row = hb * T * G + c;
+#pragma unroll
+    for (int i = 0; i < ND; i++) *reinterpret_cast<f32x4*>(part_o + (row * nsplit + split) * HD + 16 * i + 4 * g) = o[i];
+    if (g == 0) part_ml[row * nsplit + split] = make_float2(M, L);
   }
 }
 
 // Joins the splits of a column: a wave per column, HD / 64 dims to a lane.
-template <int HD>
+// TILE: columns whose positions decide together which splits have run.
+template <int HD, int TILE>
 __global__ __launch_bounds__(64) void attn_kv8_join_kernel(const float* __restrict__ part_o, const float2* __restrict__ part_ml,
                                                            const int32_t* __restrict__ lens, const int32_t* __restrict__ counts,
-                                                           int Hkv, int G, int T, int cap, int nsplit, Mask mask,
+                                                           int Hkv, int G, int T, int cap, int nsplit, int chunk, Mask mask,
                                                            uint16_t* __restrict__ out) {
   const int c = blockIdx.x, kvh = blockIdx.y, b = blockIdx.z, lane = threadIdx.x;
   int len;
   const int n = new_tokens(lens, counts, b, T, cap, len);
   if (c >= n * G) return;
-  const int c0 = c & ~15, ncol = min(16, n * G - c0), p0 = len + c0 / G, p1 = len + (c0 + ncol - 1) / G;
+  const int c0 = c / TILE * TILE, ncol = min(TILE, n * G - c0), p0 = len + c0 / G, p1 = len + (c0 + ncol - 1) / G;
   const int64_t hb = (int64_t)b * Hkv + kvh, row = hb * T * G + c;
   float M = -INFINITY;
   int used = 0;
   for (int x = 0; x < nsplit; x++)
-    if (mask.any(p0, p1, x * kChunk, x * kChunk + kChunk)) {
+    if (mask.any(p0, p1, x * chunk, x * chunk + chunk)) {
       M = fmaxf(M, part_ml[row * nsplit + x].x);
       used++;
     }
   if (used <= 1) return;  // written by the only split
   float acc[HD / 64] = {}, L = 0.f;
   for (int x = 0; x < nsplit; x++) {
-    if (!mask.any(p0, p1, x * kChunk, x * kChunk + kChunk)) continue;
+    if (!mask.any(p0, p1, x * chunk, x * chunk + chunk)) continue;
     const float2 ml = part_ml[row * nsplit + x];
     const float a = ml.x == -INFINITY && ml.y == 0.f ? 0.f : __builtin_amdgcn_exp2f(ml.x - M);
     L += a * ml.y;
@@ -269,40 +392,71 @@ __global__ __launch_bounds__(64) void attn_kv8_join_kernel(const float* __restri
   const int t = c / G, hq = kvh * G + c % G;
 #pragma unroll
   for (int i = 0; i < HD / 64; i++)
-    out[((int64_t)b * T + t) * (Hkv * G * HD) + hq * HD + lane + 64 * i] = f32_to_bf16(acc[i] / L);
+    out[((int64_t)b * T + t) * ((int64_t)Hkv * G * HD) + hq * HD + lane + 64 * i] = f32_to_bf16(acc[i] / L);
 }
 
-// Prompts: a workgroup of eight waves takes 256 columns of one (sequence,
-// key/value head), each wave 32, and walks the cache in steps of 8 KB of keys
-// and of values (64 tokens of 128 dims, 128 of 64).  Each thread fetches 16
-// bytes of codes of both a step ahead, converts them and stores them as bf16
-// in the order of the matrix operands, so a conversion serves 256 columns and
-// the products read LDS a lane's 16 bytes in a row.  Keys run one step ahead
-// of values: the scores of step s + 1 are multiplied while the exponentials
-// of step s are taken.  The block scales cost nothing per score: the keys'
-// goes into the exponent's factor, the values' (a power of two) into its
-// summand, from which the row sums are freed once per block.
+// ---- many columns
+// A workgroup of eight waves takes 256 columns of one (sequence, key/value
+// head), each wave 32, and walks the cache block by block.  A block's codes
+// come straight to LDS kAhead steps ahead, are converted once and stored as
+// bf16 in the order of the matrix operands, so a conversion serves 256 columns
+// and the products read a lane's 16 bytes in a row.
+//
+// A step has two phases, a barrier after each: one for the vector unit
+// (maxima, exponentials), one for the matrix unit (the block's values, the
+// next block's scores; behind them the conversion, which evens them out).  The waves of a SIMD, w and w + 4, are a phase
+// apart, so that the units work side by side: in a wave's own stream, vector
+// instructions between products only delay them (64 products took 2000 cycles
+// by themselves and 2900 with 110 vector instructions among them), and with
+// both waves in the same phase a step took 5500 cycles.
+//
+// The block scales cost nothing per score: the keys' goes into the exponent's
+// factor, the values' (a power of two) into its summand, and the row sums
+// are a product too, with ones over that scale.  Up to kJoinCols columns the length is split
+// too, kPromptChunk tokens to a workgroup, and joined.
+constexpr int kTileCols = 256;
+constexpr int kJoinCols = 1024;
+constexpr int kPromptChunk = 1024;
+constexpr int kAhead = 3;  // steps that a block's codes are asked for ahead
+constexpr int kReads = 8;  // operands read ahead of their products
+
+// 16 bytes a lane from memory to LDS, lane l's at lds + 16 l.  In assembly:
+// with the builtin the compiler waits for every load before any read of the
+// ring; the waits are written out where they belong.
+__device__ inline void load_lds(const uint8_t* p, u32x4* lds) {
+  const uint32_t at = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) u32x4*)lds;
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off"
+               :: "s"(__builtin_amdgcn_readfirstlane((int)at)), "v"(p) : "m0", "memory");
+}
+
+// s_waitcnt vmcnt(n) alone
+constexpr int vmcnt_imm(int n) { return (n & 15) | ((n >> 4) << 14) | 0xF70; }
+
 template <int HD>
 __global__ __launch_bounds__(512, 2) void attn_kv8_prompt_kernel(
     const uint16_t* __restrict__ q, const uint8_t* __restrict__ kc, const float* __restrict__ ks,
     const uint8_t* __restrict__ vc, const float* __restrict__ vs, const int32_t* __restrict__ lens,
-    const int32_t* __restrict__ counts, int B, int Hkv, int G, int T, int cap, int ntile, Mask mask, float sl2,
-    uint16_t* __restrict__ out) {
-  constexpr int NC = HD / 64, ND = HD / 16, NB = 128 / HD, TB = NB * kBlk;  // blocks and tokens of a step
-  constexpr int KQ = HD / 32;                                               // 32-dim steps of a score
-  __shared__ u32x4 sk[2][1024], sv[2][1024];  // 16 KB each
+    const int32_t* __restrict__ counts, int B, int Hkv, int G, int T, int cap, int ntile, int nsplit, Mask mask, float sl2,
+    float* __restrict__ part_o, float2* __restrict__ part_ml, uint16_t* __restrict__ out) {
+  constexpr int ND = HD / 16, KQ = HD / 32;  // dim tiles; 32-dim steps of a score
+  constexpr int NP = HD / 64;                // 4 KB of codes of keys (and of values) of a block
+  __shared__ u32x4 sk[2][NP * 512], sv[2][NP * 512];
+  __shared__ u32x4 raw[kAhead][8][NP][64];  // codes on their way, by wave
   const int npair = B * Hkv;
   // pairs fastest: with a multiple of eight pairs all tiles of a pair run on
   // one XCD and share its L2; the longest tiles first
-  const int pair = blockIdx.x % npair, c0 = (ntile - 1 - (int)blockIdx.x / npair) * 256;
+  const int pair = blockIdx.x % npair, rest = blockIdx.x / npair, split = rest % nsplit;
+  const int c0 = (ntile - 1 - rest / nsplit) * kTileCols;
   const int b = pair / Hkv, kvh = pair % Hkv;
   int len;
   const int n = new_tokens(lens, counts, b, T, cap, len);
-  const int ncol = min(256, n * G - c0);
+  const int ncol = min(kTileCols, n * G - c0);
   if (ncol <= 0) return;
+  const int p0 = len + c0 / G, p1 = len + (c0 + ncol - 1) / G;
+  const int jlo = nsplit > 1 ? split * kPromptChunk : 0, jhi = nsplit > 1 ? jlo + kPromptChunk : cap;
+  if (!mask.any(p0, p1, jlo, jhi)) return;
   const int tid = threadIdx.x, lane = tid & 63, col = lane & 15, g = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int p0 = len + c0 / G, p1 = len + (c0 + ncol - 1) / G;
   // the wave's columns (past the last: the last one's again)
   const int w0 = min(c0 + wave * 32, c0 + ncol - 1), w1 = min(c0 + wave * 32 + 31, c0 + ncol - 1);
   const bool works = wave * 32 < ncol;
@@ -319,167 +473,249 @@ __global__ __launch_bounds__(512, 2) void attn_kv8_prompt_kernel(
   }
   const int64_t blk0 = (int64_t)pair * (cap / kBlk);
   const uint8_t *kp = kc + blk0 * (kBlk * HD), *vp = vc + blk0 * (kBlk * HD);
-  const int nsteps = p1 / TB + 1;
-  const int64_t bytes = (int64_t)cap * HD;
-  const int w_step = mask.window ? max(0, p0 - mask.window + 1) / TB : 0;  // first step that the window reaches
-  auto after = [&](int s) __attribute__((always_inline)) {
-    const int x = s + 1;
-    return x * TB >= mask.sinks && x < w_step ? w_step : x;
-  };
+  // blocks bfirst .. bend - 1 of this split, those between the sinks and the
+  // window left out
+  const int bend = min(min(jhi, cap) - 1, p1) / kBlk + 1;
+  const int bwin = mask.window ? max(0, p0 - mask.window + 1) / kBlk : 0;  // first block that the window reaches
+  auto skip = [&](int x) __attribute__((always_inline)) { return x * kBlk >= mask.sinks && x < bwin ? bwin : x; };
+  auto after = [&](int x) __attribute__((always_inline)) { return skip(x + 1); };
   const u32x4 zero = {0, 0, 0, 0};
-  auto fetch = [&](const uint8_t* p, int s) __attribute__((always_inline)) {
-    const int64_t off = (int64_t)s * 8192 + tid * 16;
-    return s < nsteps && off < bytes ? *reinterpret_cast<const u32x4*>(p + off) : zero;
+  // a thread's 16 bytes of a block's codes: of keys and of values (128 dims),
+  // or of one of them (64 dims: waves 0 to 3 keys, 4 to 7 values)
+  constexpr bool kBoth = HD == 128;
+  const bool keys = kBoth || wave < 4, values = kBoth || wave >= 4;
+  const int at = kBoth ? tid : tid & 255;
+  // a block's codes straight to the wave's place in LDS (past the end: the
+  // last block's again, so that the loads in flight stay countable)
+  auto fetch = [&](int slot, int xk, int xv) __attribute__((always_inline)) {
+    if (keys) load_lds(kp + (int64_t)min(xk, bend - 1) * (kBlk * HD) + at * 16, raw[slot][wave][0]);
+    if (values) load_lds(vp + (int64_t)min(xv, bend - 1) * (kBlk * HD) + at * 16, raw[slot][wave][NP - 1]);
   };
   auto stash = [&](u32x4* to, u32x4 w) __attribute__((always_inline)) {
-    u32x4* at = to + (tid >> 6) * 128 + lane;
-    at[0] = __builtin_bit_cast(u32x4, fp8_bf16(w[0], w[1]));
-    at[64] = __builtin_bit_cast(u32x4, fp8_bf16(w[2], w[3]));
-  };
-  // scores of step s: token tile i of the step, column tile x
-  f32x4 sc[NB * 4][2], sn[NB * 4][2];
-  auto scores = [&](f32x4(&o)[NB * 4][2], const u32x4* k) __attribute__((always_inline)) {
-#pragma unroll
-    for (int i = 0; i < NB * 4; i++)
-#pragma unroll
-      for (int x = 0; x < KQ; x++) {
-        const bf16x8 kf = __builtin_bit_cast(bf16x8, k[(i * KQ + x) * 64 + lane]);
-#pragma unroll
-        for (int y = 0; y < 2; y++)
-          o[i][y] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, qf[y][x], x == 0 ? f32x4{} : o[i][y], 0, 0, 0);
-      }
+    u32x4* d = to + (at >> 6) * 128 + lane;
+    d[0] = __builtin_bit_cast(u32x4, fp8_bf16(w[0], w[1]));
+    d[64] = __builtin_bit_cast(u32x4, fp8_bf16(w[2], w[3]));
   };
   f32x4 acc[ND][2] = {};
-  float m[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f};
+  f32x4 sc[4][2];   // scores of a block
+  bf16x8 pf[2][2];  // its probabilities
+  float m[2] = {-INFINITY, -INFINITY};
+  f32x4 l[2] = {};  // row sums: the product of the probabilities with ones, four times
+  // (two tiles by turns: a product waits for none of the three before it)
+  auto scores = [&](const u32x4* k) __attribute__((always_inline)) {
+#pragma unroll
+    for (int i = 0; i < 4; i += 2)
+#pragma unroll
+      for (int x = 0; x < KQ; x++)
+#pragma unroll
+        for (int e = 0; e < 2; e++) {
+          const bf16x8 kf = __builtin_bit_cast(bf16x8, k[((i + e) * KQ + x) * 64 + lane]);
+#pragma unroll
+          for (int y = 0; y < 2; y++)
+            sc[i + e][y] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, qf[y][x], x == 0 ? f32x4{} : sc[i + e][y], 0, 0, 0);
+        }
+  };
+  bf16x8 ones;  // over the values' scale, which the probabilities hold
+  auto add_values = [&](const u32x4* v) __attribute__((always_inline)) {
+#pragma unroll
+    for (int x = 0; x < 2; x++)
+#pragma unroll
+      for (int y = 0; y < 2; y++) l[y] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ones, pf[y][x], l[y], 0, 0, 0);
+#pragma unroll
+    for (int i = 0; i < ND; i += 2)
+#pragma unroll
+      for (int x = 0; x < 2; x++)
+#pragma unroll
+        for (int e = 0; e < 2; e++) {
+          const bf16x8 vf = __builtin_bit_cast(bf16x8, v[((i + e) * 2 + x) * 64 + lane]);
+#pragma unroll
+          for (int y = 0; y < 2; y++) acc[i + e][y] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, pf[y][x], acc[i + e][y], 0, 0, 0);
+        }
+  };
+  // Waits for the wave's LDS accesses and meets the others; the loads go on
+  // (__syncthreads would wait for them).
+  auto phase = [&]() __attribute__((always_inline)) {
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_s_waitcnt(0xC07F);  // lgkmcnt(0)
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+  };
 
-  int s = mask.window && mask.sinks == 0 ? w_step : 0;
-  int s1 = after(s);
-  u32x4 kr = fetch(kp, s), vr = fetch(vp, s);
-  stash(sk[0], kr);
-  stash(sv[0], vr);
-  kr = fetch(kp, s1);
-  vr = fetch(vp, s1);
+  // a step works on block x[0], the ones after it are x[1], x[2], ..
+  int x[kAhead + 3];
+  x[0] = skip(jlo / kBlk);
+#pragma unroll
+  for (int i = 1; i < kAhead + 3; i++) x[i] = after(x[i - 1]);
+  if (keys) {
+    const u32x4* p = reinterpret_cast<const u32x4*>(kp + at * 16);
+    stash(sk[0], p[(int64_t)x[0] * (kBlk * HD / 16)]);
+    stash(sk[1], x[1] < bend ? p[(int64_t)x[1] * (kBlk * HD / 16)] : zero);
+  }
+  if (values) stash(sv[0], reinterpret_cast<const u32x4*>(vp + at * 16)[(int64_t)x[0] * (kBlk * HD / 16)]);
+#pragma unroll
+  for (int i = 0; i < kAhead; i++) fetch(i, x[i + 2], x[i + 1]);
+  float fk = ks[blk0 + x[0]] * sl2, fv = vs[blk0 + x[0]];
   __syncthreads();
-  scores(sc, sk[0]);
-  stash(sk[1], kr);
-  kr = fetch(kp, after(s1));
+  scores(sk[0]);
   __syncthreads();
-  for (int it = 0; s < nsteps; it++) {
-    // here: sc the scores of s; sk[(it + 1) & 1] the keys of s1, kr the next
-    // ones; sv[it & 1] the values of s, vr those of s1
-    const int s2 = after(s1);
-    stash(sv[(it + 1) & 1], vr);
-    vr = fetch(vp, s2);
+  // Step t, phase one (the vector unit): the probabilities of x[0] from its
+  // scores.  Phase two (the matrix unit): x[0]'s values, x[1]'s scores; then
+  // the keys of x[2] and the values of x[1] are stored, at places that the
+  // last wave has read a phase ago.
+  int par = 0, slot = 0;
+  if (wave >= 4) phase();
+  while (x[0] < bend) {
+    // the next block's scales, asked for before the phase's work
+    const int64_t bn = blk0 + min(x[1], bend - 1);
+    const float nk = ks[bn], nv = vs[bn];
+    __builtin_amdgcn_sched_barrier(0);
     if (works) {
-      scores(sn, sk[(it + 1) & 1]);
+      const int j0 = x[0] * kBlk;
+      if (!mask.all(q0, q1, j0, j0 + kBlk)) {
+        // NaN in a scale: the visible tokens' scores take it, and the others
+        // are left out as ever
+        const bool nan = fk != fk || fv != fv;
 #pragma unroll
-      for (int h = 0; h < NB; h++) {
-        const int j0 = s * TB + h * kBlk;
-        if (j0 >= cap || !mask.any(q0, q1, j0, j0 + kBlk)) continue;
-        const float fk = ks[blk0 + j0 / kBlk] * sl2, fv = vs[blk0 + j0 / kBlk];
-        // log2 of the values' scale (a power of two; NaN stays NaN)
-        const float ev = fv == fv ? (float)((int)(__builtin_bit_cast(uint32_t, fv) >> 23) - 127) : fv;
-        const float unscale = fv == fv ? 1.0f / fv : 1.0f;
-        const bool whole = mask.all(q0, q1, j0, j0 + kBlk);
-        bf16x8 pf[2][2];
+        for (int i = 0; i < 4; i++)
 #pragma unroll
-        for (int y = 0; y < 2; y++) {
-          float mx = -INFINITY;
-          if (!whole) {
-#pragma unroll
-            for (int i = 0; i < 4; i++)
-#pragma unroll
-              for (int r = 0; r < 4; r++)
-                if (!mask.sees(pos[y], j0 + 16 * i + 4 * g + r)) sc[4 * h + i][y][r] = -INFINITY;
-          }
-#pragma unroll
-          for (int i = 0; i < 4; i++)
-#pragma unroll
-            for (int r = 0; r < 4; r++) mx = fmaxf(mx, sc[4 * h + i][y][r]);
-          mx *= fk;
-          // a column's reference moves only when a score passes it by 2^8
-          if (__ballot(mx > m[y] + 8.0f)) {
-            mx = fmaxf(mx, __shfl_xor(mx, 16, 64));
-            mx = fmaxf(mx, __shfl_xor(mx, 32, 64));
-            if (mx > m[y] + 8.0f) {
-              const float a = __builtin_amdgcn_exp2f(m[y] - mx);
-              l[y] *= a;
-#pragma unroll
-              for (int i = 0; i < ND; i++) acc[i][y] *= a;
-              m[y] = mx;
-            }
-          }
-          const float sub = ev - (m[y] == -INFINITY ? 0.f : m[y]);
-          float sum = 0.f;
-#pragma unroll
-          for (int i = 0; i < 4; i++) {
-            float p[4];
+          for (int y = 0; y < 2; y++)
 #pragma unroll
             for (int r = 0; r < 4; r++) {
-              p[r] = __builtin_amdgcn_exp2f(fmaf(sc[4 * h + i][y][r], fk, sub));
-              if (!whole && sc[4 * h + i][y][r] == -INFINITY) p[r] = 0.f;
+              const bool sees = mask.sees(pos[y], j0 + 16 * i + 4 * g + r);
+              if (nan) sc[i][y][r] = __builtin_bit_cast(float, 0x7fc00000u);
+              if (!sees) sc[i][y][r] = -INFINITY;
             }
-            const bf16x2 a = {(__bf16)p[0], (__bf16)p[1]}, c = {(__bf16)p[2], (__bf16)p[3]}, one = {(__bf16)1.0f, (__bf16)1.0f};
-            sum = __builtin_amdgcn_fdot2_f32_bf16(a, one, sum, false);
-            sum = __builtin_amdgcn_fdot2_f32_bf16(c, one, sum, false);
-#pragma unroll
-            for (int r = 0; r < 2; r++) {
-              pf[y][i >> 1][(i & 1) * 4 + r] = a[r];
-              pf[y][i >> 1][(i & 1) * 4 + 2 + r] = c[r];
-            }
-          }
-          l[y] = fmaf(sum, unscale, l[y]);
-        }
-#pragma unroll
-        for (int i = 0; i < ND; i++)
-#pragma unroll
-          for (int x = 0; x < 2; x++) {
-            const bf16x8 vf = __builtin_bit_cast(bf16x8, sv[it & 1][((h * ND + i) * 2 + x) * 64 + lane]);
-#pragma unroll
-            for (int y = 0; y < 2; y++) acc[i][y] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, pf[y][x], acc[i][y], 0, 0, 0);
-          }
+        if (nan) fk = fv = 1.0f;
       }
+      float mx[2];
 #pragma unroll
-      for (int i = 0; i < NB * 4; i++)
+      for (int y = 0; y < 2; y++) {
+        float v = -INFINITY;
 #pragma unroll
-        for (int y = 0; y < 2; y++) sc[i][y] = sn[i][y];
+        for (int i = 0; i < 4; i++)
+#pragma unroll
+          for (int r = 0; r < 4; r++) v = fmaxf(v, sc[i][y][r]);
+        mx[y] = v * fk;
+      }
+      // a column's reference moves only when a score passes it by 2^8
+      if (__ballot(mx[0] > m[0] + 8.0f || mx[1] > m[1] + 8.0f)) {
+#pragma unroll
+        for (int y = 0; y < 2; y++) {
+          float v = fmaxf(mx[y], __shfl_xor(mx[y], 16, 64));
+          v = fmaxf(v, __shfl_xor(v, 32, 64));
+          if (v > m[y] + 8.0f) {
+            const float a = __builtin_amdgcn_exp2f(m[y] - v);
+            l[y] *= a;
+#pragma unroll
+            for (int i = 0; i < ND; i++) acc[i][y] *= a;
+            m[y] = v;
+          }
+        }
+      }
+      // log2 of the values' scale (a power of two; NaN stays NaN)
+      const float ev = fv == fv ? (float)((int)(__builtin_bit_cast(uint32_t, fv) >> 23) - 127) : fv;
+      const __bf16 unscale = (__bf16)(fv == fv ? __builtin_amdgcn_rcpf(fv) : 1.0f);  // exact
+      ones = bf16x8{unscale, unscale, unscale, unscale, unscale, unscale, unscale, unscale};
+#pragma unroll
+      for (int y = 0; y < 2; y++) {
+        const float sub = ev - (m[y] == -INFINITY ? 0.f : m[y]);
+#pragma unroll
+        for (int i = 0; i < 4; i++) {
+          float p[4];
+#pragma unroll
+          for (int r = 0; r < 4; r++) p[r] = __builtin_amdgcn_exp2f(fmaf(sc[i][y][r], fk, sub));
+          const bf16x2 u = {(__bf16)p[0], (__bf16)p[1]}, w = {(__bf16)p[2], (__bf16)p[3]};
+#pragma unroll
+          for (int r = 0; r < 2; r++) {
+            pf[y][i >> 1][(i & 1) * 4 + r] = u[r];
+            pf[y][i >> 1][(i & 1) * 4 + 2 + r] = w[r];
+          }
+        }
+      }
+      // (kept here: the compiler would move the exponentials to their use)
+#pragma unroll
+      for (int y = 0; y < 2; y++)
+#pragma unroll
+        for (int e = 0; e < 2; e++) asm volatile("" : "+v"(pf[y][e]));
     }
-    stash(sk[it & 1], kr);
-    kr = fetch(kp, after(s2));
-    __syncthreads();
-    s = s1;
-    s1 = s2;
+    __builtin_amdgcn_sched_barrier(0);
+    fk = nk * sl2;
+    fv = nv;
+    phase();
+    __builtin_amdgcn_s_waitcnt(vmcnt_imm((kAhead - 1) * NP));
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_sched_barrier(0);
+    u32x4 kr = zero, vr = zero;
+    if (keys) kr = raw[slot][wave][0][lane];
+    if (values) vr = raw[slot][wave][NP - 1][lane];
+    __builtin_amdgcn_sched_barrier(0);
+    if (works) {
+      add_values(sv[par]);
+      scores(sk[par ^ 1]);
+      // operands read kReads ahead, two products to a read
+      __builtin_amdgcn_sched_group_barrier(0x100, kReads, 0);
+#pragma unroll
+      for (int i = 0; i < 2 + 2 * ND + 4 * KQ; i++) {
+        __builtin_amdgcn_sched_group_barrier(0x008, 2, 0);
+        __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+      }
+    }
+    __builtin_amdgcn_sched_barrier(0);
+    if (keys) stash(sk[par], kr);
+    if (values) stash(sv[par ^ 1], vr);
+    __builtin_amdgcn_sched_barrier(0);
+    phase();
+    __builtin_amdgcn_sched_barrier(0);
+    fetch(slot, x[kAhead + 2], x[kAhead + 1]);  // into what this step has read
+    slot = slot == kAhead - 1 ? 0 : slot + 1;
+    par ^= 1;
+#pragma unroll
+    for (int i = 0; i < kAhead + 2; i++) x[i] = x[i + 1];
+    x[kAhead + 2] = after(x[kAhead + 1]);
   }
+  if (wave < 4) phase();
+  __builtin_amdgcn_s_waitcnt(vmcnt_imm(0));  // no load to LDS outlives the workgroup
   if (!works) return;
+  bool only = true;
+  for (int x = 0; x < nsplit; x++)
+    if (nsplit > 1 && x != split && mask.any(p0, p1, x * kPromptChunk, x * kPromptChunk + kPromptChunk)) only = false;
 #pragma unroll
   for (int y = 0; y < 2; y++) {
     const int c = w0 + 16 * y + col;
-    float L = l[y];
-    L += __shfl_xor(L, 16, 64);
-    L += __shfl_xor(L, 32, 64);
+    const float L = l[y][0];
     if (c > w1) continue;
-    const float inv = 1.0f / L;
-    uint16_t* op = out + ((int64_t)b * T + c / G) * ((int64_t)Hkv * G * HD) + (kvh * G + c % G) * HD + 4 * g;
+    if (only) {
+      const float inv = 1.0f / L;
+      uint16_t* op = out + ((int64_t)b * T + c / G) * ((int64_t)Hkv * G * HD) + (kvh * G + c % G) * HD + 4 * g;
 #pragma unroll
-    for (int i = 0; i < ND; i++) {
-      mx_u32x2 w;
+      for (int i = 0; i < ND; i++) {
+        mx_u32x2 w;
 #pragma unroll
-      for (int e = 0; e < 2; e++)
-        w[e] = (uint32_t)f32_to_bf16(acc[i][y][2 * e] * inv) | ((uint32_t)f32_to_bf16(acc[i][y][2 * e + 1] * inv) << 16);
-      *reinterpret_cast<mx_u32x2*>(op + 16 * i) = w;
+        for (int e = 0; e < 2; e++)
+          w[e] = (uint32_t)f32_to_bf16(acc[i][y][2 * e] * inv) | ((uint32_t)f32_to_bf16(acc[i][y][2 * e + 1] * inv) << 16);
+        *reinterpret_cast<mx_u32x2*>(op + 16 * i) = w;
+      }
+    } else {
+      const int64_t row = (int64_t)pair * T * G + c;
+#pragma unroll
+      for (int i = 0; i < ND; i++) *reinterpret_cast<f32x4*>(part_o + (row * nsplit + split) * HD + 16 * i + 4 * g) = acc[i][y];
+      if (g == 0) part_ml[row * nsplit + split] = make_float2(m[y], L);
     }
   }
 }
 
-// Columns up to which a (sequence, key/value head) takes the split form.
-constexpr int kSplitCols = 64;
+// Splits of the length: by the number of columns and the cache alone, so that
+// a query's result does not depend on the other sequences.
+int splits_of(int64_t cols, int hd, int cap) {
+  const int chunk = cols <= kSplitCols ? split_tokens(hd) : kPromptChunk;
+  return cols <= kJoinCols ? (cap + chunk - 1) / chunk : 1;
+}
 
 }  // namespace
 
 int64_t kv8_workspace_bytes(int B, int Hq, int Hkv, int T, int hd, int cap) {
-  const int64_t nsplit = (cap + kChunk - 1) / kChunk;
-  if (nsplit <= 1 || (int64_t)T * (Hq / Hkv) > kSplitCols) return 0;
-  return (int64_t)B * Hq * T * nsplit * (hd + 2) * 4;
+  const int64_t nsplit = splits_of((int64_t)T * (Hq / Hkv), hd, cap);
+  return nsplit > 1 ? (int64_t)B * Hq * T * nsplit * (hd + 2) * 4 : 0;
 }
 
 hipError_t launch_kv8_append(const uint16_t* k, const uint16_t* v, int B, int Hkv, int T, int hd, int cap,
@@ -494,23 +730,28 @@ hipError_t launch_kv8_append(const uint16_t* k, const uint16_t* v, int B, int Hk
 hipError_t launch_attention_kv8(const uint16_t* q, int B, int Hq, int Hkv, int T, int hd, int cap, const int32_t* lens,
                                 const int32_t* counts, const uint8_t* kc, const float* ks, const uint8_t* vc,
                                 const float* vs, int window, int sinks, void* ws, uint16_t* out, hipStream_t s) {
-  const int G = Hq / Hkv, nsplit = (cap + kChunk - 1) / kChunk, ntile = (T * G + 15) / 16;
+  const int G = Hq / Hkv;
+  const int64_t cols = (int64_t)T * G;
+  const int nsplit = splits_of(cols, hd, cap);
   const Mask mask{window, sinks};
   const float sl2 = (float)(1.4426950408889634 / sqrt((double)hd));
   float* po = (float*)ws;
-  float2* pml = (float2*)(po + (int64_t)B * Hq * T * nsplit * hd);
+  float2* pml = nsplit > 1 ? (float2*)(po + (int64_t)B * Hq * T * nsplit * hd) : nullptr;
   auto go = [&](auto h) {
     constexpr int HD = decltype(h)::value;
-    if ((int64_t)T * G > kSplitCols) {
-      const int tiles = (int)(((int64_t)T * G + 255) / 256);
-      attn_kv8_prompt_kernel<HD><<<dim3((unsigned)tiles * B * Hkv), 512, 0, s>>>(q, kc, ks, vc, vs, lens, counts, B, Hkv, G, T,
-                                                                               cap, tiles, mask, sl2, out);
-      return;
+    const dim3 join((unsigned)cols, Hkv, B);
+    if (cols <= kSplitCols) {
+      attn_kv8_split_kernel<HD><<<dim3(nsplit * (unsigned)((cols + 15) / 16), Hkv, B), kSplitWaves * 64, 0, s>>>(
+          q, kc, ks, vc, vs, lens, counts, Hkv, G, T, cap, nsplit, mask, sl2, po, pml, out);
+      if (nsplit > 1)
+        attn_kv8_join_kernel<HD, 16><<<join, 64, 0, s>>>(po, pml, lens, counts, Hkv, G, T, cap, nsplit, split_tokens(HD), mask, out);
+    } else {
+      const int ntile = (int)((cols + kTileCols - 1) / kTileCols);
+      attn_kv8_prompt_kernel<HD><<<(unsigned)((int64_t)ntile * nsplit * B * Hkv), 512, 0, s>>>(
+          q, kc, ks, vc, vs, lens, counts, B, Hkv, G, T, cap, ntile, nsplit, mask, sl2, po, pml, out);
+      if (nsplit > 1)
+        attn_kv8_join_kernel<HD, kTileCols><<<join, 64, 0, s>>>(po, pml, lens, counts, Hkv, G, T, cap, nsplit, kPromptChunk, mask, out);
     }
-    attn_kv8_split_kernel<HD><<<dim3(nsplit * ntile, Hkv, B), 256, 0, s>>>(q, kc, ks, vc, vs, lens, counts, Hkv, G, T, cap,
-                                                                           nsplit, mask, sl2, po, pml, out);
-    if (nsplit > 1)
-      attn_kv8_join_kernel<HD><<<dim3(T * G, Hkv, B), 64, 0, s>>>(po, pml, lens, counts, Hkv, G, T, cap, nsplit, mask, out);
   };
   if (hd == 64) go(std::integral_constant<int, 64>{});
   else go(std::integral_constant<int, 128>{});

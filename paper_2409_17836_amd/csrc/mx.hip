@@ -2,6 +2,7 @@
 // the way back, the block layout of weights, and the residual add with
 // RMSNorm whose output is microscaled.  All are bound by the bytes they move.
 #include <algorithm>
+#include <type_traits>
 
 #include "mx.h"
 
@@ -35,7 +36,20 @@ __global__ __launch_bounds__(256) void mx_quantize_kernel(const T* __restrict__ 
 }
 
 // -------------------------------------------------------------- dequantise
-template <int FMT, typename T>
+__device__ inline void store8(float* p, const float (&v)[8]) {
+  *reinterpret_cast<mx_f32x4*>(p) = mx_f32x4{v[0], v[1], v[2], v[3]};
+  *reinterpret_cast<mx_f32x4*>(p + 4) = mx_f32x4{v[4], v[5], v[6], v[7]};
+}
+__device__ inline void store8(uint16_t* p, const float (&v)[8]) {
+  typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+  mx_u32x4 w;
+#pragma unroll
+  for (int i = 0; i < 4; i++) w[i] = __builtin_bit_cast(uint32_t, bf16x2{(__bf16)v[2 * i], (__bf16)v[2 * i + 1]});
+  *reinterpret_cast<mx_u32x4*>(p) = w;
+}
+
+// A thread: 8 columns.  VEC: as above, for the output.
+template <int FMT, typename T, bool VEC>
 __global__ __launch_bounds__(256) void mx_dequantize_kernel(const uint8_t* __restrict__ codes,
                                                             const uint8_t* __restrict__ scales, int64_t rows, int cols,
                                                             T* __restrict__ out, int64_t ld) {
@@ -64,10 +78,16 @@ __global__ __launch_bounds__(256) void mx_dequantize_kernel(const uint8_t* __res
     }
     T* p = out + row * ld + 8 * (int64_t)c;
 #pragma unroll
-    for (int i = 0; i < 8; i++) {
-      if (8 * c + i >= cols) continue;
-      if constexpr (sizeof(T) == 2) p[i] = f32_to_bf16(v[i] * s);
-      else p[i] = v[i] * s;
+    for (int i = 0; i < 8; i++) v[i] *= s;
+    if constexpr (VEC) {
+      store8(p, v);
+    } else {
+#pragma unroll
+      for (int i = 0; i < 8; i++) {
+        if (8 * c + i >= cols) continue;
+        if constexpr (sizeof(T) == 2) p[i] = f32_to_bf16(v[i]);
+        else p[i] = v[i];
+      }
     }
   }
 }
@@ -98,71 +118,67 @@ __global__ __launch_bounds__(256) void mx_block_kernel(const uint8_t* __restrict
 }
 
 // -------------------------------------------------------- add and RMSNorm
-__device__ inline float wave_sum(float v) {
-#pragma unroll
-  for (int o = 32; o; o >>= 1) v += __shfl_xor(v, o, 64);
-  return v;
-}
-
-__device__ inline void store8(float* p, const float (&v)[8]) {
-  *reinterpret_cast<mx_f32x4*>(p) = mx_f32x4{v[0], v[1], v[2], v[3]};
-  *reinterpret_cast<mx_f32x4*>(p + 4) = mx_f32x4{v[4], v[5], v[6], v[7]};
-}
-__device__ inline void store8(uint16_t* p, const float (&v)[8]) {
-  mx_u32x4 w;
-#pragma unroll
-  for (int i = 0; i < 4; i++) w[i] = (uint32_t)f32_to_bf16(v[2 * i]) | ((uint32_t)f32_to_bf16(v[2 * i + 1]) << 16);
-  *reinterpret_cast<mx_u32x4*>(p) = w;
-}
-
 // A block per row; thread t keeps columns 8 (t + 256 i) .. + 7 in registers
 // between the sum of squares and the codes, so a row is read once.  The sum
 // that is normalised is the one that is stored.
+//
+// A code is the rounding of y, and an error in y of e turns some e / 2^-4 of
+// the codes into their neighbours, so y is kept closer than its float32
+// factors: the lanes' sums meet in float64, the root's reciprocal is taken as
+// a float32 and what that leaves, and the product with x carries its rounding
+// error along.  The kernel is bound by its memory traffic either way.
 template <int FMT, typename TH, typename TX, typename TG, int NC>
 __global__ __launch_bounds__(256) void add_norm_mx_kernel(const TH* h, const TX* __restrict__ x,
                                                           const TG* __restrict__ gain, float eps, int d,
                                                           TH* out, uint8_t* __restrict__ codes,
                                                           uint8_t* __restrict__ scales) {
 #pragma clang fp contract(off)
-  __shared__ float part[4];
+  __shared__ double part[4];
   const int64_t row = blockIdx.x;
   const int t = threadIdx.x, nchunks = d / 8;
   const int kcols = (int)mx_cols(d), ns = (int)mx_row_scales(d);
-  float v[NC][8];
+  float v[NC][8], w[NC][8], gn[NC][8];
+#pragma unroll
+  for (int i = 0; i < NC; i++) {
+    const int c = t + 256 * i;
+#pragma unroll
+    for (int e = 0; e < 8; e++) v[i][e] = w[i][e] = gn[i][e] = 0.f;
+    if (c >= nchunks) continue;
+    load8(h + row * d + 8 * c, v[i]);
+    if (x) load8(x + row * d + 8 * c, w[i]);
+    load8(gain + 8 * c, gn[i]);
+  }
   float ss = 0.f;
 #pragma unroll
   for (int i = 0; i < NC; i++) {
     const int c = t + 256 * i;
-#pragma unroll
-    for (int e = 0; e < 8; e++) v[i][e] = 0.f;
-    if (c >= nchunks) continue;
-    load8(h + row * d + 8 * c, v[i]);
     if (x) {
-      float w[8];
-      load8(x + row * d + 8 * c, w);
 #pragma unroll
       for (int e = 0; e < 8; e++) {
-        v[i][e] += w[e];
+        v[i][e] += w[i][e];
         if constexpr (sizeof(TH) == 2) v[i][e] = bf16_to_f32(f32_to_bf16(v[i][e]));
       }
     }
-    if (out) store8(out + row * d + 8 * c, v[i]);
+    if (out && c < nchunks) store8(out + row * d + 8 * c, v[i]);
 #pragma unroll
     for (int e = 0; e < 8; e++) ss += v[i][e] * v[i][e];
   }
-  ss = wave_sum(ss);
-  if ((t & 63) == 0) part[t >> 6] = ss;
+  double sd = ss;
+#pragma unroll
+  for (int o = 32; o; o >>= 1) sd += __shfl_xor(sd, o, 64);
+  if ((t & 63) == 0) part[t >> 6] = sd;
   __syncthreads();
-  ss = (part[0] + part[1]) + (part[2] + part[3]);
-  const float r = 1.0f / sqrtf(ss / (float)d + eps);
+  sd = (part[0] + part[1]) + (part[2] + part[3]);
+  const double rd = 1.0 / sqrt(sd / (double)d + (double)eps);
+  const float r = (float)rd, rlo = (float)(rd - (double)r);
 #pragma unroll
   for (int i = 0; i < NC; i++) {
     const int c = t + 256 * i;
-    if (c < nchunks) {
-      float g[8];
-      load8(gain + 8 * c, g);
 #pragma unroll
-      for (int e = 0; e < 8; e++) v[i][e] = v[i][e] * r * g[e];
+    for (int e = 0; e < 8; e++) {
+      const float p = v[i][e] * r, q = fmaf(v[i][e], r, -p) + v[i][e] * rlo;
+      // (an infinite p has no remainder)
+      v[i][e] = abs_bits(p) < 0x7f800000u ? fmaf(p, gn[i][e], q * gn[i][e]) : p * gn[i][e];
     }
     mx_store8<FMT>(v[i], c, kcols, ns, codes + row * (FMT == LMGC_MX_FP8 ? kcols : kcols / 2), scales + row * ns);
   }
@@ -210,13 +226,21 @@ hipError_t launch_mx_quantize(const void* src, int dtype, int64_t rows, int cols
 hipError_t launch_mx_dequantize(const uint8_t* codes, const uint8_t* scales, int fmt, int64_t rows, int cols, void* out,
                                 int dtype, int64_t ld, hipStream_t s) {
   const int grid = grid_of((rows * ((cols + 7) / 8) + 255) / 256);
-  auto go = [&](auto f) {
-    constexpr int F = decltype(f)::value;
-    if (dtype == LMGC_DTYPE_BF16) mx_dequantize_kernel<F><<<grid, 256, 0, s>>>(codes, scales, rows, cols, (uint16_t*)out, ld);
-    else mx_dequantize_kernel<F><<<grid, 256, 0, s>>>(codes, scales, rows, cols, (float*)out, ld);
+  const bool vec = cols % 8 == 0 && ld * (dtype == LMGC_DTYPE_BF16 ? 2 : 4) % 16 == 0 && ((uintptr_t)out & 15) == 0;
+  auto go = [&](auto f, auto t, auto v) {
+    using T = decltype(t);
+    mx_dequantize_kernel<decltype(f)::value, T, decltype(v)::value><<<grid, 256, 0, s>>>(codes, scales, rows, cols, (T*)out, ld);
   };
-  if (fmt == LMGC_MX_FP8) go(std::integral_constant<int, LMGC_MX_FP8>{});
-  else go(std::integral_constant<int, LMGC_MX_FP4>{});
+  auto go_t = [&](auto f, auto t) {
+    if (vec) go(f, t, std::true_type{});
+    else go(f, t, std::false_type{});
+  };
+  auto go_f = [&](auto f) {
+    if (dtype == LMGC_DTYPE_BF16) go_t(f, uint16_t{});
+    else go_t(f, float{});
+  };
+  if (fmt == LMGC_MX_FP8) go_f(std::integral_constant<int, LMGC_MX_FP8>{});
+  else go_f(std::integral_constant<int, LMGC_MX_FP4>{});
   return hipGetLastError();
 }
 
