@@ -118,29 +118,35 @@ __global__ __launch_bounds__(256) void mx_block_kernel(const uint8_t* __restrict
 }
 
 // -------------------------------------------------------- add and RMSNorm
-// A block per row; thread t keeps columns 8 (t + 256 i) .. + 7 in registers
-// between the sum of squares and the codes, so a row is read once.  The sum
-// that is normalised is the one that is stored.
+// NT threads per row (a wave where d <= 1024, else the block); thread t keeps
+// columns 8 (t + NT i) .. + 7 in registers between the sum of squares and the
+// codes, so a row is read once.  The sum that is normalised is the one that is
+// stored.
 //
 // A code is the rounding of y, and an error in y of e turns some e / 2^-4 of
 // the codes into their neighbours, so y is kept closer than its float32
-// factors: the lanes' sums meet in float64, the root's reciprocal is taken as
-// a float32 and what that leaves, and the product with x carries its rounding
-// error along.  The kernel is bound by its memory traffic either way.
-template <int FMT, typename TH, typename TX, typename TG, int NC>
+// factors: the squares are summed in float64, the root's reciprocal is taken as
+// a float32 and what that leaves, and the products with x and the gain carry
+// their rounding errors along.  What the float32 y at the end leaves decides
+// its lowest bit: where the remainder is not zero an even y becomes the odd
+// neighbour on the remainder's side, so that y lies on a border between two
+// codes only if the value does.  The kernel is bound by its memory traffic
+// either way.
+template <int FMT, typename TH, typename TX, typename TG, int NC, int NT>
 __global__ __launch_bounds__(256) void add_norm_mx_kernel(const TH* h, const TX* __restrict__ x,
-                                                          const TG* __restrict__ gain, float eps, int d,
+                                                          const TG* __restrict__ gain, float eps, int64_t M, int d,
                                                           TH* out, uint8_t* __restrict__ codes,
                                                           uint8_t* __restrict__ scales) {
 #pragma clang fp contract(off)
   __shared__ double part[4];
-  const int64_t row = blockIdx.x;
-  const int t = threadIdx.x, nchunks = d / 8;
+  const int64_t row = (int64_t)blockIdx.x * (256 / NT) + threadIdx.x / NT;
+  if (NT == 64 && row >= M) return;
+  const int t = threadIdx.x % NT, nchunks = d / 8;
   const int kcols = (int)mx_cols(d), ns = (int)mx_row_scales(d);
   float v[NC][8], w[NC][8], gn[NC][8];
 #pragma unroll
   for (int i = 0; i < NC; i++) {
-    const int c = t + 256 * i;
+    const int c = t + NT * i;
 #pragma unroll
     for (int e = 0; e < 8; e++) v[i][e] = w[i][e] = gn[i][e] = 0.f;
     if (c >= nchunks) continue;
@@ -148,10 +154,10 @@ __global__ __launch_bounds__(256) void add_norm_mx_kernel(const TH* h, const TX*
     if (x) load8(x + row * d + 8 * c, w[i]);
     load8(gain + 8 * c, gn[i]);
   }
-  float ss = 0.f;
+  double sd = 0.0;
 #pragma unroll
   for (int i = 0; i < NC; i++) {
-    const int c = t + 256 * i;
+    const int c = t + NT * i;
     if (x) {
 #pragma unroll
       for (int e = 0; e < 8; e++) {
@@ -161,24 +167,33 @@ __global__ __launch_bounds__(256) void add_norm_mx_kernel(const TH* h, const TX*
     }
     if (out && c < nchunks) store8(out + row * d + 8 * c, v[i]);
 #pragma unroll
-    for (int e = 0; e < 8; e++) ss += v[i][e] * v[i][e];
+    for (int e = 0; e < 8; e++) sd = fma((double)v[i][e], (double)v[i][e], sd);
   }
-  double sd = ss;
 #pragma unroll
   for (int o = 32; o; o >>= 1) sd += __shfl_xor(sd, o, 64);
-  if ((t & 63) == 0) part[t >> 6] = sd;
-  __syncthreads();
-  sd = (part[0] + part[1]) + (part[2] + part[3]);
+  if constexpr (NT == 256) {
+    if ((t & 63) == 0) part[t >> 6] = sd;
+    __syncthreads();
+    sd = (part[0] + part[1]) + (part[2] + part[3]);
+  }
   const double rd = 1.0 / sqrt(sd / (double)d + (double)eps);
   const float r = (float)rd, rlo = (float)(rd - (double)r);
 #pragma unroll
   for (int i = 0; i < NC; i++) {
-    const int c = t + 256 * i;
+    const int c = t + NT * i;
 #pragma unroll
     for (int e = 0; e < 8; e++) {
       const float p = v[i][e] * r, q = fmaf(v[i][e], r, -p) + v[i][e] * rlo;
-      // (an infinite p has no remainder)
-      v[i][e] = abs_bits(p) < 0x7f800000u ? fmaf(p, gn[i][e], q * gn[i][e]) : p * gn[i][e];
+      const float a = p * gn[i][e], lo = fmaf(p, gn[i][e], -a) + q * gn[i][e];
+      float y = a;
+      if (abs_bits(a) < 0x7f800000u) {  // (an infinite product has no remainder)
+        y = a + lo;
+        const float rem = lo - (y - a);
+        uint32_t u = __builtin_bit_cast(uint32_t, y);
+        if (rem != 0.f && (u & 1) == 0) u += (rem < 0.f) == (y < 0.f) ? 1u : -1u;
+        y = __builtin_bit_cast(float, u);
+      }
+      v[i][e] = y;
     }
     mx_store8<FMT>(v[i], c, kcols, ns, codes + row * (FMT == LMGC_MX_FP8 ? kcols : kcols / 2), scales + row * ns);
   }
@@ -197,15 +212,20 @@ void quantize(const T* src, int64_t rows, int cols, int64_t ld, uint8_t* codes, 
 template <int FMT, typename TH, typename TX, typename TG>
 void add_norm(const void* h, const void* x, const void* gain, float eps, int64_t M, int d, void* out, uint8_t* codes,
               uint8_t* scales, hipStream_t s) {
-  const int nc = (int)((mx_row_scales(d) * 4 + 255) / 256);  // 512-column groups, 64 threads each
-  auto go = [&](auto n) {
-    add_norm_mx_kernel<FMT, TH, TX, TG, decltype(n)::value><<<(unsigned)M, 256, 0, s>>>(
-        (const TH*)h, (const TX*)x, (const TG*)gain, eps, d, (TH*)out, codes, scales);
+  const int nc = (int)mx_row_scales(d) / 16;  // groups of 512 columns, 64 threads each
+  auto go = [&](auto n, auto nt) {
+    constexpr int NT = decltype(nt)::value;
+    add_norm_mx_kernel<FMT, TH, TX, TG, decltype(n)::value, NT><<<(unsigned)((M + 256 / NT - 1) / (256 / NT)), 256, 0, s>>>(
+        (const TH*)h, (const TX*)x, (const TG*)gain, eps, M, d, (TH*)out, codes, scales);
   };
-  if (nc <= 1) go(std::integral_constant<int, 1>{});
-  else if (nc <= 2) go(std::integral_constant<int, 2>{});
-  else if (nc <= 4) go(std::integral_constant<int, 4>{});
-  else go(std::integral_constant<int, 8>{});
+  using wave = std::integral_constant<int, 64>;
+  using block = std::integral_constant<int, 256>;
+  if (nc <= 1) go(std::integral_constant<int, 1>{}, wave{});
+  else if (nc <= 2) go(std::integral_constant<int, 2>{}, wave{});
+  else if (nc <= 4) go(std::integral_constant<int, 1>{}, block{});
+  else if (nc <= 8) go(std::integral_constant<int, 2>{}, block{});
+  else if (nc <= 16) go(std::integral_constant<int, 4>{}, block{});
+  else go(std::integral_constant<int, 8>{}, block{});
 }
 
 }  // namespace

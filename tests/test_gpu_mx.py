@@ -97,13 +97,12 @@ def test_block_layout(N, K):
 
 
 # ----------------------------------------------------------- add and RMSNorm
-def _check_norm(codes, scales, fmt, y):
-    """Codes and scales of y known to 2^-18 (the float32 sum of d squares of at
-    most 64 terms a lane, its root and three products: under 43 2^-24): the
-    scale is y's, or the neighbour's where amax lies that close to its border;
-    the values are within half a step of y, and that."""
+def _check_norm(codes, scales, fmt, y, delta=2.0 ** -18):
+    """Codes and scales of y known to `delta` (2^-18 would do for a float32 sum
+    of d squares of at most 64 terms a lane, its root and three products: under
+    43 2^-24): the scale is y's, or the neighbour's where amax lies that close
+    to its border; the values are within half a step of y, and that."""
     d = y.shape[1]
-    delta = 2.0 ** -18
     nb = R.up(d, 128) // 32
     byte = np.stack([scales[:, 16 * (j // 16) + 4 * (j % 4) + (j % 16) // 4] for j in range(nb)], 1)
     z = np.zeros((y.shape[0], nb * 32))
@@ -146,6 +145,25 @@ def test_add_norm(fmt, h, x, g, M, d):
     # a row alone gives the row's bits
     c1, s1 = B.op_add_norm_mx(th[M - 1:], None if tx is None else tx[M - 1:], tg, 1e-5, fmt)
     assert torch.equal(c1[0], codes[M - 1]) and torch.equal(s1[0], scales[M - 1])
+
+
+@pytest.mark.parametrize("fmt", ["fp8", "fp4"])
+@pytest.mark.parametrize("h,M,d", [("bf16", 1500, 4096), ("f32", 4003, 768), ("f32", 2001, 1024), ("bf16", 999, 1056)])
+def test_add_norm_next_to_a_border(fmt, h, M, d):
+    """Some values of millions lie within a float32's rounding of the border
+    between two codes; theirs are the nearer codes all the same.  The kernel's y
+    before its last step is off by the float32 corrections' own rounding: of
+    the root's (2^-48), of the two products' (2^-48 each) and of their sums
+    (2 2^-48), under 2^-45, and that step keeps the side of the border."""
+    import torch
+    log(f"add_norm border {fmt} {h} {M}x{d}")
+    r = np.random.default_rng(d)
+    th = _torch(r.standard_normal((M, d)) * 3, h)
+    tg = _torch(1 + 0.1 * r.standard_normal(d), "f32")
+    codes, scales = B.op_add_norm_mx(th, None, tg, 1e-5, fmt)
+    v = _host(th).astype(np.float64)
+    y = v / np.sqrt((v * v).mean(-1, keepdims=True) + float(np.float32(1e-5))) * _host(tg).astype(np.float64)
+    _check_norm(codes.cpu().numpy(), scales.cpu().numpy(), fmt, y, 2.0 ** -44)
 
 
 def test_add_norm_nonfinite_and_zero_rows():
