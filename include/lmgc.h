@@ -572,6 +572,17 @@ enum { LMGC_OP_STORE_BF16 = 3 };
 int lmgc_op_gemm_mx(const uint8_t* d_a, const uint8_t* d_a_scales, int32_t a_fmt,
                     const uint8_t* d_b, const uint8_t* d_b_scales, const float* d_add, void* d_out,
                     int32_t M, int32_t N, int32_t K, int32_t kind, void* stream);
+/* The same on a given tile of the output (tests compare the tiles, which give
+ * the same bits), or on the one the library takes for the shape (tile < 0).
+ * EINVAL for LMGC_MX_TILE_256X256 with FP4 in A, which does not have it. */
+enum {
+  LMGC_MX_TILE_16X16 = 0, LMGC_MX_TILE_32X128 = 1, LMGC_MX_TILE_64X64 = 2, LMGC_MX_TILE_128X128 = 3,
+  LMGC_MX_TILE_128X256 = 4, LMGC_MX_TILE_256X256 = 5
+};
+int lmgc_op_gemm_mx_tile(const uint8_t* d_a, const uint8_t* d_a_scales, int32_t a_fmt,
+                         const uint8_t* d_b, const uint8_t* d_b_scales, const float* d_add,
+                         void* d_out, int32_t M, int32_t N, int32_t K, int32_t kind, int32_t tile,
+                         void* stream);
 
 /*
  * Key/value cache of one layer in 8 bits: B sequences, Hkv heads of hd (64 or
@@ -613,10 +624,14 @@ int lmgc_op_kv8_append(const uint16_t* d_k, const uint16_t* d_v, int32_t B, int3
  *   d_ws: lmgc_kv8_workspace bytes, 16-byte aligned, its contents free; calls
  *   that may run at the same time need one each.
  * Masked keys count for nothing, whatever their block holds; a visible key of
- * a block with a NaN scale gives NaN.  A query's result depends on the cache,
- * on its position and on whether T Hq / Hkv <= 16, not on the other sequences
- * or queries.
- * GPU, async.  Errors: EINVAL, ESIZE, EUNSUPPORTED (hd).
+ * a block with a NaN scale gives NaN.  Scales are powers of two, 2^-64 or more
+ * as appending leaves them; above 2^100 (values of 5e32) sums may overflow.  A
+ * query's result depends on the cache, cap and its position and on which of
+ * three forms T Hq / Hkv falls into (up to 32, to 1024, and above), not on the
+ * other sequences or queries.
+ * T Hq / Hkv <= 2^30; above 32, B Hkv ceil(T Hq / Hkv / 256) < 2^23 (times the
+ * splits of the cache, 16 at most, up to 1024).
+ * GPU, async.  Errors: EINVAL, ESIZE, EUNSUPPORTED (hd, the limit above).
  */
 int64_t lmgc_kv8_workspace(int32_t B, int32_t Hq, int32_t Hkv, int32_t T, int32_t hd, int32_t cap);
 int lmgc_op_attention_kv8(const uint16_t* d_q, int32_t B, int32_t Hq, int32_t Hkv, int32_t T,

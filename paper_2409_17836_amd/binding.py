@@ -117,6 +117,7 @@ def lib():
         "lmgc_op_add_norm_mx": (ctypes.c_int, [vp, i32, vp, i32, vp, i32, ctypes.c_float, i64, i64, i32,
                                                vp, vp, vp, vp]),
         "lmgc_op_gemm_mx": (ctypes.c_int, [vp, vp, i32, vp, vp, vp, vp, i32, i32, i32, i32, vp]),
+        "lmgc_op_gemm_mx_tile": (ctypes.c_int, [vp, vp, i32, vp, vp, vp, vp, i32, i32, i32, i32, i32, vp]),
         "lmgc_op_kv8_append": (ctypes.c_int, [vp, vp, i32, i32, i32, i32, i32, vp, vp, vp, vp, vp, vp, vp]),
         "lmgc_kv8_workspace": (i64, [i32, i32, i32, i32, i32, i32]),
         "lmgc_op_attention_kv8": (ctypes.c_int, [vp, i32, i32, i32, i32, i32, i32, vp, vp, vp, vp, vp, vp,
@@ -580,13 +581,14 @@ def _dtype(t) -> int:
     return 1 if t.dtype == torch.bfloat16 else 0
 
 
-def _on(t, stream):
-    """The stream to launch on (the current one unless given): the tensors'
-    device has to be the current device, as for every call of the library."""
+def _on(stream, *tensors):
+    """The stream to launch on (the current one unless given).  Every tensor
+    has to be on the current device, as for every call of the library."""
     import torch
-    dev = t.get_device()
-    if dev != torch.cuda.current_device():
-        raise ValueError(f"tensors on device {dev}, the current device is {torch.cuda.current_device()}")
+    dev = torch.cuda.current_device()
+    for t in tensors:
+        if t is not None and t.get_device() != dev:
+            raise ValueError(f"a tensor is on {t.device}, the current device is cuda:{dev}")
     return stream.cuda_stream if stream is not None else _raw_stream(dev)
 
 
@@ -632,7 +634,7 @@ def op_mx_quantize(x, fmt: str, codes=None, scales=None, stream=None):
     codes, scales = _mx_empty(rows, cols, fmt, codes, scales, x.device)
     ld = x.stride(0) if rows > 1 else cols
     _check(lib().lmgc_op_mx_quantize(_ptr(x), _dtype(x), rows, cols, ld, MX_FORMATS[fmt], _ptr(codes),
-                                     _ptr(scales), _on(x, stream)))
+                                     _ptr(scales), _on(stream, x, codes, scales)))
     return codes, scales
 
 
@@ -646,7 +648,7 @@ def op_mx_dequantize(codes, scales, fmt: str, cols: int, dtype=None, out=None, s
     assert tuple(out.shape) == (rows, cols) and (cols == 1 or out.stride(1) == 1)
     ld = out.stride(0) if rows > 1 else cols
     _check(lib().lmgc_op_mx_dequantize(_ptr(codes), _ptr(scales), MX_FORMATS[fmt], rows, cols, _ptr(out),
-                                       _dtype(out), ld, _on(codes, stream)))
+                                       _dtype(out), ld, _on(stream, codes, scales, out)))
     return out
 
 
@@ -657,7 +659,7 @@ def op_mx_block(codes, scales, cols: int, stream=None):
     _mx_check(codes, scales, rows, cols, "fp4")
     bc = torch.empty(_size(lib().lmgc_mx_block_code_bytes(rows, cols)), dtype=torch.uint8, device=codes.device)
     bs = torch.empty(_size(lib().lmgc_mx_block_scale_bytes(rows, cols)), dtype=torch.uint8, device=codes.device)
-    _check(lib().lmgc_op_mx_block(_ptr(codes), _ptr(scales), rows, cols, _ptr(bc), _ptr(bs), _on(codes, stream)))
+    _check(lib().lmgc_op_mx_block(_ptr(codes), _ptr(scales), rows, cols, _ptr(bc), _ptr(bs), _on(stream, codes, scales)))
     return bc, bs
 
 
@@ -672,22 +674,23 @@ def op_add_norm_mx(h, x, gain, eps: float, fmt: str, out=None, codes=None, scale
     codes, scales = _mx_empty(M, d, fmt, codes, scales, h.device)
     _check(lib().lmgc_op_add_norm_mx(_ptr(h), _dtype(h), _ptr(x), _dtype(x) if x is not None else 0, _ptr(gain),
                                      _dtype(gain), float(eps), M, d, MX_FORMATS[fmt], _ptr(out), _ptr(codes),
-                                     _ptr(scales), _on(h, stream)))
+                                     _ptr(scales), _on(stream, h, x, gain, out, codes, scales)))
     return codes, scales
 
 
 MX_KINDS = {"store": 0, "bf16": 3}
+MX_TILES = ("16x16", "32x128", "64x64", "128x128", "128x256", "256x256")  # LMGC_MX_TILE_*
 
 
 def op_gemm_mx(a, a_scales, a_fmt: str, b, b_scales, N: int, K: int, kind: str = "store", add=None, out=None,
-               stream=None):
+               tile: str = None, stream=None):
     """a (rows layout, "fp8" or "fp4") times the 4-bit weights b [N, K] (blocks
     layout), transposed -> [M, N] float32 ("store") or bf16 ("bf16"), plus the
-    float32 `add` [M, N] if given (out may be add)."""
+    float32 `add` [M, N] if given (out may be add).  tile (MX_TILES): the tile
+    of the output, for comparing them; by itself the library takes one by shape."""
     import torch
     M = a.shape[0]
     _mx_check(a, a_scales, M, K, a_fmt)
-    L = lib()
     nc, ns = _mx_sizes(N, K, "fp4")
     n16 = -(-N // 16) * 16
     assert b.dtype == torch.uint8 and b.is_contiguous() and b.numel() == n16 * nc
@@ -698,8 +701,9 @@ def op_gemm_mx(a, a_scales, a_fmt: str, b, b_scales, N: int, K: int, kind: str =
     assert out.dtype == dt and out.is_contiguous() and tuple(out.shape) == (M, N)
     if add is not None:
         assert add.dtype == torch.float32 and add.is_contiguous() and tuple(add.shape) == (M, N)
-    _check(L.lmgc_op_gemm_mx(_ptr(a), _ptr(a_scales), MX_FORMATS[a_fmt], _ptr(b), _ptr(b_scales), _ptr(add),
-                             _ptr(out), M, N, K, MX_KINDS[kind], _on(a, stream)))
+    _check(lib().lmgc_op_gemm_mx_tile(_ptr(a), _ptr(a_scales), MX_FORMATS[a_fmt], _ptr(b), _ptr(b_scales), _ptr(add),
+                                      _ptr(out), M, N, K, MX_KINDS[kind], -1 if tile is None else MX_TILES.index(tile),
+                                      _on(stream, a, a_scales, b, b_scales, add, out)))
     return out
 
 
@@ -739,7 +743,7 @@ def op_kv8_append(cache, k, v, lens, counts=None, stream=None):
     assert k.dtype == v.dtype == torch.bfloat16 and k.is_contiguous() and v.is_contiguous() and v.shape == k.shape
     _kv8_lens(lens, counts, B)
     _check(lib().lmgc_op_kv8_append(_ptr(k), _ptr(v), B, Hkv, T, hd, cap, _ptr(lens), _ptr(counts), _ptr(kc),
-                                    _ptr(ks), _ptr(vc), _ptr(vs), _on(k, stream)))
+                                    _ptr(ks), _ptr(vc), _ptr(vs), _on(stream, k, v, lens, counts, *cache)))
 
 
 def kv8_workspace(B: int, Hq: int, Hkv: int, T: int, hd: int, cap: int) -> int:
@@ -760,9 +764,11 @@ def op_attention_kv8(q, cache, lens, counts=None, window: int = 0, sinks: int = 
     assert out.dtype == torch.bfloat16 and out.is_contiguous() and out.numel() == q.numel()
     if ws is None:
         ws = workspace(kv8_workspace(B, Hq, Hkv, T, hd, cap), q.device)
+        if stream is not None:
+            ws.record_stream(stream)  # its memory is given out again only behind this call
     _check(lib().lmgc_op_attention_kv8(_ptr(q), B, Hq, Hkv, T, hd, cap, _ptr(lens), _ptr(counts), _ptr(kc), _ptr(ks),
                                        _ptr(vc), _ptr(vs), int(window), int(sinks), _ptr(out), _ptr(ws), ws.numel(),
-                                       _on(q, stream)))
+                                       _on(stream, q, out, ws, lens, counts, *cache)))
     return out
 
 

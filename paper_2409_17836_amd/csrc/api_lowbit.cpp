@@ -36,17 +36,26 @@ int done(hipError_t e, const char* what) {
 int check_cache(int32_t B, int32_t Hkv, int32_t T, int32_t hd, int32_t cap, const int32_t* lens, const uint8_t* kc,
                 const float* ks, const uint8_t* vc, const float* vs) {
   if (B <= 0 || Hkv <= 0 || T <= 0 || cap <= 0) return set_error(LMGC_EINVAL, "B, Hkv, T and cap must be positive");
-  if (B > 16383 || Hkv > 65535 || T > (1 << 24) || cap > (1 << 24))
-    return set_error(LMGC_EINVAL, "B above 16383, Hkv above 65535, or T or cap above 2^24");
+  if (B > 16383 || Hkv > 32767 || T > (1 << 24) || cap > (1 << 24))
+    return set_error(LMGC_EINVAL, "B above 16383, Hkv above 32767, or T or cap above 2^24");
   if (cap % 64) return set_error(LMGC_EINVAL, "cap must be a multiple of 64");
   if (hd != 64 && hd != 128) return set_error(LMGC_EUNSUPPORTED, "need hd in {64, 128}");
   if (!lens || !kc || !ks || !vc || !vs) return set_error(LMGC_EINVAL, "NULL device buffer");
   if (!aligned(kc) || !aligned(ks) || !aligned(vc) || !aligned(vs) || ((uintptr_t)lens & 3))
     return set_error(LMGC_EINVAL, "cache pointers must be 16-byte aligned");
   const int64_t blocks = (int64_t)B * Hkv * (cap / 64), codes = blocks * 64 * hd;
-  if (overlap(kc, codes, vc, codes) || overlap(ks, 4 * blocks, vs, 4 * blocks))
-    return set_error(LMGC_EINVAL, "the cache's buffers overlap");
+  const void* p[4] = {kc, vc, ks, vs};
+  const int64_t bytes[4] = {codes, codes, 4 * blocks, 4 * blocks};
+  for (int i = 0; i < 4; i++)
+    for (int j = 0; j < i; j++)
+      if (overlap(p[i], bytes[i], p[j], bytes[j])) return set_error(LMGC_EINVAL, "the cache's buffers overlap");
   return LMGC_OK;
+}
+// whether n bytes at p share memory with the cache
+bool in_cache(const void* p, int64_t n, int32_t B, int32_t Hkv, int32_t hd, int32_t cap, const void* kc, const void* ks,
+              const void* vc, const void* vs) {
+  const int64_t blocks = (int64_t)B * Hkv * (cap / 64), codes = blocks * 64 * hd;
+  return overlap(p, n, kc, codes) || overlap(p, n, vc, codes) || overlap(p, n, ks, 4 * blocks) || overlap(p, n, vs, 4 * blocks);
 }
 
 }  // namespace
@@ -162,10 +171,18 @@ int lmgc_op_add_norm_mx(const void* d_h, int32_t h_dtype, const void* d_x, int32
 int lmgc_op_gemm_mx(const uint8_t* d_a, const uint8_t* d_a_scales, int32_t a_fmt, const uint8_t* d_b,
                     const uint8_t* d_b_scales, const float* d_add, void* d_out, int32_t M, int32_t N, int32_t K,
                     int32_t kind, void* stream) {
+  return lmgc_op_gemm_mx_tile(d_a, d_a_scales, a_fmt, d_b, d_b_scales, d_add, d_out, M, N, K, kind, -1, stream);
+}
+
+int lmgc_op_gemm_mx_tile(const uint8_t* d_a, const uint8_t* d_a_scales, int32_t a_fmt, const uint8_t* d_b,
+                         const uint8_t* d_b_scales, const float* d_add, void* d_out, int32_t M, int32_t N, int32_t K,
+                         int32_t kind, int32_t tile, void* stream) {
   clear_error();
   if (M < 0 || M > (1 << 26) || N <= 0 || N > kMaxCols || K <= 0 || K > kMaxCols)
     return set_error(LMGC_EINVAL, "need 0 <= M <= 2^26 and N, K in [1, 2^20]");
   if (!is_fmt(a_fmt)) return set_error(LMGC_EINVAL, "unknown format %d", a_fmt);
+  if (tile > LMGC_MX_TILE_256X256 || (tile == LMGC_MX_TILE_256X256 && a_fmt == LMGC_MX_FP4))
+    return set_error(LMGC_EINVAL, "unknown tile %d", tile);
   if (kind != LMGC_OP_STORE && kind != LMGC_OP_STORE_BF16) return set_error(LMGC_EINVAL, "unknown kind %d", kind);
   if (M == 0) return LMGC_OK;
   if (!d_a || !d_a_scales || !d_b || !d_b_scales || !d_out) return set_error(LMGC_EINVAL, "NULL device buffer");
@@ -181,7 +198,7 @@ int lmgc_op_gemm_mx(const uint8_t* d_a, const uint8_t* d_a_scales, int32_t a_fmt
       overlap(d_out, nout, d_b, code_bytes(LMGC_MX_FP4, n16, K)) || overlap(d_out, nout, d_b_scales, n16 * row_scales(K)))
     return set_error(LMGC_EINVAL, "d_out overlaps an operand");
   return done(launch_gemm_mx(d_a, d_a_scales, a_fmt, d_b, d_b_scales, M, N, K, d_add, d_out, kind == LMGC_OP_STORE_BF16,
-                             (hipStream_t)stream), "gemm");
+                             tile, (hipStream_t)stream), "gemm");
 }
 
 int lmgc_op_kv8_append(const uint16_t* d_k, const uint16_t* d_v, int32_t B, int32_t Hkv, int32_t T, int32_t hd,
@@ -192,6 +209,9 @@ int lmgc_op_kv8_append(const uint16_t* d_k, const uint16_t* d_v, int32_t B, int3
   if (rc) return rc;
   if (!d_k || !d_v) return set_error(LMGC_EINVAL, "NULL device buffer");
   if (!aligned(d_k) || !aligned(d_v) || ((uintptr_t)d_counts & 3)) return set_error(LMGC_EINVAL, "pointers must be 16-byte aligned");
+  const int64_t nk = (int64_t)B * Hkv * T * hd * 2;
+  if (in_cache(d_k, nk, B, Hkv, hd, cap, d_kc, d_ks, d_vc, d_vs) || in_cache(d_v, nk, B, Hkv, hd, cap, d_kc, d_ks, d_vc, d_vs))
+    return set_error(LMGC_EINVAL, "d_k or d_v overlaps the cache");
   return done(launch_kv8_append(d_k, d_v, B, Hkv, T, hd, cap, d_lens, d_counts, d_kc, d_ks, d_vc, d_vs, (hipStream_t)stream),
               "append");
 }
@@ -214,6 +234,8 @@ int lmgc_op_attention_kv8(const uint16_t* d_q, int32_t B, int32_t Hq, int32_t Hk
   if (rc) return rc;
   if (Hq <= 0 || Hq > 65535 || Hq % Hkv) return set_error(LMGC_EINVAL, "Hq must be a positive multiple of Hkv");
   if ((int64_t)T * (Hq / Hkv) > (1 << 30)) return set_error(LMGC_EINVAL, "T Hq / Hkv above 2^30");
+  if (kv8_workgroups(B, Hq, Hkv, T, hd, cap) >= 1 << 23)  // 2^32 threads
+    return set_error(LMGC_EUNSUPPORTED, "too many columns for one launch");
   if (window < 0 || sinks < 0) return set_error(LMGC_EINVAL, "window and sinks must be >= 0");
   if (!d_q || !d_out) return set_error(LMGC_EINVAL, "NULL device buffer");
   if (!aligned(d_q) || !aligned(d_out) || !aligned(d_ws) || ((uintptr_t)d_counts & 3))
@@ -221,7 +243,8 @@ int lmgc_op_attention_kv8(const uint16_t* d_q, int32_t B, int32_t Hq, int32_t Hk
   const int64_t nq = (int64_t)B * Hq * T * hd * 2, need = kv8_workspace_bytes(B, Hq, Hkv, T, hd, cap);
   if (need > 0 && (!d_ws || ws_bytes < (size_t)need))
     return set_error(LMGC_ESIZE, "workspace too small: %zu < %lld", d_ws ? ws_bytes : (size_t)0, (long long)need);
-  if (overlap(d_q, nq, d_out, nq) || overlap(d_ws, need, d_q, nq) || overlap(d_ws, need, d_out, nq))
+  if (overlap(d_q, nq, d_out, nq) || overlap(d_ws, need, d_q, nq) || overlap(d_ws, need, d_out, nq) ||
+      in_cache(d_out, nq, B, Hkv, hd, cap, d_kc, d_ks, d_vc, d_vs) || in_cache(d_ws, need, B, Hkv, hd, cap, d_kc, d_ks, d_vc, d_vs))
     return set_error(LMGC_EINVAL, "buffers overlap");
   return done(launch_attention_kv8(d_q, B, Hq, Hkv, T, hd, cap, d_lens, d_counts, d_kc, d_ks, d_vc, d_vs, window, sinks,
                                    d_ws, d_out, (hipStream_t)stream), "attention");

@@ -181,8 +181,10 @@ hipError_t launch_add_norm_mx(const void* h, int h_dtype, const void* x, int x_d
                               float eps, int64_t M, int d, int fmt, void* out, uint8_t* codes, uint8_t* scales,
                               hipStream_t s);
 hipError_t launch_gemm_mx(const uint8_t* a, const uint8_t* as, int a_fmt, const uint8_t* b, const uint8_t* bs, int M,
-                          int N, int K, const float* add, void* out, int bf16, hipStream_t s);
+                          int N, int K, const float* add, void* out, int bf16, int tile, hipStream_t s);
 int64_t kv8_workspace_bytes(int B, int Hq, int Hkv, int T, int hd, int cap);
+// Workgroups of the attention over its columns, where they are one dimension of the grid.
+int64_t kv8_workgroups(int B, int Hq, int Hkv, int T, int hd, int cap);
 hipError_t launch_kv8_append(const uint16_t* k, const uint16_t* v, int B, int Hkv, int T, int hd, int cap,
                              const int32_t* lens, const int32_t* counts, uint8_t* kc, float* ks, uint8_t* vc, float* vs,
                              hipStream_t s);

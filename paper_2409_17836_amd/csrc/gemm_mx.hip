@@ -49,8 +49,9 @@ constexpr int vmcnt_imm(int n) { return (n & 15) | ((n >> 4) << 14) | 0xF70; }
 constexpr int kLgkm0 = 0xF0FF;
 
 // Buffer resource over `bytes` bytes at p (gfx9: stride 0, word 3
-// 0x00020000); a lane offset at or past them loads zero.  The scalar offset
-// is not part of that check.
+// 0x00020000); a lane offset at or past them loads zero.  The scalar offset is
+// not counted on in that check: with one, lanes past the end are also past the
+// bytes without it.
 __device__ inline __amdgpu_buffer_rsrc_t buffer_of(const uint8_t* p, int bytes) {
   return __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t*>(p), (short)0, bytes, 0x00020000);
 }
@@ -147,6 +148,7 @@ struct Tile {
   static constexpr int kStage = L * 1024, kScale = S * 1024;
   static constexpr int kLds = ST * kStage + (PS + 1) * kScale;
   static_assert(LB % NW == 0 && kLds <= 160 * 1024, "stage does not fit");
+  static_assert((ST - 2) * LPW + PS * SPW < 64, "more loads in flight than the wait counts");
   // loads that may be in flight when stage G u + s + 1 is needed: those of
   // the ST - 2 stages after it, and the scales asked for among them
   static constexpr int in_flight(int s) {
@@ -204,11 +206,14 @@ __global__ __launch_bounds__(WM * WN * 64, 1) void gemm_mx_tile_kernel(
     vsb[i] = (min(wave * C::SPB + i, C::SB - 1) * 4 + (lane >> 4)) * ns * 16 + (lane & 15) * 16;
   auto load_stage = [&](int s, int slot) __attribute__((always_inline)) {
     const lds_bytes_t at = lds0 + slot * C::kStage;
-    const __amdgpu_buffer_rsrc_t ra = buffer_of(pa, s < nst ? mrows * lda : 0), rb = buffer_of(pb, s < nst ? groups * nk * 1024 : 0);
+    // from the stage's first column on: of a last stage with one step of two
+    // (e2m1, an odd number of steps) the last row's second half is past the end
+    const int ka = s * 128, kb = s * (C::KPS * 1024);
+    const __amdgpu_buffer_rsrc_t ra = buffer_of(pa + ka, s < nst ? mrows * lda - ka : 0), rb = buffer_of(pb + kb, s < nst ? groups * nk * 1024 - kb : 0);
 #pragma unroll
-    for (int i = 0; i < C::LPA; i++) load_lds(ra, at + min(wave * C::LPA + i, C::LA - 1) * 1024, va[i], s * 128);
+    for (int i = 0; i < C::LPA; i++) load_lds(ra, at + min(wave * C::LPA + i, C::LA - 1) * 1024, va[i], 0);
 #pragma unroll
-    for (int i = 0; i < C::LPB; i++) load_lds(rb, at + (C::LA + wave * C::LPB + i) * 1024, vb[i], s * (C::KPS * 1024));
+    for (int i = 0; i < C::LPB; i++) load_lds(rb, at + (C::LA + wave * C::LPB + i) * 1024, vb[i], 0);
   };
   const int nu = ns / 16;
   auto load_scales = [&](int u) __attribute__((always_inline)) {
@@ -376,8 +381,6 @@ void launch_tile(const uint8_t* a, const uint8_t* as, const uint8_t* b, const ui
                                                                                      kGroupM, add, out, bf16);
 }
 
-enum MxTile { k16x16, k32x128, k64x64, k128x128, k128x256, k256x256, kTiles };
-
 // The tile with the least modelled time: a fixed part, and for every round of
 // tiles over the 256 CUs a part per tile and one per step of 128 columns
 // (microseconds, fitted to launches from a graph with N x K of 768 x 768 to
@@ -389,43 +392,44 @@ enum MxTile { k16x16, k32x128, k64x64, k128x128, k128x256, k256x256, kTiles };
 // 16x16 tiles run three to a CU and, past that, fetch the rows of A too often
 // (22016 columns: 13.4 us); 32x128 is for 32 rows at most.  256x256 is left to
 // e4m3: with e2m1 128x256 is as fast (16384 x 4096 x 11008: 364 and 365 us).
-MxTile pick_tile(int fmt, int64_t M, int64_t N, int K) {
+int pick_tile(int fmt, int64_t M, int64_t N, int K) {
   struct Cost {
     int bm, bn;
     double fixed, tile, step;
   };
+  constexpr int kTiles = LMGC_MX_TILE_256X256 + 1;
   static const Cost cost[2][kTiles] = {
       {{16, 16, 2.0, 0.4, 0.100}, {32, 128, 2.0, 0.8, 0.200}, {64, 64, 2.0, 0.7, 0.146}, {128, 128, 2.0, 1.5, 0.400},
        {128, 256, 2.0, 3.0, 0.555}, {256, 256, 3.0, 5.0, 1.070}},
       {{16, 16, 2.0, 0.4, 0.071}, {32, 128, 2.0, 0.8, 0.152}, {64, 64, 2.0, 0.9, 0.145}, {128, 128, 2.0, 1.8, 0.310},
        {128, 256, 2.0, 2.2, 0.425}, {256, 256, 0, 1e30, 0}}};
   const int nk = (int)(mx_cols(K) / 128);
-  int best = k64x64;
+  int best = LMGC_MX_TILE_64X64;
   double least = 1e300;
   for (int t = 0; t < kTiles; t++) {
     const Cost& c = cost[fmt == LMGC_MX_FP8 ? 0 : 1][t];
     const int64_t tiles = (M + c.bm - 1) / c.bm * ((N + c.bn - 1) / c.bn);
-    if (t == k16x16 ? tiles > 3 * 256 : t == k32x128 && M > 32) continue;
-    const double rounds = t == k16x16 ? 1.0 : (double)((tiles + 255) / 256);
+    if (t == LMGC_MX_TILE_16X16 ? tiles > 3 * 256 : t == LMGC_MX_TILE_32X128 && M > 32) continue;
+    const double rounds = t == LMGC_MX_TILE_16X16 ? 1.0 : (double)((tiles + 255) / 256);
     const double us = c.fixed + rounds * (c.tile + c.step * nk);
     if (us < least) {
       least = us;
       best = t;
     }
   }
-  return (MxTile)best;
+  return best;
 }
 
 template <int FMT>
 void launch_fmt(const uint8_t* a, const uint8_t* as, const uint8_t* b, const uint8_t* bs, int M, int N, int K,
-                const float* add, void* out, int bf16, hipStream_t s) {
+                const float* add, void* out, int bf16, int tile, hipStream_t s) {
   constexpr bool F8 = FMT == LMGC_MX_FP8;
-  switch (pick_tile(FMT, M, N, K)) {
-    case k16x16: return launch_tile<FMT, 16, 16, 1, 1, F8 ? 8 : 6>(a, as, b, bs, M, N, K, add, out, bf16, s);
-    case k32x128: return launch_tile<FMT, 32, 128, 1, 4, F8 ? 6 : 4>(a, as, b, bs, M, N, K, add, out, bf16, s);
-    case k64x64: return launch_tile<FMT, 64, 64, 2, 2, 4>(a, as, b, bs, M, N, K, add, out, bf16, s);
-    case k128x128: return launch_tile<FMT, 128, 128, 2, 2, F8 ? 4 : 3>(a, as, b, bs, M, N, K, add, out, bf16, s);
-    case k128x256: return launch_tile<FMT, 128, 256, 2, 4, F8 ? 4 : 2>(a, as, b, bs, M, N, K, add, out, bf16, s);
+  switch (tile < 0 ? pick_tile(FMT, M, N, K) : tile) {
+    case LMGC_MX_TILE_16X16: return launch_tile<FMT, 16, 16, 1, 1, F8 ? 8 : 6>(a, as, b, bs, M, N, K, add, out, bf16, s);
+    case LMGC_MX_TILE_32X128: return launch_tile<FMT, 32, 128, 1, 4, F8 ? 6 : 4>(a, as, b, bs, M, N, K, add, out, bf16, s);
+    case LMGC_MX_TILE_64X64: return launch_tile<FMT, 64, 64, 2, 2, 4>(a, as, b, bs, M, N, K, add, out, bf16, s);
+    case LMGC_MX_TILE_128X128: return launch_tile<FMT, 128, 128, 2, 2, F8 ? 4 : 3>(a, as, b, bs, M, N, K, add, out, bf16, s);
+    case LMGC_MX_TILE_128X256: return launch_tile<FMT, 128, 256, 2, 4, F8 ? 4 : 2>(a, as, b, bs, M, N, K, add, out, bf16, s);
     default:
       if constexpr (F8) launch_tile<FMT, 256, 256, 4, 2, 3>(a, as, b, bs, M, N, K, add, out, bf16, s);
   }
@@ -434,9 +438,9 @@ void launch_fmt(const uint8_t* a, const uint8_t* as, const uint8_t* b, const uin
 }  // namespace
 
 hipError_t launch_gemm_mx(const uint8_t* a, const uint8_t* as, int a_fmt, const uint8_t* b, const uint8_t* bs, int M,
-                          int N, int K, const float* add, void* out, int bf16, hipStream_t s) {
-  if (a_fmt == LMGC_MX_FP8) launch_fmt<LMGC_MX_FP8>(a, as, b, bs, M, N, K, add, out, bf16, s);
-  else launch_fmt<LMGC_MX_FP4>(a, as, b, bs, M, N, K, add, out, bf16, s);
+                          int N, int K, const float* add, void* out, int bf16, int tile, hipStream_t s) {
+  if (a_fmt == LMGC_MX_FP8) launch_fmt<LMGC_MX_FP8>(a, as, b, bs, M, N, K, add, out, bf16, tile, s);
+  else launch_fmt<LMGC_MX_FP4>(a, as, b, bs, M, N, K, add, out, bf16, tile, s);
   return hipGetLastError();
 }
 

@@ -38,10 +38,8 @@ __device__ inline int value_at(int t, int d) {
 // New tokens of a sequence that fit the cache: rows past this are left alone.
 __device__ inline int new_tokens(const int32_t* lens, const int32_t* counts, int b, int T, int cap, int& len) {
   len = lens[b];
-  if (len < 0 || len >= cap) return 0;
-  int n = min(T, cap - len);
-  if (counts) n = min(n, counts[b]);
-  return n;
+  const int n = counts ? min(T, counts[b]) : T;
+  return len < 0 || len >= cap ? 0 : min(n, cap - len);
 }
 
 // ------------------------------------------------------------------ append
@@ -181,9 +179,9 @@ __global__ __launch_bounds__(256) void kv8_append_kernel(const uint16_t* __restr
 // pos - window or j < sinks.
 struct Mask {
   int window, sinks;
-  __device__ inline bool sees(int pos, int j) const {
-    return j <= pos && (window == 0 || j > pos - window || j < sinks);
-  }
+  // low(pos): the last key before the window (no short circuits: a select costs less than a branch)
+  __device__ inline int low(int pos) const { return window ? pos - window : -1; }
+  __device__ inline bool sees(int pos, int low, int j) const { return (j <= pos) & ((j > low) | (j < sinks)); }
   // whether any query at positions p0 .. p1 may see a key of [j0, j1)
   __device__ inline bool any(int p0, int p1, int j0, int j1) const {
     return j0 <= p1 && (window == 0 || j1 - 1 > p0 - window || j0 < sinks);
@@ -192,6 +190,8 @@ struct Mask {
   __device__ inline bool all(int p0, int p1, int j0, int j1) const {
     return j1 - 1 <= p0 && (window == 0 || j0 > p1 - window || j1 <= sinks);
   }
+  // whether split [j0, j1) of the cache is the only one that any of them sees
+  __device__ inline bool only(int p0, int p1, int j0, int j1) const { return j1 > p1 && (j0 == 0 || !any(p0, p1, 0, j0)); }
 };
 
 __device__ inline bf16x8 fp8_bf16(uint32_t w0, uint32_t w1) {
@@ -205,38 +205,47 @@ __device__ inline bf16x8 fp8_bf16(uint32_t w0, uint32_t w1) {
 // query and of the cache, whatever columns, sequences and splits run with it:
 // blocks that a column does not see add exact zeros.
 
-// ---- few columns (kSplitCols at most)
-// Grid: (splits x tiles of 16 columns, Hkv, B), 512 threads.  A split is 256
-// KB of the cache; wave w takes its blocks w, w + 8, ..: S^T = K Q^T, so lane
-// (col, g) holds the scores of its column and tokens 16 i + 4 g + r of a
-// block, an online softmax, O^T += V^T P^T.  The waves' parts meet in LDS.
-constexpr int kSplitCols = 32;
-constexpr int kSplitBytes = 256 << 10;
-constexpr int kSplitWaves = 8;
+// Buffer over the codes of one block (stride 0, word 3 of gfx9).
+template <int HD>
+__device__ inline __amdgpu_buffer_rsrc_t block_buffer(const uint8_t* codes, int64_t blk) {
+  return __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t*>(codes + blk * (kBlk * HD)), (short)0, kBlk * HD, 0x00020000);
+}
 
-__host__ __device__ constexpr int split_tokens(int hd) { return kSplitBytes / (2 * hd); }
+// ---- few columns (kSplitCols at most)
+// Grid: (splits, tiles of 16 columns x Hkv, B), 512 threads.  A cache of up to
+// kOneBytes is one split (and the call one launch), a longer one is cut into
+// kSplitBytes (more where that were over kMaxSplits).  Wave w takes its blocks
+// w, w + 8, ..: S^T = K Q^T, so lane (col, g) holds the scores of its column
+// and tokens 16 i + 4 g + r of a block, an online softmax, O^T += V^T P^T.
+// The waves' parts meet in LDS.
+constexpr int kSplitCols = 32;
+constexpr int kOneBytes = 256 << 10, kSplitBytes = 128 << 10;
+constexpr int kSplitWaves = 8;
+constexpr int kMaxSplits = 64;  // a lane each in the join
 
 template <int HD>
 __global__ __launch_bounds__(kSplitWaves * 64, 4) void attn_kv8_split_kernel(
     const uint16_t* __restrict__ q, const uint8_t* __restrict__ kc, const float* __restrict__ ks,
     const uint8_t* __restrict__ vc, const float* __restrict__ vs, const int32_t* __restrict__ lens,
-    const int32_t* __restrict__ counts, int Hkv, int G, int T, int cap, int nsplit, Mask mask, float sl2,
-    float* __restrict__ part_o, float2* __restrict__ part_ml, uint16_t* __restrict__ out) {
-  constexpr int NC = HD / 64, ND = HD / 16, CH = split_tokens(HD), NW = kSplitWaves;
-  __shared__ float so[NW / 2][16][HD + 4];
+    const int32_t* __restrict__ counts, int Hkv, int G, int ginv, int T, int cap, int nsplit, int chunk, Mask mask,
+    float sl2, float* __restrict__ part_o, float2* __restrict__ part_ml, uint16_t* __restrict__ out) {
+  constexpr int NC = HD / 64, ND = HD / 16, NW = kSplitWaves;
+  __shared__ float so[NW][16][HD + 4];
   __shared__ float sm[NW][16], sl[NW][16];
-  const int split = blockIdx.x % nsplit, c0 = blockIdx.x / nsplit * 16, kvh = blockIdx.y, b = blockIdx.z;
+  const int split = blockIdx.x, tile = blockIdx.y >= Hkv, c0 = 16 * tile, kvh = blockIdx.y - tile * Hkv, b = blockIdx.z;
   const int tid = threadIdx.x, lane = tid & 63, col = lane & 15, g = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  auto over_g = [&](int c) __attribute__((always_inline)) { return c * ginv >> 16; };  // c / G
   int len;
   const int n = new_tokens(lens, counts, b, T, cap, len);
   const int ncol = min(16, n * G - c0);
   if (ncol <= 0) return;
-  const int p0 = len + c0 / G, p1 = len + (c0 + ncol - 1) / G;  // positions of the tile's queries
-  if (!mask.any(p0, p1, split * CH, split * CH + CH)) return;
-  const int c = c0 + min(col, ncol - 1), t = c / G, pos = len + t;
+  const int p0 = len + over_g(c0), p1 = len + over_g(c0 + ncol - 1);  // positions of the tile's queries
+  const int jlo = split * chunk, jhi = min(cap, jlo + chunk);
+  if (!mask.any(p0, p1, jlo, jhi)) return;
+  const int c = c0 + min(col, ncol - 1), t = over_g(c), pos = len + t, low = mask.low(pos);
   const int64_t hb = (int64_t)b * Hkv + kvh, nblk = cap / kBlk;
-  const uint16_t* qp = q + (((int64_t)b * Hkv * G + kvh * G + c % G) * T + t) * HD + 16 * g;
+  const uint16_t* qp = q + ((hb * G + (c - t * G)) * T + t) * HD + 16 * g;
   bf16x8 qf[NC][2];
 #pragma unroll
   for (int x = 0; x < NC; x++)
@@ -245,28 +254,39 @@ __global__ __launch_bounds__(kSplitWaves * 64, 4) void attn_kv8_split_kernel(
 
   float m = -INFINITY, l = 0.f;
   f32x4 o[ND] = {};
-  const int jend = min(min(cap, split * CH + CH), p1 + 1);
-  for (int j0 = split * CH + wave * kBlk; j0 < jend; j0 += NW * kBlk) {
+  const int jend = min(jhi, p1 + 1);
+  for (int j0 = jlo + wave * kBlk; j0 < jend; j0 += NW * kBlk) {
     if (!mask.any(p0, p1, j0, j0 + kBlk)) continue;
     const int64_t blk = hb * nblk + j0 / kBlk;
-    const u32x4* kp = reinterpret_cast<const u32x4*>(kc + blk * (kBlk * HD)) + lane;
-    const u32x4* vp = reinterpret_cast<const u32x4*>(vc + blk * (kBlk * HD)) + lane;
+    // (through buffers of a block each: their addresses take no vector registers)
+    const __amdgpu_buffer_rsrc_t kb = block_buffer<HD>(kc, blk), vb = block_buffer<HD>(vc, blk);
+    auto codes = [&](__amdgpu_buffer_rsrc_t block, int i) __attribute__((always_inline)) {
+      return __builtin_amdgcn_raw_buffer_load_b128(block, lane * 16, i * 1024, 0);
+    };
     u32x4 kr[4][NC], vr[ND];
 #pragma unroll
     for (int i = 0; i < 4; i++)
 #pragma unroll
-      for (int x = 0; x < NC; x++) kr[i][x] = kp[(i * NC + x) * 64];
+      for (int x = 0; x < NC; x++) kr[i][x] = codes(kb, i * NC + x);
 #pragma unroll
-    for (int i = 0; i < ND; i++) vr[i] = vp[i * 64];
+    for (int i = 0; i < ND / 2; i++) vr[i] = codes(vb, i);
     const float fk = ks[blk] * sl2, fv = vs[blk];
     f32x4 s[4] = {};
+    // tile by tile, half of the values asked for behind the first tile: mixed
+    // with each other and with what follows, 128 dims do not fit the registers
 #pragma unroll
-    for (int x = 0; x < NC; x++)
+    for (int i = 0; i < 4; i++) {
+      __builtin_amdgcn_sched_barrier(0);
+      if (i == 1)
 #pragma unroll
-      for (int y = 0; y < 2; y++)
+        for (int e = ND / 2; e < ND; e++) vr[e] = codes(vb, e);
 #pragma unroll
-        for (int i = 0; i < 4; i++)
+      for (int x = 0; x < NC; x++)
+#pragma unroll
+        for (int y = 0; y < 2; y++)
           s[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fp8_bf16(kr[i][x][2 * y], kr[i][x][2 * y + 1]), qf[x][y], s[i], 0, 0, 0);
+    }
+    __builtin_amdgcn_sched_barrier(0);
     const bool whole = mask.all(p0, p1, j0, j0 + kBlk);
     bool see[4][4];
     float mx = -INFINITY;
@@ -274,7 +294,7 @@ __global__ __launch_bounds__(kSplitWaves * 64, 4) void attn_kv8_split_kernel(
     for (int i = 0; i < 4; i++)
 #pragma unroll
       for (int r = 0; r < 4; r++) {
-        see[i][r] = whole || mask.sees(pos, j0 + 16 * i + 4 * g + r);
+        see[i][r] = whole | mask.sees(pos, low, j0 + 16 * i + 4 * g + r);
         s[i][r] = see[i][r] ? s[i][r] * fk : -INFINITY;
         mx = fmaxf(mx, s[i][r]);  // (drops a NaN; it comes back through the exponential)
       }
@@ -310,57 +330,42 @@ __global__ __launch_bounds__(kSplitWaves * 64, 4) void attn_kv8_split_kernel(
     sm[wave][col] = m;
     sl[wave][col] = l;
   }
+#pragma unroll
+  for (int i = 0; i < ND; i++) *reinterpret_cast<f32x4*>(&so[wave][col][16 * i + 4 * g]) = o[i];
   __syncthreads();
-  // waves without a token they see (m = -inf, l = 0) count for nothing
-  float M = sm[0][col];
+  // HD / 32 dims of a column to a thread
+  typedef float f32xd __attribute__((ext_vector_type(HD / 32)));
+  const int oc = tid >> 5, d0 = (tid & 31) * (HD / 32);
+  if (oc >= ncol) return;
+  float M = sm[0][oc];
 #pragma unroll
-  for (int w = 1; w < NW; w++) M = fmaxf(M, sm[w][col]);
+  for (int w = 1; w < NW; w++) M = fmaxf(M, sm[w][oc]);
   float L = 0.f;
-  auto weight = [&](float mw, float lw) __attribute__((always_inline)) {
-    return mw == -INFINITY && lw == 0.f ? 0.f : __builtin_amdgcn_exp2f(mw - M);
-  };
+  f32xd r = {};
 #pragma unroll
-  for (int w = 0; w < NW; w++) L += weight(sm[w][col], sl[w][col]) * sl[w][col];
-  const float a = weight(m, l);
-#pragma unroll
-  for (int i = 0; i < ND; i++) o[i] *= a;
-#pragma unroll
-  for (int half = NW / 2; half; half >>= 1) {
-    if (wave >= half && wave < 2 * half)
-#pragma unroll
-      for (int i = 0; i < ND; i++) *reinterpret_cast<f32x4*>(&so[wave - half][col][16 * i + 4 * g]) = o[i];
-    __syncthreads();
-    if (wave < half)
-#pragma unroll
-      for (int i = 0; i < ND; i++) o[i] += *reinterpret_cast<const f32x4*>(&so[wave][col][16 * i + 4 * g]);
-    __syncthreads();
+  for (int w = 0; w < NW; w++) {
+    // waves without a token they see (m = -inf, l = 0) count for nothing
+    const float mw = sm[w][oc], lw = sl[w][oc], a = mw == -INFINITY && lw == 0.f ? 0.f : __builtin_amdgcn_exp2f(mw - M);
+    L += a * lw;
+    r += a * *reinterpret_cast<const f32xd*>(&so[w][oc][d0]);
   }
-  if (wave != 0 || col >= ncol) return;
-  // whether this split is all that the tile's queries see
-  bool only = true;
-  for (int x = 0; x < nsplit; x++)
-    if (x != split && mask.any(p0, p1, x * CH, x * CH + CH)) only = false;
-  if (only) {
+  const int ot = over_g(c0 + oc);
+  if (mask.only(p0, p1, jlo, jhi)) {
     const float inv = 1.0f / L;
-    uint16_t* op = out + ((int64_t)b * T + t) * ((int64_t)Hkv * G * HD) + (kvh * G + c % G) * HD + 4 * g;
+    uint32_t* op = reinterpret_cast<uint32_t*>(out + (((int64_t)b * T + ot) * Hkv + kvh) * ((int64_t)G * HD) + (c0 + oc - ot * G) * HD + d0);
 #pragma unroll
-    for (int i = 0; i < ND; i++) {
-      mx_u32x2 w;
-#pragma unroll
-      for (int e = 0; e < 2; e++)
-        w[e] = (uint32_t)f32_to_bf16(o[i][2 * e] * inv) | ((uint32_t)f32_to_bf16(o[i][2 * e + 1] * inv) << 16);
-      *reinterpret_cast<mx_u32x2*>(op + 16 * i) = w;
-    }
+    for (int e = 0; e < HD / 64; e++)
+      op[e] = __builtin_bit_cast(uint32_t, bf16x2{(__bf16)(r[2 * e] * inv), (__bf16)(r[2 * e + 1] * inv)});
   } else {
-    const int64_t row = hb * T * G + c;
-#pragma unroll
-    for (int i = 0; i < ND; i++) *reinterpret_cast<f32x4*>(part_o + (row * nsplit + split) * HD + 16 * i + 4 * g) = o[i];
-    if (g == 0) part_ml[row * nsplit + split] = make_float2(M, L);
+    const int64_t row = (hb * T * G + c0 + oc) * nsplit + split;
+    *reinterpret_cast<f32xd*>(part_o + row * HD + d0) = r;
+    if (d0 == 0) part_ml[row] = make_float2(M, L);
   }
 }
 
-// Joins the splits of a column: a wave per column, HD / 64 dims to a lane.
-// TILE: columns whose positions decide together which splits have run.
+// Joins the splits of a column: a wave per column, first a lane per split (its
+// weight), then HD / 64 dims to a lane.  TILE: columns whose positions decide
+// together which splits have run.
 template <int HD, int TILE>
 __global__ __launch_bounds__(64) void attn_kv8_join_kernel(const float* __restrict__ part_o, const float2* __restrict__ part_ml,
                                                            const int32_t* __restrict__ lens, const int32_t* __restrict__ counts,
@@ -372,27 +377,35 @@ __global__ __launch_bounds__(64) void attn_kv8_join_kernel(const float* __restri
   if (c >= n * G) return;
   const int c0 = c / TILE * TILE, ncol = min(TILE, n * G - c0), p0 = len + c0 / G, p1 = len + (c0 + ncol - 1) / G;
   const int64_t hb = (int64_t)b * Hkv + kvh, row = hb * T * G + c;
-  float M = -INFINITY;
-  int used = 0;
-  for (int x = 0; x < nsplit; x++)
-    if (mask.any(p0, p1, x * chunk, x * chunk + chunk)) {
-      M = fmaxf(M, part_ml[row * nsplit + x].x);
-      used++;
-    }
-  if (used <= 1) return;  // written by the only split
-  float acc[HD / 64] = {}, L = 0.f;
-  for (int x = 0; x < nsplit; x++) {
-    if (!mask.any(p0, p1, x * chunk, x * chunk + chunk)) continue;
-    const float2 ml = part_ml[row * nsplit + x];
-    const float a = ml.x == -INFINITY && ml.y == 0.f ? 0.f : __builtin_amdgcn_exp2f(ml.x - M);
-    L += a * ml.y;
+  const bool ran = lane < nsplit && mask.any(p0, p1, lane * chunk, min(cap, lane * chunk + chunk));
+  const uint64_t used = __ballot(ran);
+  if ((used & (used - 1)) == 0) return;  // written by the only split
+  const float2 ml = ran ? part_ml[row * nsplit + lane] : make_float2(-INFINITY, 0.f);
+  float M = ml.x;
+  for (int o = 32; o; o >>= 1) M = fmaxf(M, __shfl_xor(M, o, 64));
+  // splits without a token that the column sees (m = -inf, l = 0) count for nothing
+  const float a = ml.x == -INFINITY && ml.y == 0.f ? 0.f : __builtin_amdgcn_exp2f(ml.x - M);
+  float L = a * ml.y;
+  for (int o = 32; o; o >>= 1) L += __shfl_xor(L, o, 64);
+  typedef float f32xd __attribute__((ext_vector_type(HD / 64)));
+  f32xd acc = {};
+  const f32xd* p = reinterpret_cast<const f32xd*>(part_o + row * nsplit * HD) + lane;
+  // 16 at a time, so that their loads are under way together (those of splits
+  // that have not run, between the sinks and the window, are dropped)
+  for (int x0 = 0; x0 < nsplit; x0 += 16) {
+    f32xd v[16];
 #pragma unroll
-    for (int i = 0; i < HD / 64; i++) acc[i] += a * part_o[(row * nsplit + x) * HD + lane + 64 * i];
+    for (int x = 0; x < 16; x++) v[x] = p[min(x0 + x, nsplit - 1) * 64];
+#pragma unroll
+    for (int x = 0; x < 16; x++) {
+      const float ax = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, a), x0 + x));
+      if (used >> (x0 + x) & 1) acc += ax * v[x];
+    }
   }
   const int t = c / G, hq = kvh * G + c % G;
+  uint16_t* op = out + ((int64_t)b * T + t) * ((int64_t)Hkv * G * HD) + hq * HD + lane * (HD / 64);
 #pragma unroll
-  for (int i = 0; i < HD / 64; i++)
-    out[((int64_t)b * T + t) * ((int64_t)Hkv * G * HD) + hq * HD + lane + 64 * i] = f32_to_bf16(acc[i] / L);
+  for (int i = 0; i < HD / 64; i++) op[i] = f32_to_bf16(acc[i] / L);
 }
 
 // ---- many columns
@@ -412,11 +425,13 @@ __global__ __launch_bounds__(64) void attn_kv8_join_kernel(const float* __restri
 //
 // The block scales cost nothing per score: the keys' goes into the exponent's
 // factor, the values' (a power of two) into its summand, and the row sums
-// are a product too, with ones over that scale.  Up to kJoinCols columns the length is split
-// too, kPromptChunk tokens to a workgroup, and joined.
+// are a product too, with ones over that scale.  Up to kJoinCols columns the
+// length is split too, kPromptChunk tokens to a workgroup (more where that
+// were over kMaxPromptSplits), and joined.
 constexpr int kTileCols = 256;
 constexpr int kJoinCols = 1024;
 constexpr int kPromptChunk = 1024;
+constexpr int kMaxPromptSplits = 16;
 constexpr int kAhead = 3;  // steps that a block's codes are asked for ahead
 constexpr int kReads = 8;  // operands read ahead of their products
 
@@ -436,7 +451,7 @@ template <int HD>
 __global__ __launch_bounds__(512, 2) void attn_kv8_prompt_kernel(
     const uint16_t* __restrict__ q, const uint8_t* __restrict__ kc, const float* __restrict__ ks,
     const uint8_t* __restrict__ vc, const float* __restrict__ vs, const int32_t* __restrict__ lens,
-    const int32_t* __restrict__ counts, int B, int Hkv, int G, int T, int cap, int ntile, int nsplit, Mask mask, float sl2,
+    const int32_t* __restrict__ counts, int B, int Hkv, int G, int T, int cap, int ntile, int nsplit, int chunk, Mask mask, float sl2,
     float* __restrict__ part_o, float2* __restrict__ part_ml, uint16_t* __restrict__ out) {
   constexpr int ND = HD / 16, KQ = HD / 32;  // dim tiles; 32-dim steps of a score
   constexpr int NP = HD / 64;                // 4 KB of codes of keys (and of values) of a block
@@ -453,7 +468,7 @@ __global__ __launch_bounds__(512, 2) void attn_kv8_prompt_kernel(
   const int ncol = min(kTileCols, n * G - c0);
   if (ncol <= 0) return;
   const int p0 = len + c0 / G, p1 = len + (c0 + ncol - 1) / G;
-  const int jlo = nsplit > 1 ? split * kPromptChunk : 0, jhi = nsplit > 1 ? jlo + kPromptChunk : cap;
+  const int jlo = split * chunk, jhi = min(cap, jlo + chunk);
   if (!mask.any(p0, p1, jlo, jhi)) return;
   const int tid = threadIdx.x, lane = tid & 63, col = lane & 15, g = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -475,7 +490,7 @@ __global__ __launch_bounds__(512, 2) void attn_kv8_prompt_kernel(
   const uint8_t *kp = kc + blk0 * (kBlk * HD), *vp = vc + blk0 * (kBlk * HD);
   // blocks bfirst .. bend - 1 of this split, those between the sinks and the
   // window left out
-  const int bend = min(min(jhi, cap) - 1, p1) / kBlk + 1;
+  const int bend = min(jhi - 1, p1) / kBlk + 1;
   const int bwin = mask.window ? max(0, p0 - mask.window + 1) / kBlk : 0;  // first block that the window reaches
   auto skip = [&](int x) __attribute__((always_inline)) { return x * kBlk >= mask.sinks && x < bwin ? bwin : x; };
   auto after = [&](int x) __attribute__((always_inline)) { return skip(x + 1); };
@@ -581,7 +596,7 @@ __global__ __launch_bounds__(512, 2) void attn_kv8_prompt_kernel(
           for (int y = 0; y < 2; y++)
 #pragma unroll
             for (int r = 0; r < 4; r++) {
-              const bool sees = mask.sees(pos[y], j0 + 16 * i + 4 * g + r);
+              const bool sees = mask.sees(pos[y], mask.low(pos[y]), j0 + 16 * i + 4 * g + r);
               if (nan) sc[i][y][r] = __builtin_bit_cast(float, 0x7fc00000u);
               if (!sees) sc[i][y][r] = -INFINITY;
             }
@@ -676,9 +691,7 @@ __global__ __launch_bounds__(512, 2) void attn_kv8_prompt_kernel(
   if (wave < 4) phase();
   __builtin_amdgcn_s_waitcnt(vmcnt_imm(0));  // no load to LDS outlives the workgroup
   if (!works) return;
-  bool only = true;
-  for (int x = 0; x < nsplit; x++)
-    if (nsplit > 1 && x != split && mask.any(p0, p1, x * kPromptChunk, x * kPromptChunk + kPromptChunk)) only = false;
+  const bool only = mask.only(p0, p1, jlo, jhi);
 #pragma unroll
   for (int y = 0; y < 2; y++) {
     const int c = w0 + 16 * y + col;
@@ -692,7 +705,7 @@ __global__ __launch_bounds__(512, 2) void attn_kv8_prompt_kernel(
         mx_u32x2 w;
 #pragma unroll
         for (int e = 0; e < 2; e++)
-          w[e] = (uint32_t)f32_to_bf16(acc[i][y][2 * e] * inv) | ((uint32_t)f32_to_bf16(acc[i][y][2 * e + 1] * inv) << 16);
+          w[e] = __builtin_bit_cast(uint32_t, bf16x2{(__bf16)(acc[i][y][2 * e] * inv), (__bf16)(acc[i][y][2 * e + 1] * inv)});
         *reinterpret_cast<mx_u32x2*>(op + 16 * i) = w;
       }
     } else {
@@ -704,18 +717,28 @@ __global__ __launch_bounds__(512, 2) void attn_kv8_prompt_kernel(
   }
 }
 
-// Splits of the length: by the number of columns and the cache alone, so that
-// a query's result does not depend on the other sequences.
-int splits_of(int64_t cols, int hd, int cap) {
-  const int chunk = cols <= kSplitCols ? split_tokens(hd) : kPromptChunk;
-  return cols <= kJoinCols ? (cap + chunk - 1) / chunk : 1;
+// Tokens in a split of the length: by the number of columns and the cache
+// alone, so that a query's result does not depend on the other sequences.
+int chunk_of(int64_t cols, int hd, int cap) {
+  if (cols > kJoinCols) return cap;
+  if (cols <= kSplitCols && cap <= kOneBytes / (2 * hd)) return cap;
+  const int least = cols <= kSplitCols ? kSplitBytes / (2 * hd) : kPromptChunk;
+  const int most = cols <= kSplitCols ? kMaxSplits : kMaxPromptSplits;
+  return std::max(least, ((cap + most - 1) / most + kBlk - 1) / kBlk * kBlk);
 }
+int splits_of(int chunk, int cap) { return (cap + chunk - 1) / chunk; }
+int64_t tiles_of(int64_t cols) { return (cols + kTileCols - 1) / kTileCols; }
 
 }  // namespace
 
 int64_t kv8_workspace_bytes(int B, int Hq, int Hkv, int T, int hd, int cap) {
-  const int64_t nsplit = splits_of((int64_t)T * (Hq / Hkv), hd, cap);
+  const int64_t nsplit = splits_of(chunk_of((int64_t)T * (Hq / Hkv), hd, cap), cap);
   return nsplit > 1 ? (int64_t)B * Hq * T * nsplit * (hd + 2) * 4 : 0;
+}
+
+int64_t kv8_workgroups(int B, int Hq, int Hkv, int T, int hd, int cap) {
+  const int64_t cols = (int64_t)T * (Hq / Hkv);
+  return cols <= kSplitCols ? 1 : tiles_of(cols) * splits_of(chunk_of(cols, hd, cap), cap) * B * Hkv;
 }
 
 hipError_t launch_kv8_append(const uint16_t* k, const uint16_t* v, int B, int Hkv, int T, int hd, int cap,
@@ -732,7 +755,7 @@ hipError_t launch_attention_kv8(const uint16_t* q, int B, int Hq, int Hkv, int T
                                 const float* vs, int window, int sinks, void* ws, uint16_t* out, hipStream_t s) {
   const int G = Hq / Hkv;
   const int64_t cols = (int64_t)T * G;
-  const int nsplit = splits_of(cols, hd, cap);
+  const int chunk = chunk_of(cols, hd, cap), nsplit = splits_of(chunk, cap);
   const Mask mask{window, sinks};
   const float sl2 = (float)(1.4426950408889634 / sqrt((double)hd));
   float* po = (float*)ws;
@@ -741,16 +764,16 @@ hipError_t launch_attention_kv8(const uint16_t* q, int B, int Hq, int Hkv, int T
     constexpr int HD = decltype(h)::value;
     const dim3 join((unsigned)cols, Hkv, B);
     if (cols <= kSplitCols) {
-      attn_kv8_split_kernel<HD><<<dim3(nsplit * (unsigned)((cols + 15) / 16), Hkv, B), kSplitWaves * 64, 0, s>>>(
-          q, kc, ks, vc, vs, lens, counts, Hkv, G, T, cap, nsplit, mask, sl2, po, pml, out);
+      attn_kv8_split_kernel<HD><<<dim3(nsplit, (cols > 16 ? 2 : 1) * Hkv, B), kSplitWaves * 64, 0, s>>>(
+          q, kc, ks, vc, vs, lens, counts, Hkv, G, 65536 / G + 1, T, cap, nsplit, chunk, mask, sl2, po, pml, out);
       if (nsplit > 1)
-        attn_kv8_join_kernel<HD, 16><<<join, 64, 0, s>>>(po, pml, lens, counts, Hkv, G, T, cap, nsplit, split_tokens(HD), mask, out);
+        attn_kv8_join_kernel<HD, 16><<<join, 64, 0, s>>>(po, pml, lens, counts, Hkv, G, T, cap, nsplit, chunk, mask, out);
     } else {
-      const int ntile = (int)((cols + kTileCols - 1) / kTileCols);
+      const int ntile = (int)tiles_of(cols);
       attn_kv8_prompt_kernel<HD><<<(unsigned)((int64_t)ntile * nsplit * B * Hkv), 512, 0, s>>>(
-          q, kc, ks, vc, vs, lens, counts, B, Hkv, G, T, cap, ntile, nsplit, mask, sl2, po, pml, out);
+          q, kc, ks, vc, vs, lens, counts, B, Hkv, G, T, cap, ntile, nsplit, chunk, mask, sl2, po, pml, out);
       if (nsplit > 1)
-        attn_kv8_join_kernel<HD, kTileCols><<<join, 64, 0, s>>>(po, pml, lens, counts, Hkv, G, T, cap, nsplit, kPromptChunk, mask, out);
+        attn_kv8_join_kernel<HD, kTileCols><<<join, 64, 0, s>>>(po, pml, lens, counts, Hkv, G, T, cap, nsplit, chunk, mask, out);
     }
   };
   if (hd == 64) go(std::integral_constant<int, 64>{});

@@ -213,10 +213,16 @@ template <int FMT, typename TH, typename TX, typename TG>
 void add_norm(const void* h, const void* x, const void* gain, float eps, int64_t M, int d, void* out, uint8_t* codes,
               uint8_t* scales, hipStream_t s) {
   const int nc = (int)mx_row_scales(d) / 16;  // groups of 512 columns, 64 threads each
+  constexpr int64_t kRows = 1 << 23;  // of a launch: under 2^32 threads
+  const int64_t nc_row = FMT == LMGC_MX_FP8 ? mx_cols(d) : mx_cols(d) / 2, ns_row = mx_row_scales(d);
   auto go = [&](auto n, auto nt) {
     constexpr int NT = decltype(nt)::value;
-    add_norm_mx_kernel<FMT, TH, TX, TG, decltype(n)::value, NT><<<(unsigned)((M + 256 / NT - 1) / (256 / NT)), 256, 0, s>>>(
-        (const TH*)h, (const TX*)x, (const TG*)gain, eps, M, d, (TH*)out, codes, scales);
+    for (int64_t m = 0; m < M; m += kRows) {
+      const int64_t rows = std::min(kRows, M - m);
+      add_norm_mx_kernel<FMT, TH, TX, TG, decltype(n)::value, NT><<<(unsigned)((rows + 256 / NT - 1) / (256 / NT)), 256, 0, s>>>(
+          (const TH*)h + m * d, x ? (const TX*)x + m * d : nullptr, (const TG*)gain, eps, rows, d,
+          out ? (TH*)out + m * d : nullptr, codes + m * nc_row, scales + m * ns_row);
+    }
   };
   using wave = std::integral_constant<int, 64>;
   using block = std::integral_constant<int, 256>;

@@ -72,6 +72,18 @@ def test_append_counts_and_the_end_of_the_cache():
     _same(cache, ref)
 
 
+def test_append_after_tokens_are_dropped():
+    """Lengths that go back (tokens that were tried and not taken), into a block
+    and to a block's start, one sequence at a time."""
+    Bn, H, cap, hd = 2, 2, 256, 64
+    cache, ref = B.kv8_cache(Bn, H, cap, hd), R.Cache(Bn, H, cap, hd)
+    for i, (lens, T) in enumerate((([0, 0], 150), ([140, 64], 8), ([128, 70], 5), ([3, 75], 1), ([4, 76], 130))):
+        k, v = _kv((Bn, H, T, hd), 10 + i, 1.5), _kv((Bn, H, T, hd), 50 + i, 1.5)
+        B.op_kv8_append(cache, k, v, _int32(lens))
+        ref.append(_host(k), _host(v), lens)
+        _same(cache, ref)
+
+
 def test_append_special_values():
     """Zeros, tiny and huge values; a NaN or an infinity marks its block until
     the block is begun anew, and leaves the other blocks alone."""
@@ -165,6 +177,53 @@ def test_attention_window_and_sinks(T, lens, window, sinks):
     _check_attention(out, q, kv, lens, window=window, sinks=sinks)
 
 
+@pytest.mark.parametrize("hd", [64, 128])
+@pytest.mark.parametrize("T,masks", [(1, [(0, 0), (100000, 5000), (70, 0)]), (20, [(100000, 5000), (70, 0)]), (600, [(3000, 4)])])
+def test_attention_over_a_long_cache(hd, T, masks):
+    """More tokens than the largest number of splits has by itself: longer
+    splits, a lane for each in the join; windows that leave some of them out."""
+    log(f"long cache hd={hd} T={T}")
+    cap, Hq = 1 << 18, 2
+    cache, kv = _filled(1, 1, cap, hd, cap, 35)
+    q = _kv((1, Hq, T, hd), 39)
+    n = cap - 700
+    for window, sinks in masks:
+        out = B.op_attention_kv8(q, cache, _int32([n]), window=window, sinks=sinks)
+        _check_attention(out, q, kv, [n], window=window, sinks=sinks)
+
+
+@pytest.mark.parametrize("T", [1, 40, 1100])
+def test_attention_and_append_past_32_bits(T):
+    """Codes past 4 GB and blocks past the last sequence's 2^31 bytes: the last
+    sequence's tokens, seen through a window, as in a small cache."""
+    import torch
+    Bn, Hkv, Hq, hd, cap, window = 3, 16, 16, 128, 1 << 20, 100
+    cache = tuple(torch.empty(s, dtype=dt, device="cuda") for s, dt in
+                  ((((Bn, Hkv, cap // 64, 64 * hd)), torch.uint8), ((Bn, Hkv, cap // 64), torch.float32)) * 2)
+    first = cap - 64 * 20
+    k, v = _kv((1, Hkv, 1280, hd), 45), _kv((1, Hkv, 1280, hd), 46)
+    three = lambda t: t.expand(Bn, -1, -1, -1).contiguous()
+    B.op_kv8_append(cache, three(k), three(v), _int32([0, 0, first]), _int32([0, 0, 1280]))
+    small = B.kv8_cache(1, Hkv, 1280, hd)
+    B.op_kv8_append(small, k, v, _int32([0]))
+    assert all(torch.equal(c[2:, :, -20:], s) for c, s in zip(cache, small))
+    q = _kv((1, Hq, T, hd), 49)
+    out = B.op_attention_kv8(three(q), cache, _int32([0, 0, first + 150]), _int32([0, 0, T]), window=window)
+    _check_attention(out.reshape(Bn, T, -1)[2], q, _values(small, hd), [150], window=window)
+
+
+def test_attention_refuses_lengths_on_the_host():
+    import torch
+    cache, _ = _filled(1, 1, 64, 64, 64, 1)
+    q, k = _kv((1, 1, 1, 64), 2), _kv((1, 1, 1, 64), 3)
+    host = torch.tensor([5], dtype=torch.int32)
+    for call in (lambda: B.op_attention_kv8(q, cache, host), lambda: B.op_kv8_append(cache, k, k, host),
+                 lambda: B.op_kv8_append(cache, k.cpu(), k, _int32([5])),
+                 lambda: B.op_attention_kv8(q, cache, _int32([5]), host)):
+        with pytest.raises(ValueError):
+            call()
+
+
 @pytest.mark.parametrize("T", [1, 3, 33, 150])
 def test_attention_ragged_rows_are_left(T):
     """counts, lengths at and past the cache's ends: rows without a token keep what they held."""
@@ -225,12 +284,13 @@ def test_attention_extreme_scores(hd):
 
 @pytest.mark.parametrize("T", [1, 4, 30, 90])
 def test_attention_queries_do_not_depend_on_others(T):
-    """A sequence alone gives the bits it has in a batch; so does a wider cache."""
+    """A sequence alone gives the bits it has in a batch; so does a wider
+    cache that is split alike."""
     import torch
-    cap, hd, Hkv = 640, 128, 2
+    cap, hd, Hkv = 1152, 128, 2
     cache, _ = _filled(3, Hkv, cap, hd, cap, 55)
     q = _kv((3, 4, T, hd), 59)
-    lens = [500, 30, 257]
+    lens = [1000, 30, 513]
     whole = B.op_attention_kv8(q, cache, _int32(lens), window=400, sinks=3).reshape(3, T, -1)
     for b in range(3):
         one = [t[b:b + 1].contiguous() for t in cache]

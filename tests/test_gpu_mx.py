@@ -235,6 +235,133 @@ def test_product(fmt, M, N, K):
 
 
 @pytest.mark.parametrize("fmt", ["fp8", "fp4"])
+@pytest.mark.parametrize("tile", B.MX_TILES)
+@pytest.mark.parametrize("M,N,K", [(1, 1, 1), (3, 50, 129), (40, 264, 385), (300, 130, 640), (517, 777, 897), (260, 600, 2200)])
+def test_product_tiles(fmt, tile, M, N, K):
+    """Every tile, with odd numbers of steps and of pieces past the ends: within
+    the bound, and bit for bit the tile that the library takes."""
+    import torch
+    log(f"gemm_mx {fmt} tile {tile} {M}x{N}x{K}")
+    ac, ab, a = _operand(M, K, fmt, 1)
+    bc, bb, b = _operand(N, K, "fp4", 2)
+    da, dsa = _device(ac, ab, fmt, K)
+    db, dsb = B.op_mx_block(*_device(bc, bb, "fp4", K), K)
+    if fmt == "fp4" and tile == "256x256":
+        with pytest.raises(B.LMGCError):
+            B.op_gemm_mx(da, dsa, fmt, db, dsb, N, K, tile=tile)
+        return
+    out = B.op_gemm_mx(da, dsa, fmt, db, dsb, N, K, tile=tile)
+    ref = a @ b.T
+    err = np.abs(_host(out).astype(np.float64) - ref)
+    assert (err <= _product_tol(a, b, fmt, "store", ref, None)).all(), err.max()
+    assert torch.equal(out, B.op_gemm_mx(da, dsa, fmt, db, dsb, N, K))
+    add = torch.randn(M, N, device="cuda")
+    for kind, dt in (("store", torch.float32), ("bf16", torch.bfloat16)):
+        room = torch.full((M * N + 512,), 7.0, dtype=dt, device="cuda")
+        got = B.op_gemm_mx(da, dsa, fmt, db, dsb, N, K, kind, add=add, out=room[256:256 + M * N].view(M, N), tile=tile)
+        assert torch.equal(got, (out + add).to(dt))
+        assert (room[:256] == 7).all() and (room[256 + M * N:] == 7).all()
+
+
+@pytest.mark.parametrize("fmt,M,N,K", [("fp8", 2000, 2050, 900), ("fp8", 4100, 4100, 1200), ("fp8", 9000, 4600, 700),
+                                       ("fp4", 1030, 2050, 1200), ("fp4", 4100, 4100, 600), ("fp4", 20, 13001, 700)])
+def test_product_large(fmt, M, N, K):
+    """Sizes at which the library takes its large tiles, against float64 on the
+    device; the bound is _product_tol's, with the largest products of all steps
+    in the place of each step's."""
+    import torch
+    log(f"gemm_mx {fmt} {M}x{N}x{K}")
+    g = torch.Generator(device="cuda").manual_seed(M)
+    a, sa = B.op_mx_quantize(torch.randn(M, K, generator=g, device="cuda"), fmt)
+    w, sw = B.op_mx_quantize(0.02 * torch.randn(N, K, generator=g, device="cuda"), "fp4")
+    b, sb = B.op_mx_block(w, sw, K)
+    va, vb = B.op_mx_dequantize(a, sa, fmt, K).double(), B.op_mx_dequantize(w, sw, "fp4", K).double()
+    out = B.op_gemm_mx(a, sa, fmt, b, sb, N, K)
+    nk = -(-K // 128)
+    tol = (nk + 1) * 2.0 ** -23 * (va.abs() @ vb.abs().T)
+    if fmt == "fp8":
+        tol += nk * 128 * 2.0 ** -18 * torch.outer(va.abs().amax(1), vb.abs().amax(1))
+    assert ((out.double() - va @ vb.T).abs() <= tol).all()
+
+
+def test_norm_and_product_in_graphs():
+    """Add + norm, product and quantisation captured once and replayed over new
+    inputs, with eager work between; two graphs, one after the other, on the
+    same buffers."""
+    import torch
+    M, d, N = 37, 768, 640
+    g = torch.Generator(device="cuda").manual_seed(3)
+    h, x, gain = (torch.zeros(M, d, device="cuda"), torch.zeros(M, d, dtype=torch.bfloat16, device="cuda"),
+                  torch.ones(d, device="cuda"))
+    b, sb = B.op_mx_block(*B.op_mx_quantize(0.02 * torch.randn(N, d, generator=g, device="cuda"), "fp4"), d)
+    codes, scales = B.op_mx_quantize(h, "fp8")
+    y, yc, ys = torch.empty(M, N, device="cuda"), *B.op_mx_quantize(torch.zeros(M, N, device="cuda"), "fp4")
+
+    def step(h, x, y, codes, scales, yc, ys):
+        B.op_add_norm_mx(h, x, gain, 1e-5, "fp8", out=h, codes=codes, scales=scales)
+        B.op_gemm_mx(codes, scales, "fp8", b, sb, N, d, out=y)
+        B.op_mx_quantize(y, "fp4", codes=yc, scales=ys)
+
+    bufs = (h, x, y, codes, scales, yc, ys)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        step(*bufs)
+    torch.cuda.current_stream().wait_stream(side)
+    graphs = []
+    for _ in range(2):
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            step(*bufs)
+        graphs.append(graph)
+    for i in range(6):
+        nh, nx = torch.randn(M, d, generator=g, device="cuda"), torch.randn(M, d, generator=g, device="cuda").to(torch.bfloat16)
+        h.copy_(nh), x.copy_(nx)
+        graphs[i % 2].replay()
+        torch.cuda.synchronize()
+        mine = (nh, nx) + tuple(t.clone().zero_() for t in bufs[2:])
+        step(*mine)
+        assert all(torch.equal(p, q) for p, q in zip(bufs, mine)), i
+
+
+def test_tensors_on_another_device_are_refused():
+    import torch
+    h, g = torch.randn(4, 64, device="cuda"), torch.ones(64, device="cuda")
+    codes, scales = B.op_mx_quantize(h, "fp4")
+    b, sb = B.op_mx_block(codes, scales, 64)
+    for call in (lambda: B.op_mx_quantize(h.cpu(), "fp8"), lambda: B.op_mx_dequantize(codes, scales.cpu(), "fp4", 64),
+                 lambda: B.op_mx_block(codes.cpu(), scales, 64), lambda: B.op_add_norm_mx(h, h.cpu(), g, 1e-5, "fp8"),
+                 lambda: B.op_add_norm_mx(h, None, g.cpu(), 1e-5, "fp8"),
+                 lambda: B.op_gemm_mx(codes, scales, "fp4", b.cpu(), sb, 4, 64),
+                 lambda: B.op_gemm_mx(codes, scales, "fp4", b, sb, 4, 64, add=torch.zeros(4, 4))):
+        with pytest.raises(ValueError):
+            call()
+
+
+def test_rows_past_32_bits():
+    """Rows 2^31 elements apart, and more rows than one launch takes."""
+    import torch
+    ld = (1 << 31) + 64
+    big = torch.empty(ld + 96, dtype=torch.bfloat16, device="cuda")
+    x = big.as_strided((2, 96), (ld, 1))
+    x.copy_(torch.randn(2, 96, device="cuda"))
+    codes, scales = B.op_mx_quantize(x, "fp8")
+    c2, s2 = B.op_mx_quantize(x.contiguous(), "fp8")
+    assert torch.equal(codes, c2) and torch.equal(scales, s2)
+    back = B.op_mx_dequantize(codes, scales, "fp8", 96, dtype=torch.bfloat16)
+    B.op_mx_dequantize(codes, scales, "fp8", 96, out=x)
+    assert torch.equal(x, back)
+    del big, x
+    M, d = (1 << 23) + 5, 32
+    h = torch.randn(M, d, device="cuda").to(torch.bfloat16)
+    g = torch.ones(d, device="cuda")
+    codes, scales = B.op_add_norm_mx(h, None, g, 1e-5, "fp4")
+    for lo, hi in ((0, 9), ((1 << 23) - 4, M)):
+        c2, s2 = B.op_add_norm_mx(h[lo:hi].contiguous(), None, g, 1e-5, "fp4")
+        assert torch.equal(codes[lo:hi], c2) and torch.equal(scales[lo:hi], s2)
+
+
+@pytest.mark.parametrize("fmt", ["fp8", "fp4"])
 @pytest.mark.parametrize("N,K", [(272, 1184), (2048, 640)])
 def test_product_rows_do_not_depend_on_m(fmt, N, K):
     """A row's bits are the same alone, in a step's batch and in a prompt."""

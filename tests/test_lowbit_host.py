@@ -79,7 +79,11 @@ def test_add_norm_refuses():
 def test_gemm_refuses():
     def g(a=A[0], asc=A[1], fmt=0, b=A[2], bsc=A[3], add=None, out=A[4], M=4, N=32, K=128, kind=0):
         return rc("lmgc_op_gemm_mx", a, asc, fmt, b, bsc, add, out, M, N, K, kind, None)
+
+    def t(fmt, tile):
+        return rc("lmgc_op_gemm_mx_tile", A[0], A[1], fmt, A[2], A[3], None, A[4], 0, 32, 128, 0, tile, None)
     assert g(M=0) == 0
+    assert [t(0, i) for i in (-1, 0, 5, 6)] == [0, 0, 0, EINVAL] and [t(1, i) for i in (4, 5)] == [0, EINVAL]
     for bad in (dict(a=None), dict(asc=None), dict(b=None), dict(bsc=None), dict(out=None), dict(fmt=2), dict(kind=1),
                 dict(kind=2), dict(kind=4), dict(M=-1), dict(M=(1 << 26) + 1), dict(N=0), dict(K=0), dict(K=(1 << 20) + 1),
                 dict(out=A[0]), dict(out=A[1]), dict(out=A[2]), dict(out=A[3]), dict(a=A[0] + 8), dict(out=A[4] + 4),
@@ -95,7 +99,8 @@ def _cache_args(**kw):
 
 CACHE_BAD = [dict(B=0), dict(Hkv=0), dict(T=0), dict(cap=0), dict(cap=100), dict(B=16384), dict(cap=(1 << 24) + 64),
              dict(lens=None), dict(kc=None), dict(ks=None), dict(vc=None), dict(vs=None), dict(kc=A[1] + 8),
-             dict(ks=A[2] + 4), dict(lens=A[0] + 2), dict(counts=A[5] + 1), dict(vc=A[1]), dict(vs=A[2])]
+             dict(ks=A[2] + 4), dict(lens=A[0] + 2), dict(counts=A[5] + 1), dict(vc=A[1]), dict(vs=A[2]),
+             dict(ks=A[1] + 16), dict(vs=A[3] + 64), dict(ks=A[3])]
 
 
 def test_append_refuses():
@@ -103,7 +108,8 @@ def test_append_refuses():
         a = _cache_args(**kw)
         return rc("lmgc_op_kv8_append", k, v, a["B"], a["Hkv"], a["T"], a["hd"], a["cap"], a["lens"], a["counts"],
                   a["kc"], a["ks"], a["vc"], a["vs"], None)
-    for bad in CACHE_BAD + [dict(k=None), dict(v=None), dict(k=A[6] + 8)]:
+    for bad in CACHE_BAD + [dict(k=None), dict(v=None), dict(k=A[6] + 8), dict(k=A[1] + 64), dict(v=A[3]), dict(v=A[2]),
+                            dict(k=A[4])]:
         assert ap(**bad) == EINVAL, bad
     for hd in (32, 96, 256):
         assert ap(hd=hd) == EUNSUPPORTED
@@ -116,9 +122,12 @@ def test_attention_refuses():
                   a["kc"], a["ks"], a["vc"], a["vs"], window, sinks, out, ws, nws, None)
     for bad in CACHE_BAD + [dict(q=None), dict(out=None), dict(Hq=3), dict(Hq=0), dict(window=-1), dict(sinks=-1),
                             dict(out=A[6]), dict(q=A[6] + 8), dict(ws=A[8] + 8), dict(cap=4096, ws=A[6]),
-                            dict(cap=4096, ws=A[7])]:
+                            dict(cap=4096, ws=A[7]), dict(out=A[1] + 64), dict(out=A[4]), dict(cap=4096, ws=A[3])]:
         assert at(**bad) == EINVAL, bad
     assert at(hd=80) == EUNSUPPORTED
+    # over 2^32 threads in one launch (far apart: the buffers of such a call do not overlap)
+    far = dict(kc=1 << 50, ks=1 << 51, vc=1 << 52, vs=1 << 53, q=1 << 54, out=1 << 55, cap=1 << 24, T=1 << 24, B=64)
+    assert at(**far) == EUNSUPPORTED
     need = rc("lmgc_kv8_workspace", 2, 4, 2, 3, 64, 4096)
     assert need > 0
     assert at(cap=4096, nws=need - 1) == ESIZE and at(cap=4096, ws=None) == ESIZE
@@ -130,4 +139,8 @@ def test_workspace():
         assert rc("lmgc_kv8_workspace", *bad) == EINVAL
     assert rc("lmgc_kv8_workspace", 1, 4, 2, 1, 96, 128) == EUNSUPPORTED
     assert rc("lmgc_kv8_workspace", 1, 4, 2, 1, 64, 128) >= 0
+    # a long cache is split into 64 parts at most, 16 with many columns
+    assert rc("lmgc_kv8_workspace", 1, 4, 2, 1, 64, 1 << 24) == 4 * 64 * 66 * 4
+    assert rc("lmgc_kv8_workspace", 1, 4, 2, 512, 64, 1 << 24) == 4 * 512 * 16 * 66 * 4
+    assert rc("lmgc_kv8_workspace", 1, 4, 2, 513, 64, 1 << 24) == 0
     assert ctypes.sizeof(ctypes.c_int64) == 8
