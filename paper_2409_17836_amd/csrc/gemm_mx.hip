@@ -206,14 +206,17 @@ __global__ __launch_bounds__(WM * WN * 64, 1) void gemm_mx_tile_kernel(
     vsb[i] = (min(wave * C::SPB + i, C::SB - 1) * 4 + (lane >> 4)) * ns * 16 + (lane & 15) * 16;
   auto load_stage = [&](int s, int slot) __attribute__((always_inline)) {
     const lds_bytes_t at = lds0 + slot * C::kStage;
-    // from the stage's first column on: of a last stage with one step of two
-    // (e2m1, an odd number of steps) the last row's second half is past the end
-    const int ka = s * 128, kb = s * (C::KPS * 1024);
-    const __amdgpu_buffer_rsrc_t ra = buffer_of(pa + ka, s < nst ? mrows * lda - ka : 0), rb = buffer_of(pb + kb, s < nst ? groups * nk * 1024 - kb : 0);
+    // e4m3: stages are whole steps, and their place a scalar offset.  e2m1: of
+    // a last stage with one step of two (an odd number of steps) the last row's
+    // second half is past the end, so the buffers begin at the stage (590 us
+    // for 570 at 16384 x 12288 x 4096 in e4m3, which does not need it).
+    const int ka = s * 128, kb = s * (C::KPS * 1024), shift = C::KPS > 1 ? 1 : 0;
+    const __amdgpu_buffer_rsrc_t ra = buffer_of(pa + shift * ka, s < nst ? mrows * lda - shift * ka : 0),
+                                 rb = buffer_of(pb + shift * kb, s < nst ? groups * nk * 1024 - shift * kb : 0);
 #pragma unroll
-    for (int i = 0; i < C::LPA; i++) load_lds(ra, at + min(wave * C::LPA + i, C::LA - 1) * 1024, va[i], 0);
+    for (int i = 0; i < C::LPA; i++) load_lds(ra, at + min(wave * C::LPA + i, C::LA - 1) * 1024, va[i], shift ? 0 : ka);
 #pragma unroll
-    for (int i = 0; i < C::LPB; i++) load_lds(rb, at + (C::LA + wave * C::LPB + i) * 1024, vb[i], 0);
+    for (int i = 0; i < C::LPB; i++) load_lds(rb, at + (C::LA + wave * C::LPB + i) * 1024, vb[i], shift ? 0 : kb);
   };
   const int nu = ns / 16;
   auto load_scales = [&](int u) __attribute__((always_inline)) {
@@ -386,9 +389,10 @@ void launch_tile(const uint8_t* a, const uint8_t* as, const uint8_t* b, const ui
 // (microseconds, fitted to launches from a graph with N x K of 768 x 768 to
 // 22016 x 4096 and 1 to 16384 rows).  At K = 4096, e4m3, the choice and what
 // the next tile would take:
-//   16 x 4096      16x16   5.8 us   64x64  7.5      1 x 22016   32x128 10.2   64x64 11.2
-//   256 x 4096     64x64   8.5      32x128 9.8      1000 x 4096 128x128 19.7  128x256 23.4
-//   2048 x 4096    128x256 28.2     128x128 35.4    16384 x 12288 256x256 585 128x256 630
+//   16 x 4096    16x16   5.8 us   64x64  7.5      1 x 22016     32x128 10.2   64x64 11.2
+//   500 x 2048   64x64   8.2      128x64 11.6     512 x 4096    128x64 12.3   64x64 13.0
+//   1000 x 4096  128x128 17.6     128x64 22.4     2048 x 4096   128x256 28.9  128x128 30.5
+//   4096 x 4096  256x256 51.2     128x128 56.6    16384 x 12288 256x256 567   128x256 630
 // 16x16 tiles run three to a CU and, past that, fetch the rows of A too often
 // (22016 columns: 13.4 us); 32x128 is for 32 rows at most.  256x256 is left to
 // e4m3: with e2m1 128x256 is as fast (16384 x 4096 x 11008: 364 and 365 us).
@@ -399,10 +403,10 @@ int pick_tile(int fmt, int64_t M, int64_t N, int K) {
   };
   constexpr int kTiles = LMGC_MX_TILE_256X256 + 1;
   static const Cost cost[2][kTiles] = {
-      {{16, 16, 2.0, 0.4, 0.100}, {32, 128, 2.0, 0.8, 0.200}, {64, 64, 2.0, 0.7, 0.146}, {128, 128, 2.0, 1.5, 0.400},
-       {128, 256, 2.0, 3.0, 0.555}, {256, 256, 3.0, 5.0, 1.070}},
-      {{16, 16, 2.0, 0.4, 0.071}, {32, 128, 2.0, 0.8, 0.152}, {64, 64, 2.0, 0.9, 0.145}, {128, 128, 2.0, 1.8, 0.310},
-       {128, 256, 2.0, 2.2, 0.425}, {256, 256, 0, 1e30, 0}}};
+      {{16, 16, 2.0, 0.4, 0.100}, {32, 128, 2.0, 0.8, 0.200}, {64, 64, 2.0, 0.7, 0.146}, {128, 64, 2.5, 0.9, 0.285},
+       {128, 128, 2.5, 0.9, 0.400}, {128, 256, 2.5, 2.5, 0.720}, {256, 256, 4.0, 3.5, 1.330}},
+      {{16, 16, 2.0, 0.4, 0.071}, {32, 128, 2.0, 0.8, 0.152}, {64, 64, 2.3, 0.9, 0.125}, {128, 64, 2.5, 1.1, 0.230},
+       {128, 128, 2.5, 1.2, 0.290}, {128, 256, 2.5, 3.0, 0.530}, {256, 256, 0, 1e30, 0}}};
   const int nk = (int)(mx_cols(K) / 128);
   int best = LMGC_MX_TILE_64X64;
   double least = 1e300;
@@ -428,7 +432,8 @@ void launch_fmt(const uint8_t* a, const uint8_t* as, const uint8_t* b, const uin
     case LMGC_MX_TILE_16X16: return launch_tile<FMT, 16, 16, 1, 1, F8 ? 8 : 6>(a, as, b, bs, M, N, K, add, out, bf16, s);
     case LMGC_MX_TILE_32X128: return launch_tile<FMT, 32, 128, 1, 4, F8 ? 6 : 4>(a, as, b, bs, M, N, K, add, out, bf16, s);
     case LMGC_MX_TILE_64X64: return launch_tile<FMT, 64, 64, 2, 2, 4>(a, as, b, bs, M, N, K, add, out, bf16, s);
-    case LMGC_MX_TILE_128X128: return launch_tile<FMT, 128, 128, 2, 2, F8 ? 4 : 3>(a, as, b, bs, M, N, K, add, out, bf16, s);
+    case LMGC_MX_TILE_128X64: return launch_tile<FMT, 128, 64, 4, 1, 4>(a, as, b, bs, M, N, K, add, out, bf16, s);
+    case LMGC_MX_TILE_128X128: return launch_tile<FMT, 128, 128, 4, 2, F8 ? 3 : 2>(a, as, b, bs, M, N, K, add, out, bf16, s);
     case LMGC_MX_TILE_128X256: return launch_tile<FMT, 128, 256, 2, 4, F8 ? 4 : 2>(a, as, b, bs, M, N, K, add, out, bf16, s);
     default:
       if constexpr (F8) launch_tile<FMT, 256, 256, 4, 2, 3>(a, as, b, bs, M, N, K, add, out, bf16, s);

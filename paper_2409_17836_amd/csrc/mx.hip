@@ -135,10 +135,9 @@ __global__ __launch_bounds__(256) void mx_block_kernel(const uint8_t* __restrict
 // codes only if the value does.  The kernel is bound by its memory traffic
 // either way.
 template <int FMT, typename TH, typename TX, typename TG, int NC, int NT>
-__global__ __launch_bounds__(NT < 256 ? 256 : NT) void add_norm_mx_kernel(const TH* h, const TX* __restrict__ x,
-                                                          const TG* __restrict__ gain, float eps, int64_t M, int d,
-                                                          TH* out, uint8_t* __restrict__ codes,
-                                                          uint8_t* __restrict__ scales) {
+__global__ __launch_bounds__(NT < 256 ? 256 : NT) void add_norm_mx_kernel(
+    const TH* h, const TX* __restrict__ x, const TG* __restrict__ gain, float eps, int64_t M, int d, TH* out,
+    uint8_t* __restrict__ codes, uint8_t* __restrict__ scales) {
 #pragma clang fp contract(off)
   constexpr int NW = NT / 64, kRows = NT < 256 ? 256 / NT : 1;  // waves of a row, rows of a block
   __shared__ double part[NW];
