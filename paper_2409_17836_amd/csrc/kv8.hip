@@ -218,12 +218,21 @@ __device__ inline __amdgpu_buffer_rsrc_t block_buffer(const uint8_t* codes, int6
 // w, w + 8, ..: S^T = K Q^T, so lane (col, g) holds the scores of its column
 // and tokens 16 i + 4 g + r of a block, an online softmax, O^T += V^T P^T.
 // The waves' parts meet in LDS.
+//
+// Bound by the bytes of the cache.  ONCE, a single tile of columns: nothing
+// reads the codes again before the next step, so they are loaded past the
+// caches' order of use.  8 sequences x 32 heads of 128 over 4094 tokens, 268
+// MB, from a cache not in any cache: 48.8 us, 5.5 TB/s (54.6 without ONCE); 32
+// sequences 171 us, 6.1 TB/s; one sequence 11.8 us.  A cache in the L2 costs a
+// little more that way (32 x 4 heads of 64 over 2000 tokens: 12.2 us for
+// 11.2), and with two tiles the second one misses it (24.5 us for 22.3).
 constexpr int kSplitCols = 32;
+constexpr int kNonTemporal = 2;  // the instruction's nt bit
 constexpr int kOneBytes = 256 << 10, kSplitBytes = 128 << 10;
 constexpr int kSplitWaves = 8;
 constexpr int kMaxSplits = 64;  // a lane each in the join
 
-template <int HD>
+template <int HD, bool ONCE>
 __global__ __launch_bounds__(kSplitWaves * 64, 4) void attn_kv8_split_kernel(
     const uint16_t* __restrict__ q, const uint8_t* __restrict__ kc, const float* __restrict__ ks,
     const uint8_t* __restrict__ vc, const float* __restrict__ vs, const int32_t* __restrict__ lens,
@@ -261,7 +270,7 @@ __global__ __launch_bounds__(kSplitWaves * 64, 4) void attn_kv8_split_kernel(
     // (through buffers of a block each: their addresses take no vector registers)
     const __amdgpu_buffer_rsrc_t kb = block_buffer<HD>(kc, blk), vb = block_buffer<HD>(vc, blk);
     auto codes = [&](__amdgpu_buffer_rsrc_t block, int i) __attribute__((always_inline)) {
-      return __builtin_amdgcn_raw_buffer_load_b128(block, lane * 16, i * 1024, 0);
+      return __builtin_amdgcn_raw_buffer_load_b128(block, lane * 16, i * 1024, ONCE ? kNonTemporal : 0);
     };
     u32x4 kr[4][NC], vr[ND];
 #pragma unroll
@@ -764,8 +773,13 @@ hipError_t launch_attention_kv8(const uint16_t* q, int B, int Hq, int Hkv, int T
     constexpr int HD = decltype(h)::value;
     const dim3 join((unsigned)cols, Hkv, B);
     if (cols <= kSplitCols) {
-      attn_kv8_split_kernel<HD><<<dim3(nsplit, (cols > 16 ? 2 : 1) * Hkv, B), kSplitWaves * 64, 0, s>>>(
-          q, kc, ks, vc, vs, lens, counts, Hkv, G, 65536 / G + 1, T, cap, nsplit, chunk, mask, sl2, po, pml, out);
+      const dim3 grid(nsplit, (cols > 16 ? 2 : 1) * Hkv, B);
+      auto split = [&](auto once) {
+        attn_kv8_split_kernel<HD, decltype(once)::value><<<grid, kSplitWaves * 64, 0, s>>>(
+            q, kc, ks, vc, vs, lens, counts, Hkv, G, 65536 / G + 1, T, cap, nsplit, chunk, mask, sl2, po, pml, out);
+      };
+      if (cols > 16) split(std::false_type{});
+      else split(std::true_type{});
       if (nsplit > 1)
         attn_kv8_join_kernel<HD, 16><<<join, 64, 0, s>>>(po, pml, lens, counts, Hkv, G, T, cap, nsplit, chunk, mask, out);
     } else {
