@@ -576,8 +576,8 @@ int lmgc_op_gemm_mx(const uint8_t* d_a, const uint8_t* d_a_scales, int32_t a_fmt
  * the same bits), or on the one the library takes for the shape (tile < 0).
  * EINVAL for LMGC_MX_TILE_256X256 with FP4 in A, which does not have it. */
 enum {
-  LMGC_MX_TILE_16X16 = 0, LMGC_MX_TILE_32X128 = 1, LMGC_MX_TILE_64X64 = 2, LMGC_MX_TILE_128X64 = 3,
-  LMGC_MX_TILE_128X128 = 4, LMGC_MX_TILE_128X256 = 5, LMGC_MX_TILE_256X256 = 6
+  LMGC_MX_TILE_16X16 = 0, LMGC_MX_TILE_16X32 = 1, LMGC_MX_TILE_16X64 = 2, LMGC_MX_TILE_64X64 = 3,
+  LMGC_MX_TILE_128X64 = 4, LMGC_MX_TILE_128X128 = 5, LMGC_MX_TILE_128X256 = 6, LMGC_MX_TILE_256X256 = 7
 };
 int lmgc_op_gemm_mx_tile(const uint8_t* d_a, const uint8_t* d_a_scales, int32_t a_fmt,
                          const uint8_t* d_b, const uint8_t* d_b_scales, const float* d_add,

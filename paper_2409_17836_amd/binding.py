@@ -679,7 +679,7 @@ def op_add_norm_mx(h, x, gain, eps: float, fmt: str, out=None, codes=None, scale
 
 
 MX_KINDS = {"store": 0, "bf16": 3}
-MX_TILES = ("16x16", "32x128", "64x64", "128x64", "128x128", "128x256", "256x256")  # LMGC_MX_TILE_*
+MX_TILES = ("16x16", "16x32", "16x64", "64x64", "128x64", "128x128", "128x256", "256x256")  # LMGC_MX_TILE_*
 
 
 def op_gemm_mx(a, a_scales, a_fmt: str, b, b_scales, N: int, K: int, kind: str = "store", add=None, out=None,

@@ -71,7 +71,7 @@ __device__ inline void store_rows(const float* src, int64_t at, int rows, int nc
                                   int bf16) {
   constexpr int RS = COLS + 4;
   if (bf16) {
-    constexpr int PER = 8, LPR = COLS / PER, RPI = 64 / LPR < 16 ? 64 / LPR : 16;  // values a lane, lanes a row, rows at once
+    constexpr int PER = 8, LPR = COLS / PER, RPI = 64 / LPR;  // values a lane, lanes a row, rows at once
     const bool vec = (N & 7) == 0;
 #pragma unroll
     for (int q = 0; q < 16 / RPI; q++) {
@@ -94,7 +94,7 @@ __device__ inline void store_rows(const float* src, int64_t at, int rows, int nc
       }
     }
   } else {
-    constexpr int PER = 4, LPR = COLS / PER, RPI = 64 / LPR < 16 ? 64 / LPR : 16;
+    constexpr int PER = 4, LPR = COLS / PER, RPI = 64 / LPR;
     const bool vec = (N & 3) == 0;
 #pragma unroll
     for (int q = 0; q < 16 / RPI; q++) {
@@ -137,15 +137,14 @@ __device__ inline void store_rows(const float* src, int64_t at, int rows, int nc
 // constants.
 //
 // ONCE, a single row of tiles: nothing reads the weights again before the next
-// step, so they are loaded past the caches' order of use (1 x 11008 x 4096
-// from memory 7.5 us for 8.1, 64 x 22016 x 4096 18.4 for 19.3; with more rows
-// of tiles the others miss them).
+// step, so they are loaded past the caches' order of use (64 x 22016 x 4096
+// from memory 18.4 us for 19.3; with more rows of tiles the others miss them).
 template <int FMT, int BM, int BN, int WM, int WN, int ST>
 struct Tile {
   static constexpr int NW = WM * WN, PA = FMT == LMGC_MX_FP8 ? 2 : 1, KPS = 2 / PA;  // steps per stage
   static constexpr int G = 4 / KPS;                                                   // stages per group of scales
   static constexpr int LA = BM / 8, LB = BN / 16 * KPS, L = LA + LB;                  // pieces of a stage
-  static constexpr int LPA = (LA + NW - 1) / NW, LPB = LB / NW, LPW = LPA + LPB;      // loads of a stage, each wave
+  static constexpr int LPA = LA / NW, LPB = LB / NW, LPW = LPA + LPB;                 // loads of a stage, each wave
   static constexpr int SA = (BM + 63) / 64, SB = (BN + 63) / 64, S = SA + SB;  // pieces of a group's scales
   // with fewer pieces than waves, some waves load one again, so that all have
   // the same loads in flight
@@ -154,7 +153,7 @@ struct Tile {
   static constexpr int FM = BM / WM / 16, FN = BN / WN / 16;
   static constexpr int kStage = L * 1024, kScale = S * 1024;
   static constexpr int kLds = ST * kStage + (PS + 1) * kScale;
-  static_assert(LB % NW == 0 && kLds <= 160 * 1024, "stage does not fit");
+  static_assert(LA % NW == 0 && LB % NW == 0 && kLds <= 160 * 1024, "stage does not fit");
   static_assert((ST - 2) * LPW + PS * SPW < 64, "more loads in flight than the wait counts");
   // loads that may be in flight when stage G u + s + 1 is needed: those of
   // the ST - 2 stages after it, and the scales asked for among them
@@ -198,7 +197,7 @@ __global__ __launch_bounds__(WM * WN * 64, 1) void gemm_mx_tile_kernel(
   int va[C::LPA], vb[C::LPB], vsa[C::SPA], vsb[C::SPB];
 #pragma unroll
   for (int i = 0; i < C::LPA; i++) {
-    const int row = min(wave * C::LPA + i, C::LA - 1) * 8 + (lane >> 3);
+    const int row = (wave * C::LPA + i) * 8 + (lane >> 3);
     va[i] = row * lda + (((lane & 7) ^ ((row >> 1) & 7)) << 4);
   }
 #pragma unroll
@@ -221,7 +220,7 @@ __global__ __launch_bounds__(WM * WN * 64, 1) void gemm_mx_tile_kernel(
     const __amdgpu_buffer_rsrc_t ra = buffer_of(pa + shift * ka, s < nst ? mrows * lda - shift * ka : 0),
                                  rb = buffer_of(pb + shift * kb, s < nst ? groups * nk * 1024 - shift * kb : 0);
 #pragma unroll
-    for (int i = 0; i < C::LPA; i++) load_lds(ra, at + min(wave * C::LPA + i, C::LA - 1) * 1024, va[i], shift ? 0 : ka);
+    for (int i = 0; i < C::LPA; i++) load_lds(ra, at + (wave * C::LPA + i) * 1024, va[i], shift ? 0 : ka);
 #pragma unroll
     for (int i = 0; i < C::LPB; i++) load_lds<ONCE ? kNonTemporal : 0>(rb, at + (C::LA + wave * C::LPB + i) * 1024, vb[i], shift ? 0 : kb);
   };
@@ -376,6 +375,108 @@ __global__ __launch_bounds__(WM * WN * 64, 1) void gemm_mx_tile_kernel(
   }
 }
 
+// Few rows.  A wave by itself takes 16 rows x 16 FN columns and needs no LDS:
+// B's blocks and A's rows lie in the operands' order, so a load fills the
+// instruction's registers.  D steps are under way: step k's operands are used
+// and the loads of step k + D go into their registers.  Bound by the latency
+// of memory and then by the bytes of the weights, and with 16 rows by the rows
+// of A that every tile fetches, hence wider tiles for more columns.  1 x 4096 x
+// 4096 3.2 us, 16 x 4096 x 11008 8.7 us, 1 x 22016 x 4096 8.6 us (5.6 TB/s);
+// with the operands through LDS, whose latency was a step's time, 5.7, 11.5
+// and 10.4.
+template <int FMT, int FN, int D, bool ONCE>
+__global__ __launch_bounds__(64) void gemm_mx_rows_kernel(const uint8_t* __restrict__ A, const uint8_t* __restrict__ As,
+                                                          const uint8_t* __restrict__ B, const uint8_t* __restrict__ Bs,
+                                                          int M, int N, int nk, int ns, const float* add, void* out,
+                                                          int bf16) {
+  constexpr int PA = FMT == LMGC_MX_FP8 ? 2 : 1, AUX = ONCE ? kNonTemporal : 0;
+  static_assert(D % 4 == 0, "whole groups of scales");
+  const int lane = threadIdx.x, r = lane & 15, g = lane >> 4;
+  const int64_t m0 = (int64_t)blockIdx.y * 16;
+  const int n0 = blockIdx.x * 16 * FN, mrows = (int)min<int64_t>(16, M - m0), groups = min(FN, (N + 15) / 16 - n0 / 16);
+  const int lda = nk * 64 * PA;
+  const uint8_t *pa = A + m0 * lda, *psa = As + m0 * ns, *pb = B + (int64_t)(n0 / 16) * nk * 1024,
+                *psb = Bs + (int64_t)(n0 / 16) * ns * 16;
+  const int va = r * lda + 16 * g, vsa = r * ns + 4 * g;
+  u32x4 a[D][PA], b[D][FN];
+  uint32_t sa[D / 4], sb[D / 4][FN];
+  // past the last step the buffers are empty: such loads give zeros and move nothing
+  auto load = [&](int s, int k) __attribute__((always_inline)) {
+    const __amdgpu_buffer_rsrc_t ra = buffer_of(pa, k < nk ? mrows * lda : 0), rb = buffer_of(pb, k < nk ? groups * nk * 1024 : 0);
+#pragma unroll
+    for (int j = 0; j < FN; j++) b[s][j] = __builtin_amdgcn_raw_buffer_load_b128(rb, j * nk * 1024 + lane * 16, k * 1024, AUX);
+#pragma unroll
+    for (int q = 0; q < PA; q++) a[s][q] = __builtin_amdgcn_raw_buffer_load_b128(ra, va + 64 * q, k * 64 * PA, 0);
+    if (s % 4 == 0) {
+      const __amdgpu_buffer_rsrc_t rsa = buffer_of(psa, k < nk ? mrows * ns : 0), rsb = buffer_of(psb, k < nk ? groups * ns * 16 : 0);
+      sa[s / 4] = __builtin_amdgcn_raw_buffer_load_b32(rsa, vsa, k * 4, 0);
+#pragma unroll
+      for (int j = 0; j < FN; j++) sb[s / 4][j] = __builtin_amdgcn_raw_buffer_load_b32(rsb, j * ns * 16 + lane * 4, k * 64, AUX);
+    }
+  };
+  f32x4 acc[FN] = {};
+  auto step = [&](auto s_tag) __attribute__((always_inline)) {
+    constexpr int S = decltype(s_tag)::value;
+    i32x8 av = {};
+#pragma unroll
+    for (int e = 0; e < 4; e++) {
+      av[e] = (int)a[S][0][e];
+      av[4 + e] = PA == 2 ? (int)a[S][PA - 1][e] : 0;
+    }
+#pragma unroll
+    for (int j = 0; j < FN; j++) acc[j] = mma<FMT, S % 4>(__builtin_bit_cast(i32x4, b[S][j]), av, acc[j], sb[S / 4][j], sa[S / 4]);
+  };
+  auto steps = [&](auto self, auto s_tag, int k0, auto loads) __attribute__((always_inline)) -> void {
+    constexpr int S = decltype(s_tag)::value;
+    if constexpr (S < D) {
+      if (!decltype(loads)::value && k0 + S >= nk) return;
+      step(s_tag);
+      // (the scales of a group are in use to its last step)
+      if constexpr (decltype(loads)::value && S % 4 == 3) {
+#pragma unroll
+        for (int i = S - 3; i <= S; i++) load(i, k0 + D + i);
+      }
+      self(self, std::integral_constant<int, S + 1>{}, k0, loads);
+    }
+  };
+#pragma unroll
+  for (int s = 0; s < D; s++) load(s, s);
+  int k = 0;
+  for (; k + D < nk; k += D) steps(steps, std::integral_constant<int, 0>{}, k, std::true_type{});
+  steps(steps, std::integral_constant<int, 0>{}, k, std::false_type{});
+
+  if (r >= mrows) return;
+#pragma unroll
+  for (int j = 0; j < FN; j++) {
+    const int n = n0 + 16 * j + 4 * g;
+    if (n >= N) continue;
+    const int64_t at = (m0 + r) * N + n;
+    f32x4 v = acc[j];
+    if ((N & 3) == 0) {
+      if (add) v += *reinterpret_cast<const f32x4*>(add + at);
+      if (bf16) *reinterpret_cast<mx_u32x2*>((uint16_t*)out + at) = mx_u32x2{pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3])};
+      else *reinterpret_cast<f32x4*>((float*)out + at) = v;
+    } else {
+#pragma unroll
+      for (int e = 0; e < 4; e++) {
+        if (n + e >= N) continue;
+        const float x = add ? v[e] + add[at + e] : v[e];
+        if (bf16) ((uint16_t*)out)[at + e] = f32_to_bf16(x);
+        else ((float*)out)[at + e] = x;
+      }
+    }
+  }
+}
+
+template <int FMT, int FN, int D>
+void launch_rows(const uint8_t* a, const uint8_t* as, const uint8_t* b, const uint8_t* bs, int M, int N, int K,
+                 const float* add, void* out, int bf16, hipStream_t s) {
+  const int nk = (int)(mx_cols(K) / 128), ns = (int)mx_row_scales(K);
+  const dim3 grid((N + 16 * FN - 1) / (16 * FN), (M + 15) / 16);
+  if (M <= 16) gemm_mx_rows_kernel<FMT, FN, D, true><<<grid, 64, 0, s>>>(a, as, b, bs, M, N, nk, ns, add, out, bf16);
+  else gemm_mx_rows_kernel<FMT, FN, D, false><<<grid, 64, 0, s>>>(a, as, b, bs, M, N, nk, ns, add, out, bf16);
+}
+
 // Row tiles per group of the tile order: an XCD's 32 workgroups then cover
 // about as many bytes of A as of B (16384 x 12288 x 4096, e4m3: 573 us with 4,
 // 594 with 8, 604 with 16).
@@ -400,13 +501,14 @@ void launch_tile(const uint8_t* a, const uint8_t* as, const uint8_t* b, const ui
 // (microseconds, fitted to launches from a graph with N x K of 768 x 768 to
 // 22016 x 4096 and 1 to 16384 rows).  At K = 4096, e4m3, the choice and what
 // the next tile would take:
-//   16 x 4096    16x16   5.8 us   64x64  7.5      1 x 22016     32x128 10.2   64x64 11.2
+//   16 x 4096    16x16   4.3 us   16x32  4.9      16 x 22016    16x64  10.2   16x32 10.5
+//   32 x 4096    16x32   4.7      16x64  5.4      64 x 4096     16x64  5.6    16x32 7.0
 //   500 x 2048   64x64   8.2      128x64 11.6     512 x 4096    128x64 12.3   64x64 13.0
 //   1000 x 4096  128x128 17.6     128x64 22.4     2048 x 4096   128x256 28.9  128x128 30.5
 //   4096 x 4096  256x256 51.2     128x128 56.6    16384 x 12288 256x256 567   128x256 630
-// 16x16 tiles run three to a CU and, past that, fetch the rows of A too often
-// (22016 columns: 13.4 us); 32x128 is for 32 rows at most.  256x256 is left to
-// e4m3: with e2m1 128x256 is as fast (16384 x 4096 x 11008: 364 and 365 us).
+// The first three are gemm_mx_rows_kernel's: many waves to a CU, so their
+// rounds are counted in fractions.  256x256 is left to e4m3: with e2m1 128x256
+// is as fast (16384 x 4096 x 11008: 364 and 365 us).
 int pick_tile(int fmt, int64_t M, int64_t N, int K) {
   struct Cost {
     int bm, bn;
@@ -414,9 +516,9 @@ int pick_tile(int fmt, int64_t M, int64_t N, int K) {
   };
   constexpr int kTiles = LMGC_MX_TILE_256X256 + 1;
   static const Cost cost[2][kTiles] = {
-      {{16, 16, 2.0, 0.4, 0.100}, {32, 128, 2.0, 0.8, 0.200}, {64, 64, 2.0, 0.7, 0.146}, {128, 64, 2.5, 0.9, 0.285},
+      {{16, 16, 2.0, 0, 0.080}, {16, 32, 2.0, 0, 0.085}, {16, 64, 2.0, 0, 0.118}, {64, 64, 2.0, 0.7, 0.146}, {128, 64, 2.5, 0.9, 0.285},
        {128, 128, 2.5, 0.9, 0.400}, {128, 256, 2.5, 2.5, 0.720}, {256, 256, 4.0, 3.5, 1.330}},
-      {{16, 16, 2.0, 0.4, 0.071}, {32, 128, 2.0, 0.8, 0.152}, {64, 64, 2.3, 0.9, 0.125}, {128, 64, 2.5, 1.1, 0.230},
+      {{16, 16, 2.0, 0, 0.052}, {16, 32, 2.0, 0, 0.062}, {16, 64, 2.0, 0, 0.092}, {64, 64, 2.3, 0.9, 0.125}, {128, 64, 2.5, 1.1, 0.230},
        {128, 128, 2.5, 1.2, 0.290}, {128, 256, 2.5, 3.0, 0.530}, {256, 256, 0, 1e30, 0}}};
   const int nk = (int)(mx_cols(K) / 128);
   int best = LMGC_MX_TILE_64X64;
@@ -424,8 +526,9 @@ int pick_tile(int fmt, int64_t M, int64_t N, int K) {
   for (int t = 0; t < kTiles; t++) {
     const Cost& c = cost[fmt == LMGC_MX_FP8 ? 0 : 1][t];
     const int64_t tiles = (M + c.bm - 1) / c.bm * ((N + c.bn - 1) / c.bn);
-    if (t == LMGC_MX_TILE_16X16 ? tiles > 3 * 256 : t == LMGC_MX_TILE_32X128 && M > 32) continue;
-    const double rounds = t == LMGC_MX_TILE_16X16 ? 1.0 : (double)((tiles + 255) / 256);
+    const bool rows = t <= LMGC_MX_TILE_16X64;
+    if (rows && M > 1 << 19) continue;  // their grid is two-dimensional
+    const double rounds = rows ? std::max(1.0, tiles / 256.0) : (double)((tiles + 255) / 256);
     const double us = c.fixed + rounds * (c.tile + c.step * nk);
     if (us < least) {
       least = us;
@@ -440,8 +543,9 @@ void launch_fmt(const uint8_t* a, const uint8_t* as, const uint8_t* b, const uin
                 const float* add, void* out, int bf16, int tile, hipStream_t s) {
   constexpr bool F8 = FMT == LMGC_MX_FP8;
   switch (tile < 0 ? pick_tile(FMT, M, N, K) : tile) {
-    case LMGC_MX_TILE_16X16: return launch_tile<FMT, 16, 16, 1, 1, F8 ? 8 : 6>(a, as, b, bs, M, N, K, add, out, bf16, s);
-    case LMGC_MX_TILE_32X128: return launch_tile<FMT, 32, 128, 1, 4, F8 ? 6 : 4>(a, as, b, bs, M, N, K, add, out, bf16, s);
+    case LMGC_MX_TILE_16X16: return launch_rows<FMT, 1, 16>(a, as, b, bs, M, N, K, add, out, bf16, s);
+    case LMGC_MX_TILE_16X32: return launch_rows<FMT, 2, 16>(a, as, b, bs, M, N, K, add, out, bf16, s);
+    case LMGC_MX_TILE_16X64: return launch_rows<FMT, 4, 8>(a, as, b, bs, M, N, K, add, out, bf16, s);
     case LMGC_MX_TILE_64X64: return launch_tile<FMT, 64, 64, 2, 2, 4>(a, as, b, bs, M, N, K, add, out, bf16, s);
     case LMGC_MX_TILE_128X64: return launch_tile<FMT, 128, 64, 4, 1, 4>(a, as, b, bs, M, N, K, add, out, bf16, s);
     case LMGC_MX_TILE_128X128: return launch_tile<FMT, 128, 128, 4, 2, F8 ? 3 : 2>(a, as, b, bs, M, N, K, add, out, bf16, s);

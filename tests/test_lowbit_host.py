@@ -83,7 +83,7 @@ def test_gemm_refuses():
     def t(fmt, tile):
         return rc("lmgc_op_gemm_mx_tile", A[0], A[1], fmt, A[2], A[3], None, A[4], 0, 32, 128, 0, tile, None)
     assert g(M=0) == 0
-    assert [t(0, i) for i in (-1, 0, 6, 7)] == [0, 0, 0, EINVAL] and [t(1, i) for i in (5, 6)] == [0, EINVAL]
+    assert [t(0, i) for i in (-1, 0, 7, 8)] == [0, 0, 0, EINVAL] and [t(1, i) for i in (6, 7)] == [0, EINVAL]
     for bad in (dict(a=None), dict(asc=None), dict(b=None), dict(bsc=None), dict(out=None), dict(fmt=2), dict(kind=1),
                 dict(kind=2), dict(kind=4), dict(M=-1), dict(M=(1 << 26) + 1), dict(N=0), dict(K=0), dict(K=(1 << 20) + 1),
                 dict(out=A[0]), dict(out=A[1]), dict(out=A[2]), dict(out=A[3]), dict(a=A[0] + 8), dict(out=A[4] + 4),
