@@ -589,7 +589,21 @@ def _on(stream, *tensors):
     for t in tensors:
         if t is not None and t.get_device() != dev:
             raise ValueError(f"a tensor is on {t.device}, the current device is cuda:{dev}")
-    return stream.cuda_stream if stream is not None else _raw_stream(dev)
+    if stream is None:
+        return _raw_stream(dev)
+    if stream.device_index != dev:
+        raise ValueError(f"a stream of cuda:{stream.device_index}, the current device is cuda:{dev}")
+    return stream.cuda_stream
+
+
+def _empty(shape, dtype, device, stream):
+    """A tensor that is free for `stream` to write: with a stream other than the
+    current one it is allocated there, as torch.cuda.stream(stream) would."""
+    import torch
+    if stream is None:
+        return torch.empty(shape, dtype=dtype, device=device)
+    with torch.cuda.stream(stream):
+        return torch.empty(shape, dtype=dtype, device=device)
 
 
 def _raw_stream(dev: int) -> int:
@@ -606,14 +620,14 @@ def _mx_sizes(rows: int, cols: int, fmt: str) -> Tuple[int, int]:
     return kp if MX_FORMATS[fmt] == 0 else kp // 2, 16 * -(-cols // 512)
 
 
-def _mx_empty(rows, cols, fmt, codes, scales, device):
+def _mx_empty(rows, cols, fmt, codes, scales, device, stream):
     """Code and scale tensors of the rows layout: uint8 [rows, bytes of a row]."""
     import torch
     nc, ns = _mx_sizes(rows, cols, fmt)
     if codes is None:
-        codes = torch.empty((rows, nc), dtype=torch.uint8, device=device)
+        codes = _empty((rows, nc), torch.uint8, device, stream)
     if scales is None:
-        scales = torch.empty((rows, ns), dtype=torch.uint8, device=device)
+        scales = _empty((rows, ns), torch.uint8, device, stream)
     _mx_check(codes, scales, rows, cols, fmt)
     return codes, scales
 
@@ -631,7 +645,7 @@ def op_mx_quantize(x, fmt: str, codes=None, scales=None, stream=None):
     fmt "fp8" (e4m3) or "fp4" (e2m1)."""
     rows, cols = x.shape
     assert cols == 1 or x.stride(1) == 1
-    codes, scales = _mx_empty(rows, cols, fmt, codes, scales, x.device)
+    codes, scales = _mx_empty(rows, cols, fmt, codes, scales, x.device, stream)
     ld = x.stride(0) if rows > 1 else cols
     _check(lib().lmgc_op_mx_quantize(_ptr(x), _dtype(x), rows, cols, ld, MX_FORMATS[fmt], _ptr(codes),
                                      _ptr(scales), _on(stream, x, codes, scales)))
@@ -644,8 +658,8 @@ def op_mx_dequantize(codes, scales, fmt: str, cols: int, dtype=None, out=None, s
     rows = codes.shape[0]
     _mx_check(codes, scales, rows, cols, fmt)
     if out is None:
-        out = torch.empty((rows, cols), dtype=dtype or torch.float32, device=codes.device)
-    assert tuple(out.shape) == (rows, cols) and (cols == 1 or out.stride(1) == 1)
+        out = _empty((rows, cols), dtype or torch.float32, codes.device, stream)
+    assert out.shape == (rows, cols) and (cols == 1 or out.stride(1) == 1)
     ld = out.stride(0) if rows > 1 else cols
     _check(lib().lmgc_op_mx_dequantize(_ptr(codes), _ptr(scales), MX_FORMATS[fmt], rows, cols, _ptr(out),
                                        _dtype(out), ld, _on(stream, codes, scales, out)))
@@ -657,8 +671,8 @@ def op_mx_block(codes, scales, cols: int, stream=None):
     import torch
     rows = codes.shape[0]
     _mx_check(codes, scales, rows, cols, "fp4")
-    bc = torch.empty(_size(lib().lmgc_mx_block_code_bytes(rows, cols)), dtype=torch.uint8, device=codes.device)
-    bs = torch.empty(_size(lib().lmgc_mx_block_scale_bytes(rows, cols)), dtype=torch.uint8, device=codes.device)
+    bc = _empty(_size(lib().lmgc_mx_block_code_bytes(rows, cols)), torch.uint8, codes.device, stream)
+    bs = _empty(_size(lib().lmgc_mx_block_scale_bytes(rows, cols)), torch.uint8, codes.device, stream)
     _check(lib().lmgc_op_mx_block(_ptr(codes), _ptr(scales), rows, cols, _ptr(bc), _ptr(bs), _on(stream, codes, scales)))
     return bc, bs
 
@@ -669,9 +683,9 @@ def op_add_norm_mx(h, x, gain, eps: float, fmt: str, out=None, codes=None, scale
     place; None: not stored)."""
     M, d = h.shape
     assert h.is_contiguous() and gain.is_contiguous() and gain.numel() == d
-    assert x is None or (x.is_contiguous() and tuple(x.shape) == (M, d))
-    assert out is None or (out.is_contiguous() and tuple(out.shape) == (M, d) and out.dtype == h.dtype)
-    codes, scales = _mx_empty(M, d, fmt, codes, scales, h.device)
+    assert x is None or (x.is_contiguous() and x.shape == (M, d))
+    assert out is None or (out.is_contiguous() and out.shape == (M, d) and out.dtype == h.dtype)
+    codes, scales = _mx_empty(M, d, fmt, codes, scales, h.device, stream)
     _check(lib().lmgc_op_add_norm_mx(_ptr(h), _dtype(h), _ptr(x), _dtype(x) if x is not None else 0, _ptr(gain),
                                      _dtype(gain), float(eps), M, d, MX_FORMATS[fmt], _ptr(out), _ptr(codes),
                                      _ptr(scales), _on(stream, h, x, gain, out, codes, scales)))
@@ -697,10 +711,10 @@ def op_gemm_mx(a, a_scales, a_fmt: str, b, b_scales, N: int, K: int, kind: str =
     assert b_scales.dtype == torch.uint8 and b_scales.is_contiguous() and b_scales.numel() == n16 * ns
     dt = torch.bfloat16 if kind == "bf16" else torch.float32
     if out is None:
-        out = torch.empty((M, N), dtype=dt, device=a.device)
-    assert out.dtype == dt and out.is_contiguous() and tuple(out.shape) == (M, N)
+        out = _empty((M, N), dt, a.device, stream)
+    assert out.dtype == dt and out.is_contiguous() and out.shape == (M, N)
     if add is not None:
-        assert add.dtype == torch.float32 and add.is_contiguous() and tuple(add.shape) == (M, N)
+        assert add.dtype == torch.float32 and add.is_contiguous() and add.shape == (M, N)
     _check(lib().lmgc_op_gemm_mx_tile(_ptr(a), _ptr(a_scales), MX_FORMATS[a_fmt], _ptr(b), _ptr(b_scales), _ptr(add),
                                       _ptr(out), M, N, K, MX_KINDS[kind], -1 if tile is None else MX_TILES.index(tile),
                                       _on(stream, a, a_scales, b, b_scales, add, out)))
@@ -722,8 +736,8 @@ def _kv8_check(cache, B, Hkv, hd):
     kc, ks, vc, vs = cache
     cap = 64 * kc.shape[2]
     for c, s in ((kc, ks), (vc, vs)):
-        assert c.dtype == torch.uint8 and c.is_contiguous() and tuple(c.shape) == (B, Hkv, cap // 64, 64 * hd)
-        assert s.dtype == torch.float32 and s.is_contiguous() and tuple(s.shape) == (B, Hkv, cap // 64)
+        assert c.dtype == torch.uint8 and c.is_contiguous() and c.shape == (B, Hkv, cap // 64, 64 * hd)
+        assert s.dtype == torch.float32 and s.is_contiguous() and s.shape == (B, Hkv, cap // 64)
     return kc, ks, vc, vs, cap
 
 
@@ -760,12 +774,10 @@ def op_attention_kv8(q, cache, lens, counts=None, window: int = 0, sinks: int = 
     assert q.dtype == torch.bfloat16 and q.is_contiguous()
     _kv8_lens(lens, counts, B)
     if out is None:
-        out = torch.empty((B * T, Hq * hd), dtype=torch.bfloat16, device=q.device)
+        out = _empty((B * T, Hq * hd), torch.bfloat16, q.device, stream)
     assert out.dtype == torch.bfloat16 and out.is_contiguous() and out.numel() == q.numel()
     if ws is None:
-        ws = workspace(kv8_workspace(B, Hq, Hkv, T, hd, cap), q.device)
-        if stream is not None:
-            ws.record_stream(stream)  # its memory is given out again only behind this call
+        ws = _empty(kv8_workspace(B, Hq, Hkv, T, hd, cap), torch.uint8, q.device, stream)
     _check(lib().lmgc_op_attention_kv8(_ptr(q), B, Hq, Hkv, T, hd, cap, _ptr(lens), _ptr(counts), _ptr(kc), _ptr(ks),
                                        _ptr(vc), _ptr(vs), int(window), int(sinks), _ptr(out), _ptr(ws), ws.numel(),
                                        _on(stream, q, out, ws, lens, counts, *cache)))

@@ -264,7 +264,7 @@ def test_product_tiles(fmt, tile, M, N, K):
 
 
 @pytest.mark.parametrize("fmt,M,N,K", [("fp8", 2000, 2050, 900), ("fp8", 4100, 4100, 1200), ("fp8", 9000, 4600, 700),
-                                       ("fp4", 1030, 2050, 1200), ("fp4", 4100, 4100, 600), ("fp4", 20, 13001, 700)])
+                                       ("fp8", 600000, 24, 130), ("fp4", 1030, 2050, 1200), ("fp4", 4100, 4100, 600), ("fp4", 20, 13001, 700)])
 def test_product_large(fmt, M, N, K):
     """Sizes at which the library takes its large tiles, against float64 on the
     device; the bound is _product_tol's, with the largest products of all steps
@@ -322,6 +322,32 @@ def test_norm_and_product_in_graphs():
         mine = (nh, nx) + tuple(t.clone().zero_() for t in bufs[2:])
         step(*mine)
         assert all(torch.equal(p, q) for p, q in zip(bufs, mine)), i
+
+
+def test_calls_on_a_stream():
+    """Results and workspaces that the call allocates belong to its stream: long
+    work on the current stream does not touch them."""
+    import torch
+    x = torch.randn(300, 768, device="cuda")
+    h, g = torch.randn(300, 768, device="cuda"), torch.ones(768, device="cuda")
+    want = B.op_mx_quantize(x, "fp4")
+    b, sb = B.op_mx_block(*want, 768)
+    norm = B.op_add_norm_mx(h, x, g, 1e-5, "fp8")
+    prod = B.op_gemm_mx(*norm, "fp8", b, sb, 300, 768)
+    torch.cuda.synchronize()
+    s = torch.cuda.Stream()
+    for _ in range(3):
+        junk = [torch.full((300, 768), 3.0, device="cuda") for _ in range(20)]
+        del junk  # their memory is the current stream's to give out
+        c, sc = B.op_mx_quantize(x, "fp4", stream=s)
+        bb, sbb = B.op_mx_block(c, sc, 768, stream=s)
+        n, ns = B.op_add_norm_mx(h, x, g, 1e-5, "fp8", stream=s)
+        p = B.op_gemm_mx(n, ns, "fp8", bb, sbb, 300, 768, stream=s)
+        y = B.op_mx_dequantize(c, sc, "fp4", 768, stream=s)
+        s.synchronize()
+        assert torch.equal(c, want[0]) and torch.equal(sc, want[1]) and torch.equal(bb, b) and torch.equal(sbb, sb)
+        assert torch.equal(n, norm[0]) and torch.equal(ns, norm[1]) and torch.equal(p, prod)
+        assert torch.equal(y, B.op_mx_dequantize(*want, "fp4", 768))
 
 
 def test_tensors_on_another_device_are_refused():
