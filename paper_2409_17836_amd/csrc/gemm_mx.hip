@@ -70,6 +70,7 @@ template <int COLS>
 __device__ inline void store_rows(const float* src, int64_t at, int rows, int nc, int N, int lane, const float* add, void* out,
                                   int bf16) {
   constexpr int RS = COLS + 4;
+  static_assert(COLS >= 32, "at most 16 rows at once");
   if (bf16) {
     constexpr int PER = 8, LPR = COLS / PER, RPI = 64 / LPR;  // values a lane, lanes a row, rows at once
     const bool vec = (N & 7) == 0;
@@ -518,7 +519,7 @@ int pick_tile(int fmt, int64_t M, int64_t N, int K) {
   static const Cost cost[2][kTiles] = {
       {{16, 16, 2.0, 0, 0.080}, {16, 32, 2.0, 0, 0.085}, {16, 64, 2.0, 0, 0.118}, {64, 64, 2.0, 0.7, 0.146}, {128, 64, 2.5, 0.9, 0.285},
        {128, 128, 2.5, 0.9, 0.400}, {128, 256, 2.5, 2.5, 0.720}, {256, 256, 4.0, 3.5, 1.330}},
-      {{16, 16, 2.0, 0, 0.052}, {16, 32, 2.0, 0, 0.062}, {16, 64, 2.0, 0, 0.092}, {64, 64, 2.3, 0.9, 0.125}, {128, 64, 2.5, 1.1, 0.230},
+      {{16, 16, 2.0, 0, 0.052}, {16, 32, 2.0, 0, 0.062}, {16, 64, 2.0, 0, 0.092}, {64, 64, 2.3, 0.9, 0.125}, {128, 64, 2.5, 0.9, 0.210},
        {128, 128, 2.5, 1.2, 0.290}, {128, 256, 2.5, 3.0, 0.530}, {256, 256, 0, 1e30, 0}}};
   const int nk = (int)(mx_cols(K) / 128);
   int best = LMGC_MX_TILE_64X64;
@@ -547,7 +548,7 @@ void launch_fmt(const uint8_t* a, const uint8_t* as, const uint8_t* b, const uin
     case LMGC_MX_TILE_16X32: return launch_rows<FMT, 2, 16>(a, as, b, bs, M, N, K, add, out, bf16, s);
     case LMGC_MX_TILE_16X64: return launch_rows<FMT, 4, 8>(a, as, b, bs, M, N, K, add, out, bf16, s);
     case LMGC_MX_TILE_64X64: return launch_tile<FMT, 64, 64, 2, 2, 4>(a, as, b, bs, M, N, K, add, out, bf16, s);
-    case LMGC_MX_TILE_128X64: return launch_tile<FMT, 128, 64, 4, 1, 4>(a, as, b, bs, M, N, K, add, out, bf16, s);
+    case LMGC_MX_TILE_128X64: return launch_tile<FMT, 128, 64, 4, F8 ? 1 : 2, F8 ? 4 : 3>(a, as, b, bs, M, N, K, add, out, bf16, s);
     case LMGC_MX_TILE_128X128: return launch_tile<FMT, 128, 128, 4, 2, F8 ? 3 : 2>(a, as, b, bs, M, N, K, add, out, bf16, s);
     case LMGC_MX_TILE_128X256: return launch_tile<FMT, 128, 256, 2, 4, F8 ? 4 : 2>(a, as, b, bs, M, N, K, add, out, bf16, s);
     default:
