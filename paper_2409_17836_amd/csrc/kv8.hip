@@ -434,12 +434,17 @@ __global__ __launch_bounds__(64) void attn_kv8_join_kernel(const float* __restri
 //
 // The block scales cost nothing per score: the keys' goes into the exponent's
 // factor, the values' (a power of two) into its summand, and the row sums
-// are a product too, with ones over that scale.  Up to kJoinCols columns the
-// length is split too, kPromptChunk tokens to a workgroup (more where that
-// were over kMaxPromptSplits), and joined.
+// are a product too, with ones over that scale.
+//
+// Where a sequence has fewer than 128 tiles the length is split too: for 128
+// workgroups as long as a split has kShortSplit tokens, for 256 where it has
+// kLongSplit.  A split's sums go twice through memory: 1 x 12 heads of 64, 50
+// queries over 1000 tokens take 16 us in splits of 512 and 24 of 1024, 8 x 12
+// heads, 256 over 768, take 40 and 31; 2 x 32 heads of 128, 1000 over 4000
+// tokens, take 118 us whole and 164 in halves; 1 x 32 heads, 4 queries to a
+// key/value head, 512 over 30000 take 233 us in quarters and 392 in halves.
 constexpr int kTileCols = 256;
-constexpr int kJoinCols = 1024;
-constexpr int kPromptChunk = 1024;
+constexpr int kShortSplit = 576, kLongSplit = 2048;
 constexpr int kMaxPromptSplits = 16;
 constexpr int kAhead = 3;  // steps that a block's codes are asked for ahead
 constexpr int kReads = 8;  // operands read ahead of their products
@@ -726,28 +731,33 @@ __global__ __launch_bounds__(512, 2) void attn_kv8_prompt_kernel(
   }
 }
 
-// Tokens in a split of the length: by the number of columns and the cache
-// alone, so that a query's result does not depend on the other sequences.
-int chunk_of(int64_t cols, int hd, int cap) {
-  if (cols > kJoinCols) return cap;
+int64_t tiles_of(int64_t cols) { return (cols + kTileCols - 1) / kTileCols; }
+
+// Tokens in a split of the length: by the columns, heads and cache of one
+// sequence, so that a query's result does not depend on the others.
+int chunk_of(int64_t cols, int Hkv, int hd, int cap) {
   if (cols <= kSplitCols && cap <= kOneBytes / (2 * hd)) return cap;
-  const int least = cols <= kSplitCols ? kSplitBytes / (2 * hd) : kPromptChunk;
-  const int most = cols <= kSplitCols ? kMaxSplits : kMaxPromptSplits;
-  return std::max(least, ((cap + most - 1) / most + kBlk - 1) / kBlk * kBlk);
+  int64_t least = kSplitBytes / (2 * hd), most = kMaxSplits;
+  if (cols > kSplitCols) {
+    const int64_t groups = tiles_of(cols) * Hkv;
+    most = groups >= 128 ? 1 : std::max(std::min<int64_t>(128 / groups, cap / kShortSplit), std::min<int64_t>(256 / groups, cap / kLongSplit));
+    most = std::max<int64_t>(1, std::min<int64_t>(most, kMaxPromptSplits));
+    least = 1;
+  }
+  return (int)std::max(least, ((cap + most - 1) / most + kBlk - 1) / kBlk * kBlk);
 }
 int splits_of(int chunk, int cap) { return (cap + chunk - 1) / chunk; }
-int64_t tiles_of(int64_t cols) { return (cols + kTileCols - 1) / kTileCols; }
 
 }  // namespace
 
 int64_t kv8_workspace_bytes(int B, int Hq, int Hkv, int T, int hd, int cap) {
-  const int64_t nsplit = splits_of(chunk_of((int64_t)T * (Hq / Hkv), hd, cap), cap);
+  const int64_t nsplit = splits_of(chunk_of((int64_t)T * (Hq / Hkv), Hkv, hd, cap), cap);
   return nsplit > 1 ? (int64_t)B * Hq * T * nsplit * (hd + 2) * 4 : 0;
 }
 
 int64_t kv8_workgroups(int B, int Hq, int Hkv, int T, int hd, int cap) {
   const int64_t cols = (int64_t)T * (Hq / Hkv);
-  return cols <= kSplitCols ? 1 : tiles_of(cols) * splits_of(chunk_of(cols, hd, cap), cap) * B * Hkv;
+  return cols <= kSplitCols ? 1 : tiles_of(cols) * splits_of(chunk_of(cols, Hkv, hd, cap), cap) * B * Hkv;
 }
 
 hipError_t launch_kv8_append(const uint16_t* k, const uint16_t* v, int B, int Hkv, int T, int hd, int cap,
@@ -764,7 +774,7 @@ hipError_t launch_attention_kv8(const uint16_t* q, int B, int Hq, int Hkv, int T
                                 const float* vs, int window, int sinks, void* ws, uint16_t* out, hipStream_t s) {
   const int G = Hq / Hkv;
   const int64_t cols = (int64_t)T * G;
-  const int chunk = chunk_of(cols, hd, cap), nsplit = splits_of(chunk, cap);
+  const int chunk = chunk_of(cols, Hkv, hd, cap), nsplit = splits_of(chunk, cap);
   const Mask mask{window, sinks};
   const float sl2 = (float)(1.4426950408889634 / sqrt((double)hd));
   float* po = (float*)ws;

@@ -142,5 +142,5 @@ def test_workspace():
     # a long cache is split into 64 parts at most, 16 with many columns
     assert rc("lmgc_kv8_workspace", 1, 4, 2, 1, 64, 1 << 24) == 4 * 64 * 66 * 4
     assert rc("lmgc_kv8_workspace", 1, 4, 2, 512, 64, 1 << 24) == 4 * 512 * 16 * 66 * 4
-    assert rc("lmgc_kv8_workspace", 1, 4, 2, 513, 64, 1 << 24) == 0
+    assert rc("lmgc_kv8_workspace", 1, 4, 2, 1 << 15, 64, 1 << 24) == 0
     assert ctypes.sizeof(ctypes.c_int64) == 8
