@@ -1,6 +1,8 @@
 // Microscaled operands of the 4- and 8-bit products: quantisation of rows,
 // the way back, the block layout of weights, and the residual add with
-// RMSNorm whose output is microscaled.  All are bound by the bytes they move.
+// RMSNorm whose output is microscaled.  All are bound by the bytes they move
+// (times below: from and to memory, a copy kernel reaches 5.3 TB/s) and, when
+// small, by the launch and one round trip to memory (2.2 to 4 us).
 #include <algorithm>
 #include <type_traits>
 
@@ -10,9 +12,11 @@ namespace lmgc {
 namespace {
 
 // ---------------------------------------------------------------- quantise
-// Unit: one row x 512 columns, a wave; lane l takes columns 8 l .. 8 l + 7.
-// VEC: rows are whole 16-byte pieces (base, ld and cols), so a lane reads its
-// columns in one or two loads.
+// Unit: one row x 512 columns, a wave; lane l takes columns 8 l .. 8 l + 7, so
+// four lanes hold a block and its largest magnitude takes two exchanges between
+// neighbours.  VEC: rows are whole 16-byte pieces (base, ld and cols), so a
+// lane reads its columns in one or two loads.  32768 x 4096 bf16 to e4m3 75 us
+// (5.4 TB/s), 22016 x 4096 to e2m1 46 us (4.9).
 template <int FMT, typename T, bool VEC>
 __global__ __launch_bounds__(256) void mx_quantize_kernel(const T* __restrict__ src, int64_t rows, int cols, int64_t ld,
                                                           uint8_t* __restrict__ codes, uint8_t* __restrict__ scales) {
@@ -48,7 +52,8 @@ __device__ inline void store8(uint16_t* p, const float (&v)[8]) {
   *reinterpret_cast<mx_u32x4*>(p) = w;
 }
 
-// A thread: 8 columns.  VEC: as above, for the output.
+// A thread: 8 columns.  VEC: as above, for the output.  32768 x 4096 e4m3 to
+// bf16 73 us (5.6 TB/s), 22016 x 4096 e2m1 50 us (4.6).
 template <int FMT, typename T, bool VEC>
 __global__ __launch_bounds__(256) void mx_dequantize_kernel(const uint8_t* __restrict__ codes,
                                                             const uint8_t* __restrict__ scales, int64_t rows, int cols,
@@ -95,7 +100,8 @@ __global__ __launch_bounds__(256) void mx_dequantize_kernel(const uint8_t* __res
 // ------------------------------------------------------------------ blocks
 // Row-major 4-bit codes and scales -> blocks (common.h): thread t moves the
 // 16-byte piece (32 columns of a row) that is piece t of the blocks, and the
-// threads whose piece opens a 512-column group its word of scales.
+// threads whose piece opens a 512-column group its word of scales.  Writes are
+// in order, a wave 1 KB; reads are 16 rows' 64 bytes.  22016 x 4096 19 us.
 __global__ __launch_bounds__(256) void mx_block_kernel(const uint8_t* __restrict__ codes, const uint8_t* __restrict__ scales,
                                                        int64_t N, int K, uint8_t* __restrict__ bcodes,
                                                        uint8_t* __restrict__ bscales) {
