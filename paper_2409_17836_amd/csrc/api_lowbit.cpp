@@ -3,6 +3,7 @@
 
 #include "common.h"
 #include "host.h"
+#include "lowbit.h"
 
 using namespace lmgc;
 

@@ -169,29 +169,6 @@ hipError_t lossy_scratch(void** ptr, size_t* bytes);
 hipError_t launch_quantize_linear(const float* v, int64_t n, int bits, void* idx, void* ws, hipStream_t s);
 hipError_t launch_sign_pack(const float* v, int64_t n, uint8_t* out, hipStream_t s);
 
-// Microscaled operands (mx.hip, gemm_mx.hip) and the 8-bit key/value cache
-// (kv8.hip); arguments as in lmgc.h, checked by the callers.
-hipError_t launch_mx_quantize(const void* src, int dtype, int64_t rows, int cols, int64_t ld, int fmt, uint8_t* codes,
-                              uint8_t* scales, hipStream_t s);
-hipError_t launch_mx_dequantize(const uint8_t* codes, const uint8_t* scales, int fmt, int64_t rows, int cols, void* out,
-                                int dtype, int64_t ld, hipStream_t s);
-hipError_t launch_mx_block(const uint8_t* codes, const uint8_t* scales, int64_t N, int K, uint8_t* bcodes,
-                           uint8_t* bscales, hipStream_t s);
-hipError_t launch_add_norm_mx(const void* h, int h_dtype, const void* x, int x_dtype, const void* gain, int g_dtype,
-                              float eps, int64_t M, int d, int fmt, void* out, uint8_t* codes, uint8_t* scales,
-                              hipStream_t s);
-hipError_t launch_gemm_mx(const uint8_t* a, const uint8_t* as, int a_fmt, const uint8_t* b, const uint8_t* bs, int M,
-                          int N, int K, const float* add, void* out, int bf16, int tile, hipStream_t s);
-int64_t kv8_workspace_bytes(int B, int Hq, int Hkv, int T, int hd, int cap);
-// Workgroups of the attention over its columns, where they are one dimension of the grid.
-int64_t kv8_workgroups(int B, int Hq, int Hkv, int T, int hd, int cap);
-hipError_t launch_kv8_append(const uint16_t* k, const uint16_t* v, int B, int Hkv, int T, int hd, int cap,
-                             const int32_t* lens, const int32_t* counts, uint8_t* kc, float* ks, uint8_t* vc, float* vs,
-                             hipStream_t s);
-hipError_t launch_attention_kv8(const uint16_t* q, int B, int Hq, int Hkv, int T, int hd, int cap, const int32_t* lens,
-                                const int32_t* counts, const uint8_t* kc, const float* ks, const uint8_t* vc,
-                                const float* vs, int window, int sinks, void* ws, uint16_t* out, hipStream_t s);
-
 // dst[r, :] = srcs.p[idx[r] >> 28][(idx[r] & 0x0fffffff), :] for r < rows;
 // idx[r] == -1 gives a zero row.  Rows are cols * elem_bytes bytes (multiple of 4).
 struct GatherSrcs {

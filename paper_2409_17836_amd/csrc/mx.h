@@ -7,6 +7,7 @@
 #include <stdint.h>
 
 #include "common.h"
+#include "lowbit.h"
 
 namespace lmgc {
 
