@@ -192,6 +192,45 @@ def test_attention_over_a_long_cache(hd, T, masks):
         _check_attention(out, q, kv, [n], window=window, sinks=sinks)
 
 
+@pytest.mark.parametrize("hd", [64, 128])
+@pytest.mark.parametrize("window,sinks", [(0, 0), (300, 5), (700, 0), (64, 600)])
+def test_attention_prompt_in_splits(hd, window, sinks):
+    """Few tiles and a cache of several splits: parts joined, some of them empty
+    for all of a tile's queries, some for a few of them."""
+    log(f"prompt splits hd={hd} window {window} sinks {sinks}")
+    cap, T, lens, counts = 2368, 300, [0, 1900, 560], [300, 300, 17]
+    cache, kv = _filled(3, 2, cap, hd, cap, 85)
+    q = _kv((3, 4, T, hd), 89)
+    out = B.op_attention_kv8(q, cache, _int32(lens), _int32(counts), window=window, sinks=sinks)
+    _check_attention(out, q, kv, lens, counts, window=window, sinks=sinks)
+
+
+@pytest.mark.parametrize("hd", [64, 128])
+@pytest.mark.parametrize("Hq,Hkv,T", [(2, 2, 130), (24, 8, 11), (5, 1, 51), (255, 1, 1), (256, 1, 1), (257, 1, 1), (34, 2, 15), (3, 3, 256)])
+def test_attention_few_columns(hd, Hq, Hkv, T):
+    """Tiles of 16 columns up to 256 of them, heads that are no power of two."""
+    log(f"few columns hd={hd} heads {Hq}/{Hkv} T={T}")
+    cap, lens = 1216, [0, 900]
+    cache, kv = _filled(2, Hkv, cap, hd, cap, 95)
+    q = _kv((2, Hq, T, hd), 99)
+    out = B.op_attention_kv8(q, cache, _int32(lens), window=500, sinks=2)
+    _check_attention(out, q, kv, lens, window=500, sinks=2)
+
+
+@pytest.mark.parametrize("T", [1, 20, 90, 300])
+def test_attention_nan_queries_stay_in_their_rows(T):
+    import torch
+    cache, _ = _filled(1, 2, 640, 64, 640, 105)
+    q = _kv((1, 4, T, 64), 109)
+    clean = B.op_attention_kv8(q, cache, _int32([300])).reshape(T, 4, 64)
+    q[0, 1, T // 2, 7] = float("nan")
+    q[0, 2, T - 1, 3] = float("inf")
+    out = B.op_attention_kv8(q, cache, _int32([300])).reshape(T, 4, 64)
+    bad = torch.zeros(T, 4, dtype=torch.bool, device="cuda")
+    bad[T // 2, 1] = bad[T - 1, 2] = True
+    assert torch.equal(out[~bad], clean[~bad]) and torch.isnan(out[bad]).any(-1).all()
+
+
 @pytest.mark.parametrize("T", [1, 40, 1100])
 def test_attention_and_append_past_32_bits(T):
     """Codes past 4 GB and blocks past the last sequence's 2^31 bytes: the last
@@ -240,7 +279,7 @@ def test_attention_ragged_rows_are_left(T):
     assert not there[1].any() and not there[4].any() and not there[5].any()
 
 
-@pytest.mark.parametrize("T", [1, 20, 100])
+@pytest.mark.parametrize("T", [1, 20, 100, 150])
 def test_attention_masked_tokens_count_for_nothing(T):
     """Blocks with a NaN scale (keys or values) behind the window and past the
     last token change no bit; a visible one gives NaN."""
@@ -276,13 +315,13 @@ def test_attention_extreme_scores(hd):
     cache = B.kv8_cache(1, 2, cap, hd)
     B.op_kv8_append(cache, k, v, _int32([0]))
     kv = _values(cache, hd)
-    for T, n in ((1, 575), (30, 500), (200, 376)):
+    for T, n in ((1, 575), (30, 500), (200, 376), (300, 276)):
         for f in (0.0, 1.0, 6.0):
             q = _kv((1, 2, T, hd), 47) * f
             _check_attention(B.op_attention_kv8(q, cache, _int32([n])), q, kv, [n])
 
 
-@pytest.mark.parametrize("T", [1, 4, 30, 90])
+@pytest.mark.parametrize("T", [1, 4, 30, 90, 150])
 def test_attention_queries_do_not_depend_on_others(T):
     """A sequence alone gives the bits it has in a batch; and a few queries
     (whose splits have a length of their own) those of a wider cache."""
