@@ -627,7 +627,7 @@ int lmgc_op_kv8_append(const uint16_t* d_k, const uint16_t* d_v, int32_t B, int3
  * a block with a NaN scale gives NaN.  Scales are powers of two, 2^-64 or more
  * as appending leaves them; above 2^100 (values of 5e32) sums may overflow.  A
  * query's result depends on the cache and its position, and on cap, T, Hq, Hkv
- * (which say how the length is split), not on the other sequences or queries.
+ * (which say how the work is split), not on the other sequences or queries.
  * T Hq / Hkv <= 2^30; above 32, B Hkv ceil(T Hq / Hkv / 256) < 2^23, times the
  * splits of the cache (16 at most).
  * GPU, async.  Errors: EINVAL, ESIZE, EUNSUPPORTED (hd, the limit above).

@@ -214,12 +214,13 @@ __device__ inline __amdgpu_buffer_rsrc_t block_buffer(const uint8_t* codes, int6
 }
 
 // ---- few columns
-// Up to 256 columns whose tiles of 16, times Hkv, are at most few_tiles, and up
-// to 32 anyway: every tile walks the cache by itself, which takes less time than
-// the form for many columns as long as a sequence alone does not fill the chip
-// (12 heads of 64, 128 queries over 1000 tokens: 7.9 us and 19.8, 16 such
-// sequences 26.9 and 23.5; 32 heads of 128, 48 queries: 19 us and 29, 8 such
-// sequences 134 and 107).
+// Up to kFewCols columns whose tiles of 16, times Hkv, the cache's blocks and
+// the head's halves, are at most kFewBlocks, and up to 32 anyway: every tile
+// walks the cache by itself, eight waves at a time, which takes less time than
+// the form for many columns as long as the sequences do not fill the chip.  12
+// heads of 64, 200 queries behind 800 tokens: 7.6 us (the other form 28.8), 4
+// such sequences 14 (29), 16 of them 39 (31); 1000 queries from the start, past
+// the limit: 12 us (29.5), 4 of them 35 (31), 8 of them 62 (41).
 // Grid: (splits, tiles of 16 columns x Hkv, B), 512 threads.  A cache of up to
 // kOneBytes is one split (and the call one launch), a longer one is cut into
 // kSplitBytes (more where that were over kMaxSplits).  Wave w takes its blocks
@@ -234,7 +235,7 @@ __device__ inline __amdgpu_buffer_rsrc_t block_buffer(const uint8_t* codes, int6
 // sequences 171 us, 6.1 TB/s; one sequence 11.8 us.  A cache in the L2 costs a
 // little more that way (32 x 4 heads of 64 over 2000 tokens: 12.2 us for
 // 11.2), and with two tiles the second one misses it (24.5 us for 22.3).
-constexpr int few_tiles(int hd) { return 8192 / hd; }
+constexpr int kFewCols = 1024, kFewBlocks = 8192;
 constexpr int kNonTemporal = 2;  // the instruction's nt bit
 constexpr int kOneBytes = 256 << 10, kSplitBytes = 128 << 10;
 constexpr int kSplitWaves = 8;
@@ -244,7 +245,7 @@ template <int HD, bool ONCE>
 __global__ __launch_bounds__(kSplitWaves * 64, 4) void attn_kv8_split_kernel(
     const uint16_t* __restrict__ q, const uint8_t* __restrict__ kc, const float* __restrict__ ks,
     const uint8_t* __restrict__ vc, const float* __restrict__ vs, const int32_t* __restrict__ lens,
-    const int32_t* __restrict__ counts, int Hkv, uint32_t hinv, int G, int ginv, int T, int cap, int nsplit, int chunk, Mask mask,
+    const int32_t* __restrict__ counts, int Hkv, uint32_t hinv, int G, uint32_t ginv, int T, int cap, int nsplit, int chunk, Mask mask,
     float sl2, float* __restrict__ part_o, float2* __restrict__ part_ml, uint16_t* __restrict__ out) {
   constexpr int NC = HD / 64, ND = HD / 16, NW = kSplitWaves;
   __shared__ float so[NW][16][HD + 4];
@@ -253,7 +254,7 @@ __global__ __launch_bounds__(kSplitWaves * 64, 4) void attn_kv8_split_kernel(
   const int split = blockIdx.x, c0 = 16 * tile, kvh = blockIdx.y - tile * Hkv, b = blockIdx.z;
   const int tid = threadIdx.x, lane = tid & 63, col = lane & 15, g = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  auto over_g = [&](int c) __attribute__((always_inline)) { return c * ginv >> 16; };  // c / G
+  auto over_g = [&](int c) __attribute__((always_inline)) { return G > 1 ? (int)__umulhi(c, ginv) : c; };  // c / G
   int len;
   const int n = new_tokens(lens, counts, b, T, cap, len);
   const int ncol = min(16, n * G - c0);
@@ -747,11 +748,13 @@ int64_t tiles_of(int64_t cols) { return (cols + kTileCols - 1) / kTileCols; }
 
 // The form and the tokens in a split of the length: by the columns, heads and
 // cache of one sequence, so that a query's result does not depend on the others.
-bool few(int64_t cols, int Hkv, int hd) { return cols <= 32 || (cols <= 256 && (cols + 15) / 16 * Hkv <= few_tiles(hd)); }
+bool few(int64_t cols, int Hkv, int hd, int cap) {
+  return cols <= 32 || (cols <= kFewCols && (cols + 15) / 16 * Hkv * (cap / kBlk) * (hd / 64) <= kFewBlocks);
+}
 int chunk_of(int64_t cols, int Hkv, int hd, int cap) {
-  if (few(cols, Hkv, hd) && cap <= kOneBytes / (2 * hd)) return cap;
+  if (few(cols, Hkv, hd, cap) && cap <= kOneBytes / (2 * hd)) return cap;
   int64_t least = kSplitBytes / (2 * hd), most = kMaxSplits;
-  if (!few(cols, Hkv, hd)) {
+  if (!few(cols, Hkv, hd, cap)) {
     const int64_t groups = tiles_of(cols) * Hkv;
     most = groups >= 128 ? 1 : std::max(std::min<int64_t>(128 / groups, cap / kShortSplit), std::min<int64_t>(256 / groups, cap / kLongSplit));
     most = std::max<int64_t>(1, std::min<int64_t>(most, kMaxPromptSplits));
@@ -770,7 +773,7 @@ int64_t kv8_workspace_bytes(int B, int Hq, int Hkv, int T, int hd, int cap) {
 
 int64_t kv8_workgroups(int B, int Hq, int Hkv, int T, int hd, int cap) {
   const int64_t cols = (int64_t)T * (Hq / Hkv);
-  return few(cols, Hkv, hd) ? 1 : tiles_of(cols) * splits_of(chunk_of(cols, Hkv, hd, cap), cap) * B * Hkv;
+  return few(cols, Hkv, hd, cap) ? 1 : tiles_of(cols) * splits_of(chunk_of(cols, Hkv, hd, cap), cap) * B * Hkv;
 }
 
 hipError_t launch_kv8_append(const uint16_t* k, const uint16_t* v, int B, int Hkv, int T, int hd, int cap,
@@ -795,13 +798,13 @@ hipError_t launch_attention_kv8(const uint16_t* q, int B, int Hq, int Hkv, int T
   auto go = [&](auto h) {
     constexpr int HD = decltype(h)::value;
     const dim3 join((unsigned)cols, Hkv, B);
-    if (few(cols, Hkv, hd)) {
-      // exact quotients: c / G for c, G <= 256, y / Hkv for y < 2^16, Hkv < 2^15
-      const uint32_t hinv = (uint32_t)((1ull << 32) / Hkv + 1);
+    if (few(cols, Hkv, hd, cap)) {
+      // exact quotients of numbers below 2^16: x / n = x (2^32 / n + 1) / 2^32
+      const uint32_t hinv = (uint32_t)((1ull << 32) / Hkv + 1), ginv = (uint32_t)((1ull << 32) / G + 1);
       const dim3 grid(nsplit, (unsigned)((cols + 15) / 16) * Hkv, B);
       auto split = [&](auto once) {
         attn_kv8_split_kernel<HD, decltype(once)::value><<<grid, kSplitWaves * 64, 0, s>>>(
-            q, kc, ks, vc, vs, lens, counts, Hkv, hinv, G, 65536 / G + 1, T, cap, nsplit, chunk, mask, sl2, po, pml, out);
+            q, kc, ks, vc, vs, lens, counts, Hkv, hinv, G, ginv, T, cap, nsplit, chunk, mask, sl2, po, pml, out);
       };
       if (cols > 16) split(std::false_type{});
       else split(std::true_type{});

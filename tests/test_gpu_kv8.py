@@ -141,6 +141,12 @@ def _values(cache, hd):
     return out
 
 
+def _heads(Hkv, T):
+    """Query heads: two to a key/value head, and with 100 queries and more so
+    many that the form for many columns (over 1024) runs."""
+    return Hkv * (2 if T < 100 else -(-1100 // T))
+
+
 def _check_attention(got, q, kv, lens, counts=None, window=0, sinks=0):
     """The output's rounding to bf16 (2^-8 of it), the probabilities' rounding
     to bf16 in the sum (2^-8 of sum p |v|) and in the sum that divides it
@@ -172,7 +178,7 @@ def test_attention(hd, Hq, Hkv, T, lens):
 def test_attention_window_and_sinks(T, lens, window, sinks):
     log(f"window {window} sinks {sinks} T={T} lens={lens}")
     cache, kv = _filled(2, 2, 768, 64, 768, 15)
-    q = _kv((2, 4, T, 64), 19)
+    q = _kv((2, _heads(2, T), T, 64), 19)
     out = B.op_attention_kv8(q, cache, _int32(lens), window=window, sinks=sinks)
     _check_attention(out, q, kv, lens, window=window, sinks=sinks)
 
@@ -200,15 +206,15 @@ def test_attention_prompt_in_splits(hd, window, sinks):
     log(f"prompt splits hd={hd} window {window} sinks {sinks}")
     cap, T, lens, counts = 2368, 300, [0, 1900, 560], [300, 300, 17]
     cache, kv = _filled(3, 2, cap, hd, cap, 85)
-    q = _kv((3, 4, T, hd), 89)
+    q = _kv((3, _heads(2, T), T, hd), 89)
     out = B.op_attention_kv8(q, cache, _int32(lens), _int32(counts), window=window, sinks=sinks)
     _check_attention(out, q, kv, lens, counts, window=window, sinks=sinks)
 
 
 @pytest.mark.parametrize("hd", [64, 128])
-@pytest.mark.parametrize("Hq,Hkv,T", [(2, 2, 130), (24, 8, 11), (5, 1, 51), (255, 1, 1), (256, 1, 1), (257, 1, 1), (34, 2, 15), (3, 3, 256)])
+@pytest.mark.parametrize("Hq,Hkv,T", [(2, 2, 130), (24, 8, 11), (5, 1, 51), (255, 1, 1), (256, 1, 1), (1024, 1, 1), (34, 2, 15), (3, 3, 256), (341, 1, 3)])
 def test_attention_few_columns(hd, Hq, Hkv, T):
-    """Tiles of 16 columns up to 256 of them, heads that are no power of two."""
+    """Tiles of 16 columns up to 1024 of them, heads that are no power of two."""
     log(f"few columns hd={hd} heads {Hq}/{Hkv} T={T}")
     cap, lens = 1216, [0, 900]
     cache, kv = _filled(2, Hkv, cap, hd, cap, 95)
@@ -221,12 +227,12 @@ def test_attention_few_columns(hd, Hq, Hkv, T):
 def test_attention_nan_queries_stay_in_their_rows(T):
     import torch
     cache, _ = _filled(1, 2, 640, 64, 640, 105)
-    q = _kv((1, 4, T, 64), 109)
-    clean = B.op_attention_kv8(q, cache, _int32([300])).reshape(T, 4, 64)
+    q = _kv((1, _heads(2, T), T, 64), 109)
+    clean = B.op_attention_kv8(q, cache, _int32([300])).reshape(T, -1, 64)
     q[0, 1, T // 2, 7] = float("nan")
     q[0, 2, T - 1, 3] = float("inf")
-    out = B.op_attention_kv8(q, cache, _int32([300])).reshape(T, 4, 64)
-    bad = torch.zeros(T, 4, dtype=torch.bool, device="cuda")
+    out = B.op_attention_kv8(q, cache, _int32([300])).reshape(T, -1, 64)
+    bad = torch.zeros(clean.shape[:2], dtype=torch.bool, device="cuda")
     bad[T // 2, 1] = bad[T - 1, 2] = True
     assert torch.equal(out[~bad], clean[~bad]) and torch.isnan(out[bad]).any(-1).all()
 
@@ -267,7 +273,7 @@ def test_attention_refuses_lengths_on_the_host():
 def test_attention_ragged_rows_are_left(T):
     """counts, lengths at and past the cache's ends: rows without a token keep what they held."""
     import torch
-    Bn, Hq, Hkv, hd, cap = 7, 4, 2, 64, 320
+    Bn, Hq, Hkv, hd, cap = 7, _heads(2, T), 2, 64, 320
     lens, counts = [0, 10, 300, 319, 320, -5, 64], [T, 0, T, T, T, T, max(1, T - 2)]
     cache, kv = _filled(Bn, Hkv, cap, hd, cap, 25)
     q = _kv((Bn, Hq, T, hd), 29)
@@ -286,7 +292,7 @@ def test_attention_masked_tokens_count_for_nothing(T):
     import torch
     cap, hd, n = 512, 64, 300
     cache, _ = _filled(1, 1, cap, hd, cap, 35)
-    q = _kv((1, 2, T, hd), 39)
+    q = _kv((1, _heads(1, T), T, hd), 39)
     clean = B.op_attention_kv8(q, cache, _int32([n]), window=64, sinks=0)
     bad = [t.clone() for t in cache]
     first = (n - 63) // 64       # block of the first query's first key
@@ -317,7 +323,7 @@ def test_attention_extreme_scores(hd):
     kv = _values(cache, hd)
     for T, n in ((1, 575), (30, 500), (200, 376), (300, 276)):
         for f in (0.0, 1.0, 6.0):
-            q = _kv((1, 2, T, hd), 47) * f
+            q = _kv((1, _heads(2, T), T, hd), 47) * f
             _check_attention(B.op_attention_kv8(q, cache, _int32([n])), q, kv, [n])
 
 
@@ -328,7 +334,7 @@ def test_attention_queries_do_not_depend_on_others(T):
     import torch
     cap, hd, Hkv = 1152, 128, 2
     cache, _ = _filled(3, Hkv, cap, hd, cap, 55)
-    q = _kv((3, 4, T, hd), 59)
+    q = _kv((3, _heads(Hkv, T), T, hd), 59)
     lens = [1000, 30, 513]
     whole = B.op_attention_kv8(q, cache, _int32(lens), window=400, sinks=3).reshape(3, T, -1)
     for b in range(3):
