@@ -289,7 +289,9 @@ __global__ __launch_bounds__(kSplitWaves * 64, 4) void attn_kv8_split_kernel(
       for (int x = 0; x < NC; x++) kr[i][x] = codes(kb, i * NC + x);
 #pragma unroll
     for (int i = 0; i < ND / 2; i++) vr[i] = codes(vb, i);
-    const float fk = ks[blk] * sl2, fv = vs[blk];
+    // NaN in the values' scale: the visible tokens' scores take it, and the
+    // others are left out as ever
+    const float vscale = vs[blk], fk = vscale == vscale ? ks[blk] * sl2 : vscale, fv = vscale == vscale ? vscale : 1.0f;
     f32x4 s[4] = {};
     // tile by tile, half of the values asked for behind the first tile: mixed
     // with each other and with what follows, 128 dims do not fit the registers
@@ -307,14 +309,13 @@ __global__ __launch_bounds__(kSplitWaves * 64, 4) void attn_kv8_split_kernel(
     }
     __builtin_amdgcn_sched_barrier(0);
     const bool whole = mask.all(p0, p1, j0, j0 + kBlk);
-    bool see[4][4];
     float mx = -INFINITY;
 #pragma unroll
     for (int i = 0; i < 4; i++)
 #pragma unroll
       for (int r = 0; r < 4; r++) {
-        see[i][r] = whole | mask.sees(pos, low, j0 + 16 * i + 4 * g + r);
-        s[i][r] = see[i][r] ? s[i][r] * fk : -INFINITY;
+        const bool sees = whole | mask.sees(pos, low, j0 + 16 * i + 4 * g + r);
+        s[i][r] = sees ? s[i][r] * fk : -INFINITY;
         mx = fmaxf(mx, s[i][r]);  // (drops a NaN; it comes back through the exponential)
       }
     mx = fmaxf(mx, __shfl_xor(mx, 16, 64));
@@ -335,7 +336,7 @@ __global__ __launch_bounds__(kSplitWaves * 64, 4) void attn_kv8_split_kernel(
         // rounded to bf16 for the second product; the sum is of the rounded values
         const __bf16 p = (__bf16)__builtin_amdgcn_exp2f(s[i][r] - ref);
         l += (float)p;
-        pf[i >> 1][(i & 1) * 4 + r] = see[i][r] ? (__bf16)((float)p * fv) : (__bf16)0.f;
+        pf[i >> 1][(i & 1) * 4 + r] = (__bf16)((float)p * fv);
       }
 #pragma unroll
     for (int i = 0; i < ND; i++)
