@@ -308,16 +308,19 @@ __global__ __launch_bounds__(kSplitWaves * 64, 4) void attn_kv8_split_kernel(
           s[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fp8_bf16(kr[i][x][2 * y], kr[i][x][2 * y + 1]), qf[x][y], s[i], 0, 0, 0);
     }
     __builtin_amdgcn_sched_barrier(0);
-    const bool whole = mask.all(p0, p1, j0, j0 + kBlk);
+#pragma unroll
+    for (int i = 0; i < 4; i++) s[i] *= fk;
+    if (!mask.all(p0, p1, j0, j0 + kBlk))
+#pragma unroll
+      for (int i = 0; i < 4; i++)
+#pragma unroll
+        for (int r = 0; r < 4; r++)
+          if (!mask.sees(pos, low, j0 + 16 * i + 4 * g + r)) s[i][r] = -INFINITY;
     float mx = -INFINITY;
 #pragma unroll
     for (int i = 0; i < 4; i++)
 #pragma unroll
-      for (int r = 0; r < 4; r++) {
-        const bool sees = whole | mask.sees(pos, low, j0 + 16 * i + 4 * g + r);
-        s[i][r] = sees ? s[i][r] * fk : -INFINITY;
-        mx = fmaxf(mx, s[i][r]);  // (drops a NaN; it comes back through the exponential)
-      }
+      for (int r = 0; r < 4; r++) mx = fmaxf(mx, s[i][r]);  // (drops a NaN; it comes back through the exponential)
     mx = fmaxf(mx, __shfl_xor(mx, 16, 64));
     mx = fmaxf(mx, __shfl_xor(mx, 32, 64));
     if (mx > m) {
