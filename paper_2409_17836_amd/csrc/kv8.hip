@@ -207,6 +207,13 @@ __device__ inline bf16x8 fp8_bf16(uint32_t w0, uint32_t w1) {
 // query and of the cache, whatever columns, sequences and splits run with it:
 // blocks that a column does not see add exact zeros.
 
+// (in integers: a block's scales are the same in all lanes, and so stay scalar)
+__device__ inline bool is_nan(float v) { return (__builtin_bit_cast(uint32_t, v) & 0x7fffffffu) > 0x7f800000u; }
+// log2 of a block's scale, a power of two; NaN stays NaN.
+__device__ inline float log2_scale(float v) {
+  return is_nan(v) ? v : (float)((int)(__builtin_bit_cast(uint32_t, v) >> 23) - 127);
+}
+
 // Buffer over the codes of one block (stride 0, word 3 of gfx9).
 template <int HD>
 __device__ inline __amdgpu_buffer_rsrc_t block_buffer(const uint8_t* codes, int64_t blk) {
@@ -242,7 +249,7 @@ constexpr int kSplitWaves = 8;
 constexpr int kMaxSplits = 64;  // a lane each in the join
 
 template <int HD, bool ONCE>
-__global__ __launch_bounds__(kSplitWaves * 64, 4) void attn_kv8_split_kernel(
+__global__ __launch_bounds__(kSplitWaves * 64, HD == 64 ? 6 : 4) void attn_kv8_split_kernel(
     const uint16_t* __restrict__ q, const uint8_t* __restrict__ kc, const float* __restrict__ ks,
     const uint8_t* __restrict__ vc, const float* __restrict__ vs, const int32_t* __restrict__ lens,
     const int32_t* __restrict__ counts, int Hkv, uint32_t hinv, int G, uint32_t ginv, int T, int cap, int nsplit, int chunk, Mask mask,
@@ -271,7 +278,8 @@ __global__ __launch_bounds__(kSplitWaves * 64, 4) void attn_kv8_split_kernel(
 #pragma unroll
     for (int y = 0; y < 2; y++) qf[x][y] = *reinterpret_cast<const bf16x8*>(qp + 64 * x + 8 * y);
 
-  float m = -INFINITY, l = 0.f;
+  float m = -INFINITY;
+  f32x4 l = {};  // the row sum, four times: a product of the probabilities with ones
   f32x4 o[ND] = {};
   const int jend = min(jhi, p1 + 1);
   for (int j0 = jlo + wave * kBlk; j0 < jend; j0 += NW * kBlk) {
@@ -289,9 +297,8 @@ __global__ __launch_bounds__(kSplitWaves * 64, 4) void attn_kv8_split_kernel(
       for (int x = 0; x < NC; x++) kr[i][x] = codes(kb, i * NC + x);
 #pragma unroll
     for (int i = 0; i < ND / 2; i++) vr[i] = codes(vb, i);
-    // NaN in the values' scale: the visible tokens' scores take it, and the
-    // others are left out as ever
-    const float vscale = vs[blk], fk = vscale == vscale ? ks[blk] * sl2 : vscale, fv = vscale == vscale ? vscale : 1.0f;
+    const float kscale = ks[blk];
+    float fk = kscale * sl2, fv = vs[blk];
     f32x4 s[4] = {};
     // tile by tile, half of the values asked for behind the first tile: mixed
     // with each other and with what follows, 128 dims do not fit the registers
@@ -308,21 +315,27 @@ __global__ __launch_bounds__(kSplitWaves * 64, 4) void attn_kv8_split_kernel(
           s[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fp8_bf16(kr[i][x][2 * y], kr[i][x][2 * y + 1]), qf[x][y], s[i], 0, 0, 0);
     }
     __builtin_amdgcn_sched_barrier(0);
+    if (!mask.all(p0, p1, j0, j0 + kBlk)) {
+      // NaN in a scale: the visible tokens' scores take it, and the others are
+      // left out as ever
+      if (is_nan(kscale) || is_nan(fv)) {
 #pragma unroll
-    for (int i = 0; i < 4; i++) s[i] *= fk;
-    if (!mask.all(p0, p1, j0, j0 + kBlk))
+        for (int i = 0; i < 4; i++) s[i] *= __builtin_bit_cast(float, 0x7fc00000u);
+        fk = fv = 1.0f;
+      }
 #pragma unroll
       for (int i = 0; i < 4; i++)
 #pragma unroll
         for (int r = 0; r < 4; r++)
           if (!mask.sees(pos, low, j0 + 16 * i + 4 * g + r)) s[i][r] = -INFINITY;
+    }
     float mx = -INFINITY;
 #pragma unroll
     for (int i = 0; i < 4; i++)
 #pragma unroll
       for (int r = 0; r < 4; r++) mx = fmaxf(mx, s[i][r]);  // (drops a NaN; it comes back through the exponential)
     mx = fmaxf(mx, __shfl_xor(mx, 16, 64));
-    mx = fmaxf(mx, __shfl_xor(mx, 32, 64));
+    mx = fmaxf(mx, __shfl_xor(mx, 32, 64)) * fk;
     if (mx > m) {
       const float a = __builtin_amdgcn_exp2f(m - mx);
       l *= a;
@@ -330,28 +343,27 @@ __global__ __launch_bounds__(kSplitWaves * 64, 4) void attn_kv8_split_kernel(
       for (int i = 0; i < ND; i++) o[i] *= a;
       m = mx;
     }
-    const float ref = m == -INFINITY ? 0.f : m;
-    bf16x8 pf[2];
+    // the keys' scale is the exponent's factor, the values' (a power of two) a
+    // summand of it: log2_scale; the row sum has ones over that scale
+    const float sub = log2_scale(fv) - (m == -INFINITY ? 0.f : m);
+    const __bf16 unscale = (__bf16)(is_nan(fv) ? 1.0f : __builtin_amdgcn_rcpf(fv));  // exact
+    const bf16x8 ones = {unscale, unscale, unscale, unscale, unscale, unscale, unscale, unscale};
+    bf16x8 pf[2];  // rounded to bf16 for the second product; the sum is of the rounded values
 #pragma unroll
     for (int i = 0; i < 4; i++)
 #pragma unroll
-      for (int r = 0; r < 4; r++) {
-        // rounded to bf16 for the second product; the sum is of the rounded values
-        const __bf16 p = (__bf16)__builtin_amdgcn_exp2f(s[i][r] - ref);
-        l += (float)p;
-        pf[i >> 1][(i & 1) * 4 + r] = (__bf16)((float)p * fv);
-      }
+      for (int r = 0; r < 4; r++) pf[i >> 1][(i & 1) * 4 + r] = (__bf16)__builtin_amdgcn_exp2f(fmaf(s[i][r], fk, sub));
+#pragma unroll
+    for (int y = 0; y < 2; y++) l = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ones, pf[y], l, 0, 0, 0);
 #pragma unroll
     for (int i = 0; i < ND; i++)
 #pragma unroll
       for (int y = 0; y < 2; y++)
         o[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fp8_bf16(vr[i][2 * y], vr[i][2 * y + 1]), pf[y], o[i], 0, 0, 0);
   }
-  l += __shfl_xor(l, 16, 64);
-  l += __shfl_xor(l, 32, 64);
   if (g == 0) {
     sm[wave][col] = m;
-    sl[wave][col] = l;
+    sl[wave][col] = l[0];
   }
 #pragma unroll
   for (int i = 0; i < ND; i++) *reinterpret_cast<f32x4*>(&so[wave][col][16 * i + 4 * g]) = o[i];
@@ -658,8 +670,7 @@ __global__ __launch_bounds__(512, 2) void attn_kv8_prompt_kernel(
           }
         }
       }
-      // log2 of the values' scale (a power of two; NaN stays NaN)
-      const float ev = fv == fv ? (float)((int)(__builtin_bit_cast(uint32_t, fv) >> 23) - 127) : fv;
+      const float ev = log2_scale(fv);
       const __bf16 unscale = (__bf16)(fv == fv ? __builtin_amdgcn_rcpf(fv) : 1.0f);  // exact
       ones = bf16x8{unscale, unscale, unscale, unscale, unscale, unscale, unscale, unscale};
 #pragma unroll
