@@ -225,9 +225,9 @@ __device__ inline __amdgpu_buffer_rsrc_t block_buffer(const uint8_t* codes, int6
 // the head's halves, are at most kFewBlocks, and up to 32 anyway: every tile
 // walks the cache by itself, eight waves at a time, which takes less time than
 // the form for many columns as long as the sequences do not fill the chip.  12
-// heads of 64, 200 queries behind 800 tokens: 7.6 us (the other form 28.8), 4
-// such sequences 14 (29), 16 of them 39 (31); 1000 queries from the start, past
-// the limit: 12 us (29.5), 4 of them 35 (31), 8 of them 62 (41).
+// heads of 64, 1000 queries from the start: 9.9 us (the other form 29.5), 4
+// such sequences 27 (31), 8 of them 47 (42); 32 heads on 8 of 128, 50 queries
+// over 3900 tokens: 19 us (31), 4 of them 46 (37).
 // Grid: (splits, tiles of 16 columns x Hkv, B), 512 threads.  A cache of up to
 // kOneBytes is one split (and the call one launch), a longer one is cut into
 // kSplitBytes (more where that were over kMaxSplits).  Wave w takes its blocks
@@ -242,7 +242,7 @@ __device__ inline __amdgpu_buffer_rsrc_t block_buffer(const uint8_t* codes, int6
 // sequences 171 us, 6.1 TB/s; one sequence 11.8 us.  A cache in the L2 costs a
 // little more that way (32 x 4 heads of 64 over 2000 tokens: 12.2 us for
 // 11.2), and with two tiles the second one misses it (24.5 us for 22.3).
-constexpr int kFewCols = 1024, kFewBlocks = 8192;
+constexpr int kFewCols = 2048, kFewBlocks = 16384;
 constexpr int kNonTemporal = 2;  // the instruction's nt bit
 constexpr int kOneBytes = 256 << 10, kSplitBytes = 128 << 10;
 constexpr int kSplitWaves = 8;
@@ -766,16 +766,23 @@ int64_t tiles_of(int64_t cols) { return (cols + kTileCols - 1) / kTileCols; }
 bool few(int64_t cols, int Hkv, int hd, int cap) {
   return cols <= 32 || (cols <= kFewCols && (cols + 15) / 16 * Hkv * (cap / kBlk) * (hd / 64) <= kFewBlocks);
 }
+// Whole blocks, so that n of them hold cap tokens.
+int64_t round_up(int64_t cap, int64_t n) { return ((cap + n - 1) / n + kBlk - 1) / kBlk * kBlk; }
 int chunk_of(int64_t cols, int Hkv, int hd, int cap) {
   if (few(cols, Hkv, hd, cap) && cap <= kOneBytes / (2 * hd)) return cap;
-  int64_t least = kSplitBytes / (2 * hd), most = kMaxSplits;
-  if (!few(cols, Hkv, hd, cap)) {
+  const int64_t tokens = kSplitBytes / (2 * hd);
+  // a few queries: splits of `tokens`, longer ones where that were too many;
+  // more queries: as many splits as have an eighth more than that
+  if (cols <= 32) return (int)std::max(tokens, round_up(cap, kMaxSplits));
+  int64_t n;
+  if (few(cols, Hkv, hd, cap)) {
+    n = std::min<int64_t>(cap / (tokens + tokens / 8), kMaxSplits);
+  } else {
     const int64_t groups = tiles_of(cols) * Hkv;
-    most = groups >= 128 ? 1 : std::max(std::min<int64_t>(128 / groups, cap / kShortSplit), std::min<int64_t>(256 / groups, cap / kLongSplit));
-    most = std::max<int64_t>(1, std::min<int64_t>(most, kMaxPromptSplits));
-    least = 1;
+    n = groups >= 128 ? 1 : std::max(std::min<int64_t>(128 / groups, cap / kShortSplit), std::min<int64_t>(256 / groups, cap / kLongSplit));
+    n = std::min<int64_t>(n, kMaxPromptSplits);
   }
-  return (int)std::max(least, ((cap + most - 1) / most + kBlk - 1) / kBlk * kBlk);
+  return (int)round_up(cap, std::max<int64_t>(n, 1));
 }
 int splits_of(int chunk, int cap) { return (cap + chunk - 1) / chunk; }
 

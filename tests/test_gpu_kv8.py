@@ -143,8 +143,8 @@ def _values(cache, hd):
 
 def _heads(Hkv, T):
     """Query heads: two to a key/value head, and with 100 queries and more so
-    many that the form for many columns (over 1024) runs."""
-    return Hkv * (2 if T < 100 else -(-1100 // T))
+    many that the form for many columns (over 2048) runs."""
+    return Hkv * (2 if T < 100 else -(-2100 // T))
 
 
 def _check_attention(got, q, kv, lens, counts=None, window=0, sinks=0):
@@ -212,15 +212,16 @@ def test_attention_prompt_in_splits(hd, window, sinks):
 
 
 @pytest.mark.parametrize("hd", [64, 128])
-@pytest.mark.parametrize("Hq,Hkv,T", [(2, 2, 130), (24, 8, 11), (5, 1, 51), (255, 1, 1), (256, 1, 1), (1024, 1, 1), (34, 2, 15), (3, 3, 256), (341, 1, 3)])
+@pytest.mark.parametrize("Hq,Hkv,T", [(2, 2, 130), (24, 8, 11), (5, 1, 51), (255, 1, 1), (256, 1, 1), (1024, 1, 1), (34, 2, 15), (3, 3, 256), (341, 1, 3), (682, 1, 3)])
 def test_attention_few_columns(hd, Hq, Hkv, T):
-    """Tiles of 16 columns up to 1024 of them, heads that are no power of two."""
+    """Tiles of 16 columns up to 2048 of them, heads that are no power of two."""
     log(f"few columns hd={hd} heads {Hq}/{Hkv} T={T}")
-    cap, lens = 1216, [0, 900]
+    cap, lens = 1216 * (128 // hd), [0, 900 * (128 // hd)]  # two splits
     cache, kv = _filled(2, Hkv, cap, hd, cap, 95)
     q = _kv((2, Hq, T, hd), 99)
-    out = B.op_attention_kv8(q, cache, _int32(lens), window=500, sinks=2)
-    _check_attention(out, q, kv, lens, window=500, sinks=2)
+    for window, sinks in ((500, 2), (0, 0)):
+        out = B.op_attention_kv8(q, cache, _int32(lens), window=window, sinks=sinks)
+        _check_attention(out, q, kv, lens, window=window, sinks=sinks)
 
 
 @pytest.mark.parametrize("T", [1, 20, 90, 300])
@@ -237,12 +238,12 @@ def test_attention_nan_queries_stay_in_their_rows(T):
     assert torch.equal(out[~bad], clean[~bad]) and torch.isnan(out[bad]).any(-1).all()
 
 
-@pytest.mark.parametrize("T", [1, 40, 1100])
+@pytest.mark.parametrize("T", [1, 40, 200])
 def test_attention_and_append_past_32_bits(T):
     """Codes past 4 GB and blocks past the last sequence's 2^31 bytes: the last
     sequence's tokens, seen through a window, as in a small cache."""
     import torch
-    Bn, Hkv, Hq, hd, cap, window = 3, 16, 16, 128, 1 << 20, 100
+    Bn, Hkv, Hq, hd, cap, window = 3, 16, 32, 128, 1 << 20, 100
     cache = tuple(torch.empty(s, dtype=dt, device="cuda") for s, dt in
                   ((((Bn, Hkv, cap // 64, 64 * hd)), torch.uint8), ((Bn, Hkv, cap // 64), torch.float32)) * 2)
     first = cap - 64 * 20
