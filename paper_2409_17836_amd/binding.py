@@ -581,37 +581,49 @@ def _dtype(t) -> int:
     return 1 if t.dtype == torch.bfloat16 else 0
 
 
+_cuda = None  # (current device, its current stream's handle): torch's own calls without the objects around them
+
+
+def _cuda_calls():
+    global _cuda
+    if _cuda is None:
+        import torch
+        dev = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
+        raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+        _cuda = dev, raw or (lambda d: torch.cuda.current_stream(d).cuda_stream)
+    return _cuda
+
+
 def _on(stream, *tensors):
-    """The stream to launch on (the current one unless given).  Every tensor
-    has to be on the current device, as for every call of the library."""
-    import torch
-    dev = torch.cuda.current_device()
+    """The stream to launch on (the current one unless given) and the tensors'
+    addresses.  Every tensor has to be on the current device, as for every call
+    of the library."""
+    current, raw = _cuda_calls()
+    dev = current()
+    at = []
     for t in tensors:
-        if t is not None and t.get_device() != dev:
+        if t is None:
+            at.append(None)
+            continue
+        if t.get_device() != dev:
             raise ValueError(f"a tensor is on {t.device}, the current device is cuda:{dev}")
+        at.append(t.data_ptr())
     if stream is None:
-        return _raw_stream(dev)
+        return raw(dev), at
     if stream.device_index != dev:
         raise ValueError(f"a stream of cuda:{stream.device_index}, the current device is cuda:{dev}")
-    return stream.cuda_stream
+    return stream.cuda_stream, at
 
 
-def _empty(shape, dtype, device, stream):
-    """A tensor that is free for `stream` to write: with a stream other than the
-    current one it is allocated there, as torch.cuda.stream(stream) would."""
-    import torch
+def _empty(shape, dtype, like, stream):
+    """A tensor on like's device that is free for `stream` to write: with a stream
+    other than the current one it is allocated there, as torch.cuda.stream(stream)
+    would."""
     if stream is None:
-        return torch.empty(shape, dtype=dtype, device=device)
-    with torch.cuda.stream(stream):
-        return torch.empty(shape, dtype=dtype, device=device)
-
-
-def _raw_stream(dev: int) -> int:
-    """The current stream's handle, without building a Stream object (2.6 us)
-    where torch offers that."""
+        return like.new_empty(shape, dtype=dtype)
     import torch
-    get = getattr(torch._C, "_cuda_getCurrentRawStream", None)
-    return get(dev) if get is not None else torch.cuda.current_stream(dev).cuda_stream
+    with torch.cuda.stream(stream):
+        return like.new_empty(shape, dtype=dtype)
 
 
 def _mx_sizes(rows: int, cols: int, fmt: str) -> Tuple[int, int]:
@@ -620,14 +632,14 @@ def _mx_sizes(rows: int, cols: int, fmt: str) -> Tuple[int, int]:
     return kp if MX_FORMATS[fmt] == 0 else kp // 2, 16 * -(-cols // 512)
 
 
-def _mx_empty(rows, cols, fmt, codes, scales, device, stream):
+def _mx_empty(rows, cols, fmt, codes, scales, like, stream):
     """Code and scale tensors of the rows layout: uint8 [rows, bytes of a row]."""
     import torch
     nc, ns = _mx_sizes(rows, cols, fmt)
     if codes is None:
-        codes = _empty((rows, nc), torch.uint8, device, stream)
+        codes = _empty((rows, nc), torch.uint8, like, stream)
     if scales is None:
-        scales = _empty((rows, ns), torch.uint8, device, stream)
+        scales = _empty((rows, ns), torch.uint8, like, stream)
     _mx_check(codes, scales, rows, cols, fmt)
     return codes, scales
 
@@ -645,10 +657,10 @@ def op_mx_quantize(x, fmt: str, codes=None, scales=None, stream=None):
     fmt "fp8" (e4m3) or "fp4" (e2m1)."""
     rows, cols = x.shape
     assert cols == 1 or x.stride(1) == 1
-    codes, scales = _mx_empty(rows, cols, fmt, codes, scales, x.device, stream)
+    codes, scales = _mx_empty(rows, cols, fmt, codes, scales, x, stream)
     ld = x.stride(0) if rows > 1 else cols
-    _check(lib().lmgc_op_mx_quantize(_ptr(x), _dtype(x), rows, cols, ld, MX_FORMATS[fmt], _ptr(codes),
-                                     _ptr(scales), _on(stream, x, codes, scales)))
+    st, (px, pc, ps) = _on(stream, x, codes, scales)
+    _check(lib().lmgc_op_mx_quantize(px, _dtype(x), rows, cols, ld, MX_FORMATS[fmt], pc, ps, st))
     return codes, scales
 
 
@@ -658,11 +670,11 @@ def op_mx_dequantize(codes, scales, fmt: str, cols: int, dtype=None, out=None, s
     rows = codes.shape[0]
     _mx_check(codes, scales, rows, cols, fmt)
     if out is None:
-        out = _empty((rows, cols), dtype or torch.float32, codes.device, stream)
+        out = _empty((rows, cols), dtype or torch.float32, codes, stream)
     assert out.shape == (rows, cols) and (cols == 1 or out.stride(1) == 1)
     ld = out.stride(0) if rows > 1 else cols
-    _check(lib().lmgc_op_mx_dequantize(_ptr(codes), _ptr(scales), MX_FORMATS[fmt], rows, cols, _ptr(out),
-                                       _dtype(out), ld, _on(stream, codes, scales, out)))
+    st, (pc, ps, po) = _on(stream, codes, scales, out)
+    _check(lib().lmgc_op_mx_dequantize(pc, ps, MX_FORMATS[fmt], rows, cols, po, _dtype(out), ld, st))
     return out
 
 
@@ -671,9 +683,10 @@ def op_mx_block(codes, scales, cols: int, stream=None):
     import torch
     rows = codes.shape[0]
     _mx_check(codes, scales, rows, cols, "fp4")
-    bc = _empty(_size(lib().lmgc_mx_block_code_bytes(rows, cols)), torch.uint8, codes.device, stream)
-    bs = _empty(_size(lib().lmgc_mx_block_scale_bytes(rows, cols)), torch.uint8, codes.device, stream)
-    _check(lib().lmgc_op_mx_block(_ptr(codes), _ptr(scales), rows, cols, _ptr(bc), _ptr(bs), _on(stream, codes, scales)))
+    bc = _empty(_size(lib().lmgc_mx_block_code_bytes(rows, cols)), torch.uint8, codes, stream)
+    bs = _empty(_size(lib().lmgc_mx_block_scale_bytes(rows, cols)), torch.uint8, codes, stream)
+    st, (pc, ps, pbc, pbs) = _on(stream, codes, scales, bc, bs)
+    _check(lib().lmgc_op_mx_block(pc, ps, rows, cols, pbc, pbs, st))
     return bc, bs
 
 
@@ -685,10 +698,10 @@ def op_add_norm_mx(h, x, gain, eps: float, fmt: str, out=None, codes=None, scale
     assert h.is_contiguous() and gain.is_contiguous() and gain.numel() == d
     assert x is None or (x.is_contiguous() and x.shape == (M, d))
     assert out is None or (out.is_contiguous() and out.shape == (M, d) and out.dtype == h.dtype)
-    codes, scales = _mx_empty(M, d, fmt, codes, scales, h.device, stream)
-    _check(lib().lmgc_op_add_norm_mx(_ptr(h), _dtype(h), _ptr(x), _dtype(x) if x is not None else 0, _ptr(gain),
-                                     _dtype(gain), float(eps), M, d, MX_FORMATS[fmt], _ptr(out), _ptr(codes),
-                                     _ptr(scales), _on(stream, h, x, gain, out, codes, scales)))
+    codes, scales = _mx_empty(M, d, fmt, codes, scales, h, stream)
+    st, (ph, px, pg, po, pc, ps) = _on(stream, h, x, gain, out, codes, scales)
+    _check(lib().lmgc_op_add_norm_mx(ph, _dtype(h), px, _dtype(x) if x is not None else 0, pg, _dtype(gain), float(eps),
+                                     M, d, MX_FORMATS[fmt], po, pc, ps, st))
     return codes, scales
 
 
@@ -711,13 +724,13 @@ def op_gemm_mx(a, a_scales, a_fmt: str, b, b_scales, N: int, K: int, kind: str =
     assert b_scales.dtype == torch.uint8 and b_scales.is_contiguous() and b_scales.numel() == n16 * ns
     dt = torch.bfloat16 if kind == "bf16" else torch.float32
     if out is None:
-        out = _empty((M, N), dt, a.device, stream)
+        out = _empty((M, N), dt, a, stream)
     assert out.dtype == dt and out.is_contiguous() and out.shape == (M, N)
     if add is not None:
         assert add.dtype == torch.float32 and add.is_contiguous() and add.shape == (M, N)
-    _check(lib().lmgc_op_gemm_mx_tile(_ptr(a), _ptr(a_scales), MX_FORMATS[a_fmt], _ptr(b), _ptr(b_scales), _ptr(add),
-                                      _ptr(out), M, N, K, MX_KINDS[kind], -1 if tile is None else MX_TILES.index(tile),
-                                      _on(stream, a, a_scales, b, b_scales, add, out)))
+    st, (pa, psa, pb, psb, padd, po) = _on(stream, a, a_scales, b, b_scales, add, out)
+    _check(lib().lmgc_op_gemm_mx_tile(pa, psa, MX_FORMATS[a_fmt], pb, psb, padd, po, M, N, K, MX_KINDS[kind],
+                                      -1 if tile is None else MX_TILES.index(tile), st))
     return out
 
 
@@ -732,20 +745,20 @@ def kv8_cache(B: int, Hkv: int, cap: int, hd: int, device="cuda"):
 
 
 def _kv8_check(cache, B, Hkv, hd):
+    """The cache's tokens, its tensors checked."""
     import torch
     kc, ks, vc, vs = cache
-    cap = 64 * kc.shape[2]
-    for c, s in ((kc, ks), (vc, vs)):
-        assert c.dtype == torch.uint8 and c.is_contiguous() and c.shape == (B, Hkv, cap // 64, 64 * hd)
-        assert s.dtype == torch.float32 and s.is_contiguous() and s.shape == (B, Hkv, cap // 64)
-    return kc, ks, vc, vs, cap
+    n = kc.shape[2]
+    assert kc.dtype == vc.dtype == torch.uint8 and kc.shape == vc.shape == (B, Hkv, n, 64 * hd)
+    assert ks.dtype == vs.dtype == torch.float32 and ks.shape == vs.shape == (B, Hkv, n)
+    assert kc.is_contiguous() and ks.is_contiguous() and vc.is_contiguous() and vs.is_contiguous()
+    return 64 * n
 
 
 def _kv8_lens(lens, counts, B):
     import torch
-    for t in (lens, counts):
-        assert t is None or (t.dtype == torch.int32 and t.is_contiguous() and t.numel() == B)
-    assert lens is not None
+    assert lens.dtype == torch.int32 and lens.is_contiguous() and lens.numel() == B
+    assert counts is None or (counts.dtype == torch.int32 and counts.is_contiguous() and counts.numel() == B)
 
 
 def op_kv8_append(cache, k, v, lens, counts=None, stream=None):
@@ -753,11 +766,11 @@ def op_kv8_append(cache, k, v, lens, counts=None, stream=None):
     sequence (lens, counts: CUDA int32 [B])."""
     import torch
     B, Hkv, T, hd = k.shape
-    kc, ks, vc, vs, cap = _kv8_check(cache, B, Hkv, hd)
+    cap = _kv8_check(cache, B, Hkv, hd)
     assert k.dtype == v.dtype == torch.bfloat16 and k.is_contiguous() and v.is_contiguous() and v.shape == k.shape
     _kv8_lens(lens, counts, B)
-    _check(lib().lmgc_op_kv8_append(_ptr(k), _ptr(v), B, Hkv, T, hd, cap, _ptr(lens), _ptr(counts), _ptr(kc),
-                                    _ptr(ks), _ptr(vc), _ptr(vs), _on(stream, k, v, lens, counts, *cache)))
+    st, (pk, pv, *rest) = _on(stream, k, v, lens, counts, *cache)
+    _check(lib().lmgc_op_kv8_append(pk, pv, B, Hkv, T, hd, cap, *rest, st))
 
 
 def kv8_workspace(B: int, Hq: int, Hkv: int, T: int, hd: int, cap: int) -> int:
@@ -770,17 +783,16 @@ def op_attention_kv8(q, cache, lens, counts=None, window: int = 0, sinks: int = 
     import torch
     B, Hq, T, hd = q.shape
     Hkv = cache[0].shape[1]
-    kc, ks, vc, vs, cap = _kv8_check(cache, B, Hkv, hd)
+    cap = _kv8_check(cache, B, Hkv, hd)
     assert q.dtype == torch.bfloat16 and q.is_contiguous()
     _kv8_lens(lens, counts, B)
     if out is None:
-        out = _empty((B * T, Hq * hd), torch.bfloat16, q.device, stream)
+        out = _empty((B * T, Hq * hd), torch.bfloat16, q, stream)
     assert out.dtype == torch.bfloat16 and out.is_contiguous() and out.numel() == q.numel()
     if ws is None:
-        ws = _empty(kv8_workspace(B, Hq, Hkv, T, hd, cap), torch.uint8, q.device, stream)
-    _check(lib().lmgc_op_attention_kv8(_ptr(q), B, Hq, Hkv, T, hd, cap, _ptr(lens), _ptr(counts), _ptr(kc), _ptr(ks),
-                                       _ptr(vc), _ptr(vs), int(window), int(sinks), _ptr(out), _ptr(ws), ws.numel(),
-                                       _on(stream, q, out, ws, lens, counts, *cache)))
+        ws = _empty(kv8_workspace(B, Hq, Hkv, T, hd, cap), torch.uint8, q, stream)
+    st, (pq, po, pw, *rest) = _on(stream, q, out, ws, lens, counts, *cache)
+    _check(lib().lmgc_op_attention_kv8(pq, B, Hq, Hkv, T, hd, cap, *rest, int(window), int(sinks), po, pw, ws.numel(), st))
     return out
 
 
