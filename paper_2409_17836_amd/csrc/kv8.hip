@@ -228,6 +228,7 @@ __device__ inline __amdgpu_buffer_rsrc_t block_buffer(const uint8_t* codes, int6
 // heads of 64, 1000 queries from the start: 9.9 us (the other form 29.5), 4
 // such sequences 27 (31), 8 of them 47 (42); 32 heads on 8 of 128, 50 queries
 // over 3900 tokens: 19 us (31), 4 of them 46 (37).
+//
 // Grid: (splits, tiles of 16 columns x Hkv, B), 512 threads.  A cache of up to
 // kOneBytes is one split (and the call one launch), a longer one is cut into
 // kSplitBytes (more where that were over kMaxSplits).  Wave w takes its blocks
@@ -235,13 +236,14 @@ __device__ inline __amdgpu_buffer_rsrc_t block_buffer(const uint8_t* codes, int6
 // and tokens 16 i + 4 g + r of a block, an online softmax, O^T += V^T P^T.
 // The waves' parts meet in LDS.
 //
-// Bound by the bytes of the cache.  ONCE, a single tile of columns: nothing
-// reads the codes again before the next step, so they are loaded past the
-// caches' order of use.  8 sequences x 32 heads of 128 over 4094 tokens, 268
-// MB, from a cache not in any cache: 48.8 us, 5.5 TB/s (54.6 without ONCE); 32
-// sequences 171 us, 6.1 TB/s; one sequence 11.8 us.  A cache in the L2 costs a
-// little more that way (32 x 4 heads of 64 over 2000 tokens: 12.2 us for
-// 11.2), and with two tiles the second one misses it (24.5 us for 22.3).
+// Bound by the bytes of the cache, with many tiles by the vector unit (codes to
+// bf16, exponentials), and with few tokens by a chain of dependent loads (5.9 us
+// for 512 + 4 of them).  ONCE, a single tile of columns: nothing reads the codes
+// again before the next step, so they are loaded past the caches' order of use.
+// From memory, 8 sequences x 32 heads of 128 over 4094 tokens, 268 MB: 49 us,
+// 5.5 TB/s (55 without ONCE); 32 sequences 170 us, 6.2 TB/s (187); one sequence
+// 11.6 us (12.5).  With two tiles the second one misses them (23.7 us for 21.7
+// at 8 x 8 heads, 32 columns over 2000).
 constexpr int kFewCols = 2048, kFewBlocks = 16384;
 constexpr int kNonTemporal = 2;  // the instruction's nt bit
 constexpr int kOneBytes = 256 << 10, kSplitBytes = 128 << 10;
