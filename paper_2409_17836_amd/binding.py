@@ -638,17 +638,18 @@ def _mx_empty(rows, cols, fmt, codes, scales, like, stream):
     nc, ns = _mx_sizes(rows, cols, fmt)
     if codes is None:
         codes = _empty((rows, nc), torch.uint8, like, stream)
+    else:
+        assert codes.dtype == torch.uint8 and codes.is_contiguous() and codes.numel() == rows * nc, (tuple(codes.shape), rows, cols, fmt)
     if scales is None:
         scales = _empty((rows, ns), torch.uint8, like, stream)
-    _mx_check(codes, scales, rows, cols, fmt)
+    else:
+        assert scales.dtype == torch.uint8 and scales.is_contiguous() and scales.numel() == rows * ns, (tuple(scales.shape), rows, cols)
     return codes, scales
 
 
 def _mx_check(codes, scales, rows, cols, fmt):
-    import torch
-    nc, ns = _mx_sizes(rows, cols, fmt)
-    assert codes.dtype == torch.uint8 and codes.is_contiguous() and codes.numel() == rows * nc, (tuple(codes.shape), rows, cols, fmt)
-    assert scales.dtype == torch.uint8 and scales.is_contiguous() and scales.numel() == rows * ns, (tuple(scales.shape), rows, cols)
+    assert codes is not None and scales is not None
+    _mx_empty(rows, cols, fmt, codes, scales, None, None)
 
 
 def op_mx_quantize(x, fmt: str, codes=None, scales=None, stream=None):
@@ -725,7 +726,8 @@ def op_gemm_mx(a, a_scales, a_fmt: str, b, b_scales, N: int, K: int, kind: str =
     dt = torch.bfloat16 if kind == "bf16" else torch.float32
     if out is None:
         out = _empty((M, N), dt, a, stream)
-    assert out.dtype == dt and out.is_contiguous() and out.shape == (M, N)
+    else:
+        assert out.dtype == dt and out.is_contiguous() and out.shape == (M, N)
     if add is not None:
         assert add.dtype == torch.float32 and add.is_contiguous() and add.shape == (M, N)
     st, (pa, psa, pb, psb, padd, po) = _on(stream, a, a_scales, b, b_scales, add, out)
@@ -788,7 +790,8 @@ def op_attention_kv8(q, cache, lens, counts=None, window: int = 0, sinks: int = 
     _kv8_lens(lens, counts, B)
     if out is None:
         out = _empty((B * T, Hq * hd), torch.bfloat16, q, stream)
-    assert out.dtype == torch.bfloat16 and out.is_contiguous() and out.numel() == q.numel()
+    else:
+        assert out.dtype == torch.bfloat16 and out.is_contiguous() and out.numel() == q.numel()
     if ws is None:
         ws = _empty(kv8_workspace(B, Hq, Hkv, T, hd, cap), torch.uint8, q, stream)
     st, (pq, po, pw, *rest) = _on(stream, q, out, ws, lens, counts, *cache)
