@@ -794,8 +794,11 @@ def op_attention_kv8(q, cache, lens, counts=None, window: int = 0, sinks: int = 
         assert out.dtype == torch.bfloat16 and out.is_contiguous() and out.numel() == q.numel()
     if ws is None:
         ws = _empty(kv8_workspace(B, Hq, Hkv, T, hd, cap), torch.uint8, q, stream)
+    else:
+        assert ws.is_contiguous()  # its bytes lie one behind the other
     st, (pq, po, pw, *rest) = _on(stream, q, out, ws, lens, counts, *cache)
-    _check(lib().lmgc_op_attention_kv8(pq, B, Hq, Hkv, T, hd, cap, *rest, int(window), int(sinks), po, pw, ws.numel(), st))
+    _check(lib().lmgc_op_attention_kv8(pq, B, Hq, Hkv, T, hd, cap, *rest, int(window), int(sinks), po, pw,
+                                       ws.numel() * ws.element_size(), st))
     return out
 
 

@@ -1,0 +1,56 @@
+"""Calls of the operators in fewer bits that have to be refused, or whose
+arguments have to be brought into range, before anything is launched."""
+import pytest
+
+from paper_2409_17836_amd import binding as B
+
+EINVAL = -1
+SRC, CODES, SCALES, OUT = 1 << 44, 1 << 45, 1 << 46, 1 << 47  # addresses that are never read
+
+
+def test_attention_workspace_is_plain_bytes():
+    """A workspace whose elements do not lie one behind the other has less memory
+    behind its address than it has elements; refused like every other tensor
+    that is not contiguous (so without a GPU too)."""
+    import torch
+    B_, Hq, Hkv, T, hd, cap = 1, 4, 2, 1, 64, 4096
+    need = B.kv8_workspace(B_, Hq, Hkv, T, hd, cap)
+    assert need > 0
+    cache = B.kv8_cache(B_, Hkv, cap, hd, device="cpu")
+    q = torch.zeros((B_, Hq, T, hd), dtype=torch.bfloat16)
+    lens = torch.zeros(B_, dtype=torch.int32)
+    one = torch.zeros(1, dtype=torch.uint8)
+    for ws in (one.expand(need), torch.zeros(2 * need, dtype=torch.uint8)[::2], one.expand(2, need)):
+        with pytest.raises(AssertionError):
+            B.op_attention_kv8(q, cache, lens, ws=ws)
+
+
+class _Library:
+    """Takes the place of the library: keeps the arguments of the attention call."""
+
+    def __init__(self, real):
+        self.real, self.args = real, None
+
+    def __getattr__(self, name):
+        return getattr(self.real, name)
+
+    def lmgc_op_attention_kv8(self, *args):
+        self.args = args
+        return 0
+
+
+def _attention_args(monkeypatch, **kw):
+    import torch
+    fake = _Library(B.lib())
+    monkeypatch.setattr(B, "lib", lambda: fake)
+    monkeypatch.setattr(B, "_on", lambda stream, *tensors: (0, [0] * len(tensors)))
+    cache = B.kv8_cache(1, 2, 4096, 64, device="cpu")
+    B.op_attention_kv8(torch.zeros((1, 4, 1, 64), dtype=torch.bfloat16), cache, torch.zeros(1, dtype=torch.int32), **kw)
+    return fake.args
+
+
+def test_attention_workspace_counts_bytes(monkeypatch):
+    """The size that the library is told is in bytes, whatever the tensor's elements are."""
+    import torch
+    need = B.kv8_workspace(1, 4, 2, 1, 64, 4096)
+    assert _attention_args(monkeypatch, ws=torch.zeros(need // 4, dtype=torch.float32))[-2] == need
