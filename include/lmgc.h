@@ -524,8 +524,8 @@ int64_t lmgc_mx_block_scale_bytes(int64_t rows, int64_t cols);
 
 /*
  * Quantise d_src [rows, cols] (dtype LMGC_DTYPE_F32 or _BF16, rows `ld`
- * elements apart, any alignment of its elements) into the rows layout.
- * GPU, async.  Errors: EINVAL.
+ * elements apart, any alignment of its elements) into the rows layout.  cols <=
+ * ld <= 2^40, (rows - 1) ld <= 2^46, as below.  GPU, async.  Errors: EINVAL.
  */
 int lmgc_op_mx_quantize(const void* d_src, int32_t dtype, int64_t rows, int64_t cols, int64_t ld,
                         int32_t fmt, uint8_t* d_codes, uint8_t* d_scales, void* stream);

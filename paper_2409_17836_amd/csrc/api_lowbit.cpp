@@ -25,6 +25,13 @@ int check_shape(int64_t rows, int64_t cols) {
   return LMGC_OK;
 }
 
+// rows `ld` elements apart, their extent within the address space (2^46 elements: its bytes do not pass 64 bits)
+int check_ld(int64_t rows, int64_t cols, int64_t ld) {
+  if (ld < cols || ld > ((int64_t)1 << 40)) return set_error(LMGC_EINVAL, "ld must be in [cols, 2^40]");
+  if (rows > 1 && rows - 1 > ((int64_t)1 << 46) / ld) return set_error(LMGC_EINVAL, "rows ld passes 2^46 elements");
+  return LMGC_OK;
+}
+
 int64_t kcols(int64_t cols) { return (cols + 127) / 128 * 128; }
 int64_t row_scales(int64_t cols) { return (cols + 511) / 512 * 16; }
 int64_t code_bytes(int32_t fmt, int64_t rows, int64_t cols) { return rows * (fmt == LMGC_MX_FP8 ? kcols(cols) : kcols(cols) / 2); }
@@ -95,7 +102,7 @@ int lmgc_op_mx_quantize(const void* d_src, int32_t dtype, int64_t rows, int64_t 
   if (rc) return rc;
   if (!is_dtype(dtype)) return set_error(LMGC_EINVAL, "unknown dtype %d", dtype);
   if (!is_fmt(fmt)) return set_error(LMGC_EINVAL, "unknown format %d", fmt);
-  if (ld < cols || ld > ((int64_t)1 << 40)) return set_error(LMGC_EINVAL, "ld must be in [cols, 2^40]");
+  if ((rc = check_ld(rows, cols, ld))) return rc;
   if (rows == 0) return LMGC_OK;
   if (!d_src || !d_codes || !d_scales) return set_error(LMGC_EINVAL, "NULL device buffer");
   if ((uintptr_t)d_src % dtype_bytes(dtype) || !aligned(d_codes) || !aligned(d_scales))
@@ -113,7 +120,7 @@ int lmgc_op_mx_dequantize(const uint8_t* d_codes, const uint8_t* d_scales, int32
   if (rc) return rc;
   if (!is_dtype(dtype)) return set_error(LMGC_EINVAL, "unknown dtype %d", dtype);
   if (!is_fmt(fmt)) return set_error(LMGC_EINVAL, "unknown format %d", fmt);
-  if (ld < cols || ld > ((int64_t)1 << 40)) return set_error(LMGC_EINVAL, "ld must be in [cols, 2^40]");
+  if ((rc = check_ld(rows, cols, ld))) return rc;
   if (rows == 0) return LMGC_OK;
   if (!d_out || !d_codes || !d_scales) return set_error(LMGC_EINVAL, "NULL device buffer");
   if ((uintptr_t)d_out % dtype_bytes(dtype) || !aligned(d_codes) || !aligned(d_scales))

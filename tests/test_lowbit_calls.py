@@ -54,3 +54,15 @@ def test_attention_workspace_counts_bytes(monkeypatch):
     import torch
     need = B.kv8_workspace(1, 4, 2, 1, 64, 4096)
     assert _attention_args(monkeypatch, ws=torch.zeros(need // 4, dtype=torch.float32))[-2] == need
+
+
+def test_strides_past_the_address_space_are_refused():
+    """Rows that lie so far apart that the matrix's extent in bytes passes 64
+    bits: its overlap with the other buffers cannot be told from a wrapped
+    extent, and no such matrix exists.  (2^24 rows 2^40 elements apart: 2^66 and
+    2^65 bytes, zero in 64 bits.)"""
+    rows = (1 << 24) + 1
+    for dtype in (0, 1):
+        for r, ld in ((rows, 1 << 40), ((1 << 31) - 1, 1 << 40), (rows, (1 << 39) + 1), (1 << 30, 1 << 20)):
+            assert B.lib().lmgc_op_mx_quantize(SRC, dtype, r, 1, ld, 0, SRC + (1 << 20), SCALES, None) == EINVAL
+            assert B.lib().lmgc_op_mx_dequantize(CODES, SCALES, 0, r, 1, CODES + (r << 8), dtype, ld, None) == EINVAL
