@@ -781,7 +781,8 @@ def kv8_workspace(B: int, Hq: int, Hkv: int, T: int, hd: int, cap: int) -> int:
 
 def op_attention_kv8(q, cache, lens, counts=None, window: int = 0, sinks: int = 0, out=None, ws=None, stream=None):
     """Attention of the T tokens just appended over the 8-bit cache: q bf16
-    [B, Hq, T, hd] -> bf16 [B T, Hq hd]."""
+    [B, Hq, T, hd] -> bf16 [B T, Hq hd].  window, sinks: any size (ctypes would
+    keep the low 32 bits of a larger one)."""
     import torch
     B, Hq, T, hd = q.shape
     Hkv = cache[0].shape[1]
@@ -797,7 +798,10 @@ def op_attention_kv8(q, cache, lens, counts=None, window: int = 0, sinks: int = 
     else:
         assert ws.is_contiguous()  # its bytes lie one behind the other
     st, (pq, po, pw, *rest) = _on(stream, q, out, ws, lens, counts, *cache)
-    _check(lib().lmgc_op_attention_kv8(pq, B, Hq, Hkv, T, hd, cap, *rest, int(window), int(sinks), po, pw,
+    window, sinks = int(window), int(sinks)
+    if not (0 <= window < 2 ** 31 and 0 <= sinks < 2 ** 31):
+        window, sinks = max(-1, min(window, 2 ** 31 - 1)), max(-1, min(sinks, 2 ** 31 - 1))
+    _check(lib().lmgc_op_attention_kv8(pq, B, Hq, Hkv, T, hd, cap, *rest, window, sinks, po, pw,
                                        ws.numel() * ws.element_size(), st))
     return out
 

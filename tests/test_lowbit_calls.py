@@ -66,3 +66,12 @@ def test_strides_past_the_address_space_are_refused():
         for r, ld in ((rows, 1 << 40), ((1 << 31) - 1, 1 << 40), (rows, (1 << 39) + 1), (1 << 30, 1 << 20)):
             assert B.lib().lmgc_op_mx_quantize(SRC, dtype, r, 1, ld, 0, SRC + (1 << 20), SCALES, None) == EINVAL
             assert B.lib().lmgc_op_mx_dequantize(CODES, SCALES, 0, r, 1, CODES + (r << 8), dtype, ld, None) == EINVAL
+
+
+@pytest.mark.parametrize("given,taken", [(0, 0), (5, 5), (2 ** 31 - 1, 2 ** 31 - 1), (2 ** 31, 2 ** 31 - 1), (2 ** 32 + 16, 2 ** 31 - 1),
+                                         (10 ** 30, 2 ** 31 - 1), (-1, -1), (-2 ** 32 + 5, -1)])
+def test_attention_windows_and_sinks_past_32_bits(monkeypatch, given, taken):
+    """Positions end at 2^24, so more than 2^31 - 1 is the same as that, and is
+    not cut to its low bits; what is negative stays so (and is refused)."""
+    assert _attention_args(monkeypatch, window=given)[-6:-4] == (taken, 0)
+    assert _attention_args(monkeypatch, sinks=given)[-6:-4] == (0, taken)
