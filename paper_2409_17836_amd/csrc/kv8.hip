@@ -440,9 +440,10 @@ __global__ __launch_bounds__(64) void attn_kv8_join_kernel(const float* __restri
     }
   }
   const int t = c / G, hq = kvh * G + c % G;
+  const float inv = 1.0f / L;  // as where a single split writes the result: a column's tile decides which does
   uint16_t* op = out + ((int64_t)b * T + t) * ((int64_t)Hkv * G * HD) + hq * HD + lane * (HD / 64);
 #pragma unroll
-  for (int i = 0; i < HD / 64; i++) op[i] = f32_to_bf16(acc[i] / L);
+  for (int i = 0; i < HD / 64; i++) op[i] = f32_to_bf16(acc[i] * inv);
 }
 
 // ---- many columns

@@ -3,6 +3,7 @@ what it sees: the other queries of its tile, the codes of tokens that no query
 sees, and every border of a mask or a split, one token at a time."""
 import pytest
 
+from gpu_util import log
 from paper_2409_17836_amd import binding as B
 
 pytestmark = pytest.mark.gpu
@@ -17,6 +18,62 @@ def _randn(shape, seed):
     import torch
     g = torch.Generator(device="cuda").manual_seed(seed)
     return torch.randn(shape, generator=g, device="cuda").to(torch.bfloat16)
+
+
+# --------------------------------------------------- the queries beside a query
+# (cap, Hq, Hkv, T, border of two splits): a tile of 16 columns, one of 256
+FORMS = {"few": (1088 * 2, 2, 2, 16, 1024), "many": (1216, 8, 1, 300, 640)}
+
+
+@pytest.mark.parametrize("form", FORMS)
+@pytest.mark.parametrize("hd", [64, 128])
+def test_a_quotient_does_not_depend_on_the_tile(form, hd):
+    """Values whose means over a window lie halfway between two bf16 numbers, at
+    480 keys, where the sum times the rounded reciprocal of 480 falls to the
+    other side than the quotient: a query gives the same bits whether its tile
+    ends before the border of two splits or behind it, and in whichever row of
+    the call it is.  (Of 32 tokens 4 d + 1 have 2 and the others 1.875 in dim d,
+    so a window's mean is 1.875 + (4 d + 1) / 256; queries of zero weigh alike,
+    and all sums are exact.)"""
+    import torch
+    cap, Hq, Hkv, T, border = FORMS[form]
+    if form == "few" and hd == 128:
+        cap, border = 1088, 512
+    log(f"quotient {form} hd={hd}")
+    j, d = torch.arange(cap, device="cuda")[:, None], torch.arange(hd, device="cuda")[None, :]
+    v = torch.where(j % 32 < 4 * (d % 8) + 1, 2.0, 1.875).to(torch.bfloat16).expand(1, Hkv, cap, hd).contiguous()
+    cache = B.kv8_cache(1, Hkv, cap, hd)
+    B.op_kv8_append(cache, _randn((1, Hkv, cap, hd), 1), v, _int32([0]))
+    q = torch.zeros((1, Hq, T, hd), dtype=torch.bfloat16, device="cuda")
+    want = {}
+    for n in (border - T, border - 20, border - 10, border - 6, border - 1):
+        for count in (6, 10, T):
+            out = B.op_attention_kv8(q, cache, _int32([n]), _int32([count]), window=480).reshape(T, -1)
+            for t in range(count):
+                row = want.setdefault(n + t, out[t].clone())
+                assert torch.equal(row, out[t]), (n, count, t)
+    assert len(want) > T
+
+
+@pytest.mark.parametrize("T,Hq,Hkv", [(1, 8, 2), (16, 2, 2), (40, 4, 2), (300, 16, 2)])
+def test_a_query_does_not_depend_on_the_others(T, Hq, Hkv):
+    """The same positions through other lengths and counts, over random values."""
+    import torch
+    hd, cap = 128, 1216
+    log(f"queries T={T} heads {Hq}/{Hkv}")
+    cache = B.kv8_cache(2, Hkv, cap, hd)
+    B.op_kv8_append(cache, _randn((2, Hkv, cap, hd), 1), _randn((2, Hkv, cap, hd), 2), _int32([0, 0]))
+    all_q = _randn((2, Hq, cap, hd), 3)  # by position
+    want = {}
+    for n in (500, 509, 600, 620, 639 - T // 2):
+        for count in (1, (T + 1) // 2, T):
+            lens = [n, n + 3]
+            q = torch.stack([all_q[b, :, m:m + T] for b, m in enumerate(lens)]).contiguous()
+            out = B.op_attention_kv8(q, cache, _int32(lens), _int32([count, T]), window=333, sinks=5).reshape(2, T, -1)
+            for b, (m, c) in enumerate(zip(lens, (count, T))):
+                for t in range(c):
+                    row = want.setdefault((b, m + t), out[b, t].clone())
+                    assert torch.equal(row, out[b, t]), (b, m, t)
 
 
 # ------------------------------------------------------------- wide arguments
