@@ -1,8 +1,10 @@
 """Attention over the 8-bit cache where a query's bits may depend on nothing but
 what it sees: the other queries of its tile, the codes of tokens that no query
 sees, and every border of a mask or a split, one token at a time."""
+import numpy as np
 import pytest
 
+import lowbit_ref as R
 from gpu_util import log
 from paper_2409_17836_amd import binding as B
 
@@ -74,6 +76,53 @@ def test_a_query_does_not_depend_on_the_others(T, Hq, Hkv):
                 for t in range(c):
                     row = want.setdefault((b, m + t), out[b, t].clone())
                     assert torch.equal(row, out[b, t]), (b, m, t)
+
+
+# ------------------------------------------------------------------- borders
+def _marks(n, T, cap, window, sinks, hd):
+    """hd tokens next to the borders of a call: of the mask for the first, a
+    middle and the last query, and of 64 and of every length that a split may
+    have."""
+    at = set()
+    for p in (n, n + T // 2, n + T - 1):
+        for j in (p, p - window, sinks):
+            at |= {j - 1, j, j + 1}
+    g = np.random.default_rng(n + T + window)
+    at |= {0, cap - 1, n - 1, n}
+    at = {j for j in at if 0 <= j < cap}
+    blocks = np.arange(64, cap, 64)
+    near = [j + e for j in g.permutation(blocks) for e in (-1, 0)]
+    at = list(at) + [j for j in near if j not in at]
+    return np.array(at[:hd] if len(at) >= hd else at + [0] * (hd - len(at)))
+
+
+@pytest.mark.parametrize("hd", [64, 128])
+@pytest.mark.parametrize("cap,T,Hq,window,sinks", [
+    (1 << 18, 1, 2, 0, 0), (1 << 18, 1, 2, 100000, 5000), (1 << 18, 20, 1, 0, 0), (1 << 18, 20, 1, 100000, 64), (1 << 18, 600, 4, 3000, 4),
+    (1 << 15, 600, 4, 0, 0), (4096, 1, 4, 0, 0), (4096, 70, 2, 1000, 3), (4096, 700, 4, 0, 0), (4096, 700, 4, 600, 130), (1088, 3, 2, 64, 1)])
+def test_every_key_counts_once(hd, cap, T, Hq, window, sinks):
+    """Queries of zero weigh all keys alike, and in dim d a single token has the
+    value 448, the others none: a result is 448 over the number of keys that the
+    query sees, or zero, exactly, where it does not see the token.  Weights,
+    their sum (below 2^24) and the product are exact; the reciprocal and its
+    product are off by 2^-23, bf16 by 2^-8."""
+    import torch
+    log(f"borders hd={hd} cap={cap} T={T} heads {Hq} window {window} sinks {sinks}")
+    k = _randn((1, 1, cap, hd), 1)
+    for n in (cap - T, cap - T - 65, cap // 2 + 1):
+        at = _marks(n, T, cap, window, sinks, hd)
+        v = torch.zeros((1, 1, cap, hd), dtype=torch.bfloat16, device="cuda")
+        v[0, 0, torch.from_numpy(at).cuda(), torch.arange(hd, device="cuda")] = 448.0
+        cache = B.kv8_cache(1, 1, cap, hd)
+        B.op_kv8_append(cache, k, v, _int32([0]))
+        q = torch.zeros((1, Hq, T, hd), dtype=torch.bfloat16, device="cuda")
+        out = B.op_attention_kv8(q, cache, _int32([n]), window=window, sinks=sinks).double().cpu().numpy().reshape(T, Hq, hd)
+        pos = n + np.arange(T)
+        low = np.maximum(pos - window, -1) if window else np.full(T, -1)
+        seen = (pos - low) + np.minimum(sinks if window else 0, low + 1)
+        sees = (at[None] <= pos[:, None]) & ((at[None] > low[:, None]) | (at[None] < sinks))
+        want = np.where(sees, 448.0 / seen[:, None], 0.0)[:, None]
+        assert (np.abs(out - want) <= (2.0 ** -8 + 2.0 ** -22) * want).all(), n
 
 
 # ------------------------------------------------------------- wide arguments
