@@ -623,9 +623,13 @@ int lmgc_op_kv8_append(const uint16_t* d_k, const uint16_t* d_v, int32_t B, int3
  *   token (as above) are left as they were.  window >= 0 (0: none), sinks >= 0.
  *   d_ws: lmgc_kv8_workspace bytes, 16-byte aligned, its contents free; calls
  *   that may run at the same time need one each.
- * Masked keys count for nothing, whatever their block holds; a visible key of
- * a block with a NaN scale gives NaN.  Scales are powers of two, 2^-64 or more
- * as appending leaves them; above 2^100 (values of 5e32) sums may overflow.  A
+ * Masked keys count for nothing: a block's scale may be NaN, and the codes of
+ * a token that no query of its sequence sees may be anything; a visible key of a
+ * block with a NaN scale gives NaN.  (Appending leaves no code that is NaN: a
+ * value code 0x7f or 0xff of a token that some query sees, written otherwise,
+ * makes its dim NaN for queries near it that do not see it, too.)  Scales are
+ * powers of two, 2^-64 or more as appending leaves them; scales and queries
+ * above 2^100 (keys and values of 5e32) may overflow in the sums.  A
  * query's result depends on the cache and its position, and on cap, T, Hq, Hkv
  * (which say how the work is split), not on the other sequences or queries.
  * T Hq / Hkv <= 2^30; above 32, B Hkv ceil(T Hq / Hkv / 256) < 2^23, times the

@@ -192,9 +192,23 @@ struct Mask {
   __device__ inline bool all(int p0, int p1, int j0, int j1) const {
     return j1 - 1 <= p0 && (window == 0 || j0 > p1 - window || j1 <= sinks);
   }
+  // the tokens of the block at j0 that some query at positions p0 .. p1 sees, a bit each
+  __device__ inline uint64_t seen(int p0, int p1, int j0) const {
+    auto first = [](int n) __attribute__((always_inline)) { return n >= kBlk ? ~0ull : (1ull << max(n, 0)) - 1; };
+    return first(p1 + 1 - j0) & (~first(max(low(p0), -1) + 1 - j0) | first(sinks - j0));
+  }
   // whether split [j0, j1) of the cache is the only one that any of them sees
   __device__ inline bool only(int p0, int p1, int j0, int j1) const { return j1 > p1 && (j0 == 0 || !any(p0, p1, 0, j0)); }
 };
+
+// Codes of values that no query sees may be anything, a NaN among it, and a
+// probability of zero times that is NaN: they are cleared.  The bytes that stay
+// in word e of a lane's 16 codes of a block, tokens 16 e + 4 g .. + 3 of `seen`.
+__device__ inline uint32_t seen_bytes(uint64_t seen, int e, int g) {
+  const uint32_t four = (uint32_t)(seen >> (e & 2 ? 32 : 0)) >> (4 * g) >> (16 * (e & 1)) & 15;
+  const uint32_t ones = four * 0x204081 & 0x01010101;  // a bit to a byte
+  return (ones << 8) - ones;
+}
 
 __device__ inline bf16x8 fp8_bf16(uint32_t w0, uint32_t w1) {
   const bf16x2 a = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w0, 1.0f, false), b = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w0, 1.0f, true);
@@ -330,6 +344,13 @@ __global__ __launch_bounds__(kSplitWaves * 64, HD == 64 ? 6 : 4) void attn_kv8_s
 #pragma unroll
         for (int r = 0; r < 4; r++)
           if (!mask.sees(pos, low, j0 + 16 * i + 4 * g + r)) s[i][r] = -INFINITY;
+      const uint64_t seen = mask.seen(p0, p1, j0);
+#pragma unroll
+      for (int e = 0; e < 4; e++) {
+        const uint32_t keep = seen_bytes(seen, e, g);
+#pragma unroll
+        for (int i = 0; i < ND; i++) vr[i][e] &= keep;
+      }
     }
     float mx = -INFINITY;
 #pragma unroll
@@ -557,6 +578,13 @@ __global__ __launch_bounds__(512, 2) void attn_kv8_prompt_kernel(
     d[0] = __builtin_bit_cast(u32x4, fp8_bf16(w[0], w[1]));
     d[64] = __builtin_bit_cast(u32x4, fp8_bf16(w[2], w[3]));
   };
+  auto stash_values = [&](u32x4* to, u32x4 w, uint64_t seen) __attribute__((always_inline)) {
+    if (seen != ~0ull) {
+#pragma unroll
+      for (int e = 0; e < 4; e++) w[e] &= seen_bytes(seen, e, g);
+    }
+    stash(to, w);
+  };
   f32x4 acc[ND][2] = {};
   f32x4 sc[4][2];   // scores of a block
   bf16x8 pf[2][2];  // its probabilities
@@ -612,7 +640,7 @@ __global__ __launch_bounds__(512, 2) void attn_kv8_prompt_kernel(
     stash(sk[0], p[(int64_t)x[0] * (kBlk * HD / 16)]);
     stash(sk[1], x[1] < bend ? p[(int64_t)x[1] * (kBlk * HD / 16)] : zero);
   }
-  if (values) stash(sv[0], reinterpret_cast<const u32x4*>(vp + at * 16)[(int64_t)x[0] * (kBlk * HD / 16)]);
+  if (values) stash_values(sv[0], reinterpret_cast<const u32x4*>(vp + at * 16)[(int64_t)x[0] * (kBlk * HD / 16)], mask.seen(p0, p1, x[0] * kBlk));
 #pragma unroll
   for (int i = 0; i < kAhead; i++) fetch(i, x[i + 2], x[i + 1]);
   float fk = ks[blk0 + x[0]] * sl2, fv = vs[blk0 + x[0]];
@@ -626,9 +654,10 @@ __global__ __launch_bounds__(512, 2) void attn_kv8_prompt_kernel(
   int par = 0, slot = 0;
   if (wave >= 4) phase();
   while (x[0] < bend) {
-    // the next block's scales, asked for before the phase's work
+    // the next block's scales, asked for before the phase's work, and its tokens that count
     const int64_t bn = blk0 + min(x[1], bend - 1);
     const float nk = ks[bn], nv = vs[bn];
+    const uint64_t next_seen = mask.seen(p0, p1, x[1] * kBlk);
     __builtin_amdgcn_sched_barrier(0);
     if (works) {
       const int j0 = x[0] * kBlk;
@@ -722,7 +751,7 @@ __global__ __launch_bounds__(512, 2) void attn_kv8_prompt_kernel(
     }
     __builtin_amdgcn_sched_barrier(0);
     if (keys) stash(sk[par], kr);
-    if (values) stash(sv[par ^ 1], vr);
+    if (values) stash_values(sv[par ^ 1], vr, next_seen);
     __builtin_amdgcn_sched_barrier(0);
     phase();
     __builtin_amdgcn_sched_barrier(0);

@@ -78,6 +78,33 @@ def test_a_query_does_not_depend_on_the_others(T, Hq, Hkv):
                     assert torch.equal(row, out[b, t]), (b, m, t)
 
 
+# ------------------------------------------------------------ unseen tokens
+@pytest.mark.parametrize("hd", [64, 128])
+@pytest.mark.parametrize("T,Hq,Hkv", [(1, 4, 2), (1, 24, 1), (5, 4, 2), (20, 2, 1), (100, 4, 2), (300, 16, 2)])
+def test_codes_of_unseen_tokens_count_for_nothing(hd, T, Hq, Hkv):
+    """Codes that are no numbers (0x7f, 0xff) in every token that no query sees,
+    in blocks that are partly seen too, change no bit."""
+    import torch
+    cap = 1216
+    log(f"unseen codes hd={hd} T={T} heads {Hq}/{Hkv}")
+    cache = B.kv8_cache(1, Hkv, cap, hd)
+    B.op_kv8_append(cache, _randn((1, Hkv, cap, hd), 1), _randn((1, Hkv, cap, hd), 2), _int32([0]))
+    q = _randn((1, Hq, T, hd), 3)
+    for n, window, sinks in ((0, 0, 0), (1, 0, 0), (37, 20, 0), (400, 0, 0), (447, 100, 0), (448, 90, 7), (700, 333, 70), (850, 64, 1)):
+        want = B.op_attention_kv8(q, cache, _int32([n]), window=window, sinks=sinks)
+        j = np.arange(cap)
+        unseen = j >= n + T
+        if window:
+            unseen |= (j <= n - window) & (j >= sinks)
+        bad = [t.clone() for t in cache]
+        for codes, index in ((bad[0], R.key_index(hd)), (bad[2], R.value_index(hd))):
+            blk, at = np.nonzero(unseen)[0] // 64, index[np.nonzero(unseen)[0] % 64]
+            blk, at = torch.from_numpy(blk).cuda()[:, None], torch.from_numpy(at).cuda()
+            codes[0][:, blk, at] = torch.where(at % 3 == 0, 0xff, 0x7f).to(torch.uint8)
+        got = B.op_attention_kv8(q, bad, _int32([n]), window=window, sinks=sinks)
+        assert torch.isfinite(want).all() and torch.equal(got, want), (n, window, sinks)
+
+
 # ------------------------------------------------------------------- borders
 def _marks(n, T, cap, window, sinks, hd):
     """hd tokens next to the borders of a call: of the mask for the first, a
