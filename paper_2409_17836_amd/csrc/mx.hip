@@ -203,7 +203,7 @@ __global__ __launch_bounds__(NT < 256 ? 256 : NT) void add_norm_mx_kernel(
         if (rem != 0.f && (u & 1) == 0) u += (rem < 0.f) == (y < 0.f) ? 1u : -1u;
         y = __builtin_bit_cast(float, u);
       }
-      v[i][e] = y;
+      v[i][e] = c < nchunks ? y : 0.f;  // (zero times a NaN or infinite root is NaN)
     }
     mx_store8<FMT>(v[i], c, kcols, ns, codes + row * (FMT == LMGC_MX_FP8 ? kcols : kcols / 2), scales + row * ns);
   }
