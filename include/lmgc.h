@@ -542,9 +542,10 @@ int lmgc_op_mx_block(const uint8_t* d_codes, const uint8_t* d_scales, int64_t N,
 
 /*
  * Residual add and RMSNorm with a microscaled output, the operand of the next
- * product: t = h + x (rounded to h's type), d_out = t, y = t / sqrt(mean(t^2)
- * + eps) * gain, and y [M, d] quantised into the rows layout: the code is the
- * nearest one also where y lies next to a border (y is held to 2^-45).
+ * product: t = h + x (a float32 sum, rounded to h's type), d_out = t, y = t /
+ * sqrt(mean(t^2) + eps) * gain, and y [M, d] quantised into the rows layout: the
+ * code is the nearest one also where y lies next to a border (y is held to
+ * 2^-45, and to 2^-149 below 2^-126), for rows and gains of any size.
  *   d_h [M, d] (h_dtype), d_x [M, d] (x_dtype; NULL: t = h), d_gain [d]
  *   (g_dtype), d_out [M, d] of h_dtype: NULL, d_h itself, or a buffer that
  *   overlaps nothing.  d % 32 == 0, d <= 16384, 0 <= M <= 2^31 - 1.

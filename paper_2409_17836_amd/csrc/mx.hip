@@ -132,14 +132,13 @@ __global__ __launch_bounds__(256) void mx_block_kernel(const uint8_t* __restrict
 // The sum that is normalised is the one that is stored.
 //
 // A code is the rounding of y, and an error in y of e turns some e / 2^-4 of
-// the codes into their neighbours, so y is kept closer than its float32
-// factors: the squares are summed in float64, the root's reciprocal is taken as
-// a float32 and what that leaves, and the products with x and the gain carry
-// their rounding errors along.  What the float32 y at the end leaves decides
-// its lowest bit: where the remainder is not zero an even y becomes the odd
-// neighbour on the remainder's side, so that y lies on a border between two
-// codes only if the value does.  The kernel is bound by its memory traffic
-// either way.
+// the codes into their neighbours, so y is kept closer than a float32: the sum
+// of the squares, the root and the products are float64 (which has room for
+// rows, gains and values of any size too), and y becomes a float32 with its last
+// bit set wherever bits are left behind it, so that it lies on a border between
+// two codes only if the value does.  The float32s of twice the precision that
+// did this before took as long, and failed near the ends of float32.  The
+// kernel is bound by its memory traffic either way.
 template <int FMT, typename TH, typename TX, typename TG, int NC, int NT>
 __global__ __launch_bounds__(NT < 256 ? 256 : NT) void add_norm_mx_kernel(
     const TH* h, const TX* __restrict__ x, const TG* __restrict__ gain, float eps, int64_t M, int d, TH* out,
@@ -186,23 +185,19 @@ __global__ __launch_bounds__(NT < 256 ? 256 : NT) void add_norm_mx_kernel(
 #pragma unroll
     for (int w = 0; w < NW; w++) sd += part[w];
   }
-  const double rd = 1.0 / sqrt(sd / (double)d + (double)eps);
-  const float r = (float)rd, rlo = (float)(rd - (double)r);
+  const double r = 1.0 / sqrt(sd / (double)d + (double)eps);
 #pragma unroll
   for (int i = 0; i < NC; i++) {
     const int c = t + NT * i;
 #pragma unroll
     for (int e = 0; e < 8; e++) {
-      const float p = v[i][e] * r, q = fmaf(v[i][e], r, -p) + v[i][e] * rlo;
-      const float a = p * gn[i][e], lo = fmaf(p, gn[i][e], -a) + q * gn[i][e];
-      float y = a;
-      if (abs_bits(a) < 0x7f800000u) {  // (an infinite product has no remainder)
-        y = a + lo;
-        const float rem = lo - (y - a);
-        uint32_t u = __builtin_bit_cast(uint32_t, y);
-        if (rem != 0.f && (u & 1) == 0) u += (rem < 0.f) == (y < 0.f) ? 1u : -1u;
-        y = __builtin_bit_cast(float, u);
-      }
+      // (converted here: with two pieces the float64s, made earlier, took the
+      // registers of a second block on the CU, 4096 x 16384 bf16 119 us)
+      if constexpr (NC > 1) asm volatile("" : "+v"(v[i][e]), "+v"(gn[i][e]));
+      const uint64_t u = __builtin_bit_cast(uint64_t, (double)v[i][e] * r * (double)gn[i][e]);
+      constexpr uint32_t kBelow = 0x1fffffffu;  // the bits behind a float32's last
+      const uint32_t lo = ((uint32_t)u | (((uint32_t)u & kBelow) + kBelow)) & ~kBelow;
+      const float y = (float)__builtin_bit_cast(double, (u & 0xffffffff00000000ull) | lo);
       v[i][e] = c < nchunks ? y : 0.f;  // (zero times a NaN or infinite root is NaN)
     }
     mx_store8<FMT>(v[i], c, kcols, ns, codes + row * (FMT == LMGC_MX_FP8 ? kcols : kcols / 2), scales + row * ns);
