@@ -220,6 +220,9 @@ int lmgc_op_kv8_append(const uint16_t* d_k, const uint16_t* d_v, int32_t B, int3
   const int64_t nk = (int64_t)B * Hkv * T * hd * 2;
   if (in_cache(d_k, nk, B, Hkv, hd, cap, d_kc, d_ks, d_vc, d_vs) || in_cache(d_v, nk, B, Hkv, hd, cap, d_kc, d_ks, d_vc, d_vs))
     return set_error(LMGC_EINVAL, "d_k or d_v overlaps the cache");
+  for (const int32_t* p : {d_lens, d_counts})
+    if (in_cache(p, (int64_t)B * 4, B, Hkv, hd, cap, d_kc, d_ks, d_vc, d_vs))
+      return set_error(LMGC_EINVAL, "d_lens or d_counts overlaps the cache");
   return done(launch_kv8_append(d_k, d_v, B, Hkv, T, hd, cap, d_lens, d_counts, d_kc, d_ks, d_vc, d_vs, (hipStream_t)stream),
               "append");
 }
@@ -254,6 +257,9 @@ int lmgc_op_attention_kv8(const uint16_t* d_q, int32_t B, int32_t Hq, int32_t Hk
   if (overlap(d_q, nq, d_out, nq) || overlap(d_ws, need, d_q, nq) || overlap(d_ws, need, d_out, nq) ||
       in_cache(d_out, nq, B, Hkv, hd, cap, d_kc, d_ks, d_vc, d_vs) || in_cache(d_ws, need, B, Hkv, hd, cap, d_kc, d_ks, d_vc, d_vs))
     return set_error(LMGC_EINVAL, "buffers overlap");
+  for (const int32_t* p : {d_lens, d_counts})
+    if (overlap(p, (int64_t)B * 4, d_out, nq) || overlap(p, (int64_t)B * 4, d_ws, need))
+      return set_error(LMGC_EINVAL, "d_lens or d_counts overlaps what the call writes");
   return done(launch_attention_kv8(d_q, B, Hq, Hkv, T, hd, cap, d_lens, d_counts, d_kc, d_ks, d_vc, d_vs, window, sinks,
                                    d_ws, d_out, (hipStream_t)stream), "attention");
 }

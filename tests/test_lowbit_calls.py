@@ -75,3 +75,22 @@ def test_attention_windows_and_sinks_past_32_bits(monkeypatch, given, taken):
     not cut to its low bits; what is negative stays so (and is refused)."""
     assert _attention_args(monkeypatch, window=given)[-6:-4] == (taken, 0)
     assert _attention_args(monkeypatch, sinks=given)[-6:-4] == (0, taken)
+
+
+def test_lengths_inside_what_a_call_writes_are_refused():
+    """lens and counts are read while the call runs: not in its output, its
+    workspace or (for an append) the cache."""
+    lib, at = B.lib(), [0x10000000 + (i << 24) for i in range(12)]
+    kc, ks, vc, vs, q, out, ws, k, v = at[1:10]
+    Bn, Hq, Hkv, T, hd, cap = 4, 4, 2, 1, 64, 4096
+    need = B.kv8_workspace(Bn, Hq, Hkv, T, hd, cap)
+
+    def attention(lens, counts=None):
+        return lib.lmgc_op_attention_kv8(q, Bn, Hq, Hkv, T, hd, cap, lens, counts, kc, ks, vc, vs, 0, 0, out, ws, need, None)
+
+    def append(lens, counts=None):
+        return lib.lmgc_op_kv8_append(k, v, Bn, Hkv, T, hd, cap, lens, counts, kc, ks, vc, vs, None)
+    for buffer in (out, out + Bn * T * Hq * hd * 2 - 4, ws, ws + need - 4):
+        assert attention(buffer) == EINVAL and attention(at[0], buffer) == EINVAL
+    for buffer in (kc, kc - 12, ks, vc + 256, vs + 4 * Bn * Hkv * (cap // 64) - 4):
+        assert append(buffer) == EINVAL and append(at[0], buffer) == EINVAL
