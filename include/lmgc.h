@@ -500,8 +500,11 @@ int lmgc_op_attention_bf16(const uint16_t* d_q, const uint16_t* d_k, const uint1
  * e4m3 (LMGC_MX_FP8, one byte) or e2m1 (LMGC_MX_FP4, two to a byte, the first
  * in the low half) number.  The scale is the smallest power of two, 2^-127 at
  * least, with |v| <= 448 s (6 s) for every v of the block, so nothing
- * saturates; codes are v / s rounded to nearest even.  A block that holds a
- * NaN or an infinity gets the scale byte 255 and reads as NaN as a whole.
+ * saturates; codes are v / s rounded to nearest even.  (The formats' text has a
+ * conversion with s = 2^(floor(log2 max|v|) - 8) (- 2) that clamps instead:
+ * codes and scales of either kind read right here, but a block whose largest
+ * value is above 448 / 256 (6 / 4) of its power of two gets twice that s from
+ * these calls.)  A block that holds a NaN or an infinity gets the scale byte 255 and reads as NaN as a whole.
  * Rows layout: with Kp = cols rounded up to 128, codes [rows, Kp] bytes
  * (FP8) or [rows, Kp / 2] (FP4), zero behind the last column; scales [rows,
  * 16 ceil(cols / 512)] bytes, block j at byte 16 (j / 16) + 4 (j % 4) +

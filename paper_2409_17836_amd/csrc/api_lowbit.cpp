@@ -32,9 +32,7 @@ int check_ld(int64_t rows, int64_t cols, int64_t ld) {
   return LMGC_OK;
 }
 
-int64_t kcols(int64_t cols) { return (cols + 127) / 128 * 128; }
-int64_t row_scales(int64_t cols) { return (cols + 511) / 512 * 16; }
-int64_t code_bytes(int32_t fmt, int64_t rows, int64_t cols) { return rows * (fmt == LMGC_MX_FP8 ? kcols(cols) : kcols(cols) / 2); }
+int64_t code_bytes(int32_t fmt, int64_t rows, int64_t cols) { return rows * (fmt == LMGC_MX_FP8 ? mx_cols(cols) : mx_cols(cols) / 2); }
 
 int done(hipError_t e, const char* what) {
   if (e != hipSuccess) return set_error(LMGC_EDEVICE, "%s launch: %s", what, hipGetErrorString(e));
@@ -80,7 +78,7 @@ int64_t lmgc_mx_code_bytes(int32_t fmt, int64_t rows, int64_t cols) {
 int64_t lmgc_mx_scale_bytes(int64_t rows, int64_t cols) {
   clear_error();
   int rc = check_shape(rows, cols);
-  return rc ? rc : rows * row_scales(cols);
+  return rc ? rc : rows * mx_row_scales(cols);
 }
 
 int64_t lmgc_mx_block_code_bytes(int64_t rows, int64_t cols) {
@@ -92,7 +90,7 @@ int64_t lmgc_mx_block_code_bytes(int64_t rows, int64_t cols) {
 int64_t lmgc_mx_block_scale_bytes(int64_t rows, int64_t cols) {
   clear_error();
   int rc = check_shape(rows, cols);
-  return rc ? rc : (rows + 15) / 16 * 16 * row_scales(cols);
+  return rc ? rc : (rows + 15) / 16 * 16 * mx_row_scales(cols);
 }
 
 int lmgc_op_mx_quantize(const void* d_src, int32_t dtype, int64_t rows, int64_t cols, int64_t ld, int32_t fmt,
@@ -107,7 +105,7 @@ int lmgc_op_mx_quantize(const void* d_src, int32_t dtype, int64_t rows, int64_t 
   if (!d_src || !d_codes || !d_scales) return set_error(LMGC_EINVAL, "NULL device buffer");
   if ((uintptr_t)d_src % dtype_bytes(dtype) || !aligned(d_codes) || !aligned(d_scales))
     return set_error(LMGC_EINVAL, "codes and scales must be 16-byte aligned, the source aligned to its elements");
-  const int64_t nsrc = ((rows - 1) * ld + cols) * dtype_bytes(dtype), nc = code_bytes(fmt, rows, cols), ns = rows * row_scales(cols);
+  const int64_t nsrc = ((rows - 1) * ld + cols) * dtype_bytes(dtype), nc = code_bytes(fmt, rows, cols), ns = rows * mx_row_scales(cols);
   if (overlap(d_src, nsrc, d_codes, nc) || overlap(d_src, nsrc, d_scales, ns) || overlap(d_codes, nc, d_scales, ns))
     return set_error(LMGC_EINVAL, "buffers overlap");
   return done(launch_mx_quantize(d_src, dtype, rows, (int)cols, ld, fmt, d_codes, d_scales, (hipStream_t)stream), "mx quantize");
@@ -126,7 +124,7 @@ int lmgc_op_mx_dequantize(const uint8_t* d_codes, const uint8_t* d_scales, int32
   if ((uintptr_t)d_out % dtype_bytes(dtype) || !aligned(d_codes) || !aligned(d_scales))
     return set_error(LMGC_EINVAL, "codes and scales must be 16-byte aligned, the output aligned to its elements");
   const int64_t nout = ((rows - 1) * ld + cols) * dtype_bytes(dtype);
-  if (overlap(d_out, nout, d_codes, code_bytes(fmt, rows, cols)) || overlap(d_out, nout, d_scales, rows * row_scales(cols)))
+  if (overlap(d_out, nout, d_codes, code_bytes(fmt, rows, cols)) || overlap(d_out, nout, d_scales, rows * mx_row_scales(cols)))
     return set_error(LMGC_EINVAL, "buffers overlap");
   return done(launch_mx_dequantize(d_codes, d_scales, fmt, rows, (int)cols, d_out, dtype, ld, (hipStream_t)stream), "mx dequantize");
 }
@@ -140,8 +138,8 @@ int lmgc_op_mx_block(const uint8_t* d_codes, const uint8_t* d_scales, int64_t N,
   if (!d_codes || !d_scales || !d_block_codes || !d_block_scales) return set_error(LMGC_EINVAL, "NULL device buffer");
   if (!aligned(d_codes) || !aligned(d_scales) || !aligned(d_block_codes) || !aligned(d_block_scales))
     return set_error(LMGC_EINVAL, "pointers must be 16-byte aligned");
-  const int64_t nc = code_bytes(LMGC_MX_FP4, N, K), ns = N * row_scales(K), n16 = (N + 15) / 16 * 16;
-  const int64_t bc = code_bytes(LMGC_MX_FP4, n16, K), bs = n16 * row_scales(K);
+  const int64_t nc = code_bytes(LMGC_MX_FP4, N, K), ns = N * mx_row_scales(K), n16 = (N + 15) / 16 * 16;
+  const int64_t bc = code_bytes(LMGC_MX_FP4, n16, K), bs = n16 * mx_row_scales(K);
   if (overlap(d_codes, nc, d_block_codes, bc) || overlap(d_codes, nc, d_block_scales, bs) ||
       overlap(d_scales, ns, d_block_codes, bc) || overlap(d_scales, ns, d_block_scales, bs) ||
       overlap(d_block_codes, bc, d_block_scales, bs))
@@ -165,7 +163,7 @@ int lmgc_op_add_norm_mx(const void* d_h, int32_t h_dtype, const void* d_x, int32
     return set_error(LMGC_EINVAL, "pointers must be 16-byte aligned");
   const int64_t nh = M * d * dtype_bytes(h_dtype), nx = d_x ? M * d * dtype_bytes(x_dtype) : 0, ng = d * dtype_bytes(g_dtype);
   const void* w[3] = {d_out == d_h ? nullptr : d_out, d_codes, d_scales};
-  const int64_t nw[3] = {nh, code_bytes(fmt, M, d), M * row_scales(d)};
+  const int64_t nw[3] = {nh, code_bytes(fmt, M, d), M * mx_row_scales(d)};
   for (int i = 0; i < 3; i++)
     if (overlap(w[i], nw[i], d_h, nh) || overlap(w[i], nw[i], d_x, nx) || overlap(w[i], nw[i], d_gain, ng) ||
         overlap(w[i], nw[i], w[(i + 1) % 3], nw[(i + 1) % 3]))
@@ -202,8 +200,8 @@ int lmgc_op_gemm_mx_tile(const uint8_t* d_a, const uint8_t* d_a_scales, int32_t 
     return set_error(LMGC_EINVAL, "d_add overlaps d_out without being equal to it");
   if (d_add && (const void*)d_add == d_out && kind != LMGC_OP_STORE)
     return set_error(LMGC_EINVAL, "d_add may be d_out only for a float32 result");
-  if (overlap(d_out, nout, d_a, code_bytes(a_fmt, M, K)) || overlap(d_out, nout, d_a_scales, M * row_scales(K)) ||
-      overlap(d_out, nout, d_b, code_bytes(LMGC_MX_FP4, n16, K)) || overlap(d_out, nout, d_b_scales, n16 * row_scales(K)))
+  if (overlap(d_out, nout, d_a, code_bytes(a_fmt, M, K)) || overlap(d_out, nout, d_a_scales, M * mx_row_scales(K)) ||
+      overlap(d_out, nout, d_b, code_bytes(LMGC_MX_FP4, n16, K)) || overlap(d_out, nout, d_b_scales, n16 * mx_row_scales(K)))
     return set_error(LMGC_EINVAL, "d_out overlaps an operand");
   return done(launch_gemm_mx(d_a, d_a_scales, a_fmt, d_b, d_b_scales, M, N, K, d_add, d_out, kind == LMGC_OP_STORE_BF16,
                              tile, (hipStream_t)stream), "gemm");

@@ -6,6 +6,11 @@
 
 namespace lmgc {
 
+// Columns of codes in a row (a whole number of 128-wide matrix steps) and
+// bytes of scales in a row (whole groups of 512 columns).
+__host__ __device__ inline int64_t mx_cols(int64_t cols) { return (cols + 127) / 128 * 128; }
+__host__ __device__ inline int64_t mx_row_scales(int64_t cols) { return (cols + 511) / 512 * 16; }
+
 // Microscaled operands (mx.hip, gemm_mx.hip) and the 8-bit key/value cache
 // (kv8.hip); arguments as in lmgc.h, checked by the callers.
 hipError_t launch_mx_quantize(const void* src, int dtype, int64_t rows, int cols, int64_t ld, int fmt, uint8_t* codes,

@@ -15,10 +15,6 @@ typedef uint32_t mx_u32x4 __attribute__((ext_vector_type(4)));
 typedef uint32_t mx_u32x2 __attribute__((ext_vector_type(2)));
 typedef float mx_f32x4 __attribute__((ext_vector_type(4)));
 
-// Columns of codes in a row (a whole number of 128-wide matrix steps) and
-// bytes of scales in a row (whole groups of 512 columns).
-__host__ __device__ inline int64_t mx_cols(int64_t cols) { return (cols + 127) / 128 * 128; }
-__host__ __device__ inline int64_t mx_row_scales(int64_t cols) { return (cols + 511) / 512 * 16; }
 // Where the scale of block j of a row sits: a lane of the 16x16x128 matrix
 // instruction takes the scale of block 4 s + g at step s, so the four steps
 // of a 512-column group are the bytes of one 32-bit word.

@@ -98,7 +98,7 @@ __global__ __launch_bounds__(256) void mx_dequantize_kernel(const uint8_t* __res
 }
 
 // ------------------------------------------------------------------ blocks
-// Row-major 4-bit codes and scales -> blocks (common.h): thread t moves the
+// Row-major 4-bit codes and scales -> blocks (lmgc.h): thread t moves the
 // 16-byte piece (32 columns of a row) that is piece t of the blocks, and the
 // threads whose piece opens a 512-column group its word of scales.  Writes are
 // in order, a wave 1 KB; reads are 16 rows' 64 bytes.  22016 x 4096 19 us.

@@ -94,3 +94,11 @@ def test_lengths_inside_what_a_call_writes_are_refused():
         assert attention(buffer) == EINVAL and attention(at[0], buffer) == EINVAL
     for buffer in (kc, kc - 12, ks, vc + 256, vs + 4 * Bn * Hkv * (cap // 64) - 4):
         assert append(buffer) == EINVAL and append(at[0], buffer) == EINVAL
+
+
+@pytest.mark.parametrize("fmt", ["fp8", "fp4"])
+def test_binding_sizes_are_the_library_s(fmt):
+    for rows, cols in ((1, 1), (3, 127), (5, 128), (7, 129), (2, 512), (9, 513), (4, 11008), (1, 1 << 20)):
+        nc, ns = B._mx_sizes(rows, cols, fmt)
+        assert rows * nc == B.lib().lmgc_mx_code_bytes(B.MX_FORMATS[fmt], rows, cols)
+        assert rows * ns == B.lib().lmgc_mx_scale_bytes(rows, cols)
