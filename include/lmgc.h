@@ -633,7 +633,10 @@ int lmgc_op_kv8_append(const uint16_t* d_k, const uint16_t* d_v, int32_t B, int3
  * value code 0x7f or 0xff of a token that some query sees, written otherwise,
  * makes its dim NaN for queries near it that do not see it, too.)  Scales are
  * powers of two, 2^-64 or more as appending leaves them; scales and queries
- * above 2^100 (keys and values of 5e32) may overflow in the sums.  A
+ * above 2^100 (keys and values of 5e32) may overflow in the sums.  The
+ * probabilities are rounded to bf16 (2^-8 at most of each) for their product
+ * with the values, and divided by the sum of the rounded ones; scores, maxima
+ * and sums are float32.  A
  * query's result depends on the cache and its position, and on cap, T, Hq, Hkv
  * (which say how the work is split), not on the other sequences or queries.
  * T Hq / Hkv <= 2^30; above 32, B Hkv ceil(T Hq / Hkv / 256) < 2^23, times the

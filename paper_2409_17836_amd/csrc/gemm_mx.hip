@@ -142,7 +142,8 @@ __device__ inline void store_rows(const float* src, int64_t at, int rows, int nc
 // 2.7 to 2.9 PFLOP/s from one machine to the next, in e2m1 470 to 495, 3.4
 // (instructions alone, from registers: 4.9 and 5.2; an 8-bit library product of
 // 8192^3 2.7); middle ones by a stage's round, waits and barrier included:
-// 1000 x 2048 x 5632 in e2m1 12 us, 0.27 a step.
+// 1000 x 2048 x 5632 in e2m1 12 us from a graph, 14 to 16 with everything from
+// memory, 0.27 a step.
 //
 // ONCE, a single row of tiles: nothing reads the weights again before the next
 // step, so they are loaded past the caches' order of use (64 x 22016 x 4096
@@ -388,10 +389,11 @@ __global__ __launch_bounds__(WM * WN * 64, 1) void gemm_mx_tile_kernel(
 // instruction's registers.  D steps are under way: step k's operands are used
 // and the loads of step k + D go into their registers.  Bound by the latency
 // of memory and then by the bytes of the weights, and with 16 rows by the rows
-// of A that every tile fetches, hence wider tiles for more columns.  1 x 4096 x
-// 4096 3.2 us, 16 x 4096 x 11008 8.7 us, 1 x 22016 x 4096 8.6 us (5.6 TB/s);
-// with the operands through LDS, whose latency was a step's time, 5.7, 11.5
-// and 10.4.
+// of A that every tile fetches, hence wider tiles for more columns.  One matrix
+// of weights again and again (out of the Infinity Cache) 1 x 4096 x 4096 3.2 us,
+// 16 x 4096 x 11008 8.7 us, 1 x 22016 x 4096 8.6 us; with the operands through
+// LDS, whose latency was a step's time, 5.7, 11.5 and 10.4.  Weights from memory
+// 3.6, 9.9 and 10.3 us (4.6 TB/s).
 template <int FMT, int FN, int D, bool ONCE>
 __global__ __launch_bounds__(64) void gemm_mx_rows_kernel(const uint8_t* __restrict__ A, const uint8_t* __restrict__ As,
                                                           const uint8_t* __restrict__ B, const uint8_t* __restrict__ Bs,

@@ -241,7 +241,9 @@ __device__ inline __amdgpu_buffer_rsrc_t block_buffer(const uint8_t* codes, int6
 // the form for many columns as long as the sequences do not fill the chip.  12
 // heads of 64, 1000 queries from the start: 9.9 us (the other form 29.5), 4
 // such sequences 27 (31), 8 of them 47 (42); 32 heads on 8 of 128, 50 queries
-// over 3900 tokens: 19 us (31), 4 of them 46 (37).
+// over 3900 tokens: 19 us (31), 4 of them 46 (37).  So the limits are those of a
+// sequence by itself, and several in one call lose some of it: the choice may
+// not go by their number, or a sequence's bits would.
 //
 // Grid: (splits, tiles of 16 columns x Hkv, B), 512 threads.  A cache of up to
 // kOneBytes is one split (and the call one launch), a longer one is cut into
@@ -254,7 +256,7 @@ __device__ inline __amdgpu_buffer_rsrc_t block_buffer(const uint8_t* codes, int6
 // bf16, exponentials), and with few tokens by a chain of dependent loads (5.9 us
 // for 512 + 4 of them).  ONCE, a single tile of columns: nothing reads the codes
 // again before the next step, so they are loaded past the caches' order of use.
-// From memory, 8 sequences x 32 heads of 128 over 4094 tokens, 268 MB: 49 us,
+// From memory, 8 sequences x 32 heads of 128 over 4094 tokens, 268 MB: 48 to 49 us,
 // 5.5 TB/s (55 without ONCE); 32 sequences 170 us, 6.2 TB/s (187); one sequence
 // 11.6 us (12.5).  With two tiles the second one misses them (23.7 us for 21.7
 // at 8 x 8 heads, 32 columns over 2000).
@@ -482,8 +484,8 @@ __global__ __launch_bounds__(64) void attn_kv8_join_kernel(const float* __restri
 // delay them (64 products took 2000 cycles by themselves and 2900 with 110
 // vector instructions among them), and with both waves in the same phase a
 // step took 5500 cycles.  Bound by the two units' turns: 2 x 32 heads of 128 on
-// 8 key/value heads, 3001 queries behind 1000 tokens, 229 to 239 us, 1.02 to
-// 1.06 PFLOP/s (a bf16 library product of 8192^3 reaches 1.45).
+// 8 key/value heads, 3001 queries behind 1000 tokens, 232 to 242 us, 1.01 to
+// 1.05 PFLOP/s (a bf16 library product of 8192^3 reaches 1.40 to 1.45).
 //
 // The block scales cost nothing per score: the keys' goes into the exponent's
 // factor, the values' (a power of two) into its summand, and the row sums

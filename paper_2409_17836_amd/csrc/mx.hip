@@ -126,8 +126,9 @@ __global__ __launch_bounds__(256) void mx_block_kernel(const uint8_t* __restrict
 // -------------------------------------------------------- add and RMSNorm
 // NT threads per row: a wave up to 1024 columns, then 256 to 1024, so that a
 // thread has one piece of 8 columns (two past 8192) and the code stays short:
-// with 256 threads throughout, 8 x 4096 took 4.7 us (now 3.8) and 32768 x 4096
-// 267 us (now 259, 5.7 TB/s).  Thread t keeps columns 8 (t + NT i) .. + 7 in
+// with 256 threads throughout, 8 x 4096 took 0.9 us more and 32768 x 4096 8 us
+// more.  From a graph 8 x 4096 takes 4.2 us, 32768 x 4096 from float32 259 (5.7
+// TB/s), from bf16 to e2m1 182 (4.8).  Thread t keeps columns 8 (t + NT i) .. + 7 in
 // registers between the sum of squares and the codes, so a row is read once.
 // The sum that is normalised is the one that is stored.
 //
