@@ -504,7 +504,8 @@ int lmgc_op_attention_bf16(const uint16_t* d_q, const uint16_t* d_k, const uint1
  * conversion with s = 2^(floor(log2 max|v|) - 8) (- 2) that clamps instead:
  * codes and scales of either kind read right here, but a block whose largest
  * value is above 448 / 256 (6 / 4) of its power of two gets twice that s from
- * these calls.)  A block that holds a NaN or an infinity gets the scale byte 255 and reads as NaN as a whole.
+ * these calls.)  A block that holds a NaN or an infinity gets the scale byte 255
+ * and reads as NaN as a whole.
  * Rows layout: with Kp = cols rounded up to 128, codes [rows, Kp] bytes
  * (FP8) or [rows, Kp / 2] (FP4), zero behind the last column; scales [rows,
  * 16 ceil(cols / 512)] bytes, block j at byte 16 (j / 16) + 4 (j % 4) +
@@ -636,9 +637,9 @@ int lmgc_op_kv8_append(const uint16_t* d_k, const uint16_t* d_v, int32_t B, int3
  * above 2^100 (keys and values of 5e32) may overflow in the sums.  The
  * probabilities are rounded to bf16 (2^-8 at most of each) for their product
  * with the values, and divided by the sum of the rounded ones; scores, maxima
- * and sums are float32.  A
- * query's result depends on the cache and its position, and on cap, T, Hq, Hkv
- * (which say how the work is split), not on the other sequences or queries.
+ * and sums are float32.  A query's result depends on the cache and its position,
+ * and on cap, T, Hq, Hkv (which say how the work is split), not on the other
+ * sequences or queries.
  * T Hq / Hkv <= 2^30; above 32, B Hkv ceil(T Hq / Hkv / 256) < 2^23, times the
  * splits of the cache (16 at most).
  * GPU, async.  Errors: EINVAL, ESIZE, EUNSUPPORTED (hd, the limit above).
