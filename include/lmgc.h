@@ -651,6 +651,117 @@ int lmgc_op_attention_kv8(const uint16_t* d_q, int32_t B, int32_t Hq, int32_t Hk
                           const float* d_vs, int32_t window, int32_t sinks, uint16_t* d_out,
                           void* d_ws, size_t ws_bytes, void* stream);
 
+/* ------------------------------------- ragged batches over a paged cache */
+/*
+ * Rotary positions and a key/value cache in pages, for decoders that serve many
+ * windows of different lengths at once, or many behind one long prefix.  Beside
+ * lmgc_probs, whose windows are all of one length (Sec. 4: each is coded by
+ * itself from BOS).
+ *
+ * Rotary table: float32 [n_pos, rot / 2, 2], entry (p, i) = mscale (cos, sin)(p
+ * freqs[i]), angles in float64.  A head's pair i is rotated by it: (a, b) -> (a
+ * cos - b sin, a sin + b cos).  Pair i is dims (i, i + rot / 2) (LMGC_ROPE_HALF,
+ * the decoder's own) or (2 i, 2 i + 1) (LMGC_ROPE_INTERLEAVED); dims from rot on
+ * are left alone.
+ */
+enum { LMGC_ROPE_HALF = 0, LMGC_ROPE_INTERLEAVED = 1 };
+/* How frequencies theta^(-2 i / rot) are stretched by `factor` for contexts
+ * longer than the `orig` tokens of training: not at all; f / factor; theta
+ * factor^(rot / (rot - 2)) in theta's place (NTK-aware, rot >= 4); or by parts
+ * (YaRN, arXiv 2309.00071): with r = orig f / 2 pi turns and keep = clamp((r -
+ * slow) / (fast - slow), 0, 1), f keep + f / factor (1 - keep). */
+enum { LMGC_ROPE_PLAIN = 0, LMGC_ROPE_LINEAR = 1, LMGC_ROPE_NTK = 2, LMGC_ROPE_YARN = 3 };
+/* freqs: host, rot / 2 numbers.  rot even, in [2, 512].  Host.  Errors: EINVAL. */
+int lmgc_rope_frequencies(double theta, int32_t rot, int32_t scaling, double factor, double orig,
+                          double slow, double fast, double* freqs);
+/* Fills d_table from any frequencies (host, read before the call returns).
+ * 1 <= n_pos <= 2^24, d_table 16-byte aligned.  GPU, async.  Errors: EINVAL. */
+int lmgc_op_rope_table(const double* freqs, int32_t rot, double mscale, int64_t n_pos,
+                       float* d_table, void* stream);
+/*
+ * Rotates n rows of `heads` heads of hd (2 .. 512) dims (dtype LMGC_DTYPE_F32 or
+ * _BF16): row m is at position d_pos[m]; backward != 0: by the negative angle,
+ * which is the transpose, and so the gradient.  Rows are ldx, heads ldhx numbers
+ * apart (either the larger), those of the result ldo and ldho; d_out is d_x with
+ * the same strides (in place) or overlaps it nowhere.  float32 arithmetic, one
+ * rounding.  Rows whose position is outside [0, n_pos) are left as they were.
+ * Any alignment of the elements; 16-byte aligned rows, and rot a multiple of 16
+ * (bf16) or 8, go faster.  0 <= n <= 2^24.  GPU, async.  Errors: EINVAL.
+ */
+int lmgc_op_rope(const void* d_x, int32_t dtype, int64_t n, int32_t heads, int32_t hd, int64_t ldx,
+                 int64_t ldhx, const int32_t* d_pos, const float* d_table, int64_t n_pos,
+                 int32_t rot, int32_t layout, int32_t backward, void* d_out, int64_t ldo,
+                 int64_t ldho, void* stream);
+
+/*
+ * Paged key/value cache of one layer: d_kc and d_vc, bf16 [n_pages, Hkv, page,
+ * hd] each, page 32, 64, 128 or 256 tokens, hd 64 or 128.  A page of a head is
+ * page / 32 groups of 32 tokens of 32 hd numbers; in a group key (t, d) is at
+ *   ((t/16) (hd/32) + d/32) 512 + ((t%16) + 16 ((d%32)/8)) 8 + d%8
+ * and value (t, d) at
+ *   (d/16) 512 + ((d%16) + 16 ((t%16)/4)) 8 + 4 (t/16) + t%4.
+ * What the places behind a sequence's last token hold does not matter.
+ *
+ * Batch: B sequences in n rows.  Sequence b's new tokens are rows d_starts[b] ..
+ * d_starts[b + 1] - 1 (d_starts [B + 1], not falling), at positions d_lens[b] ..
+ * (d_lens [B]: its tokens before them); token p of it is token p % page of page
+ * d_pages[b, p / page] (d_pages [B, max_pages]).  All three are device memory,
+ * read when the call runs.  Left out, and left as they were: rows that belong to
+ * no sequence, rows that pass max_pages page tokens, sequences whose rows are
+ * not within [0, n) or whose length is not within [0, max_pages page), and the
+ * tokens of pages outside [0, n_pages).  Sequences may have pages in common as
+ * long as no call appends to them.
+ *
+ * Appending stores k and v (dtype, rows of Hkv hd numbers, ldk and ldv apart) as
+ * bf16, k rotated by d_table (NULL: as it is); rows behind the table's end are
+ * left out, too.  d_q (NULL: none; rows of Hq hd numbers of the same dtype, ldq
+ * apart): rotated as well, into d_q_out (bf16, rows ldqo apart), which overlaps
+ * nothing.  Each number is rounded once.
+ * 0 <= n <= 2^24, B <= 65535, max_pages page <= 2^24; pools and table 16-byte
+ * aligned; rows of k, v and q that are, with rot a multiple of 16, go faster.
+ * GPU, async; no workspace.  Errors: EINVAL, EUNSUPPORTED (hd, page).
+ */
+int lmgc_op_paged_append(const void* d_k, const void* d_v, int32_t dtype, int64_t ldk, int64_t ldv,
+                         int32_t n, int32_t B, int32_t Hkv, int32_t hd, uint16_t* d_kc,
+                         uint16_t* d_vc, int32_t n_pages, int32_t page, const int32_t* d_pages,
+                         int32_t max_pages, const int32_t* d_starts, const int32_t* d_lens,
+                         const float* d_table, int64_t n_pos, int32_t rot, int32_t layout,
+                         const void* d_q, int64_t ldq, int32_t Hq, uint16_t* d_q_out, int64_t ldqo,
+                         void* stream);
+
+/*
+ * Attention of the tokens just appended (same batch) over the cache: softmax(
+ * scale q.k) v over keys j <= position and, if window > 0, j > position - window
+ * or j < sinks.  Query head h reads key/value head h Hkv / Hq.
+ *   d_q: bf16, rows of Hq hd numbers ldq apart, 16-byte aligned; d_out: bf16 [n,
+ *   Hq hd].  scale > 0 (1 / sqrt(hd), as a rule).
+ *   max_new: no sequence has more new tokens (rows behind that are left out).
+ *   shared: the first `shared` tokens of all sequences are the same, and each
+ *   sequence's pages say so (by pages in common, or by copies); they are read
+ *   and multiplied once for the batch, from the pages of sequence 0.  0: none.
+ *   d_ws: lmgc_paged_workspace bytes (with tokens = max_pages page), 16-byte
+ *   aligned, its contents free; calls that may run at the same time need one each.
+ * Masked keys count for nothing, whatever they and their values hold (NaN and
+ * infinities too); visible ones that are not finite do as in the formula.  A
+ * query that sees no key (its pages are outside the pool) gets zeros.
+ * Probabilities are rounded to bf16 (2^-8 of each at most) for their product with the
+ * values and divided by the sum of the rounded ones; scores, maxima and sums are
+ * float32.  A query's result depends on its own sequence (length and number of
+ * new tokens), max_new, Hq and Hkv, not on the other sequences; with shared > 0
+ * on n and B, too, which say how the shared part is split.
+ * GPU, async.  Errors: EINVAL, ESIZE, EUNSUPPORTED (hd, page, more than 2^32
+ * threads).
+ */
+int64_t lmgc_paged_workspace(int32_t n, int32_t B, int32_t Hq, int32_t Hkv, int32_t hd,
+                             int32_t max_new, int32_t tokens, int32_t shared);
+int lmgc_op_attention_paged(const uint16_t* d_q, int64_t ldq, int32_t n, int32_t B, int32_t Hq,
+                            int32_t Hkv, int32_t hd, const uint16_t* d_kc, const uint16_t* d_vc,
+                            int32_t n_pages, int32_t page, const int32_t* d_pages,
+                            int32_t max_pages, const int32_t* d_starts, const int32_t* d_lens,
+                            int32_t max_new, int32_t window, int32_t sinks, int32_t shared,
+                            float scale, uint16_t* d_out, void* d_ws, size_t ws_bytes,
+                            void* stream);
+
 /* ------------------------------------------------------------------ timing */
 /*
  * Per-kernel timing with HIP events recorded around each launch lmgc_probs

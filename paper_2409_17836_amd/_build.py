@@ -11,7 +11,8 @@ LIB = os.path.join(HERE, "liblmgc.so")
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 
 SOURCES = ["serialize.hip", "lossy.hip", "elementwise.hip", "gemm_bf16.hip", "gemm_bf16_tiles.hip", "gemm_f32.hip",
-           "attention.hip", "mx.hip", "gemm_mx.hip", "kv8.hip", "coder.cpp", "api.cpp", "api_lowbit.cpp"]
+           "attention.hip", "mx.hip", "gemm_mx.hip", "kv8.hip", "rope.hip", "paged.hip", "coder.cpp",
+           "api.cpp", "api_lowbit.cpp", "api_paged.cpp"]
 
 FLAGS = [
     "-O3", "--offload-arch=gfx950", "-std=c++17", "-fPIC",

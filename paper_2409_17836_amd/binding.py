@@ -65,7 +65,7 @@ def lib():
     L = ctypes.CDLL(LIB_PATH)
     vp, i32, i64, u32, u64, sz = (ctypes.c_void_p, ctypes.c_int32, ctypes.c_int64,
                                   ctypes.c_uint32, ctypes.c_uint64, ctypes.c_size_t)
-    P = ctypes.POINTER
+    P, f64 = ctypes.POINTER, ctypes.c_double
     sig = {
         "lmgc_last_error": (ctypes.c_char_p, []),
         "lmgc_version": (ctypes.c_char_p, []),
@@ -122,6 +122,14 @@ def lib():
         "lmgc_kv8_workspace": (i64, [i32, i32, i32, i32, i32, i32]),
         "lmgc_op_attention_kv8": (ctypes.c_int, [vp, i32, i32, i32, i32, i32, i32, vp, vp, vp, vp, vp, vp,
                                                  i32, i32, vp, vp, sz, vp]),
+        "lmgc_rope_frequencies": (ctypes.c_int, [f64, i32, i32, f64, f64, f64, f64, P(f64)]),
+        "lmgc_op_rope_table": (ctypes.c_int, [P(f64), i32, f64, i64, vp, vp]),
+        "lmgc_op_rope": (ctypes.c_int, [vp, i32, i64, i32, i32, i64, i64, vp, vp, i64, i32, i32, i32, vp, i64, i64, vp]),
+        "lmgc_op_paged_append": (ctypes.c_int, [vp, vp, i32, i64, i64, i32, i32, i32, i32, vp, vp, i32, i32, vp, i32,
+                                                vp, vp, vp, i64, i32, i32, vp, i64, i32, vp, i64, vp]),
+        "lmgc_paged_workspace": (i64, [i32, i32, i32, i32, i32, i32, i32, i32]),
+        "lmgc_op_attention_paged": (ctypes.c_int, [vp, i64, i32, i32, i32, i32, i32, vp, vp, i32, i32, vp, i32, vp, vp,
+                                                   i32, i32, i32, i32, ctypes.c_float, vp, vp, sz, vp]),
         "lmgc_timing_enable": (ctypes.c_int, [i32]),
         "lmgc_timing_kinds": (ctypes.c_int, [u32]),
         "lmgc_timing_read": (ctypes.c_int, [i32, P(ctypes.c_double), P(i64)]),
@@ -803,6 +811,162 @@ def op_attention_kv8(q, cache, lens, counts=None, window: int = 0, sinks: int = 
         window, sinks = max(-1, min(window, 2 ** 31 - 1)), max(-1, min(sinks, 2 ** 31 - 1))
     _check(lib().lmgc_op_attention_kv8(pq, B, Hq, Hkv, T, hd, cap, *rest, window, sinks, po, pw,
                                        ws.numel() * ws.element_size(), st))
+    return out
+
+
+# ----------------------------------------- ragged batches over a paged cache --
+ROPE_LAYOUTS = {"half": 0, "interleaved": 1}
+ROPE_SCALINGS = {"none": 0, "linear": 1, "ntk": 2, "yarn": 3}
+
+
+def rope_frequencies(rot: int, theta: float = 10000.0, scaling: str = "none", factor: float = 1.0, orig: float = 4096,
+                     slow: float = 1.0, fast: float = 32.0) -> np.ndarray:
+    """float64 [rot / 2]: the frequencies of lmgc_rope_frequencies."""
+    out = np.zeros(max(int(rot) // 2, 1), np.float64)
+    _check(lib().lmgc_rope_frequencies(float(theta), rot, ROPE_SCALINGS[scaling], float(factor), float(orig), float(slow),
+                                       float(fast), out.ctypes.data_as(ctypes.POINTER(ctypes.c_double))))
+    return out
+
+
+def rope_table(n_pos: int, rot: int, theta: float = 10000.0, scaling: str = "none", factor: float = 1.0, orig: float = 4096,
+               slow: float = 1.0, fast: float = 32.0, mscale: float = None, out=None, stream=None):
+    """(cos, sin) of positions 0 .. n_pos - 1: float32 CUDA tensor [n_pos, rot / 2,
+    2].  mscale multiplies both; YaRN's 0.1 ln(factor) + 1 with that scaling
+    unless given, else 1."""
+    import torch
+    f = rope_frequencies(rot, theta, scaling, factor, orig, slow, fast)
+    if mscale is None:
+        mscale = 0.1 * float(np.log(factor)) + 1.0 if scaling == "yarn" else 1.0
+    shape = (n_pos, rot // 2, 2)
+    if out is None:
+        if stream is None:
+            out = torch.empty(shape, dtype=torch.float32, device="cuda")
+        else:
+            with torch.cuda.stream(stream):
+                out = torch.empty(shape, dtype=torch.float32, device="cuda")
+    else:
+        assert out.dtype == torch.float32 and out.is_contiguous() and out.shape == shape
+    st, (po,) = _on(stream, out)
+    _check(lib().lmgc_op_rope_table(f.ctypes.data_as(ctypes.POINTER(ctypes.c_double)), rot, float(mscale), n_pos, po, st))
+    return out
+
+
+def _rope_check(table):
+    """Positions and dims of a table."""
+    import torch
+    assert table.dtype == torch.float32 and table.is_contiguous() and table.dim() == 3 and table.shape[2] == 2
+    return table.shape[0], 2 * table.shape[1]
+
+
+def op_rope(x, positions, table, layout: str = "half", backward: bool = False, out=None, stream=None):
+    """Rotates x [n, heads, hd] (float32 or bf16 CUDA tensor, any strides of rows
+    and heads) by the table's row of each position (CUDA int32 [n]); backward: the
+    transpose.  The result goes to `out` (x itself: in place; None: a new tensor,
+    whose rows at positions outside the table hold anything)."""
+    import torch
+    n, heads, hd = x.shape
+    n_pos, rot = _rope_check(table)
+    assert positions.dtype == torch.int32 and positions.is_contiguous() and positions.numel() == n
+    if out is None:
+        out = _empty((n, heads, hd), x.dtype, x, stream)
+    else:
+        assert out.dtype == x.dtype and out.shape == x.shape
+    assert x.stride(2) == 1 and out.stride(2) == 1
+    dt = _dtype(x)
+
+    def strides(t):  # of a single row or head: what a contiguous tensor has
+        h = t.stride(1) if heads > 1 else hd
+        return (t.stride(0) if n > 1 else heads * h), h
+    st, (px, pp, pt, po) = _on(stream, x, positions, table, out)
+    _check(lib().lmgc_op_rope(px, dt, n, heads, hd, *strides(x), pp, pt, n_pos, rot, ROPE_LAYOUTS[layout],
+                              int(backward), po, *strides(out), st))
+    return out
+
+
+def paged_cache(n_pages: int, Hkv: int, page: int, hd: int, device="cuda"):
+    """An empty paged key/value cache of one layer: (keys, values), bf16 [n_pages,
+    Hkv, page, hd] in the order of lmgc.h."""
+    import torch
+    return tuple(torch.zeros((n_pages, Hkv, page, hd), dtype=torch.bfloat16, device=device) for _ in range(2))
+
+
+def _paged_check(cache, pages, starts, lens, Hkv, hd):
+    """(n_pages, page, B, max_pages) of a cache and a batch, their tensors checked."""
+    import torch
+    kc, vc = cache
+    assert kc.dtype == vc.dtype == torch.bfloat16 and kc.shape == vc.shape and kc.is_contiguous() and vc.is_contiguous()
+    assert kc.dim() == 4 and kc.shape[1] == Hkv and kc.shape[3] == hd, (tuple(kc.shape), Hkv, hd)
+    B, most = pages.shape
+    for t, n in ((pages, B * most), (starts, B + 1), (lens, B)):
+        assert t.dtype == torch.int32 and t.is_contiguous() and t.numel() == n
+    return kc.shape[0], kc.shape[2], B, most
+
+
+def _row_stride(t):
+    """Numbers between rows of t [n, heads, hd], whose heads lie side by side."""
+    n, heads, hd = t.shape
+    assert t.stride(2) == 1 and (heads == 1 or t.stride(1) == hd), t.stride()
+    return t.stride(0) if n > 1 else heads * hd
+
+
+def op_paged_append(cache, k, v, pages, starts, lens, rope=None, layout: str = "half", q=None, q_out=None, stream=None):
+    """Stores k, v [n, Hkv, hd] (float32 or bf16, rows may be strided) of a ragged
+    batch (pages [B, max_pages], starts [B + 1], lens [B]: CUDA int32), k rotated
+    by the table `rope` if given.  q [n, Hq, hd]: rotated too, into q_out (a new
+    bf16 tensor, rows of no token left as they are, unless given), which is
+    returned."""
+    import torch
+    n, Hkv, hd = k.shape
+    n_pages, page, B, most = _paged_check(cache, pages, starts, lens, Hkv, hd)
+    assert v.shape == k.shape and v.dtype == k.dtype
+    n_pos, rot = _rope_check(rope) if rope is not None else (0, 0)
+    Hq, ldq, ldqo, ldk, ldv = 0, 0, 0, _row_stride(k), _row_stride(v)
+    if q is not None:
+        Hq = q.shape[1]
+        assert q.dtype == k.dtype and q.shape == (n, Hq, hd)
+        if q_out is None:
+            q_out = _empty((n, Hq, hd), torch.bfloat16, q, stream)
+        assert q_out.dtype == torch.bfloat16 and q_out.shape == q.shape
+        ldq, ldqo = _row_stride(q), _row_stride(q_out)
+    else:
+        assert q_out is None
+    st, (pk, pv, pq, pqo, pr, pp, ps, pl, pkc, pvc) = _on(stream, k, v, q, q_out, rope, pages, starts, lens, *cache)
+    _check(lib().lmgc_op_paged_append(pk, pv, _dtype(k), ldk, ldv, n, B, Hkv, hd, pkc, pvc, n_pages,
+                                      page, pp, most, ps, pl, pr, n_pos, rot, ROPE_LAYOUTS[layout], pq, ldq, Hq, pqo, ldqo, st))
+    return q_out
+
+
+def paged_workspace(n: int, B: int, Hq: int, Hkv: int, hd: int, max_new: int, tokens: int, shared: int = 0) -> int:
+    return _size(lib().lmgc_paged_workspace(n, B, Hq, Hkv, hd, max_new, tokens, shared))
+
+
+def op_attention_paged(q, cache, pages, starts, lens, max_new: int, window: int = 0, sinks: int = 0, shared: int = 0,
+                       scale: float = None, out=None, ws=None, stream=None):
+    """Attention of the tokens just appended over the paged cache: q bf16 [n, Hq,
+    hd] (rows may be strided) -> bf16 [n, Hq hd].  max_new: the most new tokens
+    that a sequence has; shared: leading tokens that all sequences have in common;
+    scale: 1 / sqrt(hd) unless given."""
+    import torch
+    n, Hq, hd = q.shape
+    Hkv = cache[0].shape[1]
+    n_pages, page, B, most = _paged_check(cache, pages, starts, lens, Hkv, hd)
+    assert q.dtype == torch.bfloat16
+    ldq = _row_stride(q)
+    if out is None:
+        out = _empty((n, Hq * hd), torch.bfloat16, q, stream)
+    else:
+        assert out.dtype == torch.bfloat16 and out.is_contiguous() and out.numel() == q.numel()
+    # (ctypes would keep the low 32 bits of a larger one)
+    max_new, window, sinks, shared = (max(-1, min(int(x), 2 ** 31 - 1)) for x in (max_new, window, sinks, shared))
+    if ws is None:
+        ws = _empty(paged_workspace(n, B, Hq, Hkv, hd, min(max_new, 1 << 24), most * page, shared), torch.uint8, q, stream)
+    else:
+        assert ws.is_contiguous()  # its bytes lie one behind the other
+    st, (pq, pkc, pvc, pp, ps, pl, po, pw) = _on(stream, q, *cache, pages, starts, lens, out, ws)
+    _check(lib().lmgc_op_attention_paged(pq, ldq, n, B, Hq, Hkv, hd, pkc, pvc, n_pages, page, pp, most, ps, pl,
+                                         min(max_new, 1 << 24), window, sinks, shared,
+                                         hd ** -0.5 if scale is None else float(scale), po, pw,
+                                         ws.numel() * ws.element_size(), st))
     return out
 
 

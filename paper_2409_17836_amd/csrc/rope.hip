@@ -1,0 +1,172 @@
+// Rotary positions: the table of angles, and the rotation of rows of heads.
+#include <math.h>
+
+#include <algorithm>
+#include <type_traits>
+
+#include "common.h"
+#include "paged.h"
+
+namespace lmgc {
+namespace {
+
+typedef float f32x2 __attribute__((ext_vector_type(2)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+
+// ------------------------------------------------------------------- table
+// table[p, i] = mscale (cos, sin)(p freqs[i]), angles and functions in float64:
+// at position 2^17 a float32 angle is off by 2^-7.
+struct Freqs {
+  double f[kMaxRot / 2];
+};
+
+__global__ __launch_bounds__(256) void rope_table_kernel(Freqs freqs, int half, double mscale, int64_t n, float2* __restrict__ table) {
+  const int64_t step = (int64_t)gridDim.x * 256;
+  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < n; i += step) {
+    const int64_t p = i / half;
+    double s, c;
+    sincos((double)p * freqs.f[i - p * half], &s, &c);
+    table[i] = make_float2((float)(c * mscale), (float)(s * mscale));
+  }
+}
+
+// ---------------------------------------------------------------- rotation
+// 16 bytes of a row to a run; a thread has the two runs of as many pairs, of
+// the same place in kHeads heads, so a pair's cos and sin are read once for them.
+template <class T>
+struct Run;
+template <>
+struct Run<float> {
+  static constexpr int n = 4;
+  f32x4 v;
+  __device__ inline float get(int i) const { return v[i]; }
+  __device__ inline void set(int i, float x) { v[i] = x; }
+};
+template <>
+struct Run<uint16_t> {
+  static constexpr int n = 8;
+  u32x4 v;
+  __device__ inline float get(int i) const { return __builtin_bit_cast(float, i & 1 ? v[i >> 1] & 0xffff0000u : v[i >> 1] << 16); }
+  __device__ inline void set(int i, float x) {
+    const uint32_t b = f32_to_bf16(x);
+    v[i >> 1] = i & 1 ? (v[i >> 1] & 0xffffu) | b << 16 : (v[i >> 1] & 0xffff0000u) | b;
+  }
+};
+
+__device__ inline float load1(const float* p) { return *p; }
+__device__ inline float load1(const uint16_t* p) { return bf16_to_f32(*p); }
+__device__ inline void store1(float* p, float x) { *p = x; }
+__device__ inline void store1(uint16_t* p, float x) { *p = f32_to_bf16(x); }
+
+// Grid: (blocks of rows, heads / kHeads), 256 threads: np places of a row side
+// by side.  FAST: rot a multiple of two runs, hd of a run, everything 16-byte
+// aligned.
+template <class T, bool FAST>
+__global__ __launch_bounds__(256) void rope_kernel(RopeArgs a, int np, int rows, int per) {
+  constexpr int R = Run<T>::n;
+  const int place = threadIdx.x % np, row = blockIdx.x * rows + threadIdx.x / np;
+  if ((int)threadIdx.x >= rows * np || row >= a.n) return;
+  const int64_t pos = a.pos[row];
+  if (pos < 0 || pos >= a.n_pos) return;
+  const int half = a.rot / 2, h0 = blockIdx.y * per, h1 = min(a.heads, h0 + per);
+  const float2* tab = reinterpret_cast<const float2*>(a.table) + pos * half;
+  const T* x = static_cast<const T*>(a.x) + row * a.ldx;
+  T* o = static_cast<T*>(a.out) + row * a.ldo;
+  const bool copy = a.x != a.out;  // (in place, what does not rotate stays)
+  if (FAST) {
+    const int nrot = half / R;
+    if (place < nrot) {
+      const int d0 = a.layout == LMGC_ROPE_HALF ? place * R : place * 2 * R, d1 = a.layout == LMGC_ROPE_HALF ? d0 + half : d0 + R;
+      float c[R], s[R];
+#pragma unroll
+      for (int i = 0; i < R; i += 2) {
+        const f32x4 w = *reinterpret_cast<const f32x4*>(tab + place * R + i);
+        c[i] = w[0], s[i] = a.backward ? -w[1] : w[1], c[i + 1] = w[2], s[i + 1] = a.backward ? -w[3] : w[3];
+      }
+      for (int h = h0; h < h1; h++) {
+        Run<T> u, v, y, z;
+        u.v = *reinterpret_cast<const decltype(u.v)*>(x + h * a.ldhx + d0);
+        v.v = *reinterpret_cast<const decltype(u.v)*>(x + h * a.ldhx + d1);
+        y.v = {};
+        z.v = {};
+        if (a.layout == LMGC_ROPE_HALF) {
+#pragma unroll
+          for (int i = 0; i < R; i++) {
+            const float p = u.get(i), q = v.get(i);
+            y.set(i, turn_first(p, q, c[i], s[i]));
+            z.set(i, turn_second(p, q, c[i], s[i]));
+          }
+        } else {
+#pragma unroll
+          for (int i = 0; i < R; i++) {
+            const float p = i < R / 2 ? u.get(2 * i) : v.get(2 * i - R), q = i < R / 2 ? u.get(2 * i + 1) : v.get(2 * i + 1 - R);
+            const float e = turn_first(p, q, c[i], s[i]), f = turn_second(p, q, c[i], s[i]);
+            if (i < R / 2) {
+              y.set(2 * i, e);
+              y.set(2 * i + 1, f);
+            } else {
+              z.set(2 * i - R, e);
+              z.set(2 * i + 1 - R, f);
+            }
+          }
+        }
+        *reinterpret_cast<decltype(u.v)*>(o + h * a.ldho + d0) = y.v;
+        *reinterpret_cast<decltype(u.v)*>(o + h * a.ldho + d1) = z.v;
+      }
+    } else if (copy) {
+      const int d0 = a.rot + (place - nrot) * 2 * R;
+      for (int h = h0; h < h1; h++)
+        for (int d = d0; d < min(a.hd, d0 + 2 * R); d += R)
+          *reinterpret_cast<decltype(Run<T>::v)*>(o + h * a.ldho + d) = *reinterpret_cast<const decltype(Run<T>::v)*>(x + h * a.ldhx + d);
+    }
+  } else {
+    // a pair, or two numbers that do not rotate
+    for (int i = place; i < (a.hd + 1) / 2; i += np)
+      for (int h = h0; h < h1; h++) {
+        const T* xh = x + h * a.ldhx;
+        T* oh = o + h * a.ldho;
+        if (i < half) {
+          const int d0 = a.layout == LMGC_ROPE_HALF ? i : 2 * i, d1 = a.layout == LMGC_ROPE_HALF ? i + half : 2 * i + 1;
+          const float c = tab[i].x, s = a.backward ? -tab[i].y : tab[i].y, p = load1(xh + d0), q = load1(xh + d1);
+          store1(oh + d0, turn_first(p, q, c, s));
+          store1(oh + d1, turn_second(p, q, c, s));
+        } else if (copy) {
+          for (int d = 2 * i; d < min(a.hd, 2 * i + 2); d++) oh[d] = xh[d];
+        }
+      }
+  }
+}
+
+}  // namespace
+
+hipError_t launch_rope_table(const double* freqs, int rot, double mscale, int64_t n_pos, float* table, hipStream_t s) {
+  Freqs f{};
+  for (int i = 0; i < rot / 2; i++) f.f[i] = freqs[i];
+  const int64_t n = n_pos * (rot / 2);
+  rope_table_kernel<<<(unsigned)std::min<int64_t>((n + 255) / 256, 1 << 20), 256, 0, s>>>(f, rot / 2, mscale, n, (float2*)table);
+  return hipGetLastError();
+}
+
+hipError_t launch_rope(const RopeArgs& a, hipStream_t s) {
+  auto go = [&](auto t) {
+    using T = decltype(t);
+    constexpr int R = Run<T>::n;
+    auto whole = [](int64_t x) { return x % R == 0; };
+    const bool fast = a.rot % (2 * R) == 0 && whole(a.hd) && whole(a.ldx) && whole(a.ldhx) && whole(a.ldo) && whole(a.ldho) &&
+                      ((uintptr_t)a.x & 15) == 0 && ((uintptr_t)a.out & 15) == 0;
+    const int np = fast ? a.rot / 2 / R + (a.hd - a.rot + 2 * R - 1) / (2 * R) : std::min((a.hd + 1) / 2, 64);
+    const int rows = 256 / np;
+    const int64_t blocks = ((int64_t)a.n + rows - 1) / rows;
+    int per = blocks * a.heads >= 4096 ? 4 : 1;
+    per = std::max(per, (a.heads + 65534) / 65535);
+    const dim3 grid((unsigned)blocks, (a.heads + per - 1) / per);
+    if (fast) rope_kernel<T, true><<<grid, 256, 0, s>>>(a, np, rows, per);
+    else rope_kernel<T, false><<<grid, 256, 0, s>>>(a, np, rows, per);
+  };
+  if (a.dtype == LMGC_DTYPE_BF16) go(uint16_t{});
+  else go(float{});
+  return hipGetLastError();
+}
+
+}  // namespace lmgc

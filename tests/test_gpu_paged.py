@@ -1,0 +1,461 @@
+"""The paged key/value cache and attention over it, with and without a prefix in
+common, against plain float64 references."""
+import numpy as np
+import pytest
+
+import paged_ref as R
+from gpu_util import log
+from paper_2409_17836_amd import binding as B
+
+pytestmark = pytest.mark.gpu
+
+
+def _torch():
+    import torch
+    return torch
+
+
+def _ints(v):
+    torch = _torch()
+    return torch.tensor(np.asarray(v).tolist(), dtype=torch.int32, device="cuda")
+
+
+def _np(t):
+    return t.double().cpu().numpy()
+
+
+class Setup:
+    """A batch of (new tokens, tokens before) over a pool of shuffled pages, whose every
+    place holds something."""
+
+    def __init__(self, seqs, page=64, Hkv=2, hd=64, seed=0, pad=0, shared=0, spare=2, extra_pages=0, stale=None):
+        torch = _torch()
+        g = np.random.default_rng(seed)
+        self.seqs, self.page, self.Hkv, self.hd = seqs, page, Hkv, hd
+        starts = np.concatenate([[0], np.cumsum([t for t, _ in seqs])])
+        self.n = int(starts[-1]) + pad
+        most = max(-(-(t + n) // page) for t, n in seqs) + extra_pages
+        lead = shared // page
+        n_pages = lead + sum(most - lead for _ in seqs) + spare
+        order = g.permutation(n_pages)
+        pages = np.array([np.concatenate([order[:lead], order[lead + i * (most - lead):lead + (i + 1) * (most - lead)]]) for i in range(len(seqs))])
+        self.n_pages = n_pages
+        gen = torch.Generator(device="cuda")
+        gen.manual_seed(seed + 1)
+        self.cache = tuple(torch.randn(n_pages, Hkv, page, hd, device="cuda", generator=gen).to(torch.bfloat16) for _ in range(2))
+        self.gen = gen
+        self.set(pages, starts, [n for _, n in seqs])
+        if stale is not None:  # what lies behind the tokens and on pages of no sequence
+            t = np.arange(page)
+            for i, pool in enumerate(self.cache):
+                plain = R.in_pool(np.arange(pool.numel()).reshape(pool.shape), bool(i))  # where each number is
+                hold = np.zeros((n_pages, page), bool)
+                for b, (T, n) in enumerate(seqs):
+                    for k in range(-(-(T + n) // page)):
+                        hold[pages[b, k]] |= t + k * page < T + n
+                at = plain.transpose(0, 2, 1, 3)[~hold].reshape(-1)
+                pool.view(-1)[torch.from_numpy(at).cuda()] = stale
+
+    def set(self, pages, starts, lens):
+        self.pages_h, self.starts_h, self.lens_h = np.asarray(pages), np.asarray(starts), np.asarray(lens)
+        self.pages, self.starts, self.lens = _ints(pages), _ints(starts), _ints(lens)
+        self.batch = R.Batch(self.pages_h, self.starts_h, self.lens_h, self.n, self.n_pages, self.page)
+        return self
+
+    def rows(self, heads, dtype="bfloat16"):
+        torch = _torch()
+        return torch.randn(self.n, heads, self.hd, device="cuda", generator=self.gen).to(getattr(torch, dtype))
+
+    def plain(self):
+        return [R.in_pool(_np(x), bool(i)) for i, x in enumerate(self.cache)]
+
+    @property
+    def max_new(self):
+        return max(t for t, _ in self.seqs)
+
+
+# -------------------------------------------------------------------- append
+def _append_check(s, k, v, q, table, layout, rot):
+    torch = _torch()
+    before = [x.clone() for x in s.cache]
+    q_out = torch.full((s.n, q.shape[1], s.hd), 3.0, dtype=torch.bfloat16, device="cuda") if q is not None else None
+    B.op_paged_append(s.cache, k, v, s.pages, s.starts, s.lens, rope=table, layout=layout, q=q, q_out=q_out)
+    want = [R.in_pool(_np(x), bool(i)) for i, x in enumerate(before)]
+    tol = [np.zeros_like(x) for x in want]
+    tab = _np(table) if table is not None else None
+    wq, tq = np.full((s.n, q.shape[1], s.hd), 3.0) if q is not None else None, None
+    tq = np.zeros_like(wq) if q is not None else None
+    kn, vn, qn = _np(k), _np(v), _np(q) if q is not None else None
+
+    def turned(x, pos):
+        if tab is None:
+            return x, 2.0 ** -8 * abs(x)
+        y, mag = R.rotate(x, tab[pos][None], layout)
+        return y, 2.0 ** -23 * mag + 2.0 ** -8 * abs(y) * (1 + 2.0 ** -8)  # float32, then one rounding to bf16
+    for b, row, pos in s.batch.rows():
+        if tab is not None and pos >= tab.shape[0]:
+            continue
+        page = s.pages_h[b, pos // s.page]
+        ky, kt = turned(kn[row], pos)
+        if 0 <= page < s.n_pages:
+            want[0][page, :, pos % s.page], tol[0][page, :, pos % s.page] = ky, kt
+            want[1][page, :, pos % s.page], tol[1][page, :, pos % s.page] = vn[row], 2.0 ** -8 * abs(vn[row])
+        if q is not None:
+            wq[row], tq[row] = turned(qn[row], pos)
+    for got, w, t, name in zip(s.plain(), want, tol, ("keys", "values")):
+        assert (abs(got - w) <= t).all(), name
+    if q is not None:
+        assert (abs(_np(q_out) - wq) <= tq).all()
+    return q_out
+
+
+BATCHES = [
+    [(1, 0)], [(1, 31)], [(1, 32), (1, 63)], [(5, 0), (1, 200), (70, 30), (3, 61)], [(64, 64)], [(33, 31)], [(130, 1), (1, 130)],
+    [(1, i) for i in range(0, 140, 7)], [(0, 5), (2, 0), (0, 0), (31, 1)], [(300, 17)]]
+
+
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
+@pytest.mark.parametrize("hd,page,layout,rot", [(64, 32, "half", 64), (64, 64, "interleaved", 32), (128, 128, "half", 128), (128, 32, "interleaved", 128),
+                                                (128, 64, "half", 16), (64, 256, "half", 10), (128, 64, "interleaved", 50), (64, 64, "none", 0)])
+@pytest.mark.parametrize("batch", range(len(BATCHES)))
+def test_append(batch, hd, page, layout, rot, dtype):
+    log(f"append {BATCHES[batch][:4]} hd={hd} page={page} {layout} {rot} {dtype}")
+    s = Setup(BATCHES[batch], page, 2, hd, batch, pad=batch % 3)
+    table = B.rope_table(512, rot) if layout != "none" else None
+    k, v, q = s.rows(2, dtype), s.rows(2, dtype), s.rows(6, dtype)
+    _append_check(s, k, v, q if layout != "none" else None, table, layout if layout != "none" else "half", rot)
+
+
+@pytest.mark.parametrize("shift", [0, 1])
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
+def test_append_from_a_product_s_rows(dtype, shift):
+    """k, v and q inside the rows of one QKV product, aligned or not; one head of keys."""
+    torch = _torch()
+    s = Setup([(40, 3), (1, 77)], 64, 1, 64)
+    wide = torch.randn(s.n, 10 * 64 + 8, device="cuda").to(getattr(torch, dtype))[:, shift:shift + 640].unflatten(1, (10, 64))
+    _append_check(s, wide[:, 8:9], wide[:, 9:], wide[:, :8], B.rope_table(128, 64), "half", 64)
+
+
+def test_append_leaves_what_is_out_of_range():
+    """Pages outside the pool, lengths and rows outside theirs, positions behind the table."""
+    s = Setup([(20, 35), (1, 70), (1, 3), (1, 4), (1, 20)], 32, 2, 64, extra_pages=1, pad=4)
+    pages = s.pages_h.copy()
+    pages[0, 1], pages[3, 0], pages[4, 0] = -1, s.n_pages, 2 ** 31 - 1
+    s.set(pages, s.starts_h, [35, 70, -1, 4, 20])
+    _append_check(s, s.rows(2), s.rows(2), s.rows(4), B.rope_table(64, 64), "half", 64)
+    s.set(s.pages_h, [0, 20, 10, 500, -4, 6], [30, 2, 4 * 32, 5, 6])
+    _append_check(s, s.rows(2), s.rows(2), s.rows(4), B.rope_table(64, 64), "half", 64)
+    s.set(s.pages_h, [-4, 20, 21, 22, 23, 24], [126, 127, 128, 1 << 30, 100])
+    _append_check(s, s.rows(2), s.rows(2), s.rows(4), B.rope_table(200, 64), "half", 64)
+
+
+def test_append_special_values():
+    """NaN and infinities arrive as they are, unrotated; large numbers round to infinity."""
+    torch = _torch()
+    s = Setup([(3, 62)], 64, 1, 64)
+    k = torch.zeros(3, 1, 64, device="cuda")
+    k[0, 0, 5], k[1, 0, 6], k[2, 0, 7] = float("nan"), float("-inf"), 3.4e38
+    B.op_paged_append(s.cache, k, k, s.pages, s.starts, s.lens)
+    for pool in s.plain():
+        got = [pool[s.pages_h[0, p // 64], 0, p % 64] for p in (62, 63, 64)]
+        assert np.isnan(got[0][5]) and got[1][6] == -np.inf and got[2][7] == np.inf
+        assert np.isfinite(np.delete(got[0], 5)).all()
+
+
+# ----------------------------------------------------------------- attention
+def _attend(s, q, **kw):
+    torch = _torch()
+    out = torch.full((s.n, q.shape[1] * s.hd), 7.0, dtype=torch.bfloat16, device="cuda")
+    B.op_attention_paged(q, s.cache, s.pages, s.starts, s.lens, kw.pop("max_new", s.max_new), out=out, **kw)
+    return out
+
+
+def _attend_check(s, q, **kw):
+    out = _attend(s, q, **kw)
+    kw.pop("shared", None)
+    kw.pop("ws", None)
+    want, tol, token = R.attention(_np(q), *s.plain(), s.batch, kw.pop("max_new", s.max_new), **kw)
+    got = _np(out).reshape(want.shape)
+    bad = ~(abs(got - want) <= tol) & ~(np.isnan(got) & np.isnan(want)) & ~(np.isinf(want) & (got == want))
+    assert not bad[token].any(), (np.argwhere(bad & token[:, None, None])[:5], abs(got - want)[token].max())
+    assert (got[~token] == 7.0).all()
+    return out
+
+
+ATTEND = [
+    [(1, 0)], [(1, 1), (2, 0)], [(1, 30), (1, 31), (1, 32), (1, 33)], [(1, 63), (1, 64), (1, 65), (0, 9)], [(1, 500), (1, 3), (1, 1111)],
+    [(5, 0), (1, 200), (70, 30), (3, 61)], [(17, 300)], [(33, 31), (32, 0), (31, 1)], [(200, 0)], [(150, 333), (1, 700), (20, 5)],
+    [(1, 2500)], [(3, 5000), (1, 4000)]]
+
+
+@pytest.mark.parametrize("hd,page,Hkv,G", [(64, 32, 2, 1), (64, 64, 1, 8), (128, 128, 2, 4), (128, 32, 1, 3), (64, 256, 3, 2), (128, 64, 1, 20)])
+@pytest.mark.parametrize("batch", range(len(ATTEND)))
+def test_attention(batch, hd, page, Hkv, G):
+    log(f"attention {ATTEND[batch][:4]} hd={hd} page={page} {Hkv} x {G}")
+    s = Setup(ATTEND[batch], page, Hkv, hd, batch, pad=batch % 3, stale=float("nan"))
+    _attend_check(s, s.rows(Hkv * G))
+
+
+@pytest.mark.parametrize("hd,page", [(64, 32), (128, 64)])
+@pytest.mark.parametrize("window,sinks", [(1, 0), (1, 1), (16, 0), (32, 4), (33, 32), (64, 40), (100, 0), (100, 65), (500, 7), (2 ** 31 - 1, 0), (7, 2 ** 31 - 1)])
+def test_attention_windows(window, sinks, hd, page):
+    log(f"windows {window} {sinks} {hd}")
+    s = Setup([(1, 0), (1, 99), (40, 300), (3, 64), (1, 1500), (90, 0)], page, 2, hd, 5, stale=float("inf"))
+    _attend_check(s, s.rows(4), window=window, sinks=sinks)
+
+
+@pytest.mark.parametrize("n0", [0, 27, 31, 32, 61, 63, 64])
+def test_attention_every_border(n0):
+    """Token by token over the borders of groups, pages and windows."""
+    s = Setup([(4, n0 + i) for i in range(0, 40)], 32, 1, 64, n0, stale=float("nan"))
+    _attend_check(s, s.rows(2), window=34, sinks=2)
+    _attend_check(s, s.rows(2))
+
+
+@pytest.mark.parametrize("hd", [64, 128])
+@pytest.mark.parametrize("T", [3, 45, 300])
+def test_attention_masked_numbers_count_for_nothing(T, hd):
+    """NaN and infinities in keys and values of later tokens, of tokens before the
+    window and behind the last: a query that does not see them is as without them, to
+    the bit; one that does is what the formula says."""
+    torch = _torch()
+    s = Setup([(T, 100), (1, 60)], 32, 2, hd, T, extra_pages=1)
+    q = s.rows(4)
+    clean = _attend(s, q, window=90, sinks=2)
+    at = [2 + 9, 100 + T // 2, 100 + T - 1, 100 + T]  # outside the window, between the queries, the last, behind it
+    plain = [R.in_pool(np.arange(x.numel()).reshape(x.shape), bool(i)) for i, x in enumerate(s.cache)]
+    for j, value in zip(at, (float("nan"), float("inf"), float("-inf"), float("nan"))):
+        for x, p in zip(s.cache, plain):
+            where = p[s.pages_h[0, j // 32], :, j % 32, 1::7].reshape(-1)
+            x.view(-1)[torch.from_numpy(where).cuda()] = value
+    out = _attend(s, q, window=90, sinks=2)
+    first = 100 + T // 2 - 100  # rows before it see none of them
+    lo = 11 + 90 - 100  # rows up to 11 + 90 - 1 see the first
+    same = [r for r in range(max(0, lo), first)]
+    assert torch.equal(out[same], clean[same]) and torch.equal(out[T:], clean[T:])
+    if first < T:
+        assert not torch.isfinite(out[first].float()).all()
+
+
+@pytest.mark.parametrize("T", [2, 40])
+def test_attention_visible_infinities_of_values(T):
+    torch = _torch()
+    s = Setup([(T, 30)], 32, 1, 64, 3)
+    plain = R.in_pool(np.arange(s.cache[1].numel()).reshape(s.cache[1].shape), True)
+    for j, d, value in ((30, 5, float("inf")), (31, 9, float("-inf")), (30, 60, float("nan")), (29, 17, float("inf"))):
+        s.cache[1].view(-1)[int(plain[s.pages_h[0, j // 32], 0, j % 32, d])] = value
+    _attend_check(s, s.rows(2))
+
+
+def test_attention_pages_outside_the_pool():
+    """Their tokens count as masked; a query that sees no other gets zeros."""
+    s = Setup([(40, 100), (1, 20), (2, 90), (1, 64)], 32, 2, 64, 4, stale=float("nan"))
+    pages = s.pages_h.copy()
+    pages[0, 1], pages[1, 0], pages[2, 2], pages[3, :] = -1, s.n_pages, 2 ** 31 - 1, -7
+    s.set(pages, s.starts_h, s.lens_h)
+    out = _attend_check(s, s.rows(4))
+    assert (out[40] == 0).all() and (out[43] == 0).all()
+
+
+def test_attention_leaves_what_is_out_of_range():
+    """Lengths and rows outside theirs, more new tokens than max_new."""
+    s = Setup([(20, 35), (1, 70), (1, 3), (5, 4), (1, 20)], 32, 2, 64, pad=3)
+    _attend_check(s, s.rows(4), max_new=4)
+    s.set(s.pages_h, s.starts_h, [35, -1, 96, 1 << 30, 95])
+    _attend_check(s, s.rows(4))
+    s.set(s.pages_h, [0, 20, 10, 500, -4, 6], [35, 2, 3, 5, 6])
+    _attend_check(s, s.rows(4))
+    s.set(s.pages_h, [0, 20, 21, 22, 27, 28], [90, 95, 94, 93, 92])
+    _attend_check(s, s.rows(4))
+
+
+def test_attention_scale_and_large_scores():
+    s = Setup([(9, 100), (1, 1000)], 64, 2, 128, 6)
+    _attend_check(s, s.rows(4), scale=0.5)
+    _attend_check(s, s.rows(4) * 8, scale=1.0)  # most probabilities vanish
+
+
+def test_attention_does_not_depend_on_the_batch():
+    """A sequence's bits are its own: alone, beside others, with wider page tables, in
+    another order, behind rows of other lengths."""
+    torch = _torch()
+    for seqs in ([(1, 3000), (1, 10), (1, 700)], [(90, 3000), (1, 10), (30, 700), (260, 5)]):
+        s = Setup(seqs, 64, 2, 64, 8)
+        q = s.rows(8)
+        whole = _attend(s, q)
+        pages, starts, lens = s.pages_h, s.starts_h, s.lens_h
+        wide = np.concatenate([pages, np.full((len(seqs), 300), -1)], 1)
+        assert torch.equal(_attend(s.set(wide, starts, lens), q), whole)
+        order = list(range(len(seqs)))[::-1]
+        new = np.concatenate([[0], np.cumsum([seqs[b][0] for b in order])])
+        rows = np.concatenate([np.arange(starts[b], starts[b + 1]) for b in order])
+        r = torch.from_numpy(rows).cuda()
+        assert torch.equal(_attend(s.set(pages[order], new, lens[order]), q[r]), whole[r])
+        for b in range(len(seqs)):
+            one = Setup([seqs[b]], 64, 2, 64)
+            one.cache, one.n_pages = s.cache, s.n_pages
+            one.set(pages[b:b + 1], [0, seqs[b][0]], lens[b:b + 1])
+            sl = slice(starts[b], starts[b + 1])
+            assert torch.equal(_attend(one, q[sl].contiguous(), max_new=s.max_new), whole[sl]), b
+
+
+# ------------------------------------------------------------------- shared
+@pytest.mark.parametrize("hd,page,Hkv,G", [(64, 32, 2, 1), (64, 64, 1, 8), (128, 128, 2, 4), (128, 64, 2, 2)])
+@pytest.mark.parametrize("shared,seqs", [
+    (64, [(1, 64), (1, 70)]), (640, [(1, 700), (1, 641), (1, 640)]), (1000, [(3, 1000), (1, 1200), (2, 1001), (20, 1100)]),
+    (2048, [(1, 2050 + 9 * i) for i in range(40)]), (300, [(100, 300), (70, 301)]), (63, [(1, 70), (1, 63)])])
+def test_shared(shared, seqs, hd, page, Hkv, G):
+    log(f"shared {shared} {seqs[:3]} hd={hd} page={page} {Hkv} x {G}")
+    torch = _torch()
+    s = Setup(seqs, page, Hkv, hd, shared, pad=2, shared=shared)
+    # the rest of the prefix, on a page of each sequence's own, is the same too
+    if shared % page:
+        k = shared // page
+        for i, x in enumerate(s.cache):
+            at = R.in_pool(np.arange(x[0].numel()).reshape((1,) + tuple(x.shape[1:])), bool(i))[0][:, :shared % page].reshape(-1)
+            for b in range(1, len(seqs)):
+                x[int(s.pages_h[b, k])].view(-1)[torch.from_numpy(at).cuda()] = x[int(s.pages_h[0, k])].view(-1)[torch.from_numpy(at).cuda()]
+    q = s.rows(Hkv * G)
+    _attend_check(s, q, shared=shared)
+    _attend_check(s, q, shared=shared, window=200, sinks=3)
+    _attend_check(s, q, shared=shared, window=shared + 20)
+
+
+def test_shared_tokens_inside_the_prefix():
+    """Sequences whose new tokens lie inside what is called shared see no later token of it."""
+    s = Setup([(3, 10), (1, 63), (2, 100), (4, 126), (1, 300)], 64, 2, 64, 3, shared=256, stale=None)
+    _attend_check(s, s.rows(4), shared=256)
+    _attend_check(s, s.rows(4), shared=256, window=40, sinks=70)
+
+
+def test_shared_of_one_sequence_and_of_none():
+    torch = _torch()
+    s = Setup([(2, 300)], 64, 2, 64, 3)
+    q = s.rows(4)
+    assert torch.equal(_attend(s, q, shared=256), _attend(s, q))
+    s = Setup([(2, 300), (1, 400)], 64, 2, 64, 3, shared=256)
+    q = s.rows(4)
+    assert torch.equal(_attend(s, q, shared=40), _attend(s, q))  # less than is worth it
+
+
+def test_shared_reads_the_first_sequence_s_pages():
+    """(and masked numbers on them count for nothing, whatever they are)"""
+    s = Setup([(1, 100), (1, 70), (1, 64)], 64, 1, 64, 3, shared=64, stale=float("nan"))
+    _attend_check(s, s.rows(4), shared=64)
+    pages = s.pages_h.copy()
+    pages[:, 0] = -1
+    s.set(pages, s.starts_h, s.lens_h)
+    _attend_check(s, s.rows(4), shared=64)
+
+
+# ------------------------------------------------------------ ways of calling
+def test_strided_queries_and_defaults():
+    torch = _torch()
+    s = Setup([(3, 100), (1, 20)], 64, 2, 64, 1)
+    wide = torch.randn(s.n, 640, device="cuda").to(torch.bfloat16)
+    q = wide[:, 64:64 + 256].unflatten(1, (4, 64))
+    got = B.op_attention_paged(q, s.cache, s.pages, s.starts, s.lens, 3)
+    assert torch.equal(got, _attend(s, q.contiguous()))
+
+
+def test_on_another_stream():
+    torch = _torch()
+    s = Setup([(30, 400), (1, 2000)], 64, 2, 64, 1)
+    q, k, v = s.rows(8), s.rows(2), s.rows(2)
+    table = B.rope_table(2048, 64)
+    saved = [x.clone() for x in s.cache]
+    q1 = B.op_paged_append(s.cache, k, v, s.pages, s.starts, s.lens, rope=table, q=q)
+    want = _attend(s, q1)
+    after = [x.clone() for x in s.cache]
+    for x, y in zip(s.cache, saved):
+        x.copy_(y)
+    st = torch.cuda.Stream()
+    st.wait_stream(torch.cuda.current_stream())
+    q2 = B.op_paged_append(s.cache, k, v, s.pages, s.starts, s.lens, rope=table, q=q, stream=st)
+    got = B.op_attention_paged(q2, s.cache, s.pages, s.starts, s.lens, s.max_new, stream=st)
+    st.synchronize()
+    assert torch.equal(got, want) and torch.equal(q1, q2) and all(torch.equal(x, y) for x, y in zip(s.cache, after))
+
+
+def test_steps_in_graphs_that_share_a_workspace():
+    """Two captured steps (one with a shared prefix) on one workspace, replayed by turns
+    with other lengths, pages and rows each time, with eager work in between."""
+    torch = _torch()
+    s = Setup([(1, 1100 + 13 * i) for i in range(6)], 64, 2, 64, 9, shared=1024, extra_pages=2)
+    q, k, v = s.rows(8), s.rows(2), s.rows(2)
+    table = B.rope_table(2048, 64)
+    q_out, out = torch.zeros_like(q), [torch.zeros(s.n, 8 * 64, dtype=torch.bfloat16, device="cuda") for _ in range(2)]
+    tokens = s.pages.shape[1] * 64
+    ws = torch.empty(max(B.paged_workspace(s.n, 6, 8, 2, 64, 1, tokens, sh) for sh in (0, 1024)), dtype=torch.uint8, device="cuda")
+
+    def step(i):
+        B.op_paged_append(s.cache, k, v, s.pages, s.starts, s.lens, rope=table, q=q, q_out=q_out)
+        B.op_attention_paged(q_out, s.cache, s.pages, s.starts, s.lens, 1, shared=1024 * i, out=out[i], ws=ws)
+    step(0), step(1)
+    torch.cuda.synchronize()
+    graphs = []
+    for i in range(2):
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            step(i)
+        graphs.append(g)
+    for turn in range(3):
+        s.lens += 1
+        q.normal_(), k.normal_(), v.normal_()
+        for i in (0, 1):
+            graphs[i].replay()
+            torch.cuda.synchronize()
+            got = out[i].clone()
+            want = B.op_attention_paged(q_out, s.cache, s.pages, s.starts, s.lens, 1, shared=1024 * i)
+            assert torch.equal(got, want), (turn, i)
+            ws.fill_(255)
+    s.set(s.pages_h, s.starts_h, s.lens.cpu().numpy())
+    _attend_check(s, q_out, max_new=1, shared=1024)
+
+
+def test_pools_past_32_bits():
+    """Pages behind 2^32 bytes and 2^31 numbers of a pool."""
+    torch = _torch()
+    page, Hkv, hd = 256, 32, 128
+    n_pages = 2200  # 2.3e9 numbers each
+    cache = tuple(torch.empty(n_pages, Hkv, page, hd, dtype=torch.bfloat16, device="cuda") for _ in range(2))
+    small = tuple(torch.zeros(4, Hkv, page, hd, dtype=torch.bfloat16, device="cuda") for _ in range(2))
+    k, v, q = (torch.randn(300, h, hd, device="cuda").to(torch.bfloat16) for h in (Hkv, Hkv, Hkv))
+    starts, lens = _ints([0, 299, 300]), _ints([0, 0])
+    got = []
+    for c, pages in ((cache, [[2199, 1], [2198, 5]]), (small, [[0, 1], [2, 3]])):
+        B.op_paged_append(c, k, v, _ints(pages), starts, lens, rope=B.rope_table(512, hd))
+        got.append(B.op_attention_paged(q, c, _ints(pages), starts, lens, 299))
+    assert torch.equal(got[0], got[1])
+    assert all(torch.equal(a[2199], b[0]) for a, b in zip(cache, small))
+
+
+def test_whole_windows_as_the_dense_attention():
+    """A batch of whole windows, appended and attended in pages, beside the decoder's own
+    kernel on dense K and V; then the last tokens again, one at a time."""
+    torch = _torch()
+    Bn, Hq, Hkv, W, hd = 3, 8, 2, 200, 64
+    s = Setup([(W, 0)] * Bn, 64, Hkv, hd, 2)
+    q, k, v = s.rows(Hq), s.rows(Hkv), s.rows(Hkv)
+    table = B.rope_table(256, hd)
+    qr = B.op_paged_append(s.cache, k, v, s.pages, s.starts, s.lens, rope=table, q=q)
+    out = _attend_check(s, qr)
+    pos = torch.arange(W, dtype=torch.int32, device="cuda").repeat(Bn)
+    kr = B.op_rope(k, pos, table)
+    assert torch.equal(B.op_rope(q, pos, table), qr)
+
+    def dense(x):
+        return x.view(Bn, W, -1, hd).transpose(1, 2).contiguous()
+    ref = B.op_attention_bf16(dense(qr), dense(kr), dense(v).transpose(2, 3).contiguous())
+    # both round their probabilities to bf16 (2^-8 each at most) and their result; values of up to 5
+    assert (abs(out.float() - ref.float()) <= 2 * 5 * 2.0 ** -8 + 2.0 ** -7 * abs(ref.float())).all()
+    # the last five tokens again, step by step
+    for t in range(W - 5, W):
+        rows = torch.arange(Bn, device="cuda") * W + t
+        one = Setup([(1, t)] * Bn, 64, Hkv, hd)
+        one.cache, one.n_pages = s.cache, s.n_pages
+        one.set(s.pages_h, [0, 1, 2, 3], [t] * Bn)
+        q1 = B.op_paged_append(one.cache, k[rows], v[rows], one.pages, one.starts, one.lens, rope=table, q=q[rows])
+        assert torch.equal(q1, qr[rows])
+        got = _attend(one, q1)
+        assert (abs(got.float() - out[rows].float()) <= 2 * 5 * 2.0 ** -8 + 2.0 ** -7 * abs(out[rows].float())).all()
