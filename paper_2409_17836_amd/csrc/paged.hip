@@ -16,6 +16,7 @@
 #include <algorithm>
 #include <type_traits>
 
+#include "async_lds.h"
 #include "common.h"
 #include "paged.h"
 
@@ -55,6 +56,21 @@ __device__ inline Seq sequence(const Ragged& r, int b, int limit) {
   const int r0 = r.starts[b], r1 = r.starts[b + 1], len = r.lens[b], tokens = r.max_pages * r.page;
   const bool ok = r0 >= 0 && r1 >= r0 && r1 <= r.n && len >= 0 && len < tokens;
   return {r0, ok ? min(min(r1 - r0, limit), tokens - len) : 0, len};
+}
+
+// A row's position; -1 if it is no token.
+__device__ inline int position_of(const Ragged& r, int row, int limit) {
+  // the last sequence that begins at or before the row
+  int lo = 0, n = r.B;
+  while (n > 1) {
+    const int h = n / 2;
+    const bool right = r.starts[lo + h] <= row;
+    lo += right ? h : 0;
+    n = right ? n - h : h;
+  }
+  const Seq s = sequence(r, lo, limit);
+  const int t = row - s.row;
+  return t >= 0 && t < s.T ? s.len + t : -1;
 }
 
 // First number of a head's group of 32 tokens on a page.
@@ -308,64 +324,66 @@ __device__ inline __amdgpu_buffer_rsrc_t buffer(const uint16_t* p, int bytes) {
   return __builtin_amdgcn_make_buffer_rsrc(const_cast<uint16_t*>(p), (short)0, bytes, 0x00020000);
 }
 
-__device__ inline bool odd_bf16(uint32_t b) { return (b & 0x7f80u) == 0x7f80u; }  // NaN or infinity
-
-// Values of a group that some, but not all, of a tile's queries see.  A
-// probability of zero times a NaN or an infinity is NaN, so the values of tokens
-// that no query sees (`seen`), which may be anything, are cleared; and where
-// another one is not finite, its products are added here, to the columns that
-// see it, and it is cleared too.  vr: a lane's operands (16 dims x 32 tokens
-// each); pf, pos, low: of the lane's column; o: its result, 4 dims of 16 each.
-template <int ND, int NT>
-__device__ inline void clear_values(u32x4 (&vr)[ND], const bf16x8 (&pf)[NT], f32x4 (&o)[NT][ND], const Mask& mask, uint32_t seen,
-                                    const int (&pos)[NT], int j0) {
-  const int lane = threadIdx.x & 63, g = lane >> 4;
-  uint32_t odd = 0;  // a bit for each half word e of the lane
+// The words of a lane's 8 values (tokens 4 g .. + 3 of both halves of a group)
+// with only those of `tokens`, a bit each.
+__device__ inline u32x4 words_of(uint32_t tokens, int g) {
+  u32x4 w;
 #pragma unroll
   for (int e = 0; e < 4; e++) {
-    // tokens 16 (e / 2) + 4 g + 2 (e % 2) and the next
-    const uint32_t two = seen >> (16 * (e >> 1) + 2 * (e & 1)) >> (4 * g) & 3;
-    const uint32_t keep = (two & 1 ? 0xffffu : 0u) | (two & 2 ? 0xffff0000u : 0u);
-#pragma unroll
-    for (int i = 0; i < ND; i++) {
-      vr[i][e] &= keep;
-      odd |= (uint32_t)odd_bf16(vr[i][e]) << (2 * e) | (uint32_t)odd_bf16(vr[i][e] >> 16) << (2 * e + 1);
-    }
+    const uint32_t two = tokens >> (16 * (e >> 1) + 2 * (e & 1)) >> (4 * g) & 3;
+    w[e] = (two & 1 ? 0xffffu : 0u) | (two & 2 ? 0xffff0000u : 0u);
   }
-  if (__ballot(odd != 0) == 0) return;
-  for (int j = 0; j < kGroup; j++) {
-    const int from = (j & 15) >> 2, e = 2 * (j >> 4) + ((j & 3) >> 1), hi = j & 1;
-    if ((__ballot(odd >> (2 * e + hi) & 1) >> (16 * from) & 0xffff) == 0) continue;
-    u32x4 w[(ND + 3) / 4];  // the token's values of the lane's dim, 16 i + lane % 16
+  return w;
+}
+
+// O^T += V^T P^T for a group of keys that some, but not all, of a wave's queries
+// see.  A probability of zero times a NaN or an infinity is NaN.  So the values
+// of tokens that no query sees (all but `seen`), which may be anything, are
+// cleared; and tokens with a value that is not finite are left to products of
+// their own, which only the columns that see them take.  value(i): a lane's
+// operand of dims 16 i ..; pf, pos: of the lane's columns; o: their results.
+template <int ND, int NT, class Value>
+__device__ inline void add_masked_values(Value value, const bf16x8 (&pf)[NT], f32x4 (&o)[NT][ND], const Mask& mask, uint32_t seen,
+                                         const int (&pos)[NT], int j0) {
+  const int g = (threadIdx.x & 63) >> 4;
+  u32x4 keep = words_of(seen, g);
+  uint32_t odd = 0;  // a bit for each half word of the lane
+#pragma unroll
+  for (int i = 0; i < ND; i++) {
+    if (i % 2 == 0) __builtin_amdgcn_sched_barrier(0);  // (side by side they take more registers than there are)
+    const u32x4 v = value(i) & keep;
+#pragma unroll
+    for (int e = 0; e < 4; e++)
+      odd |= ((v[e] & 0x7f80u) == 0x7f80u ? 1u << (2 * e) : 0u) | ((v[e] & 0x7f800000u) == 0x7f800000u ? 2u << (2 * e) : 0u);
+  }
+  uint32_t bad = 0;
+  if (__ballot(odd != 0)) {
+#pragma unroll
+    for (int e = 0; e < 8; e++) {
+      const uint64_t lanes = __ballot(odd >> e & 1);
+#pragma unroll
+      for (int k = 0; k < 4; k++) bad |= lanes >> (16 * k) & 0xffff ? 1u << (16 * (e >> 2) + 4 * k + (e & 3)) : 0u;
+    }
+    keep = words_of(seen & ~bad, g);
+  }
+#pragma unroll
+  for (int i = 0; i < ND; i++) {
+    if (i % 2 == 0) __builtin_amdgcn_sched_barrier(0);
+    const bf16x8 v = __builtin_bit_cast(bf16x8, value(i) & keep);
+#pragma unroll
+    for (int y = 0; y < NT; y++) o[y][i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, pf[y], o[y][i], 0, 0, 0);
+  }
+  for (; bad; bad &= bad - 1) {
+    const int j = __builtin_ctz(bad);
+    keep = words_of(1u << j, g);
 #pragma unroll
     for (int i = 0; i < ND; i++) {
-      const uint32_t x = e == 0 ? vr[i][0] : e == 1 ? vr[i][1] : e == 2 ? vr[i][2] : vr[i][3];
-      w[i >> 2][i & 3] = hi ? x & 0xffff0000u : x << 16;
-    }
+      __builtin_amdgcn_sched_barrier(0);
+      const bf16x8 v = __builtin_bit_cast(bf16x8, value(i) & keep);
 #pragma unroll
-    for (int y = 0; y < NT; y++) {
-      float p = 0.f;
-#pragma unroll
-      for (int k = 0; k < 8; k++)
-        if (k == 4 * (j >> 4) + (j & 3)) p = (float)pf[y][k];
-      p = __shfl(p, 16 * from + (lane & 15));
-      const bool sees = mask.sees(pos[y], mask.low(pos[y]), j0 + j);
-#pragma unroll
-      for (int i = 0; i < ND; i++)
-#pragma unroll
-        for (int r = 0; r < 4; r++) {
-          const float v = __builtin_bit_cast(float, __shfl((int)w[i >> 2][i & 3], 16 * from + 4 * g + r));
-          if (sees) o[y][i][r] = fmaf(p, v, o[y][i][r]);
-        }
-    }
-    if (g == from) {
-      const uint32_t keep = hi ? 0xffffu : 0xffff0000u;
-#pragma unroll
-      for (int i = 0; i < ND; i++) {
-        if (e == 0) vr[i][0] &= keep;
-        if (e == 1) vr[i][1] &= keep;
-        if (e == 2) vr[i][2] &= keep;
-        if (e == 3) vr[i][3] &= keep;
+      for (int y = 0; y < NT; y++) {
+        const f32x4 x = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, pf[y], f32x4{}, 0, 0, 0);
+        if (mask.sees(pos[y], mask.low(pos[y]), j0 + j)) o[y][i] += x;
       }
     }
   }
@@ -375,24 +393,24 @@ __device__ inline void clear_values(u32x4 (&vr)[ND], const bf16x8 (&pf)[NT], f32
 // Columns: column c = t G + i of a (sequence, key/value head) is query head
 // kvh G + i of its new token t; for the prefix, of row t of the batch.
 //
-// Grid: (splits, tiles of 16 NT columns x Hkv, B), 512 threads.  Wave w takes
-// groups w, w + 8, .. of its split: S^T = K Q^T, so lane (col, g) holds the
+// Grid: (splits, tiles of 16 NT columns x Hkv, B), 256 threads.  Wave w takes
+// groups w, w + 4, .. of its split: S^T = K Q^T, so lane (col, g) holds the
 // scores of its column and tokens 16 i + 4 g + r of a group, an online softmax,
 // O^T += V^T P^T.  The waves' parts meet in LDS.
-constexpr int kWaves = 8;
+constexpr int kWaves = 4;
 
 struct AttnPlan {
-  int few;               // columns that the form for few takes, at most
-  int columns;           // rows of its partial results for a sequence
+  int few, columns;      // columns of a sequence that the form for few takes, and how many of them there are at most
   Splits split;          // of the form for few columns
+  Splits prompt;         // of the form for many
   int cut;               // tokens that all share, computed for the batch
   int pre, pre_chunk;    // splits of these
-  float *po, *pre_o;     // partial results, and maxima and sums
-  float2 *pml, *pre_ml;
+  float *po, *prompt_o, *pre_o;      // partial results, and maxima and sums
+  float2 *pml, *prompt_ml, *pre_ml;
 };
 
 template <int HD, int NT, bool PREFIX>
-__global__ __launch_bounds__(kWaves * 64, NT > 1 ? 2 : HD == 64 ? 6 : 4) void attn_paged_split_kernel(
+__global__ __launch_bounds__(kWaves * 64, HD == 64 ? 4 : 3) void attn_paged_split_kernel(
     const uint16_t* __restrict__ q, int64_t ldq, const uint16_t* __restrict__ kc, const uint16_t* __restrict__ vc, Ragged r, int max_new,
     int Hkv, int G, AttnPlan plan, Mask mask, float sl2, uint16_t* __restrict__ out) {
   constexpr int KQ = HD / 32, ND = HD / 16, NW = kWaves, TILE = 16 * NT;
@@ -413,18 +431,7 @@ __global__ __launch_bounds__(kWaves * 64, NT > 1 ? 2 : HD == 64 ? 6 : 4) void at
     p1 = -1;
 #pragma unroll
     for (int y = 0; y < NT; y++) {
-      // the last sequence that begins at or before the row
-      const int row = (c0 + min(16 * y + col, ncol - 1)) / G;
-      int lo = 0, n = r.B;
-      while (n > 1) {
-        const int h = n / 2;
-        const bool right = r.starts[lo + h] <= row;
-        lo += right ? h : 0;
-        n = right ? n - h : h;
-      }
-      const Seq s = sequence(r, lo, max_new);
-      const int t = row - s.row;
-      pos[y] = t >= 0 && t < s.T ? s.len + t : -1;  // (no token: sees nothing)
+      pos[y] = position_of(r, (c0 + min(16 * y + col, ncol - 1)) / G, max_new);
       p0 = min(p0, pos[y] < 0 ? INT32_MAX : pos[y]);
       p1 = max(p1, pos[y]);
     }
@@ -440,7 +447,7 @@ __global__ __launch_bounds__(kWaves * 64, NT > 1 ? 2 : HD == 64 ? 6 : 4) void at
     p0 = sq.len + c0 / G;
     p1 = sq.len + (c0 + ncol - 1) / G;
   }
-  const Span span = PREFIX ? Span{0, 0, 0, plan.cut} : span_of(sq, mask, plan.cut);
+  const Span span = PREFIX ? Span{0, min(plan.cut, (min(mask.sinks, plan.cut) + kGroup - 1) & ~(kGroup - 1)), 0, plan.cut} : span_of(sq, mask, plan.cut);
   const int chunk = PREFIX ? plan.pre_chunk : plan.split.chunk(span.total);
   const int v0 = split * chunk, v1 = min(span.total, v0 + chunk);
   if (v0 >= v1) return;
@@ -522,15 +529,19 @@ __global__ __launch_bounds__(kWaves * 64, NT > 1 ? 2 : HD == 64 ? 6 : 4) void at
         for (int e = 0; e < 4; e++) pf[y][4 * i + e] = (__bf16)__builtin_amdgcn_exp2f(fmaf(s[i][e], sl2, sub));
       l[y] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ones, pf[y], l[y], 0, 0, 0);
     }
-    if (!whole) clear_values<ND, NT>(vr, pf, o, mask, mask.seen(p0, p1, j0), pos, j0);
+    if (whole) {
 #pragma unroll
-    for (int i = 0; i < ND; i++)
+      for (int i = 0; i < ND; i++)
 #pragma unroll
-      for (int y = 0; y < NT; y++)
-        o[y][i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, vr[i]), pf[y], o[y][i], 0, 0, 0);
+        for (int y = 0; y < NT; y++)
+          o[y][i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, vr[i]), pf[y], o[y][i], 0, 0, 0);
+    } else {
+      add_masked_values([&](int i) __attribute__((always_inline)) { return vr[i]; }, pf, o, mask, mask.seen(p0, p1, j0), pos, j0);
+    }
   }
-  // HD / 32 dims of a column to a thread
-  typedef float f32xd __attribute__((ext_vector_type(HD / 32)));
+  // HD / (4 NW) dims of a column to a thread
+  constexpr int DT = HD / (4 * NW);
+  typedef float f32xd __attribute__((ext_vector_type(DT)));
 #pragma unroll
   for (int y = 0; y < NT; y++) {
     if (y) __syncthreads();
@@ -541,7 +552,7 @@ __global__ __launch_bounds__(kWaves * 64, NT > 1 ? 2 : HD == 64 ? 6 : 4) void at
 #pragma unroll
     for (int i = 0; i < ND; i++) *reinterpret_cast<f32x4*>(&so[wave][col][16 * i + 4 * g]) = o[y][i];
     __syncthreads();
-    const int oc = tid >> 5, d0 = (tid & 31) * (HD / 32), c = c0 + 16 * y + oc;
+    const int oc = tid / (4 * NW), d0 = tid % (4 * NW) * DT, c = c0 + 16 * y + oc;
     if (16 * y + oc >= ncol) continue;
     float M = sm[0][oc];
 #pragma unroll
@@ -560,7 +571,7 @@ __global__ __launch_bounds__(kWaves * 64, NT > 1 ? 2 : HD == 64 ? 6 : 4) void at
       const float inv = L == 0.f ? 0.f : 1.0f / L;  // (no visible key: zeros)
       uint32_t* op = reinterpret_cast<uint32_t*>(out + ((int64_t)(sq.row + t) * Hkv * G + hq) * HD + d0);
 #pragma unroll
-      for (int e = 0; e < HD / 64; e++)
+      for (int e = 0; e < DT / 2; e++)
         op[e] = __builtin_bit_cast(uint32_t, bf16x2{(__bf16)(acc[2 * e] * inv), (__bf16)(acc[2 * e + 1] * inv)});
     } else {
       const int64_t at = PREFIX ? ((int64_t)t * Hkv * G + hq) * plan.pre + split
@@ -571,78 +582,448 @@ __global__ __launch_bounds__(kWaves * 64, NT > 1 ? 2 : HD == 64 ? 6 : 4) void at
   }
 }
 
+// ---- many columns
+// A workgroup of eight waves takes 256 columns of one (sequence, key/value
+// head), or of the batch, each wave 32, and walks the keys 64 at a time.  Keys
+// and values come straight to LDS, kAhead steps ahead, in the order of the
+// matrix operands; the products read a lane's 16 bytes in a row.
+//
+// A step has two phases, a barrier after each: one for the vector unit (maxima,
+// exponentials), one for the matrix unit (the step's values, the next step's
+// scores).  The waves of a SIMD, w and w + 4, are a phase apart, so that the
+// units work side by side.  Phases counted from the start: waves 0 to 3 have
+// step t's phases at 2 t and 2 t + 1, waves 4 to 7 one later.  So values t and
+// keys t + 1 (bundle t) are read in phases 2 t + 1 and 2 t + 2, have arrived by
+// the end of phase 2 t (each wave waits for its own part before that barrier),
+// and their place is free from phase 2 t + 3 on: bundle t + kAhead is asked for in
+// phase 2 t + 1, into a ring of kAhead + 1.
+constexpr int kTileCols = 256;
+constexpr int kStep = 2 * kGroup;
+constexpr int kAhead = 2, kRing = kAhead + 1;
+constexpr int kReads = 8;          // operands read ahead of their products
+constexpr int kNowhere = 1 << 30;  // where no query sees a key
+
+template <int HD, bool PREFIX>
+__global__ __launch_bounds__(512, 2) void attn_paged_prompt_kernel(
+    const uint16_t* __restrict__ q, int64_t ldq, const uint16_t* __restrict__ kc, const uint16_t* __restrict__ vc, Ragged r, int max_new,
+    int Hkv, int G, AttnPlan plan, Mask mask, float sl2, int nslot, int nsplit, uint16_t* __restrict__ out) {
+  constexpr int ND = HD / 16, KQ = HD / 32;  // dim tiles; 32-dim steps of a score
+  constexpr int PIECES = HD / 16;            // KB of a group of keys (or values)
+  constexpr int LOADS = 2 * PIECES / 8;      // KB of a step's keys (or values) to a wave
+  __shared__ u32x4 sk[kRing][2 * PIECES * 64], sv[kRing][2 * PIECES * 64];
+  // heads fastest: with a multiple of eight heads all tiles of a head run on one
+  // XCD and share its L2; the longest tiles first
+  const int kvh = blockIdx.x % Hkv, rest = blockIdx.x / Hkv, split = rest % nsplit, slot = nslot - 1 - rest / nsplit;
+  const int tid = threadIdx.x, lane = tid & 63, col = lane & 15, g = lane >> 4;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  int b = 0, c0 = slot * kTileCols;
+  Seq sq{0, r.n, 0};
+  if (!PREFIX) {
+    // slot starts[b] G / 256 + b + i is tile i of sequence b
+    b = last_at_most(r.B, slot, [&](int i) { return (int64_t)r.starts[i] * G / kTileCols + i; });
+    sq = sequence(r, b, max_new);
+    const int64_t tile = slot - ((int64_t)sq.row * G / kTileCols + b);
+    if (sq.T <= 0 || tile < 0 || tile * kTileCols >= (int64_t)sq.T * G || sq.T * G <= plan.few) return;
+    c0 = (int)tile * kTileCols;
+  }
+  const int ncol = min(kTileCols, sq.T * G - c0);
+  if (ncol <= 0) return;
+  // the wave's columns (past the last: the last one's again), their positions
+  const int w0 = min(c0 + wave * 32, c0 + ncol - 1), w1 = min(c0 + wave * 32 + 31, c0 + ncol - 1);
+  const bool works = wave * 32 < ncol;
+  int pos[2], p0, p1, q0, q1;  // p0, p1: of the tile's columns, q0, q1: of the wave's
+  if (PREFIX) {
+    __shared__ int ends[2][8];
+    q0 = INT32_MAX;
+    q1 = -1;
+#pragma unroll
+    for (int y = 0; y < 2; y++) {
+      pos[y] = position_of(r, min(w0 + 16 * y + col, w1) / G, max_new);
+      q0 = min(q0, pos[y] < 0 ? INT32_MAX : pos[y]);
+      q1 = max(q1, pos[y]);
+    }
+    for (int o = 8; o; o >>= 1) {
+      q0 = min(q0, __shfl_xor(q0, o));
+      q1 = max(q1, __shfl_xor(q1, o));
+    }
+    q0 = __builtin_amdgcn_readfirstlane(q0);
+    q1 = __builtin_amdgcn_readfirstlane(q1);
+    ends[0][wave] = q0;
+    ends[1][wave] = q1;
+    __syncthreads();
+    p0 = INT32_MAX;
+    p1 = -1;
+    for (int w = 0; w < 8; w++) {
+      p0 = min(p0, ends[0][w]);
+      p1 = max(p1, ends[1][w]);
+    }
+    p0 = __builtin_amdgcn_readfirstlane(p0);
+    p1 = __builtin_amdgcn_readfirstlane(p1);
+  } else {
+#pragma unroll
+    for (int y = 0; y < 2; y++) pos[y] = sq.len + min(w0 + 16 * y + col, w1) / G;
+    p0 = sq.len + c0 / G;
+    p1 = sq.len + (c0 + ncol - 1) / G;
+    q0 = sq.len + w0 / G;
+    q1 = sq.len + w1 / G;
+  }
+  const Span span = PREFIX ? Span{0, min(plan.cut, (min(mask.sinks, plan.cut) + kGroup - 1) & ~(kGroup - 1)), 0, plan.cut} : span_of(sq, mask, plan.cut);
+  const int chunk = PREFIX ? plan.pre_chunk : plan.prompt.chunk(span.total);
+  // the split's places of the span, without those behind the tile's last query
+  const int v0 = split * chunk, vend = min(span.total, v0 + chunk);
+  if (v0 >= vend) return;
+  const int v1 = min(vend, max(v0, p1 + 1 - span.cut - (p1 >= span.hole ? min(span.gap, p1 - span.hole) : 0)));
+  const bool only = !PREFIX && plan.cut == 0 && span.total <= chunk;  // the only split writes the result
+  bf16x8 qf[2][KQ];
+#pragma unroll
+  for (int y = 0; y < 2; y++) {
+    const int c = min(w0 + 16 * y + col, w1), t = c / G;
+    const uint16_t* qp = q + (sq.row + (int64_t)t) * ldq + ((int64_t)kvh * G + c - t * G) * HD + 8 * g;
+#pragma unroll
+    for (int x = 0; x < KQ; x++) qf[y][x] = *reinterpret_cast<const bf16x8*>(qp + 32 * x);
+  }
+  // steps: places v of the span, those between the sinks and the tile's window left out
+  const int vhole = (span.hole - span.cut + kStep - 1) / kStep * kStep;  // steps from here on hold no sink
+  const int low = mask.window ? p0 - mask.window + 1 : 0;                // the tile's first key behind the hole
+  const int vwin = low >= span.hole + span.gap ? v0 + min(max(0, low - span.cut - span.gap - v0), chunk) / kStep * kStep : 0;
+  auto skip = [&](int v) __attribute__((always_inline)) { return v >= vhole && v < vwin ? vwin : v; };
+  auto after = [&](int v) __attribute__((always_inline)) { return skip(v + kStep); };
+  const int32_t* pages = r.pages + (int64_t)b * r.max_pages;
+  const int shift = __builtin_ctz(r.page);
+  // a step's two groups: where their tokens are, and their first keys
+  struct Where {
+    int page[2], j[2];
+  };
+  auto where = [&](int v) __attribute__((always_inline)) {
+    Where w;
+#pragma unroll
+    for (int i = 0; i < 2; i++) {
+      const bool in = v + i * kGroup < vend;
+      w.j[i] = in ? span.real(v + i * kGroup) : kNowhere;
+      w.page[i] = in ? load_scalar(pages + (w.j[i] >> shift)) : -1;
+    }
+    return w;
+  };
+  // (a page that is not there is page 0 where no query sees it, so that the loads
+  // under way stay countable)
+  auto settle = [&](Where& w) __attribute__((always_inline)) {
+#pragma unroll
+    for (int i = 0; i < 2; i++)
+      if (w.page[i] < 0 || w.page[i] >= r.n_pages) {
+        w.page[i] = 0;
+        w.j[i] = kNowhere;
+      }
+  };
+  auto fetch = [&](const uint16_t* pool, const Where& w, u32x4* to) __attribute__((always_inline)) {
+#pragma unroll
+    for (int i = 0; i < LOADS; i++) {
+      // 1 KB pieces of both groups, one behind the other
+      const int piece = wave + 8 * i;
+      const bool second = HD == 128 ? i == 1 : wave >= 4;
+      const int64_t at = group_at(r, second ? w.page[1] : w.page[0], Hkv, kvh, second ? w.j[1] : w.j[0], HD);
+      load_lds(pool + at + (piece & (PIECES - 1)) * 512 + lane * 8, to + piece * 64);
+    }
+  };
+  f32x4 acc[2][ND] = {};
+  f32x4 sc[4][2];   // scores of a step
+  bf16x8 pf[2][2];  // its probabilities, by column tile and group
+  float m[2] = {-INFINITY, -INFINITY};
+  f32x4 l[2] = {};  // row sums: the product of the probabilities with ones, four times
+  const __bf16 one = (__bf16)1.0f;
+  const bf16x8 ones = {one, one, one, one, one, one, one, one};
+  // (two tiles by turns: a product waits for none of the three before it)
+  auto scores = [&](const u32x4* k) __attribute__((always_inline)) {
+#pragma unroll
+    for (int i = 0; i < 4; i += 2)
+#pragma unroll
+      for (int x = 0; x < KQ; x++)
+#pragma unroll
+        for (int e = 0; e < 2; e++) {
+          const bf16x8 kf = __builtin_bit_cast(bf16x8, k[((i + e) * KQ + x) * 64 + lane]);
+#pragma unroll
+          for (int y = 0; y < 2; y++)
+            sc[i + e][y] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, qf[y][x], x == 0 ? f32x4{} : sc[i + e][y], 0, 0, 0);
+        }
+  };
+  auto sums = [&]() __attribute__((always_inline)) {
+#pragma unroll
+    for (int x = 0; x < 2; x++)
+#pragma unroll
+      for (int y = 0; y < 2; y++) l[y] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ones, pf[y][x], l[y], 0, 0, 0);
+  };
+  auto add_values = [&](const u32x4* v) __attribute__((always_inline)) {
+    sums();
+#pragma unroll
+    for (int i = 0; i < ND; i += 2)
+#pragma unroll
+      for (int x = 0; x < 2; x++)
+#pragma unroll
+        for (int e = 0; e < 2; e++) {
+          const bf16x8 vf = __builtin_bit_cast(bf16x8, v[(x * ND + i + e) * 64 + lane]);
+#pragma unroll
+          for (int y = 0; y < 2; y++) acc[y][i + e] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, pf[y][x], acc[y][i + e], 0, 0, 0);
+        }
+  };
+  // a step works on place v, whose groups are at[0]; at[i]: those of the i-th step
+  // behind it; pages of the one after these are on their way
+  const bool late = wave >= 4;
+  Where at[kAhead + 2];
+  int v = skip(v0), ahead = v;
+#pragma unroll
+  for (int i = 0; i < kAhead + 2; i++) {
+    at[i] = where(ahead);
+    settle(at[i]);
+    ahead = after(ahead);
+  }
+  fetch(kc, at[0], sk[0]);
+#pragma unroll
+  for (int i = 0; i < kAhead; i++) {
+    fetch(kc, at[i + 1], sk[i + 1]);
+    fetch(vc, at[i], sv[i]);
+  }
+  wait_loads<kAhead * 2 * LOADS>();
+  meet();
+  if (works) scores(sk[0]);
+  int ring = 0;  // where the step's values are; the next step's keys: ring + 1
+  if (late) {
+    wait_loads<(kAhead - 1) * 2 * LOADS>();
+    meet();
+  }
+  while (v < v1) {
+    auto ask = [&]() __attribute__((always_inline)) {
+      // bundle t + kAhead: its place held bundle t - 1
+      const int to = ring == 0 ? kRing - 1 : ring - 1;
+      fetch(kc, at[kAhead + 1], sk[ring]);  // (keys are one place on)
+      fetch(vc, at[kAhead], sv[to]);
+    };
+    if (late) ask();
+    Where next = where(ahead);  // (used in the next step)
+    const bool whole = mask.all(q0, q1, at[0].j[0], at[0].j[0] + kGroup) && mask.all(q0, q1, at[0].j[1], at[0].j[1] + kGroup);
+    __builtin_amdgcn_sched_barrier(0);
+    if (works) {
+      if (!whole) {
+#pragma unroll
+        for (int i = 0; i < 4; i++)
+#pragma unroll
+          for (int y = 0; y < 2; y++)
+#pragma unroll
+            for (int e = 0; e < 4; e++)
+              if (!mask.sees(pos[y], mask.low(pos[y]), at[0].j[i >> 1] + 16 * (i & 1) + 4 * g + e)) sc[i][y][e] = -INFINITY;
+      }
+      float mx[2];
+#pragma unroll
+      for (int y = 0; y < 2; y++) {
+        float x = -INFINITY;
+#pragma unroll
+        for (int i = 0; i < 4; i++)
+#pragma unroll
+          for (int e = 0; e < 4; e++) x = fmaxf(x, sc[i][y][e]);
+        mx[y] = x * sl2;
+      }
+      // a column's reference moves only when a score passes it by 2^8
+      if (__ballot(mx[0] > m[0] + 8.0f || mx[1] > m[1] + 8.0f)) {
+#pragma unroll
+        for (int y = 0; y < 2; y++) {
+          float x = fmaxf(mx[y], __shfl_xor(mx[y], 16));
+          x = fmaxf(x, __shfl_xor(x, 32));
+          if (x > m[y] + 8.0f) {
+            const float a = __builtin_amdgcn_exp2f(m[y] - x);
+            l[y] *= a;
+#pragma unroll
+            for (int i = 0; i < ND; i++) acc[y][i] *= a;
+            m[y] = x;
+          }
+        }
+      }
+#pragma unroll
+      for (int y = 0; y < 2; y++) {
+        const float sub = m[y] == -INFINITY ? 0.f : -m[y];
+#pragma unroll
+        for (int i = 0; i < 4; i++) {
+          float p[4];
+#pragma unroll
+          for (int e = 0; e < 4; e++) p[e] = __builtin_amdgcn_exp2f(fmaf(sc[i][y][e], sl2, sub));
+          const bf16x2 lo = {(__bf16)p[0], (__bf16)p[1]}, hi = {(__bf16)p[2], (__bf16)p[3]};
+#pragma unroll
+          for (int e = 0; e < 2; e++) {
+            pf[y][i >> 1][(i & 1) * 4 + e] = lo[e];
+            pf[y][i >> 1][(i & 1) * 4 + 2 + e] = hi[e];
+          }
+        }
+      }
+      // (kept here: the compiler would move the exponentials to their use)
+      keep(pf);
+    }
+    __builtin_amdgcn_sched_barrier(0);
+    if (!late) wait_loads<(kAhead - 1) * 2 * LOADS>();
+    meet();
+    if (!late) ask();
+    __builtin_amdgcn_sched_barrier(0);
+    const int up = ring == kRing - 1 ? 0 : ring + 1;
+    if (works) {
+      if (whole) {
+        add_values(sv[ring]);
+        scores(sk[up]);
+        // operands read kReads ahead, two products to a read
+        __builtin_amdgcn_sched_group_barrier(0x100, kReads, 0);
+#pragma unroll
+        for (int i = 0; i < 2 + 2 * ND + 4 * KQ; i++) {
+          __builtin_amdgcn_sched_group_barrier(0x008, 2, 0);
+          __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+        }
+      } else {
+        sums();
+#pragma unroll
+        for (int x = 0; x < 2; x++) {
+          const bf16x8 p[2] = {pf[0][x], pf[1][x]};
+          add_masked_values([&](int i) __attribute__((always_inline)) { return sv[ring][(x * ND + i) * 64 + lane]; }, p, acc, mask,
+                            mask.seen(q0, q1, at[0].j[x]), pos, at[0].j[x]);
+        }
+        __builtin_amdgcn_sched_barrier(0);
+        scores(sk[up]);
+        __builtin_amdgcn_sched_group_barrier(0x100, kReads, 0);
+#pragma unroll
+        for (int i = 0; i < 4 * KQ; i++) {
+          __builtin_amdgcn_sched_group_barrier(0x008, 2, 0);
+          __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+        }
+      }
+    }
+    __builtin_amdgcn_sched_barrier(0);
+    if (late) wait_loads<(kAhead - 1) * 2 * LOADS>();
+    meet();
+    __builtin_amdgcn_sched_barrier(0);
+    ring = up;
+    v = after(v);
+    ahead = after(ahead);
+#pragma unroll
+    for (int i = 0; i < kAhead + 1; i++) at[i] = at[i + 1];
+    settle(next);
+    at[kAhead + 1] = next;
+  }
+  if (!late) meet();
+  wait_loads<0>();  // no load to LDS outlives the workgroup
+  if (!works) return;
+#pragma unroll
+  for (int y = 0; y < 2; y++) {
+    const int c = w0 + 16 * y + col, t = c / G;
+    const float L = l[y][0];
+    if (c > w1) continue;
+    const int64_t row = ((int64_t)sq.row + t) * Hkv * G + (int64_t)kvh * G + c - t * G;
+    if (only) {
+      const float inv = L == 0.f ? 0.f : 1.0f / L;  // (no visible key: zeros)
+      uint16_t* op = out + row * HD + 4 * g;
+#pragma unroll
+      for (int i = 0; i < ND; i++) {
+        uint2 w;
+        w.x = __builtin_bit_cast(uint32_t, bf16x2{(__bf16)(acc[y][i][0] * inv), (__bf16)(acc[y][i][1] * inv)});
+        w.y = __builtin_bit_cast(uint32_t, bf16x2{(__bf16)(acc[y][i][2] * inv), (__bf16)(acc[y][i][3] * inv)});
+        *reinterpret_cast<uint2*>(op + 16 * i) = w;
+      }
+    } else {
+      const int64_t to = row * (PREFIX ? plan.pre : plan.prompt.most) + split;
+#pragma unroll
+      for (int i = 0; i < ND; i++) *reinterpret_cast<f32x4*>((PREFIX ? plan.pre_o : plan.prompt_o) + to * HD + 16 * i + 4 * g) = acc[y][i];
+      if (g == 0) (PREFIX ? plan.pre_ml : plan.prompt_ml)[to] = make_float2(m[y], L);
+    }
+  }
+}
+
 // Joins the parts of a row and head: a wave each, first a lane per part (its
 // weight), then HD / 64 dims to a lane.
 template <int HD>
 __global__ __launch_bounds__(256) void attn_paged_join_kernel(Ragged r, int max_new, int Hkv, int G, AttnPlan plan, Mask mask,
                                                               uint16_t* __restrict__ out) {
-  const int lane = threadIdx.x & 63;
-  const int64_t at = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
-  const int Hq = Hkv * G, row = (int)(at / Hq), hq = (int)(at - (int64_t)row * Hq), kvh = hq / G;
-  if (row >= r.n) return;
-  const int b = last_at_most(r.B, row, [&](int i) { return (int64_t)r.starts[i]; });
-  const Seq q = sequence(r, b, max_new);
-  const int t = row - q.row;
-  if (t < 0 || t >= q.T) return;
-  const Span span = span_of(q, mask, plan.cut);
-  const int chunk = plan.split.chunk(span.total), nown = (span.total + chunk - 1) / chunk;
-  if (plan.cut == 0 && nown <= 1) return;  // written by the only split
-  const int64_t own = (((int64_t)b * Hkv + kvh) * plan.columns + t * G + (hq - kvh * G)) * plan.split.most, pre = at * plan.pre;
-  // parts: those of the prefix, then the sequence's own
-  const int n = plan.pre + nown;
-  float M = -INFINITY, ms[2], ls[2];
+  const int lane = threadIdx.x & 63, Hq = Hkv * G;
+  for (int64_t at = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6); at < (int64_t)r.n * Hq; at += (int64_t)gridDim.x * 4) {
+    const int row = (int)(at / Hq), hq = (int)(at - (int64_t)row * Hq), kvh = hq / G;
+    const int b = last_at_most(r.B, row, [&](int i) { return (int64_t)r.starts[i]; });
+    const Seq q = sequence(r, b, max_new);
+    const int t = row - q.row;
+    if (t < 0 || t >= q.T) continue;
+    const bool few = q.T * G <= plan.few;
+    const Span span = span_of(q, mask, plan.cut);
+    const int chunk = (few ? plan.split : plan.prompt).chunk(span.total), nown = (span.total + chunk - 1) / chunk;
+    if (plan.cut == 0 && nown <= 1) continue;  // written by the only split
+    const int64_t own = few ? (((int64_t)b * Hkv + kvh) * plan.columns + t * G + (hq - kvh * G)) * plan.split.most : at * plan.prompt.most;
+    const float2* own_ml = (few ? plan.pml : plan.prompt_ml) + own;
+    const float* own_o = (few ? plan.po : plan.prompt_o) + own * HD;
+    const float2* pre_ml = plan.pre_ml + at * plan.pre;
+    const float* pre_o = plan.pre_o + at * plan.pre * HD;
+    // parts: those of the prefix, then the sequence's own
+    const int n = plan.pre + nown;
+    float M = -INFINITY, ms[2], ls[2];
 #pragma unroll
-  for (int k = 0; k < 2; k++) {
-    const int i = lane + 64 * k;
-    const float2 ml = i < plan.pre ? plan.pre_ml[pre + i] : i < n ? plan.pml[own + i - plan.pre] : make_float2(-INFINITY, 0.f);
-    ms[k] = ml.x;
-    ls[k] = ml.y;
-    M = fmaxf(M, ml.x);
-  }
-  for (int o = 32; o; o >>= 1) M = fmaxf(M, __shfl_xor(M, o));
-  float L = 0.f, a[2];
+    for (int k = 0; k < 2; k++) {
+      const int i = lane + 64 * k;
+      const float2 ml = i < plan.pre ? pre_ml[i] : i < n ? own_ml[i - plan.pre] : make_float2(-INFINITY, 0.f);
+      ms[k] = ml.x;
+      ls[k] = ml.y;
+      M = fmaxf(M, ml.x);
+    }
+    for (int o = 32; o; o >>= 1) M = fmaxf(M, __shfl_xor(M, o));
+    float L = 0.f, a[2];
 #pragma unroll
-  for (int k = 0; k < 2; k++) {
-    // parts without a token that the query sees (m = -inf, l = 0) count for nothing
-    a[k] = ms[k] == -INFINITY && ls[k] == 0.f ? 0.f : __builtin_amdgcn_exp2f(ms[k] - M);
-    L += a[k] * ls[k];
-  }
-  for (int o = 32; o; o >>= 1) L += __shfl_xor(L, o);
-  typedef float f32xd __attribute__((ext_vector_type(HD / 64)));
-  f32xd acc = {};
-  for (int i = 0; i < n; i++) {
-    const float w = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, i < 64 ? a[0] : a[1]), i & 63));
-    const float* p = i < plan.pre ? plan.pre_o + (pre + i) * HD : plan.po + (own + i - plan.pre) * HD;
-    acc += w * reinterpret_cast<const f32xd*>(p)[lane];
-  }
-  const float inv = L == 0.f ? 0.f : 1.0f / L;
-  uint16_t* op = out + at * HD + lane * (HD / 64);
+    for (int k = 0; k < 2; k++) {
+      // parts without a token that the query sees (m = -inf, l = 0) count for nothing
+      a[k] = ms[k] == -INFINITY && ls[k] == 0.f ? 0.f : __builtin_amdgcn_exp2f(ms[k] - M);
+      L += a[k] * ls[k];
+    }
+    for (int o = 32; o; o >>= 1) L += __shfl_xor(L, o);
+    typedef float f32xd __attribute__((ext_vector_type(HD / 64)));
+    f32xd acc = {};
+    // 8 at a time, so that their loads are under way together
+    for (int i0 = 0; i0 < n; i0 += 8) {
+      f32xd x[8];
 #pragma unroll
-  for (int i = 0; i < HD / 64; i++) op[i] = f32_to_bf16(acc[i] * inv);
+      for (int k = 0; k < 8; k++) {
+        const int i = min(i0 + k, n - 1);
+        x[k] = reinterpret_cast<const f32xd*>(i < plan.pre ? pre_o + (int64_t)i * HD : own_o + (int64_t)(i - plan.pre) * HD)[lane];
+      }
+#pragma unroll
+      for (int k = 0; k < 8; k++) {
+        const int i = i0 + k;
+        const float w = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, i < 64 ? a[0] : a[1]), i & 63));
+        if (i < n && w != 0.f) acc += w * x[k];
+      }
+    }
+    const float inv = L == 0.f ? 0.f : 1.0f / L;
+    uint16_t* op = out + at * HD + lane * (HD / 64);
+#pragma unroll
+    for (int i = 0; i < HD / 64; i++) op[i] = f32_to_bf16(acc[i] * inv);
+  }
 }
 
 // Tokens that are computed for the batch: whole pairs of groups.
 int cut_of(int B, int shared) { return B > 1 ? shared / 64 * 64 : 0; }
 
+constexpr int kFew = 64;  // columns of a sequence that the form for few takes
+constexpr int kLeast = 512;
+
+int64_t slots_of(int n, int G, int B) { return (int64_t)n * G / kTileCols + B; }
+
 AttnPlan plan_of(int n, int B, int Hq, int Hkv, int hd, int max_new, int tokens, int shared, void* ws, int64_t* bytes) {
+  const int64_t cols = (int64_t)max_new * (Hq / Hkv);
   AttnPlan p{};
-  p.few = INT32_MAX;
-  p.columns = max_new * (Hq / Hkv);
+  p.few = kFew;
+  p.columns = (int)std::min<int64_t>(cols, kFew);
   p.cut = std::min(cut_of(B, shared), tokens);
   const int least = 256 * 128 / hd * 2;
-  p.split.unit = kWaves * kGroup;
-  p.split.least = least;
-  p.split.most = std::min(64, (tokens + least - 1) / least);
-  p.pre_chunk = std::max(least, (p.cut + 63) / 64);
-  p.pre_chunk = (p.pre_chunk + p.split.unit - 1) / p.split.unit * p.split.unit;
+  p.split = {std::min(64, (tokens + least - 1) / least), least, kWaves * kGroup};
+  const int64_t groups = (cols + kTileCols - 1) / kTileCols * Hkv;
+  p.prompt = {groups >= 128 ? 1 : (int)std::min<int64_t>({16, 256 / groups, (tokens + kLeast - 1) / kLeast}), kLeast, kStep};
+  p.pre_chunk = (std::max(kLeast, (p.cut + 63) / 64) + kStep * 4 - 1) / (kStep * 4) * (kStep * 4);
   p.pre = (p.cut + p.pre_chunk - 1) / p.pre_chunk;
-  const int64_t own = p.cut || p.split.most > 1 ? (int64_t)B * Hkv * p.columns * p.split.most : 0, pre = (int64_t)n * Hq * p.pre;
-  float* at = (float*)ws;
-  p.po = at;
-  p.pre_o = p.po + own * hd;
+  const int64_t own = p.cut || p.split.most > 1 ? (int64_t)B * Hkv * p.columns * p.split.most : 0;
+  const int64_t many = cols > kFew && (p.cut || p.prompt.most > 1) ? (int64_t)n * Hq * p.prompt.most : 0;
+  const int64_t pre = (int64_t)n * Hq * p.pre;
+  p.po = (float*)ws;
+  p.prompt_o = p.po + own * hd;
+  p.pre_o = p.prompt_o + many * hd;
   p.pml = (float2*)(p.pre_o + pre * hd);
-  p.pre_ml = p.pml + own;
-  if (bytes) *bytes = (own + pre) * (hd + 2) * 4;
+  p.prompt_ml = p.pml + own;
+  p.pre_ml = p.prompt_ml + many;
+  if (bytes) *bytes = (own + many + pre) * (hd + 2) * 4;
   return p;
 }
 
@@ -655,7 +1036,8 @@ int64_t paged_workspace_bytes(int n, int B, int Hq, int Hkv, int hd, int max_new
 }
 
 int64_t paged_workgroups(int n, int B, int Hq, int Hkv, int hd, int max_new, int tokens, int shared) {
-  return ((int64_t)max_new * (Hq / Hkv) + 15) / 16 * Hkv;
+  const AttnPlan p = plan_of(n, B, Hq, Hkv, hd, max_new, tokens, shared, nullptr, nullptr);
+  return slots_of(n, Hq / Hkv, B) * Hkv * std::max(p.prompt.most, p.pre);
 }
 
 hipError_t launch_paged_append(const AppendArgs& a, hipStream_t s) {
@@ -687,14 +1069,25 @@ hipError_t launch_attention_paged(const PagedAttnArgs& a, hipStream_t s) {
   const float sl2 = (float)(1.4426950408889634 * (double)a.scale);
   auto go = [&](auto h) {
     constexpr int HD = decltype(h)::value;
+    const int64_t cols = (int64_t)a.max_new * G;
+    auto split = [&](auto prefix, dim3 grid) {
+      hipLaunchKernelGGL((attn_paged_split_kernel<HD, 1, decltype(prefix)::value>), grid, kWaves * 64, 0, s, a.q, a.ldq, a.kc, a.vc, r,
+                         a.max_new, a.Hkv, G, plan, mask, sl2, a.out);
+    };
+    auto prompt = [&](auto prefix, int64_t slots, int splits) {
+      hipLaunchKernelGGL((attn_paged_prompt_kernel<HD, decltype(prefix)::value>), (unsigned)(slots * splits * a.Hkv), 512, 0, s, a.q, a.ldq,
+                         a.kc, a.vc, r, a.max_new, a.Hkv, G, plan, mask, sl2, (int)slots, splits, a.out);
+    };
     if (plan.cut) {
-      const dim3 grid(plan.pre, (unsigned)(((int64_t)r.n * G + 15) / 16 * a.Hkv));
-      hipLaunchKernelGGL((attn_paged_split_kernel<HD, 1, true>), grid, kWaves * 64, 0, s, a.q, a.ldq, a.kc, a.vc, r, a.max_new, a.Hkv, G, plan, mask, sl2, a.out);
+      const int64_t all = (int64_t)r.n * G;
+      if (all <= kFew) split(std::true_type{}, dim3(plan.pre, (unsigned)((all + 15) / 16 * a.Hkv)));
+      else prompt(std::true_type{}, (all + kTileCols - 1) / kTileCols, plan.pre);
     }
-    const dim3 grid(plan.split.most, (unsigned)(((int64_t)a.max_new * G + 15) / 16 * a.Hkv), r.B);
-    hipLaunchKernelGGL((attn_paged_split_kernel<HD, 1, false>), grid, kWaves * 64, 0, s, a.q, a.ldq, a.kc, a.vc, r, a.max_new, a.Hkv, G, plan, mask, sl2, a.out);
-    if (plan.cut || plan.split.most > 1)
-      hipLaunchKernelGGL((attn_paged_join_kernel<HD>), (unsigned)(((int64_t)r.n * a.Hq + 3) / 4), 256, 0, s, r, a.max_new, a.Hkv, G, plan, mask, a.out);
+    split(std::false_type{}, dim3(plan.split.most, (unsigned)((plan.columns + 15) / 16 * a.Hkv), r.B));
+    if (cols > kFew) prompt(std::false_type{}, slots_of(r.n, G, r.B), plan.prompt.most);
+    if (plan.cut || plan.split.most > 1 || (cols > kFew && plan.prompt.most > 1))
+      hipLaunchKernelGGL((attn_paged_join_kernel<HD>), (unsigned)std::min<int64_t>(((int64_t)r.n * a.Hq + 3) / 4, 1 << 20), 256, 0, s, r,
+                         a.max_new, a.Hkv, G, plan, mask, a.out);
   };
   if (a.hd == 64) go(std::integral_constant<int, 64>{});
   else go(std::integral_constant<int, 128>{});
