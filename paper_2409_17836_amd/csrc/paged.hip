@@ -336,12 +336,15 @@ __device__ inline u32x4 words_of(uint32_t tokens, int g) {
   return w;
 }
 
-// O^T += V^T P^T for a group of keys that some, but not all, of a wave's queries
-// see.  A probability of zero times a NaN or an infinity is NaN.  So the values
-// of tokens that no query sees (all but `seen`), which may be anything, are
-// cleared; and tokens with a value that is not finite are left to products of
-// their own, which only the columns that see them take.  value(i): a lane's
-// operand of dims 16 i ..; pf, pos: of the lane's columns; o: their results.
+// Masked values.  A probability of zero times a NaN or an infinity is NaN.  The
+// values of tokens that no query sees (all but `seen`), which may be anything,
+// are cleared before the product.  What some queries see and others do not is
+// numbers as a rule: the products are taken as they are, and only where a result
+// comes out as none the wave does its columns again, this way:
+// O^T += V^T P^T for a group of keys, tokens with a value that is not finite left
+// to products of their own, which only the columns that see them take.  value(i):
+// a lane's operand of dims 16 i ..; pf, pos: of the lane's columns; o: their
+// results.
 template <int ND, int NT, class Value>
 __device__ inline void add_masked_values(Value value, const bf16x8 (&pf)[NT], f32x4 (&o)[NT][ND], const Mask& mask, uint32_t seen,
                                          const int (&pos)[NT], int j0) {
@@ -388,6 +391,115 @@ __device__ inline void add_masked_values(Value value, const bf16x8 (&pf)[NT], f3
     }
   }
 }
+
+// The running softmax of a wave's 16 NT columns.
+template <int HD, int NT>
+struct Columns {
+  static constexpr int KQ = HD / 32, ND = HD / 16;
+  float m[NT];
+  f32x4 l[NT], o[NT][ND];  // row sums (four times), O^T: 4 dims of 16 each
+  // Groups v, v + step, .. of the span up to v1: S^T = K Q^T, an online softmax,
+  // O^T += V^T P^T.  EXACT: where masked values may be no numbers.
+  template <bool EXACT>
+  __device__ inline void walk(const bf16x8 (&qf)[NT][KQ], const uint16_t* kc, const uint16_t* vc, const Ragged& r, const int32_t* pages, int Hkv,
+                              int kvh, const Span& span, int v, int v1, int step, int p0, int p1, const int (&pos)[NT], const Mask& mask,
+                              float sl2) {
+    const int lane = threadIdx.x & 63, g = lane >> 4;
+#pragma unroll
+    for (int y = 0; y < NT; y++) {
+      m[y] = -INFINITY;
+      l[y] = f32x4{};
+#pragma unroll
+      for (int i = 0; i < ND; i++) o[y][i] = f32x4{};
+    }
+    const __bf16 one = (__bf16)1.0f;
+    const bf16x8 ones = {one, one, one, one, one, one, one, one};
+    int held = -1;
+    for (int it = 0; v < v1; v += step, it++) {
+      // a lane holds the page of each of the wave's next 64 groups
+      if ((it & 63) == 0) {
+        const int64_t mine = v + (int64_t)lane * step;
+        held = mine < v1 ? pages[span.real((int)mine) >> __builtin_ctz(r.page)] : -1;
+      }
+      const int page = __builtin_amdgcn_readlane(held, it & 63), j0 = span.real(v);
+      if (page < 0 || page >= r.n_pages || !mask.any(p0, p1, j0, j0 + kGroup)) continue;
+      const int64_t at = group_at(r, page, Hkv, kvh, j0, HD);
+      const __amdgpu_buffer_rsrc_t kb = buffer(kc + at, kGroup * HD * 2), vb = buffer(vc + at, kGroup * HD * 2);
+      u32x4 kr[2 * KQ], vr[ND];
+#pragma unroll
+      for (int i = 0; i < 2 * KQ; i++) kr[i] = __builtin_amdgcn_raw_buffer_load_b128(kb, lane * 16, i * 1024, 0);
+#pragma unroll
+      for (int i = 0; i < ND; i++) vr[i] = __builtin_amdgcn_raw_buffer_load_b128(vb, lane * 16, i * 1024, 0);
+      const bool whole = mask.all(p0, p1, j0, j0 + kGroup);
+      bf16x8 pf[NT];
+#pragma unroll
+      for (int y = 0; y < NT; y++) {
+        f32x4 s[2] = {};
+#pragma unroll
+        for (int i = 0; i < 2; i++)
+#pragma unroll
+          for (int x = 0; x < KQ; x++)
+            s[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, kr[i * KQ + x]), qf[y][x], s[i], 0, 0, 0);
+        if (!whole) {
+          const int low = mask.low(pos[y]);
+#pragma unroll
+          for (int i = 0; i < 2; i++)
+#pragma unroll
+            for (int e = 0; e < 4; e++)
+              if (!mask.sees(pos[y], low, j0 + 16 * i + 4 * g + e)) s[i][e] = -INFINITY;
+        }
+        float mx = -INFINITY;
+#pragma unroll
+        for (int i = 0; i < 2; i++)
+#pragma unroll
+          for (int e = 0; e < 4; e++) mx = fmaxf(mx, s[i][e]);  // (drops a NaN; it comes back through the exponential)
+        mx = fmaxf(mx, __shfl_xor(mx, 16));
+        mx = fmaxf(mx, __shfl_xor(mx, 32)) * sl2;
+        if (mx > m[y]) {
+          const float a = __builtin_amdgcn_exp2f(m[y] - mx);
+          l[y] *= a;
+#pragma unroll
+          for (int i = 0; i < ND; i++) o[y][i] *= a;
+          m[y] = mx;
+        }
+        const float sub = m[y] == -INFINITY ? 0.f : -m[y];
+        // rounded to bf16 for the second product; the sum is of the rounded values
+#pragma unroll
+        for (int i = 0; i < 2; i++)
+#pragma unroll
+          for (int e = 0; e < 4; e++) pf[y][4 * i + e] = (__bf16)__builtin_amdgcn_exp2f(fmaf(s[i][e], sl2, sub));
+        l[y] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ones, pf[y], l[y], 0, 0, 0);
+      }
+      const uint32_t seen = mask.seen(p0, p1, j0);
+      if (EXACT) {
+        add_masked_values([&](int i) __attribute__((always_inline)) { return vr[i]; }, pf, o, mask, seen, pos, j0);
+      } else {
+        if (seen != ~0u) {
+          const u32x4 keep = words_of(seen, g);
+#pragma unroll
+          for (int i = 0; i < ND; i++) vr[i] &= keep;
+        }
+#pragma unroll
+        for (int i = 0; i < ND; i++)
+#pragma unroll
+          for (int y = 0; y < NT; y++)
+            o[y][i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, vr[i]), pf[y], o[y][i], 0, 0, 0);
+      }
+    }
+  }
+  // Whether some number of any column's result is none: then what a masked value
+  // was may have come in.
+  __device__ inline bool odd() const {
+    float x = 0.f;
+#pragma unroll
+    for (int y = 0; y < NT; y++)
+#pragma unroll
+      for (int i = 0; i < ND; i++)
+#pragma unroll
+        for (int e = 0; e < 4; e++) x = fmaf(o[y][i][e], 0.f, x);
+    return __ballot(!(x == 0.f)) != 0;
+  }
+};
 
 // ---- few columns
 // Columns: column c = t G + i of a (sequence, key/value head) is query head
@@ -460,85 +572,10 @@ __global__ __launch_bounds__(kWaves * 64, HD == 64 ? 4 : 3) void attn_paged_spli
 #pragma unroll
     for (int x = 0; x < KQ; x++) qf[y][x] = *reinterpret_cast<const bf16x8*>(qrow + t * ldq + (c - t * G) * HD + 32 * x);
   }
-  float m[NT];
-  f32x4 l[NT], o[NT][ND];
-#pragma unroll
-  for (int y = 0; y < NT; y++) {
-    m[y] = -INFINITY;
-    l[y] = f32x4{};
-#pragma unroll
-    for (int i = 0; i < ND; i++) o[y][i] = f32x4{};
-  }
-  const __bf16 one = (__bf16)1.0f;
-  const bf16x8 ones = {one, one, one, one, one, one, one, one};
+  Columns<HD, NT> x;
   const int32_t* pages = r.pages + (int64_t)b * r.max_pages;
-  int held = -1;
-  int it = 0;
-  for (int v = v0 + wave * kGroup; v < v1; v += NW * kGroup, it++) {
-    // a lane holds the page of each of the wave's next 64 groups
-    if ((it & 63) == 0) {
-      const int mine = v + lane * (NW * kGroup);
-      held = mine < v1 ? pages[span.real(mine) >> __builtin_ctz(r.page)] : -1;
-    }
-    const int page = __builtin_amdgcn_readlane(held, it & 63), j0 = span.real(v);
-    if (page < 0 || page >= r.n_pages || !mask.any(p0, p1, j0, j0 + kGroup)) continue;
-    const int64_t at = group_at(r, page, Hkv, kvh, j0, HD);
-    const __amdgpu_buffer_rsrc_t kb = buffer(kc + at, kGroup * HD * 2), vb = buffer(vc + at, kGroup * HD * 2);
-    u32x4 kr[2 * KQ], vr[ND];
-#pragma unroll
-    for (int i = 0; i < 2 * KQ; i++) kr[i] = __builtin_amdgcn_raw_buffer_load_b128(kb, lane * 16, i * 1024, 0);
-#pragma unroll
-    for (int i = 0; i < ND; i++) vr[i] = __builtin_amdgcn_raw_buffer_load_b128(vb, lane * 16, i * 1024, 0);
-    const bool whole = mask.all(p0, p1, j0, j0 + kGroup);
-    bf16x8 pf[NT];
-#pragma unroll
-    for (int y = 0; y < NT; y++) {
-      f32x4 s[2] = {};
-#pragma unroll
-      for (int i = 0; i < 2; i++)
-#pragma unroll
-        for (int x = 0; x < KQ; x++)
-          s[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, kr[i * KQ + x]), qf[y][x], s[i], 0, 0, 0);
-      if (!whole) {
-        const int low = mask.low(pos[y]);
-#pragma unroll
-        for (int i = 0; i < 2; i++)
-#pragma unroll
-          for (int e = 0; e < 4; e++)
-            if (!mask.sees(pos[y], low, j0 + 16 * i + 4 * g + e)) s[i][e] = -INFINITY;
-      }
-      float mx = -INFINITY;
-#pragma unroll
-      for (int i = 0; i < 2; i++)
-#pragma unroll
-        for (int e = 0; e < 4; e++) mx = fmaxf(mx, s[i][e]);  // (drops a NaN; it comes back through the exponential)
-      mx = fmaxf(mx, __shfl_xor(mx, 16));
-      mx = fmaxf(mx, __shfl_xor(mx, 32)) * sl2;
-      if (mx > m[y]) {
-        const float a = __builtin_amdgcn_exp2f(m[y] - mx);
-        l[y] *= a;
-#pragma unroll
-        for (int i = 0; i < ND; i++) o[y][i] *= a;
-        m[y] = mx;
-      }
-      const float sub = m[y] == -INFINITY ? 0.f : -m[y];
-      // rounded to bf16 for the second product; the sum is of the rounded values
-#pragma unroll
-      for (int i = 0; i < 2; i++)
-#pragma unroll
-        for (int e = 0; e < 4; e++) pf[y][4 * i + e] = (__bf16)__builtin_amdgcn_exp2f(fmaf(s[i][e], sl2, sub));
-      l[y] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ones, pf[y], l[y], 0, 0, 0);
-    }
-    if (whole) {
-#pragma unroll
-      for (int i = 0; i < ND; i++)
-#pragma unroll
-        for (int y = 0; y < NT; y++)
-          o[y][i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, vr[i]), pf[y], o[y][i], 0, 0, 0);
-    } else {
-      add_masked_values([&](int i) __attribute__((always_inline)) { return vr[i]; }, pf, o, mask, mask.seen(p0, p1, j0), pos, j0);
-    }
-  }
+  x.template walk<false>(qf, kc, vc, r, pages, Hkv, kvh, span, v0 + wave * kGroup, v1, NW * kGroup, p0, p1, pos, mask, sl2);
+  if (x.odd()) x.template walk<true>(qf, kc, vc, r, pages, Hkv, kvh, span, v0 + wave * kGroup, v1, NW * kGroup, p0, p1, pos, mask, sl2);
   // HD / (4 NW) dims of a column to a thread
   constexpr int DT = HD / (4 * NW);
   typedef float f32xd __attribute__((ext_vector_type(DT)));
@@ -546,11 +583,11 @@ __global__ __launch_bounds__(kWaves * 64, HD == 64 ? 4 : 3) void attn_paged_spli
   for (int y = 0; y < NT; y++) {
     if (y) __syncthreads();
     if (g == 0) {
-      sm[wave][col] = m[y];
-      sl[wave][col] = l[y][0];
+      sm[wave][col] = x.m[y];
+      sl[wave][col] = x.l[y][0];
     }
 #pragma unroll
-    for (int i = 0; i < ND; i++) *reinterpret_cast<f32x4*>(&so[wave][col][16 * i + 4 * g]) = o[y][i];
+    for (int i = 0; i < ND; i++) *reinterpret_cast<f32x4*>(&so[wave][col][16 * i + 4 * g]) = x.o[y][i];
     __syncthreads();
     const int oc = tid / (4 * NW), d0 = tid % (4 * NW) * DT, c = c0 + 16 * y + oc;
     if (16 * y + oc >= ncol) continue;
@@ -724,32 +761,42 @@ __global__ __launch_bounds__(512, 2) void attn_paged_prompt_kernel(
       load_lds(pool + at + (piece & (PIECES - 1)) * 512 + lane * 8, to + piece * 64);
     }
   };
-  f32x4 acc[2][ND] = {};
+  Columns<HD, 2> cs = {};
+  f32x4(&acc)[2][ND] = cs.o;
   f32x4 sc[4][2];   // scores of a step
   bf16x8 pf[2][2];  // its probabilities, by column tile and group
-  float m[2] = {-INFINITY, -INFINITY};
-  f32x4 l[2] = {};  // row sums: the product of the probabilities with ones, four times
+  float(&m)[2] = cs.m;
+  m[0] = m[1] = -INFINITY;
+  f32x4(&l)[2] = cs.l;  // the product of the probabilities with ones
   const __bf16 one = (__bf16)1.0f;
   const bf16x8 ones = {one, one, one, one, one, one, one, one};
   // (two tiles by turns: a product waits for none of the three before it)
-  auto scores = [&](const u32x4* k) __attribute__((always_inline)) {
+  auto scores = [&](auto key) __attribute__((always_inline)) {
 #pragma unroll
     for (int i = 0; i < 4; i += 2)
 #pragma unroll
       for (int x = 0; x < KQ; x++)
 #pragma unroll
         for (int e = 0; e < 2; e++) {
-          const bf16x8 kf = __builtin_bit_cast(bf16x8, k[((i + e) * KQ + x) * 64 + lane]);
+          const bf16x8 kf = __builtin_bit_cast(bf16x8, key(i + e, x));
 #pragma unroll
           for (int y = 0; y < 2; y++)
             sc[i + e][y] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, qf[y][x], x == 0 ? f32x4{} : sc[i + e][y], 0, 0, 0);
         }
+  };
+  auto held = [&](const u32x4* k) __attribute__((always_inline)) {
+    return [=](int i, int x) __attribute__((always_inline)) { return k[(i * KQ + x) * 64 + lane]; };
   };
   auto sums = [&]() __attribute__((always_inline)) {
 #pragma unroll
     for (int x = 0; x < 2; x++)
 #pragma unroll
       for (int y = 0; y < 2; y++) l[y] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ones, pf[y][x], l[y], 0, 0, 0);
+  };
+  auto add_value = [&](int i, int x, u32x4 w) __attribute__((always_inline)) {
+#pragma unroll
+    for (int y = 0; y < 2; y++)
+      acc[y][i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, w), pf[y][x], acc[y][i], 0, 0, 0);
   };
   auto add_values = [&](const u32x4* v) __attribute__((always_inline)) {
     sums();
@@ -758,12 +805,71 @@ __global__ __launch_bounds__(512, 2) void attn_paged_prompt_kernel(
 #pragma unroll
       for (int x = 0; x < 2; x++)
 #pragma unroll
-        for (int e = 0; e < 2; e++) {
-          const bf16x8 vf = __builtin_bit_cast(bf16x8, v[(x * ND + i + e) * 64 + lane]);
-#pragma unroll
-          for (int y = 0; y < 2; y++) acc[y][i + e] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, pf[y][x], acc[y][i + e], 0, 0, 0);
-        }
+        for (int e = 0; e < 2; e++) add_value(i + e, x, v[(x * ND + i + e) * 64 + lane]);
   };
+  // Clears, in the wave's part of a step's values, the tokens that no query of the
+  // tile sees.
+  auto clear = [&](u32x4* v, const Where& w) __attribute__((always_inline)) {
+#pragma unroll
+    for (int i = 0; i < LOADS; i++) {
+      const uint32_t seen = mask.seen(p0, p1, HD == 128 ? w.j[i & 1] : wave >= 4 ? w.j[1] : w.j[0]);
+      if (seen != ~0u) v[(wave + 8 * i) * 64 + lane] &= words_of(seen, g);
+    }
+  };
+  // scores to probabilities
+  auto soften = [&](const Where& w, bool whole) __attribute__((always_inline)) {
+    if (!whole) {
+#pragma unroll
+      for (int i = 0; i < 4; i++)
+#pragma unroll
+        for (int y = 0; y < 2; y++)
+#pragma unroll
+          for (int e = 0; e < 4; e++)
+            if (!mask.sees(pos[y], mask.low(pos[y]), w.j[i >> 1] + 16 * (i & 1) + 4 * g + e)) sc[i][y][e] = -INFINITY;
+    }
+    float mx[2];
+#pragma unroll
+    for (int y = 0; y < 2; y++) {
+      float x = -INFINITY;
+#pragma unroll
+      for (int i = 0; i < 4; i++)
+#pragma unroll
+        for (int e = 0; e < 4; e++) x = fmaxf(x, sc[i][y][e]);
+      mx[y] = x * sl2;
+    }
+    // a column's reference moves only when a score passes it by 2^8
+    if (__ballot(mx[0] > m[0] + 8.0f || mx[1] > m[1] + 8.0f)) {
+#pragma unroll
+      for (int y = 0; y < 2; y++) {
+        float x = fmaxf(mx[y], __shfl_xor(mx[y], 16));
+        x = fmaxf(x, __shfl_xor(x, 32));
+        if (x > m[y] + 8.0f) {
+          const float a = __builtin_amdgcn_exp2f(m[y] - x);
+          l[y] *= a;
+#pragma unroll
+          for (int i = 0; i < ND; i++) acc[y][i] *= a;
+          m[y] = x;
+        }
+      }
+    }
+#pragma unroll
+    for (int y = 0; y < 2; y++) {
+      const float sub = m[y] == -INFINITY ? 0.f : -m[y];
+#pragma unroll
+      for (int i = 0; i < 4; i++) {
+        float p[4];
+#pragma unroll
+        for (int e = 0; e < 4; e++) p[e] = __builtin_amdgcn_exp2f(fmaf(sc[i][y][e], sl2, sub));
+        const bf16x2 lo = {(__bf16)p[0], (__bf16)p[1]}, hi = {(__bf16)p[2], (__bf16)p[3]};
+#pragma unroll
+        for (int e = 0; e < 2; e++) {
+          pf[y][i >> 1][(i & 1) * 4 + e] = lo[e];
+          pf[y][i >> 1][(i & 1) * 4 + 2 + e] = hi[e];
+        }
+      }
+    }
+  };
+
   // a step works on place v, whose groups are at[0]; at[i]: those of the i-th step
   // behind it; pages of the one after these are on their way
   const bool late = wave >= 4;
@@ -783,10 +889,11 @@ __global__ __launch_bounds__(512, 2) void attn_paged_prompt_kernel(
   }
   wait_loads<kAhead * 2 * LOADS>();
   meet();
-  if (works) scores(sk[0]);
+  if (works) scores(held(sk[0]));
   int ring = 0;  // where the step's values are; the next step's keys: ring + 1
   if (late) {
     wait_loads<(kAhead - 1) * 2 * LOADS>();
+    clear(sv[0], at[0]);
     meet();
   }
   while (v < v1) {
@@ -801,96 +908,35 @@ __global__ __launch_bounds__(512, 2) void attn_paged_prompt_kernel(
     const bool whole = mask.all(q0, q1, at[0].j[0], at[0].j[0] + kGroup) && mask.all(q0, q1, at[0].j[1], at[0].j[1] + kGroup);
     __builtin_amdgcn_sched_barrier(0);
     if (works) {
-      if (!whole) {
-#pragma unroll
-        for (int i = 0; i < 4; i++)
-#pragma unroll
-          for (int y = 0; y < 2; y++)
-#pragma unroll
-            for (int e = 0; e < 4; e++)
-              if (!mask.sees(pos[y], mask.low(pos[y]), at[0].j[i >> 1] + 16 * (i & 1) + 4 * g + e)) sc[i][y][e] = -INFINITY;
-      }
-      float mx[2];
-#pragma unroll
-      for (int y = 0; y < 2; y++) {
-        float x = -INFINITY;
-#pragma unroll
-        for (int i = 0; i < 4; i++)
-#pragma unroll
-          for (int e = 0; e < 4; e++) x = fmaxf(x, sc[i][y][e]);
-        mx[y] = x * sl2;
-      }
-      // a column's reference moves only when a score passes it by 2^8
-      if (__ballot(mx[0] > m[0] + 8.0f || mx[1] > m[1] + 8.0f)) {
-#pragma unroll
-        for (int y = 0; y < 2; y++) {
-          float x = fmaxf(mx[y], __shfl_xor(mx[y], 16));
-          x = fmaxf(x, __shfl_xor(x, 32));
-          if (x > m[y] + 8.0f) {
-            const float a = __builtin_amdgcn_exp2f(m[y] - x);
-            l[y] *= a;
-#pragma unroll
-            for (int i = 0; i < ND; i++) acc[y][i] *= a;
-            m[y] = x;
-          }
-        }
-      }
-#pragma unroll
-      for (int y = 0; y < 2; y++) {
-        const float sub = m[y] == -INFINITY ? 0.f : -m[y];
-#pragma unroll
-        for (int i = 0; i < 4; i++) {
-          float p[4];
-#pragma unroll
-          for (int e = 0; e < 4; e++) p[e] = __builtin_amdgcn_exp2f(fmaf(sc[i][y][e], sl2, sub));
-          const bf16x2 lo = {(__bf16)p[0], (__bf16)p[1]}, hi = {(__bf16)p[2], (__bf16)p[3]};
-#pragma unroll
-          for (int e = 0; e < 2; e++) {
-            pf[y][i >> 1][(i & 1) * 4 + e] = lo[e];
-            pf[y][i >> 1][(i & 1) * 4 + 2 + e] = hi[e];
-          }
-        }
-      }
+      soften(at[0], whole);
       // (kept here: the compiler would move the exponentials to their use)
       keep(pf);
     }
     __builtin_amdgcn_sched_barrier(0);
-    if (!late) wait_loads<(kAhead - 1) * 2 * LOADS>();
+    if (!late) {
+      wait_loads<(kAhead - 1) * 2 * LOADS>();
+      clear(sv[ring], at[0]);
+    }
     meet();
     if (!late) ask();
     __builtin_amdgcn_sched_barrier(0);
     const int up = ring == kRing - 1 ? 0 : ring + 1;
     if (works) {
-      if (whole) {
-        add_values(sv[ring]);
-        scores(sk[up]);
-        // operands read kReads ahead, two products to a read
-        __builtin_amdgcn_sched_group_barrier(0x100, kReads, 0);
+      // operands read kReads ahead, two products to a read
+      add_values(sv[ring]);
+      scores(held(sk[up]));
+      __builtin_amdgcn_sched_group_barrier(0x100, kReads, 0);
 #pragma unroll
-        for (int i = 0; i < 2 + 2 * ND + 4 * KQ; i++) {
-          __builtin_amdgcn_sched_group_barrier(0x008, 2, 0);
-          __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
-        }
-      } else {
-        sums();
-#pragma unroll
-        for (int x = 0; x < 2; x++) {
-          const bf16x8 p[2] = {pf[0][x], pf[1][x]};
-          add_masked_values([&](int i) __attribute__((always_inline)) { return sv[ring][(x * ND + i) * 64 + lane]; }, p, acc, mask,
-                            mask.seen(q0, q1, at[0].j[x]), pos, at[0].j[x]);
-        }
-        __builtin_amdgcn_sched_barrier(0);
-        scores(sk[up]);
-        __builtin_amdgcn_sched_group_barrier(0x100, kReads, 0);
-#pragma unroll
-        for (int i = 0; i < 4 * KQ; i++) {
-          __builtin_amdgcn_sched_group_barrier(0x008, 2, 0);
-          __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
-        }
+      for (int i = 0; i < 2 + 2 * ND + 4 * KQ; i++) {
+        __builtin_amdgcn_sched_group_barrier(0x008, 2, 0);
+        __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
       }
     }
     __builtin_amdgcn_sched_barrier(0);
-    if (late) wait_loads<(kAhead - 1) * 2 * LOADS>();
+    if (late) {
+      wait_loads<(kAhead - 1) * 2 * LOADS>();
+      clear(sv[up], at[1]);
+    }
     meet();
     __builtin_amdgcn_sched_barrier(0);
     ring = up;
@@ -904,6 +950,29 @@ __global__ __launch_bounds__(512, 2) void attn_paged_prompt_kernel(
   if (!late) meet();
   wait_loads<0>();  // no load to LDS outlives the workgroup
   if (!works) return;
+  if (cs.odd()) {
+    // once more, by itself and in the same order
+    cs = Columns<HD, 2>{};
+    m[0] = m[1] = -INFINITY;
+    for (v = skip(v0); v < v1; v = after(v)) {
+      Where w = where(v);
+      settle(w);
+      auto group = [&](const uint16_t* pool, int x) __attribute__((always_inline)) {
+        return reinterpret_cast<const u32x4*>(pool + group_at(r, w.page[x], Hkv, kvh, w.j[x], HD)) + lane;
+      };
+      const u32x4* k[2] = {group(kc, 0), group(kc, 1)};
+      scores([&](int i, int x) __attribute__((always_inline)) { return k[i >> 1][((i & 1) * KQ + x) * 64]; });
+      soften(w, false);
+      sums();
+#pragma unroll
+      for (int x = 0; x < 2; x++) {
+        const bf16x8 p[2] = {pf[0][x], pf[1][x]};
+        const u32x4* values = group(vc, x);
+        add_masked_values([&](int i) __attribute__((always_inline)) { return values[i * 64]; }, p, acc, mask, mask.seen(q0, q1, w.j[x]), pos,
+                          w.j[x]);
+      }
+    }
+  }
 #pragma unroll
   for (int y = 0; y < 2; y++) {
     const int c = w0 + 16 * y + col, t = c / G;
@@ -931,17 +1000,36 @@ __global__ __launch_bounds__(512, 2) void attn_paged_prompt_kernel(
 
 // Joins the parts of a row and head: a wave each, first a lane per part (its
 // weight), then HD / 64 dims to a lane.
-template <int HD>
+//
+// ROWS: all rows (those of few columns only behind a prefix); else the columns
+// of sequences with few of them.
+template <int HD, bool ROWS>
 __global__ __launch_bounds__(256) void attn_paged_join_kernel(Ragged r, int max_new, int Hkv, int G, AttnPlan plan, Mask mask,
                                                               uint16_t* __restrict__ out) {
   const int lane = threadIdx.x & 63, Hq = Hkv * G;
-  for (int64_t at = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6); at < (int64_t)r.n * Hq; at += (int64_t)gridDim.x * 4) {
-    const int row = (int)(at / Hq), hq = (int)(at - (int64_t)row * Hq), kvh = hq / G;
-    const int b = last_at_most(r.B, row, [&](int i) { return (int64_t)r.starts[i]; });
-    const Seq q = sequence(r, b, max_new);
-    const int t = row - q.row;
+  const int64_t count = ROWS ? (int64_t)r.n * Hq : (int64_t)r.B * Hkv * plan.columns;
+  for (int64_t i = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6); i < count; i += (int64_t)gridDim.x * 4) {
+    int b, t, hq;
+    Seq q;
+    if (ROWS) {
+      const int row = (int)(i / Hq);
+      hq = (int)(i - (int64_t)row * Hq);
+      b = last_at_most(r.B, row, [&](int k) { return (int64_t)r.starts[k]; });
+      q = sequence(r, b, max_new);
+      t = row - q.row;
+    } else {
+      const int64_t head = i / plan.columns;
+      const int c = (int)(i - head * plan.columns);
+      b = (int)(head / Hkv);
+      q = sequence(r, b, max_new);
+      t = c / G;
+      hq = (int)(head - (int64_t)b * Hkv) * G + c - t * G;
+    }
     if (t < 0 || t >= q.T) continue;
     const bool few = q.T * G <= plan.few;
+    if (few == ROWS && plan.cut == 0) continue;  // the other's
+    const int kvh = hq / G;
+    const int64_t at = ((int64_t)q.row + t) * Hq + hq;
     const Span span = span_of(q, mask, plan.cut);
     const int chunk = (few ? plan.split : plan.prompt).chunk(span.total), nown = (span.total + chunk - 1) / chunk;
     if (plan.cut == 0 && nown <= 1) continue;  // written by the only split
@@ -955,8 +1043,8 @@ __global__ __launch_bounds__(256) void attn_paged_join_kernel(Ragged r, int max_
     float M = -INFINITY, ms[2], ls[2];
 #pragma unroll
     for (int k = 0; k < 2; k++) {
-      const int i = lane + 64 * k;
-      const float2 ml = i < plan.pre ? pre_ml[i] : i < n ? own_ml[i - plan.pre] : make_float2(-INFINITY, 0.f);
+      const int e = lane + 64 * k;
+      const float2 ml = e < plan.pre ? pre_ml[e] : e < n ? own_ml[e - plan.pre] : make_float2(-INFINITY, 0.f);
       ms[k] = ml.x;
       ls[k] = ml.y;
       M = fmaxf(M, ml.x);
@@ -973,24 +1061,24 @@ __global__ __launch_bounds__(256) void attn_paged_join_kernel(Ragged r, int max_
     typedef float f32xd __attribute__((ext_vector_type(HD / 64)));
     f32xd acc = {};
     // 8 at a time, so that their loads are under way together
-    for (int i0 = 0; i0 < n; i0 += 8) {
+    for (int e0 = 0; e0 < n; e0 += 8) {
       f32xd x[8];
 #pragma unroll
       for (int k = 0; k < 8; k++) {
-        const int i = min(i0 + k, n - 1);
-        x[k] = reinterpret_cast<const f32xd*>(i < plan.pre ? pre_o + (int64_t)i * HD : own_o + (int64_t)(i - plan.pre) * HD)[lane];
+        const int e = min(e0 + k, n - 1);
+        x[k] = reinterpret_cast<const f32xd*>(e < plan.pre ? pre_o + (int64_t)e * HD : own_o + (int64_t)(e - plan.pre) * HD)[lane];
       }
 #pragma unroll
       for (int k = 0; k < 8; k++) {
-        const int i = i0 + k;
-        const float w = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, i < 64 ? a[0] : a[1]), i & 63));
-        if (i < n && w != 0.f) acc += w * x[k];
+        const int e = e0 + k;
+        const float w = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, e < 64 ? a[0] : a[1]), e & 63));
+        if (e < n && w != 0.f) acc += w * x[k];
       }
     }
     const float inv = L == 0.f ? 0.f : 1.0f / L;
     uint16_t* op = out + at * HD + lane * (HD / 64);
 #pragma unroll
-    for (int i = 0; i < HD / 64; i++) op[i] = f32_to_bf16(acc[i] * inv);
+    for (int e = 0; e < HD / 64; e++) op[e] = f32_to_bf16(acc[e] * inv);
   }
 }
 
@@ -1085,9 +1173,12 @@ hipError_t launch_attention_paged(const PagedAttnArgs& a, hipStream_t s) {
     }
     split(std::false_type{}, dim3(plan.split.most, (unsigned)((plan.columns + 15) / 16 * a.Hkv), r.B));
     if (cols > kFew) prompt(std::false_type{}, slots_of(r.n, G, r.B), plan.prompt.most);
-    if (plan.cut || plan.split.most > 1 || (cols > kFew && plan.prompt.most > 1))
-      hipLaunchKernelGGL((attn_paged_join_kernel<HD>), (unsigned)std::min<int64_t>(((int64_t)r.n * a.Hq + 3) / 4, 1 << 20), 256, 0, s, r,
-                         a.max_new, a.Hkv, G, plan, mask, a.out);
+    auto join = [&](auto rows, int64_t count) {
+      hipLaunchKernelGGL((attn_paged_join_kernel<HD, decltype(rows)::value>), (unsigned)std::min<int64_t>((count + 3) / 4, 1 << 20), 256, 0, s,
+                         r, a.max_new, a.Hkv, G, plan, mask, a.out);
+    };
+    if (plan.cut || (cols > kFew && plan.prompt.most > 1)) join(std::true_type{}, (int64_t)r.n * a.Hq);
+    if (!plan.cut && plan.split.most > 1) join(std::false_type{}, (int64_t)r.B * a.Hkv * plan.columns);
   };
   if (a.hd == 64) go(std::integral_constant<int, 64>{});
   else go(std::integral_constant<int, 128>{});
