@@ -7,13 +7,14 @@
 
 namespace lmgc {
 
-// 16 bytes a lane from memory to LDS, lane l's at lds + 16 l.  In assembly:
-// with the builtin the compiler waits for every load before any read of the
-// ring; the waits are written out where they belong (wait_loads).
-__device__ inline void load_lds(const void* p, void* lds) {
-  const uint32_t at = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)lds;
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off"
-               :: "s"(__builtin_amdgcn_readfirstlane((int)at)), "v"(p) : "m0", "memory");
+// 16 bytes a lane from p (the same for all lanes) + at bytes to LDS, lane l's at
+// lds + 16 l.  In assembly: with the builtin the compiler waits for every load
+// before any read of the ring; the waits are written out where they belong
+// (wait_loads).
+__device__ inline void load_lds(const void* p, uint32_t at, void* lds) {
+  const uint32_t to = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)lds;
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2"
+               :: "s"(__builtin_amdgcn_readfirstlane((int)to)), "v"(at), "s"(p) : "m0", "memory");
 }
 
 // Waits until at most n of the wave's loads are under way.
@@ -42,10 +43,6 @@ __device__ inline void keep(T (&x)[n][k]) {
 #pragma unroll
     for (int j = 0; j < k; j++) asm volatile("" : "+v"(x[i][j]));
 }
-
-// A number that is the same for all lanes, from memory that the kernel does not
-// write: a scalar load, which the loads to LDS do not count.
-__device__ inline int load_scalar(const int32_t* p) { return *(const __attribute__((address_space(4))) int32_t*)(uintptr_t)p; }
 
 }  // namespace lmgc
 

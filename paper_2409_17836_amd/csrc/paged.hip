@@ -324,6 +324,12 @@ __device__ inline __amdgpu_buffer_rsrc_t buffer(const uint16_t* p, int bytes) {
   return __builtin_amdgcn_make_buffer_rsrc(const_cast<uint16_t*>(p), (short)0, bytes, 0x00020000);
 }
 
+// A score where bit `at` of `seen` is set, else -inf.
+__device__ inline float hide(float s, uint32_t seen, int at) {
+  const int t = (int)(seen << (31 - at)) >> 31;
+  return __builtin_bit_cast(float, (__builtin_bit_cast(int, s) & t) | ((int)0xff800000 & ~t));
+}
+
 // The words of a lane's 8 values (tokens 4 g .. + 3 of both halves of a group)
 // with only those of `tokens`, a bit each.
 __device__ inline u32x4 words_of(uint32_t tokens, int g) {
@@ -441,12 +447,11 @@ struct Columns {
           for (int x = 0; x < KQ; x++)
             s[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, kr[i * KQ + x]), qf[y][x], s[i], 0, 0, 0);
         if (!whole) {
-          const int low = mask.low(pos[y]);
+          const uint32_t seen = mask.seen(pos[y], pos[y], j0) >> (4 * g);
 #pragma unroll
           for (int i = 0; i < 2; i++)
 #pragma unroll
-            for (int e = 0; e < 4; e++)
-              if (!mask.sees(pos[y], low, j0 + 16 * i + 4 * g + e)) s[i][e] = -INFINITY;
+            for (int e = 0; e < 4; e++) s[i][e] = hide(s[i][e], seen, 16 * i + e);
         }
         float mx = -INFINITY;
 #pragma unroll
@@ -719,46 +724,60 @@ __global__ __launch_bounds__(512, 2) void attn_paged_prompt_kernel(
 #pragma unroll
     for (int x = 0; x < KQ; x++) qf[y][x] = *reinterpret_cast<const bf16x8*>(qp + 32 * x);
   }
-  // steps: places v of the span, those between the sinks and the tile's window left out
-  const int vhole = (span.hole - span.cut + kStep - 1) / kStep * kStep;  // steps from here on hold no sink
-  const int low = mask.window ? p0 - mask.window + 1 : 0;                // the tile's first key behind the hole
-  const int vwin = low >= span.hole + span.gap ? v0 + min(max(0, low - span.cut - span.gap - v0), chunk) / kStep * kStep : 0;
-  auto skip = [&](int v) __attribute__((always_inline)) { return v >= vhole && v < vwin ? vwin : v; };
-  auto after = [&](int v) __attribute__((always_inline)) { return skip(v + kStep); };
+  keep(qf);  // (arrived: a wait for them further on would be one for all loads)
+  // Step k is place v0 + 64 k of the span, and `jump` more from step `hole` on:
+  // those between the sinks and the tile's window are left out.
+  const int hole = max(0, (span.hole - span.cut - v0 + kStep - 1) / kStep);
+  const int low = mask.window ? p0 - mask.window + 1 : 0;  // the tile's first key behind the hole
+  const int vlow = low >= span.hole + span.gap ? min(low - span.cut - span.gap, vend) : 0, vhole = v0 + hole * kStep;
+  const int jump = max(0, vlow - vhole) / kStep * kStep;
+  const int steps = v1 <= vhole ? (v1 - v0 + kStep - 1) / kStep : hole + max(0, v1 - vhole - jump + kStep - 1) / kStep;
   const int32_t* pages = r.pages + (int64_t)b * r.max_pages;
-  const int shift = __builtin_ctz(r.page);
-  // a step's two groups: where their tokens are, and their first keys
-  struct Where {
-    int page[2], j[2];
-  };
-  auto where = [&](int v) __attribute__((always_inline)) {
-    Where w;
+  const int stride = Hkv * r.page * HD;  // numbers of a page
+  const uint16_t *kp = kc + (int64_t)kvh * r.page * HD, *vp = vc + (int64_t)kvh * r.page * HD;
+  // A lane has one of 64 steps from step `first` on: its two groups' first keys and
+  // pages.  (A page that is not there is page 0 where no query sees it, so that the
+  // loads under way stay countable.)  And a bit for each of them: whether every
+  // query of the wave sees every key, and whether some key is seen by none of the
+  // tile.
+  int key[2], page[2], first;
+  uint64_t whole, partly;
+  auto look = [&](int k0) __attribute__((always_inline)) {
+    first = k0;
+    const int k = k0 + lane, v = v0 + k * kStep + (k >= hole ? jump : 0);
+    bool all = true, none = false;
 #pragma unroll
     for (int i = 0; i < 2; i++) {
-      const bool in = v + i * kGroup < vend;
-      w.j[i] = in ? span.real(v + i * kGroup) : kNowhere;
-      w.page[i] = in ? load_scalar(pages + (w.j[i] >> shift)) : -1;
+      const bool in = k < steps + kAhead + 1 && v + i * kGroup < vend;
+      key[i] = in ? span.real(v + i * kGroup) : kNowhere;
+      page[i] = in ? pages[key[i] >> __builtin_ctz(r.page)] : -1;
+      const bool there = (uint32_t)page[i] < (uint32_t)r.n_pages;
+      page[i] = there ? page[i] : 0;
+      key[i] = there ? key[i] : kNowhere;
+      all = all && mask.all(q0, q1, key[i], key[i] + kGroup);
+      none = none || mask.seen(p0, p1, key[i]) != ~0u;
     }
-    return w;
+    whole = __ballot(all);
+    partly = __ballot(none);
   };
-  // (a page that is not there is page 0 where no query sees it, so that the loads
-  // under way stay countable)
-  auto settle = [&](Where& w) __attribute__((always_inline)) {
+  struct Where {
+    int64_t at[2];  // numbers of a pool before the groups
+  };
+  auto key_of = [&](int k, int i) __attribute__((always_inline)) { return __builtin_amdgcn_readlane(key[i], k - first); };
+  auto where = [&](int k) __attribute__((always_inline)) {
+    Where w;
 #pragma unroll
     for (int i = 0; i < 2; i++)
-      if (w.page[i] < 0 || w.page[i] >= r.n_pages) {
-        w.page[i] = 0;
-        w.j[i] = kNowhere;
-      }
+      w.at[i] = (int64_t)__builtin_amdgcn_readlane(page[i], k - first) * stride + (key_of(k, i) & (r.page - 1)) * HD;
+    return w;
   };
   auto fetch = [&](const uint16_t* pool, const Where& w, u32x4* to) __attribute__((always_inline)) {
 #pragma unroll
     for (int i = 0; i < LOADS; i++) {
       // 1 KB pieces of both groups, one behind the other
       const int piece = wave + 8 * i;
-      const bool second = HD == 128 ? i == 1 : wave >= 4;
-      const int64_t at = group_at(r, second ? w.page[1] : w.page[0], Hkv, kvh, second ? w.j[1] : w.j[0], HD);
-      load_lds(pool + at + (piece & (PIECES - 1)) * 512 + lane * 8, to + piece * 64);
+      const int64_t at = HD == 128 ? w.at[i & 1] : wave >= 4 ? w.at[1] : w.at[0];
+      load_lds(pool + at + (piece & (PIECES - 1)) * 512, lane * 16, to + piece * 64);
     }
   };
   Columns<HD, 2> cs = {};
@@ -809,23 +828,27 @@ __global__ __launch_bounds__(512, 2) void attn_paged_prompt_kernel(
   };
   // Clears, in the wave's part of a step's values, the tokens that no query of the
   // tile sees.
-  auto clear = [&](u32x4* v, const Where& w) __attribute__((always_inline)) {
+  auto clear = [&](u32x4* v, int k) __attribute__((always_inline)) {
+    if (!(partly >> (k - first) & 1)) return;
 #pragma unroll
     for (int i = 0; i < LOADS; i++) {
-      const uint32_t seen = mask.seen(p0, p1, HD == 128 ? w.j[i & 1] : wave >= 4 ? w.j[1] : w.j[0]);
-      if (seen != ~0u) v[(wave + 8 * i) * 64 + lane] &= words_of(seen, g);
+      const uint32_t seen = mask.seen(p0, p1, HD == 128 ? key_of(k, i & 1) : wave >= 4 ? key_of(k, 1) : key_of(k, 0));
+      v[(wave + 8 * i) * 64 + lane] &= words_of(seen, g);
     }
   };
   // scores to probabilities
-  auto soften = [&](const Where& w, bool whole) __attribute__((always_inline)) {
-    if (!whole) {
+  auto soften = [&](int k) __attribute__((always_inline)) {
+    if (!(whole >> (k - first) & 1)) {
 #pragma unroll
-      for (int i = 0; i < 4; i++)
+      for (int y = 0; y < 2; y++)
 #pragma unroll
-        for (int y = 0; y < 2; y++)
+        for (int x = 0; x < 2; x++) {
+          const uint32_t seen = mask.seen(pos[y], pos[y], key_of(k, x)) >> (4 * g);
 #pragma unroll
-          for (int e = 0; e < 4; e++)
-            if (!mask.sees(pos[y], mask.low(pos[y]), w.j[i >> 1] + 16 * (i & 1) + 4 * g + e)) sc[i][y][e] = -INFINITY;
+          for (int i = 0; i < 2; i++)
+#pragma unroll
+            for (int e = 0; e < 4; e++) sc[2 * x + i][y][e] = hide(sc[2 * x + i][y][e], seen, 16 * i + e);
+        }
     }
     float mx[2];
 #pragma unroll
@@ -870,52 +893,48 @@ __global__ __launch_bounds__(512, 2) void attn_paged_prompt_kernel(
     }
   };
 
-  // a step works on place v, whose groups are at[0]; at[i]: those of the i-th step
-  // behind it; pages of the one after these are on their way
   const bool late = wave >= 4;
-  Where at[kAhead + 2];
-  int v = skip(v0), ahead = v;
+  look(0);
+  {
+    Where w = where(0);
+    fetch(kp, w, sk[0]);
 #pragma unroll
-  for (int i = 0; i < kAhead + 2; i++) {
-    at[i] = where(ahead);
-    settle(at[i]);
-    ahead = after(ahead);
+    for (int i = 0; i < kAhead; i++) {
+      fetch(vp, w, sv[i]);
+      w = where(i + 1);
+      fetch(kp, w, sk[i + 1]);
+    }
   }
-  fetch(kc, at[0], sk[0]);
-#pragma unroll
-  for (int i = 0; i < kAhead; i++) {
-    fetch(kc, at[i + 1], sk[i + 1]);
-    fetch(vc, at[i], sv[i]);
-  }
+  Where last = where(kAhead);  // of the keys asked for last: their values are next
   wait_loads<kAhead * 2 * LOADS>();
   meet();
   if (works) scores(held(sk[0]));
   int ring = 0;  // where the step's values are; the next step's keys: ring + 1
   if (late) {
     wait_loads<(kAhead - 1) * 2 * LOADS>();
-    clear(sv[0], at[0]);
+    clear(sv[0], 0);
     meet();
   }
-  while (v < v1) {
+  for (int k = 0; k < steps; k++) {
+    if (k - first == 32) look(k);
     auto ask = [&]() __attribute__((always_inline)) {
       // bundle t + kAhead: its place held bundle t - 1
       const int to = ring == 0 ? kRing - 1 : ring - 1;
-      fetch(kc, at[kAhead + 1], sk[ring]);  // (keys are one place on)
-      fetch(vc, at[kAhead], sv[to]);
+      fetch(vp, last, sv[to]);
+      last = where(k + kAhead + 1);
+      fetch(kp, last, sk[ring]);  // (keys are one place on)
     };
     if (late) ask();
-    Where next = where(ahead);  // (used in the next step)
-    const bool whole = mask.all(q0, q1, at[0].j[0], at[0].j[0] + kGroup) && mask.all(q0, q1, at[0].j[1], at[0].j[1] + kGroup);
     __builtin_amdgcn_sched_barrier(0);
     if (works) {
-      soften(at[0], whole);
+      soften(k);
       // (kept here: the compiler would move the exponentials to their use)
       keep(pf);
     }
     __builtin_amdgcn_sched_barrier(0);
     if (!late) {
       wait_loads<(kAhead - 1) * 2 * LOADS>();
-      clear(sv[ring], at[0]);
+      clear(sv[ring], k);
     }
     meet();
     if (!late) ask();
@@ -935,17 +954,11 @@ __global__ __launch_bounds__(512, 2) void attn_paged_prompt_kernel(
     __builtin_amdgcn_sched_barrier(0);
     if (late) {
       wait_loads<(kAhead - 1) * 2 * LOADS>();
-      clear(sv[up], at[1]);
+      clear(sv[up], k + 1);
     }
     meet();
     __builtin_amdgcn_sched_barrier(0);
     ring = up;
-    v = after(v);
-    ahead = after(ahead);
-#pragma unroll
-    for (int i = 0; i < kAhead + 1; i++) at[i] = at[i + 1];
-    settle(next);
-    at[kAhead + 1] = next;
   }
   if (!late) meet();
   wait_loads<0>();  // no load to LDS outlives the workgroup
@@ -954,22 +967,21 @@ __global__ __launch_bounds__(512, 2) void attn_paged_prompt_kernel(
     // once more, by itself and in the same order
     cs = Columns<HD, 2>{};
     m[0] = m[1] = -INFINITY;
-    for (v = skip(v0); v < v1; v = after(v)) {
-      Where w = where(v);
-      settle(w);
-      auto group = [&](const uint16_t* pool, int x) __attribute__((always_inline)) {
-        return reinterpret_cast<const u32x4*>(pool + group_at(r, w.page[x], Hkv, kvh, w.j[x], HD)) + lane;
-      };
-      const u32x4* k[2] = {group(kc, 0), group(kc, 1)};
-      scores([&](int i, int x) __attribute__((always_inline)) { return k[i >> 1][((i & 1) * KQ + x) * 64]; });
-      soften(w, false);
+    look(0);
+    for (int k = 0; k < steps; k++) {
+      if (k - first == 32) look(k);
+      const Where w = where(k);
+      auto group = [&](const uint16_t* pool, int x) __attribute__((always_inline)) { return reinterpret_cast<const u32x4*>(pool + w.at[x]) + lane; };
+      const u32x4* keys[2] = {group(kp, 0), group(kp, 1)};
+      scores([&](int i, int x) __attribute__((always_inline)) { return keys[i >> 1][((i & 1) * KQ + x) * 64]; });
+      soften(k);
       sums();
 #pragma unroll
       for (int x = 0; x < 2; x++) {
         const bf16x8 p[2] = {pf[0][x], pf[1][x]};
-        const u32x4* values = group(vc, x);
-        add_masked_values([&](int i) __attribute__((always_inline)) { return values[i * 64]; }, p, acc, mask, mask.seen(q0, q1, w.j[x]), pos,
-                          w.j[x]);
+        const u32x4* values = group(vp, x);
+        add_masked_values([&](int i) __attribute__((always_inline)) { return values[i * 64]; }, p, acc, mask,
+                          mask.seen(q0, q1, key_of(k, x)), pos, key_of(k, x));
       }
     }
   }

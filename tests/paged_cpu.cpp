@@ -53,7 +53,8 @@ struct CpuLoad {
 };
 static std::deque<CpuLoad> g_loads[1024];
 namespace lmgc {
-inline void load_lds(const void* p, void* lds) {
+inline void load_lds(const void* p, uint32_t at, void* lds) {
+  p = (const char*)p + at;
   volatile char probe = *(const volatile char*)p;
   (void)probe;
   const CpuLoad l{p, (char*)lds + 16 * (threadIdx.x & 63)};
@@ -68,7 +69,6 @@ void wait_loads() {
 inline void meet() { __syncthreads(); }
 template <class T, int n, int k>
 void keep(T (&)[n][k]) {}
-inline int load_scalar(const int32_t* p) { return *p; }
 }  // namespace lmgc
 inline float2 make_float2(float a, float b) { return {a, b}; }
 static int min(int a, int b) { return a < b ? a : b; }
