@@ -631,40 +631,50 @@ __global__ __launch_bounds__(kWaves * 64, HD == 64 ? 4 : 3) void attn_paged_spli
 // matrix operands; the products read a lane's 16 bytes in a row.
 //
 // A step has two phases, a barrier after each: one for the vector unit (maxima,
-// exponentials), one for the matrix unit (the step's values, the next step's
-// scores).  The waves of a SIMD, w and w + 4, are a phase apart, so that the
-// units work side by side.  Phases counted from the start: waves 0 to 3 have
-// step t's phases at 2 t and 2 t + 1, waves 4 to 7 one later.  So values t and
-// keys t + 1 (bundle t) are read in phases 2 t + 1 and 2 t + 2, have arrived by
-// the end of phase 2 t (each wave waits for its own part before that barrier),
-// and their place is free from phase 2 t + 3 on: bundle t + kAhead is asked for in
-// phase 2 t + 1, into a ring of kAhead + 1.
+// exponentials; and the loads are asked for), one for the matrix unit (the step's
+// values, the next step's scores).  The waves of a SIMD, w and w + 4, are a phase
+// apart, so that the units work side by side.  Phases counted from the start:
+// waves 0 to 3 have step t's phases at 2 t and 2 t + 1, waves 4 to 7 one later.  So
+// values t and keys t + 1 (bundle t) are read in phases 2 t + 1 and 2 t + 2, have
+// arrived by the end of phase 2 t (each wave waits for its own part before that
+// barrier), and their place, one of kRing, is free from phase 2 t + 3 on: bundle s
+// may be asked for from phase 2 (s - kRing) + 3 on, which for waves 4 to 7 is step s
+// - kAhead's first phase, and for waves 0 to 3 that of the step after it.
 constexpr int kTileCols = 256;
 constexpr int kStep = 2 * kGroup;
-constexpr int kAhead = 2, kRing = kAhead + 1;
+constexpr int kAhead = 3, kRing = kAhead + 1;
 constexpr int kReads = 8;          // operands read ahead of their products
 constexpr int kNowhere = 1 << 30;  // where no query sees a key
 
 template <int HD, bool PREFIX>
 __global__ __launch_bounds__(512, 2) void attn_paged_prompt_kernel(
     const uint16_t* __restrict__ q, int64_t ldq, const uint16_t* __restrict__ kc, const uint16_t* __restrict__ vc, Ragged r, int max_new,
-    int Hkv, int G, AttnPlan plan, Mask mask, float sl2, int nslot, int nsplit, uint16_t* __restrict__ out) {
+    int Hkv, int G, AttnPlan plan, Mask mask, float sl2, int nslot, int by_turns, int nsplit, uint16_t* __restrict__ out) {
   constexpr int ND = HD / 16, KQ = HD / 32;  // dim tiles; 32-dim steps of a score
   constexpr int PIECES = HD / 16;            // KB of a group of keys (or values)
   constexpr int LOADS = 2 * PIECES / 8;      // KB of a step's keys (or values) to a wave
   __shared__ u32x4 sk[kRing][2 * PIECES * 64], sv[kRing][2 * PIECES * 64];
   // heads fastest: with a multiple of eight heads all tiles of a head run on one
-  // XCD and share its L2; the longest tiles first
-  const int kvh = blockIdx.x % Hkv, rest = blockIdx.x / Hkv, split = rest % nsplit, slot = nslot - 1 - rest / nsplit;
+  // XCD and share its L2
+  const int kvh = blockIdx.x % Hkv, rest = blockIdx.x / Hkv, split = rest % nsplit, slot = rest / nsplit;
   const int tid = threadIdx.x, lane = tid & 63, col = lane & 15, g = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   int b = 0, c0 = slot * kTileCols;
   Seq sq{0, r.n, 0};
   if (!PREFIX) {
-    // slot starts[b] G / 256 + b + i is tile i of sequence b
-    b = last_at_most(r.B, slot, [&](int i) { return (int64_t)r.starts[i] * G / kTileCols + i; });
-    sq = sequence(r, b, max_new);
-    const int64_t tile = slot - ((int64_t)sq.row * G / kTileCols + b);
+    int64_t tile;
+    if (by_turns) {
+      // the sequences' last tiles, the longest, then those before them, ..
+      b = slot % r.B;
+      sq = sequence(r, b, max_new);
+      tile = ((int64_t)sq.T * G + kTileCols - 1) / kTileCols - 1 - slot / r.B;
+    } else {
+      // place starts[b] G / 256 + b + i is tile i of sequence b
+      const int64_t place = nslot - 1 - slot;
+      b = last_at_most(r.B, place, [&](int i) { return (int64_t)r.starts[i] * G / kTileCols + i; });
+      sq = sequence(r, b, max_new);
+      tile = place - ((int64_t)sq.row * G / kTileCols + b);
+    }
     if (sq.T <= 0 || tile < 0 || tile * kTileCols >= (int64_t)sq.T * G || sq.T * G <= plan.few) return;
     c0 = (int)tile * kTileCols;
   }
@@ -894,37 +904,28 @@ __global__ __launch_bounds__(512, 2) void attn_paged_prompt_kernel(
   };
 
   const bool late = wave >= 4;
+  const int ahead = late ? kAhead : kAhead - 1;
   look(0);
-  {
-    Where w = where(0);
-    fetch(kp, w, sk[0]);
-#pragma unroll
-    for (int i = 0; i < kAhead; i++) {
-      fetch(vp, w, sv[i]);
-      w = where(i + 1);
-      fetch(kp, w, sk[i + 1]);
-    }
-  }
-  Where last = where(kAhead);  // of the keys asked for last: their values are next
-  wait_loads<kAhead * 2 * LOADS>();
+  Where last = where(0);  // of the keys asked for last: their values are next
+  fetch(kp, last, sk[0]);
+  auto ask = [&](int s) __attribute__((always_inline)) {
+    const int to = s & (kRing - 1);
+    fetch(vp, last, sv[to]);
+    last = where(s + 1);
+    fetch(kp, last, sk[(to + 1) & (kRing - 1)]);
+  };
+  for (int s = 0; s < ahead; s++) ask(s);
+  wait_loads<(kAhead - 1) * 2 * LOADS>();
   meet();
   if (works) scores(held(sk[0]));
-  int ring = 0;  // where the step's values are; the next step's keys: ring + 1
   if (late) {
-    wait_loads<(kAhead - 1) * 2 * LOADS>();
-    clear(sv[0], 0);
+    clear(sv[0], 0);  // (bundle 0 has arrived)
     meet();
   }
   for (int k = 0; k < steps; k++) {
     if (k - first == 32) look(k);
-    auto ask = [&]() __attribute__((always_inline)) {
-      // bundle t + kAhead: its place held bundle t - 1
-      const int to = ring == 0 ? kRing - 1 : ring - 1;
-      fetch(vp, last, sv[to]);
-      last = where(k + kAhead + 1);
-      fetch(kp, last, sk[ring]);  // (keys are one place on)
-    };
-    if (late) ask();
+    ask(k + ahead);
+    const int ring = k & (kRing - 1), up = (k + 1) & (kRing - 1);  // of the step's values; of the next step's keys
     __builtin_amdgcn_sched_barrier(0);
     if (works) {
       soften(k);
@@ -937,9 +938,7 @@ __global__ __launch_bounds__(512, 2) void attn_paged_prompt_kernel(
       clear(sv[ring], k);
     }
     meet();
-    if (!late) ask();
     __builtin_amdgcn_sched_barrier(0);
-    const int up = ring == kRing - 1 ? 0 : ring + 1;
     if (works) {
       // operands read kReads ahead, two products to a read
       add_values(sv[ring]);
@@ -958,7 +957,6 @@ __global__ __launch_bounds__(512, 2) void attn_paged_prompt_kernel(
     }
     meet();
     __builtin_amdgcn_sched_barrier(0);
-    ring = up;
   }
   if (!late) meet();
   wait_loads<0>();  // no load to LDS outlives the workgroup
@@ -1100,7 +1098,18 @@ int cut_of(int B, int shared) { return B > 1 ? shared / 64 * 64 : 0; }
 constexpr int kFew = 64;  // columns of a sequence that the form for few takes
 constexpr int kLeast = 512;
 
-int64_t slots_of(int n, int G, int B) { return (int64_t)n * G / kTileCols + B; }
+// Workgroups for the tiles of many columns of one head and split: as many tiles of
+// every sequence as the longest may have, by turns, so that the longest tiles run
+// first; where that were many more than there are, the places that the rows take at
+// most (two prompts of 3001 rows: the last workgroups end 15 % later).
+struct Tiles {
+  int64_t count;
+  int by_turns;
+};
+Tiles tiles_of(int n, int G, int B, int64_t cols) {
+  const int64_t places = (int64_t)n * G / kTileCols + B, turns = (cols + kTileCols - 1) / kTileCols * B;
+  return turns <= 2 * places ? Tiles{turns, 1} : Tiles{places, 0};
+}
 
 AttnPlan plan_of(int n, int B, int Hq, int Hkv, int hd, int max_new, int tokens, int shared, void* ws, int64_t* bytes) {
   const int64_t cols = (int64_t)max_new * (Hq / Hkv);
@@ -1137,7 +1146,7 @@ int64_t paged_workspace_bytes(int n, int B, int Hq, int Hkv, int hd, int max_new
 
 int64_t paged_workgroups(int n, int B, int Hq, int Hkv, int hd, int max_new, int tokens, int shared) {
   const AttnPlan p = plan_of(n, B, Hq, Hkv, hd, max_new, tokens, shared, nullptr, nullptr);
-  return slots_of(n, Hq / Hkv, B) * Hkv * std::max(p.prompt.most, p.pre);
+  return tiles_of(n, Hq / Hkv, B, (int64_t)max_new * (Hq / Hkv)).count * Hkv * std::max(p.prompt.most, p.pre);
 }
 
 hipError_t launch_paged_append(const AppendArgs& a, hipStream_t s) {
@@ -1174,17 +1183,20 @@ hipError_t launch_attention_paged(const PagedAttnArgs& a, hipStream_t s) {
       hipLaunchKernelGGL((attn_paged_split_kernel<HD, 1, decltype(prefix)::value>), grid, kWaves * 64, 0, s, a.q, a.ldq, a.kc, a.vc, r,
                          a.max_new, a.Hkv, G, plan, mask, sl2, a.out);
     };
-    auto prompt = [&](auto prefix, int64_t slots, int splits) {
+    auto prompt = [&](auto prefix, int64_t slots, int by_turns, int splits) {
       hipLaunchKernelGGL((attn_paged_prompt_kernel<HD, decltype(prefix)::value>), (unsigned)(slots * splits * a.Hkv), 512, 0, s, a.q, a.ldq,
-                         a.kc, a.vc, r, a.max_new, a.Hkv, G, plan, mask, sl2, (int)slots, splits, a.out);
+                         a.kc, a.vc, r, a.max_new, a.Hkv, G, plan, mask, sl2, (int)slots, by_turns, splits, a.out);
     };
     if (plan.cut) {
       const int64_t all = (int64_t)r.n * G;
       if (all <= kFew) split(std::true_type{}, dim3(plan.pre, (unsigned)((all + 15) / 16 * a.Hkv)));
-      else prompt(std::true_type{}, (all + kTileCols - 1) / kTileCols, plan.pre);
+      else prompt(std::true_type{}, (all + kTileCols - 1) / kTileCols, 0, plan.pre);
     }
     split(std::false_type{}, dim3(plan.split.most, (unsigned)((plan.columns + 15) / 16 * a.Hkv), r.B));
-    if (cols > kFew) prompt(std::false_type{}, slots_of(r.n, G, r.B), plan.prompt.most);
+    if (cols > kFew) {
+      const Tiles t = tiles_of(r.n, G, r.B, cols);
+      prompt(std::false_type{}, t.count, t.by_turns, plan.prompt.most);
+    }
     auto join = [&](auto rows, int64_t count) {
       hipLaunchKernelGGL((attn_paged_join_kernel<HD, decltype(rows)::value>), (unsigned)std::min<int64_t>((count + 3) / 4, 1 << 20), 256, 0, s,
                          r, a.max_new, a.Hkv, G, plan, mask, a.out);
