@@ -7,14 +7,16 @@
 
 namespace lmgc {
 
+// A place in LDS.
+typedef uint32_t LdsAt;
+__device__ inline LdsAt lds_at(void* p) { return (LdsAt)(uintptr_t)(__attribute__((address_space(3))) char*)p; }
+
 // 16 bytes a lane from p (the same for all lanes) + at bytes to LDS, lane l's at
-// lds + 16 l.  In assembly: with the builtin the compiler waits for every load
+// to + 16 l.  In assembly: with the builtin the compiler waits for every load
 // before any read of the ring; the waits are written out where they belong
 // (wait_loads).
-__device__ inline void load_lds(const void* p, uint32_t at, void* lds) {
-  const uint32_t to = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)lds;
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2"
-               :: "s"(__builtin_amdgcn_readfirstlane((int)to)), "v"(at), "s"(p) : "m0", "memory");
+__device__ inline void load_lds(const void* p, uint32_t at, LdsAt to) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" :: "s"(to), "v"(at), "s"(p) : "m0", "memory");
 }
 
 // Waits until at most n of the wave's loads are under way.
@@ -34,14 +36,12 @@ __device__ inline void meet() {
   asm volatile("" ::: "memory");
 }
 
-// Holds the values where they are: the compiler would move what makes them to
-// their use.
-template <class T, int n, int k>
-__device__ inline void keep(T (&x)[n][k]) {
+// Holds values where they are: the compiler would move what makes them to their
+// use.
+template <class T, int n>
+__device__ inline void keep(T (&x)[n]) {
 #pragma unroll
-  for (int i = 0; i < n; i++)
-#pragma unroll
-    for (int j = 0; j < k; j++) asm volatile("" : "+v"(x[i][j]));
+  for (int i = 0; i < n; i++) asm volatile("" : "+v"(x[i]));
 }
 
 }  // namespace lmgc

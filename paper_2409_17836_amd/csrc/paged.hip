@@ -630,20 +630,20 @@ __global__ __launch_bounds__(kWaves * 64, HD == 64 ? 4 : 3) void attn_paged_spli
 // and values come straight to LDS, kAhead steps ahead, in the order of the
 // matrix operands; the products read a lane's 16 bytes in a row.
 //
-// A step has two phases, a barrier after each: one for the vector unit (maxima,
-// exponentials; and the loads are asked for), one for the matrix unit (the step's
-// values, the next step's scores).  The waves of a SIMD, w and w + 4, are a phase
-// apart, so that the units work side by side.  Phases counted from the start:
-// waves 0 to 3 have step t's phases at 2 t and 2 t + 1, waves 4 to 7 one later.  So
-// values t and keys t + 1 (bundle t) are read in phases 2 t + 1 and 2 t + 2, have
-// arrived by the end of phase 2 t (each wave waits for its own part before that
-// barrier), and their place, one of kRing, is free from phase 2 t + 3 on: bundle s
-// may be asked for from phase 2 (s - kRing) + 3 on, which for waves 4 to 7 is step s
-// - kAhead's first phase, and for waves 0 to 3 that of the step after it.
+// A step has two phases: one for the vector unit (maxima, exponentials; and the
+// loads are asked for), one for the matrix unit (the step's values, the next step's
+// scores).  The waves of a SIMD, w and w + 4, are a phase apart, so that the
+// units work side by side: all waves meet once a step, waves 0 to 3 before their
+// first phase, waves 4 to 7 between the two.  So in stretch t, behind the t-th
+// barrier, the former have both phases of step t, the latter the second of step t -
+// 1 and then the first of step t, and what is read is values t and keys t + 1
+// (bundle t) and those before them.  A bundle's place in the ring is free again two
+// stretches behind its own, so bundle t + kRing - 2 is asked for in stretch t; and
+// before a barrier each wave waits for its own part of the bundle that is read next.
 constexpr int kTileCols = 256;
 constexpr int kStep = 2 * kGroup;
-constexpr int kAhead = 3, kRing = kAhead + 1;
-constexpr int kReads = 8;          // operands read ahead of their products
+constexpr int kRing = 4, kAhead = kRing - 2;
+constexpr int kReads = 4;          // operands read ahead of their products
 constexpr int kNowhere = 1 << 30;  // where no query sees a key
 
 template <int HD, bool PREFIX>
@@ -734,7 +734,8 @@ __global__ __launch_bounds__(512, 2) void attn_paged_prompt_kernel(
 #pragma unroll
     for (int x = 0; x < KQ; x++) qf[y][x] = *reinterpret_cast<const bf16x8*>(qp + 32 * x);
   }
-  keep(qf);  // (arrived: a wait for them further on would be one for all loads)
+  keep(qf[0]);
+  keep(qf[1]);  // (arrived: a wait for them further on would be one for all loads)
   // Step k is place v0 + 64 k of the span, and `jump` more from step `hole` on:
   // those between the sinks and the tile's window are left out.
   const int hole = max(0, (span.hole - span.cut - v0 + kStep - 1) / kStep);
@@ -743,14 +744,13 @@ __global__ __launch_bounds__(512, 2) void attn_paged_prompt_kernel(
   const int jump = max(0, vlow - vhole) / kStep * kStep;
   const int steps = v1 <= vhole ? (v1 - v0 + kStep - 1) / kStep : hole + max(0, v1 - vhole - jump + kStep - 1) / kStep;
   const int32_t* pages = r.pages + (int64_t)b * r.max_pages;
-  const int stride = Hkv * r.page * HD;  // numbers of a page
-  const uint16_t *kp = kc + (int64_t)kvh * r.page * HD, *vp = vc + (int64_t)kvh * r.page * HD;
   // A lane has one of 64 steps from step `first` on: its two groups' first keys and
-  // pages.  (A page that is not there is page 0 where no query sees it, so that the
-  // loads under way stay countable.)  And a bit for each of them: whether every
-  // query of the wave sees every key, and whether some key is seen by none of the
-  // tile.
-  int key[2], page[2], first;
+  // where they are in a head's part of the pools.  (A page that is not there is page
+  // 0 where no query sees it, so that the loads under way stay countable.)  And a
+  // bit for each of them: whether every query of the wave sees every key, and
+  // whether some key is seen by none of the tile.
+  int key[2], first;
+  int64_t at[2];
   uint64_t whole, partly;
   auto look = [&](int k0) __attribute__((always_inline)) {
     first = k0;
@@ -758,11 +758,11 @@ __global__ __launch_bounds__(512, 2) void attn_paged_prompt_kernel(
     bool all = true, none = false;
 #pragma unroll
     for (int i = 0; i < 2; i++) {
-      const bool in = k < steps + kAhead + 1 && v + i * kGroup < vend;
+      const bool in = k < steps && v + i * kGroup < vend;
       key[i] = in ? span.real(v + i * kGroup) : kNowhere;
-      page[i] = in ? pages[key[i] >> __builtin_ctz(r.page)] : -1;
-      const bool there = (uint32_t)page[i] < (uint32_t)r.n_pages;
-      page[i] = there ? page[i] : 0;
+      const int page = in ? pages[key[i] >> __builtin_ctz(r.page)] : -1;
+      const bool there = (uint32_t)page < (uint32_t)r.n_pages;
+      at[i] = there ? 2 * ((int64_t)page * (Hkv * r.page * HD) + (key[i] & (r.page - 1)) * HD) : 0;
       key[i] = there ? key[i] : kNowhere;
       all = all && mask.all(q0, q1, key[i], key[i] + kGroup);
       none = none || mask.seen(p0, p1, key[i]) != ~0u;
@@ -770,25 +770,27 @@ __global__ __launch_bounds__(512, 2) void attn_paged_prompt_kernel(
     whole = __ballot(all);
     partly = __ballot(none);
   };
-  struct Where {
-    int64_t at[2];  // numbers of a pool before the groups
-  };
+  // of the i-th group of step k
   auto key_of = [&](int k, int i) __attribute__((always_inline)) { return __builtin_amdgcn_readlane(key[i], k - first); };
+  auto at_of = [&](int k, int i) __attribute__((always_inline)) {
+    const uint32_t lo = (uint32_t)__builtin_amdgcn_readlane((int)at[i], k - first), hi = (uint32_t)__builtin_amdgcn_readlane((int)(at[i] >> 32), k - first);
+    return (int64_t)((uint64_t)hi << 32 | lo);
+  };
+  // The wave's pieces of 1 KB of a step: one of each group, or one of one of them.
+  constexpr bool kBoth = LOADS == 2;
+  const int mine = wave / PIECES, piece = wave % PIECES;  // (mine: 0 where it has one of each)
+  const char *kp = reinterpret_cast<const char*>(kc + (int64_t)kvh * r.page * HD + piece * 512);
+  const char *vp = reinterpret_cast<const char*>(vc + (int64_t)kvh * r.page * HD + piece * 512);
+  const LdsAt lk = lds_at(sk) + wave * 1024, lv = lds_at(sv) + wave * 1024;
+  constexpr int kSlot = 2 * PIECES * 1024;
+  struct Where {
+    int64_t at[LOADS];
+  };
   auto where = [&](int k) __attribute__((always_inline)) {
     Where w;
 #pragma unroll
-    for (int i = 0; i < 2; i++)
-      w.at[i] = (int64_t)__builtin_amdgcn_readlane(page[i], k - first) * stride + (key_of(k, i) & (r.page - 1)) * HD;
+    for (int i = 0; i < LOADS; i++) w.at[i] = kBoth ? at_of(k, i) : mine ? at_of(k, 1) : at_of(k, 0);
     return w;
-  };
-  auto fetch = [&](const uint16_t* pool, const Where& w, u32x4* to) __attribute__((always_inline)) {
-#pragma unroll
-    for (int i = 0; i < LOADS; i++) {
-      // 1 KB pieces of both groups, one behind the other
-      const int piece = wave + 8 * i;
-      const int64_t at = HD == 128 ? w.at[i & 1] : wave >= 4 ? w.at[1] : w.at[0];
-      load_lds(pool + at + (piece & (PIECES - 1)) * 512, lane * 16, to + piece * 64);
-    }
   };
   Columns<HD, 2> cs = {};
   f32x4(&acc)[2][ND] = cs.o;
@@ -842,7 +844,7 @@ __global__ __launch_bounds__(512, 2) void attn_paged_prompt_kernel(
     if (!(partly >> (k - first) & 1)) return;
 #pragma unroll
     for (int i = 0; i < LOADS; i++) {
-      const uint32_t seen = mask.seen(p0, p1, HD == 128 ? key_of(k, i & 1) : wave >= 4 ? key_of(k, 1) : key_of(k, 0));
+      const uint32_t seen = mask.seen(p0, p1, kBoth ? key_of(k, i) : mine ? key_of(k, 1) : key_of(k, 0));
       v[(wave + 8 * i) * 64 + lane] &= words_of(seen, g);
     }
   };
@@ -904,40 +906,41 @@ __global__ __launch_bounds__(512, 2) void attn_paged_prompt_kernel(
   };
 
   const bool late = wave >= 4;
-  const int ahead = late ? kAhead : kAhead - 1;
   look(0);
   Where last = where(0);  // of the keys asked for last: their values are next
-  fetch(kp, last, sk[0]);
-  auto ask = [&](int s) __attribute__((always_inline)) {
-    const int to = s & (kRing - 1);
-    fetch(vp, last, sv[to]);
-    last = where(s + 1);
-    fetch(kp, last, sk[(to + 1) & (kRing - 1)]);
+  auto fetch = [&](const char* pool, LdsAt to) __attribute__((always_inline)) {
+#pragma unroll
+    for (int i = 0; i < LOADS; i++) load_lds(pool + last.at[i], lane * 16, to + i * (kSlot / 2));
   };
-  for (int s = 0; s < ahead; s++) ask(s);
-  wait_loads<(kAhead - 1) * 2 * LOADS>();
+  fetch(kp, lk);
+  auto ask = [&](int s) __attribute__((always_inline)) {
+    fetch(vp, lv + (s & (kRing - 1)) * kSlot);
+    last = where(s + 1);
+    fetch(kp, lk + ((s + 1) & (kRing - 1)) * kSlot);
+  };
+  for (int s = 0; s < kAhead; s++) ask(s);
+  wait_loads<(kAhead - 1) * 2 * LOADS>();  // the first keys and bundle 0
+  clear(sv[0], 0);
   meet();
   if (works) scores(held(sk[0]));
-  if (late) {
-    clear(sv[0], 0);  // (bundle 0 has arrived)
-    meet();
-  }
   for (int k = 0; k < steps; k++) {
     if (k - first == 32) look(k);
-    ask(k + ahead);
+    ask(k + kAhead);
     const int ring = k & (kRing - 1), up = (k + 1) & (kRing - 1);  // of the step's values; of the next step's keys
     __builtin_amdgcn_sched_barrier(0);
     if (works) {
       soften(k);
       // (kept here: the compiler would move the exponentials to their use)
-      keep(pf);
+      keep(pf[0]);
+      keep(pf[1]);
     }
     __builtin_amdgcn_sched_barrier(0);
-    if (!late) {
+    auto next = [&]() __attribute__((always_inline)) {
       wait_loads<(kAhead - 1) * 2 * LOADS>();
-      clear(sv[ring], k);
-    }
-    meet();
+      clear(sv[up], k + 1);
+      meet();
+    };
+    if (late) next();
     __builtin_amdgcn_sched_barrier(0);
     if (works) {
       // operands read kReads ahead, two products to a read
@@ -951,14 +954,9 @@ __global__ __launch_bounds__(512, 2) void attn_paged_prompt_kernel(
       }
     }
     __builtin_amdgcn_sched_barrier(0);
-    if (late) {
-      wait_loads<(kAhead - 1) * 2 * LOADS>();
-      clear(sv[up], k + 1);
-    }
-    meet();
+    if (!late) next();
     __builtin_amdgcn_sched_barrier(0);
   }
-  if (!late) meet();
   wait_loads<0>();  // no load to LDS outlives the workgroup
   if (!works) return;
   if (cs.odd()) {
@@ -968,16 +966,17 @@ __global__ __launch_bounds__(512, 2) void attn_paged_prompt_kernel(
     look(0);
     for (int k = 0; k < steps; k++) {
       if (k - first == 32) look(k);
-      const Where w = where(k);
-      auto group = [&](const uint16_t* pool, int x) __attribute__((always_inline)) { return reinterpret_cast<const u32x4*>(pool + w.at[x]) + lane; };
-      const u32x4* keys[2] = {group(kp, 0), group(kp, 1)};
+      auto group = [&](const uint16_t* pool, int i) __attribute__((always_inline)) {
+        return reinterpret_cast<const u32x4*>(reinterpret_cast<const char*>(pool + (int64_t)kvh * r.page * HD) + at_of(k, i)) + lane;
+      };
+      const u32x4* keys[2] = {group(kc, 0), group(kc, 1)};
       scores([&](int i, int x) __attribute__((always_inline)) { return keys[i >> 1][((i & 1) * KQ + x) * 64]; });
       soften(k);
       sums();
 #pragma unroll
       for (int x = 0; x < 2; x++) {
         const bf16x8 p[2] = {pf[0][x], pf[1][x]};
-        const u32x4* values = group(vp, x);
+        const u32x4* values = group(vc, x);
         add_masked_values([&](int i) __attribute__((always_inline)) { return values[i * 64]; }, p, acc, mask,
                           mask.seen(q0, q1, key_of(k, x)), pos, key_of(k, x));
       }

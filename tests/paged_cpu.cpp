@@ -24,6 +24,22 @@ static cpu_f32x4 cpu_mfma(cpu_bf16x8 a, cpu_bf16x8 b, cpu_f32x4 c) {
   cpu_hip::wait(cpu_hip::kWave);
   return c;
 }
+// The 32x32x16 one: lane (i, h) gives row (column) i and 8 terms from 8 h on, and
+// takes rows 8 (r / 4) + 4 h + r % 4 of column i.
+typedef float cpu_f32x16 __attribute__((ext_vector_type(16)));
+static cpu_f32x16 cpu_mfma32(cpu_bf16x8 a, cpu_bf16x8 b, cpu_f32x16 c) {
+  const unsigned t = threadIdx.x, w = t & ~63u, l = t & 63;
+  g_a[t] = a;
+  g_b[t] = b;
+  cpu_hip::wait(cpu_hip::kWave);
+  for (int r = 0; r < 16; r++)
+    for (int k = 0; k < 16; k++)
+      c[r] = fmaf((float)g_a[w + 8 * (r / 4) + 4 * (l >> 5) + r % 4 + 32 * (k / 8)][k % 8], (float)g_b[w + (l & 31) + 32 * (k / 8)][k % 8], c[r]);
+  cpu_hip::wait(cpu_hip::kWave);
+  return c;
+}
+typedef __bf16 cpu_bf16x2 __attribute__((ext_vector_type(2)));
+static float cpu_dot2(cpu_bf16x2 a, cpu_bf16x2 b, float c) { return fmaf((float)a[1], (float)b[1], fmaf((float)a[0], (float)b[0], c)); }
 struct CpuBuffer {
   const char* p;
   int n;
@@ -36,6 +52,8 @@ static cpu_u32x4 cpu_load(CpuBuffer b, int v, int s) {
 #define __builtin_amdgcn_make_buffer_rsrc(p, stride, n, flags) (CpuBuffer{(const char*)(p), n})
 #define __builtin_amdgcn_raw_buffer_load_b128(b, v, s, aux) cpu_load(b, v, s)
 #define __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, x, y, z) cpu_mfma(a, b, c)
+#define __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, x, y, z) cpu_mfma32(a, b, c)
+#define __builtin_amdgcn_fdot2_f32_bf16(a, b, c, x) cpu_dot2(a, b, c)
 #define __builtin_amdgcn_readfirstlane(x) __shfl(x, 0)
 #define __builtin_amdgcn_exp2f(x) exp2f(x)
 #define __builtin_amdgcn_sched_barrier(x)
@@ -53,11 +71,13 @@ struct CpuLoad {
 };
 static std::deque<CpuLoad> g_loads[1024];
 namespace lmgc {
-inline void load_lds(const void* p, uint32_t at, void* lds) {
+typedef char* LdsAt;
+inline LdsAt lds_at(void* p) { return (LdsAt)p; }
+inline void load_lds(const void* p, uint32_t at, LdsAt lds) {
   p = (const char*)p + at;
   volatile char probe = *(const volatile char*)p;
   (void)probe;
-  const CpuLoad l{p, (char*)lds + 16 * (threadIdx.x & 63)};
+  const CpuLoad l{p, lds + 16 * (threadIdx.x & 63)};
   if (g_late) g_loads[threadIdx.x].push_back(l);
   else memcpy(l.to, l.p, 16);
 }
@@ -67,8 +87,8 @@ void wait_loads() {
   for (; (int)q.size() > n; q.pop_front()) memcpy(q.front().to, q.front().p, 16);
 }
 inline void meet() { __syncthreads(); }
-template <class T, int n, int k>
-void keep(T (&)[n][k]) {}
+template <class T, int n>
+void keep(T (&)[n]) {}
 }  // namespace lmgc
 inline float2 make_float2(float a, float b) { return {a, b}; }
 static int min(int a, int b) { return a < b ? a : b; }
