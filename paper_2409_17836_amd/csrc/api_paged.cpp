@@ -197,7 +197,7 @@ int64_t lmgc_paged_workspace(int32_t n, int32_t B, int32_t Hq, int32_t Hkv, int3
   if (rc) return rc;
   if (max_new < 1 || max_new > kMaxTokens || tokens < 1 || tokens > kMaxTokens || shared < 0)
     return set_error(LMGC_EINVAL, "need max_new and tokens in [1, 2^24] and shared >= 0");
-  return n ? paged_workspace_bytes(n, B, Hq, Hkv, hd, std::min(max_new, n), tokens, shared) : 0;
+  return n ? paged_workspace_bytes(n, B, Hq, Hkv, hd, max_new, tokens, shared) : 0;
 }
 
 int lmgc_op_attention_paged(const uint16_t* d_q, int64_t ldq, int32_t n, int32_t B, int32_t Hq, int32_t Hkv, int32_t hd,
@@ -220,7 +220,6 @@ int lmgc_op_attention_paged(const uint16_t* d_q, int64_t ldq, int32_t n, int32_t
   if (!aligned(d_q, 16) || ldq % 8 || !aligned(d_out, 16) || !aligned(d_ws, 16))
     return set_error(LMGC_EINVAL, "pointers must be 16-byte aligned and ldq a multiple of 8");
   const int tokens = max_pages * page;
-  max_new = std::min(max_new, n);
   if (paged_workgroups(n, B, Hq, Hkv, hd, max_new, tokens, shared) >= 1 << 23)  // 2^32 threads
     return set_error(LMGC_EUNSUPPORTED, "too many columns for one launch");
   const int64_t need = paged_workspace_bytes(n, B, Hq, Hkv, hd, max_new, tokens, shared), no = (int64_t)n * Hq * hd * 2;

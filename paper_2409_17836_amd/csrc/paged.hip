@@ -157,104 +157,118 @@ __global__ __launch_bounds__(256) void paged_append_kernel(AppendArgs a) {
       c[i] = w[0], s[i] = w[1], c[i + 1] = w[2], s[i + 1] = w[3];
     }
   }
-  // the thread's 16 numbers of a row, rotated, as bf16
-  auto rotated = [&](const T* p, u32x4& y0, u32x4& y1) __attribute__((always_inline)) {
+  // the thread's 16 numbers of a row: as they are, then rotated, as bf16
+  struct Pair {
+    Eight<T> u, v;
+  };
+  auto load = [&](const T* p) __attribute__((always_inline)) { return Pair{load8(p + d0), load8(p + d1)}; };
+  auto rotated = [&](const Pair& w, u32x4& y0, u32x4& y1) __attribute__((always_inline)) {
     float y[16];
-    if (FAST) {
-      const Eight<T> u = load8(p + d0), v = load8(p + d1);
 #pragma unroll
-      for (int i = 0; i < 8; i++) {
-        y[i] = u.get(i);
-        y[8 + i] = v.get(i);
-      }
-      if (rotates) {
-        if (split) {
+    for (int i = 0; i < 8; i++) {
+      y[i] = w.u.get(i);
+      y[8 + i] = w.v.get(i);
+    }
+    if (rotates) {
+      if (split) {
 #pragma unroll
-          for (int i = 0; i < 8; i++) {
-            const float m = y[i], n = y[8 + i];
-            y[i] = turn_first(m, n, c[i], s[i]);
-            y[8 + i] = turn_second(m, n, c[i], s[i]);
-          }
-        } else {
-#pragma unroll
-          for (int i = 0; i < 8; i++) {
-            const float m = y[2 * i], n = y[2 * i + 1];
-            y[2 * i] = turn_first(m, n, c[i], s[i]);
-            y[2 * i + 1] = turn_second(m, n, c[i], s[i]);
-          }
+        for (int i = 0; i < 8; i++) {
+          const float m = y[i], n = y[8 + i];
+          y[i] = turn_first(m, n, c[i], s[i]);
+          y[8 + i] = turn_second(m, n, c[i], s[i]);
         }
-      }
-    } else {
-      for (int i = 0; i < 16; i++) {
-        const int d = d0 + i;
-        float v = load1(p + d);
-        if (a.table && d < a.rot) {
-          const bool second = split ? d >= half : d & 1;
-          const int k = split ? (second ? d - half : d) : d >> 1, e = split ? (second ? d - half : d + half) : d ^ 1;
-          const float other = load1(p + e);
-          v = second ? turn_second(other, v, tab[k].x, tab[k].y) : turn_first(v, other, tab[k].x, tab[k].y);
+      } else {
+#pragma unroll
+        for (int i = 0; i < 8; i++) {
+          const float m = y[2 * i], n = y[2 * i + 1];
+          y[2 * i] = turn_first(m, n, c[i], s[i]);
+          y[2 * i + 1] = turn_second(m, n, c[i], s[i]);
         }
-        y[i] = v;
       }
     }
     y0 = pack8(y);
     y1 = pack8(y + 8);
   };
-  if (mine) {
-    for (int h = h0; h < 1 + G; h += NH) {
-      u32x4 y0, y1;
-      if (h == 0) {
-        rotated(static_cast<const T*>(a.k) + row * a.ldk + kvh * HD, y0, y1);
-        if (there) {
-          auto put = [&](int d, u32x4 w) __attribute__((always_inline)) {
-            *reinterpret_cast<u32x4*>(a.kc + at + ((t >> 4) * (HD / 32) + (d >> 5)) * 512 + ((t & 15) + 16 * ((d & 31) >> 3)) * 8) = w;
-          };
-          put(d0, y0);
-          put(d1, y1);
-        }
-      } else {
-        const int hq = kvh * G + h - 1;
-        rotated(static_cast<const T*>(a.q) + row * a.ldq + (int64_t)hq * HD, y0, y1);
-        uint16_t* o = a.q_out + row * a.ldqo + (int64_t)hq * HD;
-        if (FAST) {
-          *reinterpret_cast<u32x4*>(o + d0) = y0;
-          *reinterpret_cast<u32x4*>(o + d1) = y1;
-        } else {
-          for (int i = 0; i < 8; i++) {
-            o[d0 + i] = (uint16_t)(y0[i >> 1] >> (16 * (i & 1)));
-            o[d1 + i] = (uint16_t)(y1[i >> 1] >> (16 * (i & 1)));
-          }
-        }
+  // the same number by number, wherever they are
+  auto rotated_slowly = [&](const T* p, u32x4& y0, u32x4& y1) __attribute__((always_inline)) {
+    float y[16];
+    for (int i = 0; i < 16; i++) {
+      const int d = d0 + i;
+      float v = load1(p + d);
+      if (a.table && d < a.rot) {
+        const bool second = split ? d >= half : d & 1;
+        const int k = split ? (second ? d - half : d) : d >> 1, e = split ? (second ? d - half : d + half) : d ^ 1;
+        const float other = load1(p + e);
+        v = second ? turn_second(other, v, tab[k].x, tab[k].y) : turn_first(v, other, tab[k].x, tab[k].y);
       }
+      y[i] = v;
     }
+    y0 = pack8(y);
+    y1 = pack8(y + 8);
+  };
+  const T* krow = static_cast<const T*>(a.k) + row * a.ldk + kvh * HD;
+  const T* vrow = static_cast<const T*>(a.v) + row * a.ldv + kvh * HD;
+  const T* qrow = static_cast<const T*>(a.q) + row * a.ldq + (int64_t)kvh * G * HD;
+  const bool keys = mine && h0 == 0;  // (with heads side by side the first of them has the keys and values)
+  // values: 8 dims of each half (or of neighbouring pieces), 64 bytes of a row to the four lanes of a token
+  const int dv0 = 32 * x + 8 * g, dv1 = dv0 + 32 * (U / 4);
+  // everything that is there from the start is asked for before anything is used
+  Pair kw{}, qw{};
+  Eight<T> v0{}, v1{};
+  if (FAST) {
+    if (keys) {
+      kw = load(krow);
+      v0 = load8(vrow + dv0);
+      v1 = load8(vrow + dv1);
+    }
+    if (mine && h0 < G) qw = load(qrow + h0 * HD);
   }
-  if (!there) return;
+  u32x4 y0, y1;
+  if (keys && there) {
+    if (FAST) rotated(kw, y0, y1);
+    else rotated_slowly(krow, y0, y1);
+    auto put = [&](int d, u32x4 w) __attribute__((always_inline)) {
+      *reinterpret_cast<u32x4*>(a.kc + at + ((t >> 4) * (HD / 32) + (d >> 5)) * 512 + ((t & 15) + 16 * ((d & 31) >> 3)) * 8) = w;
+    };
+    put(d0, y0);
+    put(d1, y1);
+  }
   // values: slot (d, 4 tokens) holds tokens 4 k .. + 3 of both halves
   auto slot = [](int s) __attribute__((always_inline)) { return s ^ ((s >> 4 & 3) | (s >> 6 & 1) << 2); };
-  if (mine && h0 == 0) {
-    const T* p = static_cast<const T*>(a.v) + row * a.ldv + kvh * HD;
+  if (keys && there) {
     uint16_t* words = reinterpret_cast<uint16_t*>(sv);
 #pragma unroll
     for (int k = 0; k < 2; k++) {
-      const int d = 32 * (x + (U / 4) * k) + 8 * g;  // (a run of 64 bytes for the four lanes of a token)
-      u32x4 w;
-      if (FAST) {
-        const Eight<T> e = load8(p + d);
-        float y[8];
+      const int d = k ? dv1 : dv0;
+      float y[8];
 #pragma unroll
-        for (int i = 0; i < 8; i++) y[i] = e.get(i);
-        w = pack8(y);
-      } else {
-        float y[8];
-        for (int i = 0; i < 8; i++) y[i] = load1(p + d + i);
-        w = pack8(y);
-      }
+      for (int i = 0; i < 8; i++) y[i] = FAST ? (k ? v1 : v0).get(i) : load1(vrow + d + i);
+      const u32x4 w = pack8(y);
 #pragma unroll
       for (int i = 0; i < 8; i++)
         words[slot(((d + i) >> 4) * 64 + ((d + i) & 15) + 16 * ((t & 15) >> 2)) * 8 + 4 * (t >> 4) + (t & 3)] =
             (uint16_t)(w[i >> 1] >> (16 * (i & 1)));
     }
   }
+  if (mine) {
+    for (int h = h0; h < G; h += NH) {
+      const Pair w = qw;
+      if (FAST && h + NH < G) qw = load(qrow + (h + NH) * HD);
+      if (FAST) rotated(w, y0, y1);
+      else rotated_slowly(qrow + h * HD, y0, y1);
+      uint16_t* o = a.q_out + row * a.ldqo + ((int64_t)kvh * G + h) * HD;
+      if (FAST) {
+        *reinterpret_cast<u32x4*>(o + d0) = y0;
+        *reinterpret_cast<u32x4*>(o + d1) = y1;
+      } else {
+        for (int i = 0; i < 8; i++) {
+          o[d0 + i] = (uint16_t)(y0[i >> 1] >> (16 * (i & 1)));
+          o[d1 + i] = (uint16_t)(y1[i >> 1] >> (16 * (i & 1)));
+        }
+      }
+    }
+  }
+  if (!there) return;
   __syncthreads();
   for (int i = tid; i < HD * 4; i += 256) {
     const int k = 4 * (i >> 4 & 3);  // tokens k .. + 3 and 16 + k .. + 3
@@ -510,21 +524,29 @@ struct Columns {
 // Columns: column c = t G + i of a (sequence, key/value head) is query head
 // kvh G + i of its new token t; for the prefix, of row t of the batch.
 //
-// Grid: (splits, tiles of 16 NT columns x Hkv, B), 256 threads.  Wave w takes
+// Grid: (splits x tiles of 16 NT columns, Hkv, B), 256 threads.  Wave w takes
 // groups w, w + 4, .. of its split: S^T = K Q^T, so lane (col, g) holds the
 // scores of its column and tokens 16 i + 4 g + r of a group, an online softmax,
 // O^T += V^T P^T.  The waves' parts meet in LDS.
 constexpr int kWaves = 4;
 
 struct AttnPlan {
-  int few, columns;      // columns of a sequence that the form for few takes, and how many of them there are at most
+  int64_t cols;          // of the longest sequence, at most
+  int few, few_short;    // columns of a sequence that the form for few takes, and of one of at most kShort keys
+  int columns;           // how many of them there are at most
+  int short_splits;      // parts of a short one, at most
   Splits split;          // of the form for few columns
   Splits prompt;         // of the form for many
+  int many, joined;      // whether the form for many is needed; whether it leaves partial results
   int cut;               // tokens that all share, computed for the batch
   int pre, pre_chunk;    // splits of these
   float *po, *prompt_o, *pre_o;      // partial results, and maxima and sums
   float2 *pml, *prompt_ml, *pre_ml;
 };
+
+constexpr int kShort = 1024;
+// Whether a sequence of so many columns and keys has few.
+__device__ inline bool is_few(const AttnPlan& p, int cols, int total) { return cols <= p.few || (cols <= p.few_short && total <= kShort); }
 
 template <int HD, int NT, bool PREFIX>
 __global__ __launch_bounds__(kWaves * 64, HD == 64 ? 4 : 3) void attn_paged_split_kernel(
@@ -535,12 +557,17 @@ __global__ __launch_bounds__(kWaves * 64, HD == 64 ? 4 : 3) void attn_paged_spli
   __shared__ float sm[NW][16], sl[NW][16];
   const int tid = threadIdx.x, lane = tid & 63, col = lane & 15, g = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int tile = blockIdx.y / Hkv, kvh = blockIdx.y - tile * Hkv, split = blockIdx.x, b = PREFIX ? 0 : blockIdx.z;
-  const int c0 = tile * TILE;
+  const int kvh = blockIdx.y, b = PREFIX ? 0 : blockIdx.z;
+  // the tiles that a sequence of any length may have, all their splits; then those of short ones, with theirs
+  const int all = PREFIX ? plan.pre : plan.split.most, of_any = PREFIX ? INT32_MAX : plan.few / TILE * all, bx = blockIdx.x;
+  const int tile = bx < of_any ? bx / all : plan.few / TILE + (bx - of_any) / plan.short_splits;
+  const int split = bx < of_any ? bx % all : (bx - of_any) % plan.short_splits, c0 = tile * TILE;
   Seq sq{0, r.n, 0};
   if (!PREFIX) sq = sequence(r, b, max_new);
   const int cols = sq.T * G, ncol = min(TILE, cols - c0);
-  if (ncol <= 0 || (!PREFIX && cols > plan.few)) return;
+  if (ncol <= 0) return;
+  const Span span = PREFIX ? Span{0, 0, 0, plan.cut} : span_of(sq, mask, plan.cut);
+  if (!PREFIX && !is_few(plan, cols, span.total)) return;
   // the lane's columns (past the last: the last one's again), their positions
   int pos[NT], p0, p1;
   if (PREFIX) {
@@ -564,7 +591,6 @@ __global__ __launch_bounds__(kWaves * 64, HD == 64 ? 4 : 3) void attn_paged_spli
     p0 = sq.len + c0 / G;
     p1 = sq.len + (c0 + ncol - 1) / G;
   }
-  const Span span = PREFIX ? Span{0, min(plan.cut, (min(mask.sinks, plan.cut) + kGroup - 1) & ~(kGroup - 1)), 0, plan.cut} : span_of(sq, mask, plan.cut);
   const int chunk = PREFIX ? plan.pre_chunk : plan.split.chunk(span.total);
   const int v0 = split * chunk, v1 = min(span.total, v0 + chunk);
   if (v0 >= v1) return;
@@ -675,11 +701,13 @@ __global__ __launch_bounds__(512, 2) void attn_paged_prompt_kernel(
       sq = sequence(r, b, max_new);
       tile = place - ((int64_t)sq.row * G / kTileCols + b);
     }
-    if (sq.T <= 0 || tile < 0 || tile * kTileCols >= (int64_t)sq.T * G || sq.T * G <= plan.few) return;
+    if (sq.T <= 0 || tile < 0 || tile * kTileCols >= (int64_t)sq.T * G) return;
     c0 = (int)tile * kTileCols;
   }
   const int ncol = min(kTileCols, sq.T * G - c0);
   if (ncol <= 0) return;
+  const Span span = PREFIX ? Span{0, min(plan.cut, (min(mask.sinks, plan.cut) + kGroup - 1) & ~(kGroup - 1)), 0, plan.cut} : span_of(sq, mask, plan.cut);
+  if (!PREFIX && is_few(plan, sq.T * G, span.total)) return;
   // the wave's columns (past the last: the last one's again), their positions
   const int w0 = min(c0 + wave * 32, c0 + ncol - 1), w1 = min(c0 + wave * 32 + 31, c0 + ncol - 1);
   const bool works = wave * 32 < ncol;
@@ -719,7 +747,6 @@ __global__ __launch_bounds__(512, 2) void attn_paged_prompt_kernel(
     q0 = sq.len + w0 / G;
     q1 = sq.len + w1 / G;
   }
-  const Span span = PREFIX ? Span{0, min(plan.cut, (min(mask.sinks, plan.cut) + kGroup - 1) & ~(kGroup - 1)), 0, plan.cut} : span_of(sq, mask, plan.cut);
   const int chunk = PREFIX ? plan.pre_chunk : plan.prompt.chunk(span.total);
   // the split's places of the span, without those behind the tile's last query
   const int v0 = split * chunk, vend = min(span.total, v0 + chunk);
@@ -1010,17 +1037,22 @@ __global__ __launch_bounds__(512, 2) void attn_paged_prompt_kernel(
 // Joins the parts of a row and head: a wave each, first a lane per part (its
 // weight), then HD / 64 dims to a lane.
 //
-// ROWS: all rows (those of few columns only behind a prefix); else the columns
-// of sequences with few of them.
+// ROWS: all rows; else the columns of sequences with few of them, where the others
+// are in one part.
 template <int HD, bool ROWS>
 __global__ __launch_bounds__(256) void attn_paged_join_kernel(Ragged r, int max_new, int Hkv, int G, AttnPlan plan, Mask mask,
                                                               uint16_t* __restrict__ out) {
   const int lane = threadIdx.x & 63, Hq = Hkv * G;
   const int64_t count = ROWS ? (int64_t)r.n * Hq : (int64_t)r.B * Hkv * plan.columns;
+  const float2 none = make_float2(-INFINITY, 0.f);
   for (int64_t i = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6); i < count; i += (int64_t)gridDim.x * 4) {
     int b, t, hq;
     Seq q;
+    // (what does not need the sequence is asked for before it is looked up)
+    float2 pre_ml = none, own_ml = none;
     if (ROWS) {
+      if (lane < plan.pre) pre_ml = plan.pre_ml[i * plan.pre + lane];
+      if (plan.joined && lane < plan.prompt.most) own_ml = plan.prompt_ml[i * plan.prompt.most + lane];
       const int row = (int)(i / Hq);
       hq = (int)(i - (int64_t)row * Hq);
       b = last_at_most(r.B, row, [&](int k) { return (int64_t)r.starts[k]; });
@@ -1035,52 +1067,44 @@ __global__ __launch_bounds__(256) void attn_paged_join_kernel(Ragged r, int max_
       hq = (int)(head - (int64_t)b * Hkv) * G + c - t * G;
     }
     if (t < 0 || t >= q.T) continue;
-    const bool few = q.T * G <= plan.few;
-    if (few == ROWS && plan.cut == 0) continue;  // the other's
-    const int kvh = hq / G;
-    const int64_t at = ((int64_t)q.row + t) * Hq + hq;
     const Span span = span_of(q, mask, plan.cut);
-    const int chunk = (few ? plan.split : plan.prompt).chunk(span.total), nown = (span.total + chunk - 1) / chunk;
+    const bool few = is_few(plan, q.T * G, span.total);
+    if (!ROWS && !few) continue;
+    const int kvh = hq / G, chunk = (few ? plan.split : plan.prompt).chunk(span.total), nown = (span.total + chunk - 1) / chunk;
     if (plan.cut == 0 && nown <= 1) continue;  // written by the only split
+    const int64_t at = ((int64_t)q.row + t) * Hq + hq;
     const int64_t own = few ? (((int64_t)b * Hkv + kvh) * plan.columns + t * G + (hq - kvh * G)) * plan.split.most : at * plan.prompt.most;
-    const float2* own_ml = (few ? plan.pml : plan.prompt_ml) + own;
     const float* own_o = (few ? plan.po : plan.prompt_o) + own * HD;
-    const float2* pre_ml = plan.pre_ml + at * plan.pre;
     const float* pre_o = plan.pre_o + at * plan.pre * HD;
-    // parts: those of the prefix, then the sequence's own
+    if (few && lane < nown) own_ml = plan.pml[own + lane];
+    if (lane >= nown) own_ml = none;
+    // parts: those of the prefix, then the sequence's own, 8 at a time, so that their
+    // loads are under way together
     const int n = plan.pre + nown;
-    float M = -INFINITY, ms[2], ls[2];
-#pragma unroll
-    for (int k = 0; k < 2; k++) {
-      const int e = lane + 64 * k;
-      const float2 ml = e < plan.pre ? pre_ml[e] : e < n ? own_ml[e - plan.pre] : make_float2(-INFINITY, 0.f);
-      ms[k] = ml.x;
-      ls[k] = ml.y;
-      M = fmaxf(M, ml.x);
-    }
-    for (int o = 32; o; o >>= 1) M = fmaxf(M, __shfl_xor(M, o));
-    float L = 0.f, a[2];
-#pragma unroll
-    for (int k = 0; k < 2; k++) {
-      // parts without a token that the query sees (m = -inf, l = 0) count for nothing
-      a[k] = ms[k] == -INFINITY && ls[k] == 0.f ? 0.f : __builtin_amdgcn_exp2f(ms[k] - M);
-      L += a[k] * ls[k];
-    }
-    for (int o = 32; o; o >>= 1) L += __shfl_xor(L, o);
     typedef float f32xd __attribute__((ext_vector_type(HD / 64)));
-    f32xd acc = {};
-    // 8 at a time, so that their loads are under way together
-    for (int e0 = 0; e0 < n; e0 += 8) {
-      f32xd x[8];
+    f32xd x[8], acc = {};
+    auto load = [&](int e0) __attribute__((always_inline)) {
 #pragma unroll
       for (int k = 0; k < 8; k++) {
         const int e = min(e0 + k, n - 1);
         x[k] = reinterpret_cast<const f32xd*>(e < plan.pre ? pre_o + (int64_t)e * HD : own_o + (int64_t)(e - plan.pre) * HD)[lane];
       }
+    };
+    load(0);
+    float M = fmaxf(pre_ml.x, own_ml.x);
+    for (int o = 32; o; o >>= 1) M = fmaxf(M, __shfl_xor(M, o));
+    // parts without a token that the query sees (m = -inf, l = 0) count for nothing
+    const float ap = pre_ml.x == -INFINITY && pre_ml.y == 0.f ? 0.f : __builtin_amdgcn_exp2f(pre_ml.x - M);
+    const float ao = own_ml.x == -INFINITY && own_ml.y == 0.f ? 0.f : __builtin_amdgcn_exp2f(own_ml.x - M);
+    float L = ap * pre_ml.y + ao * own_ml.y;
+    for (int o = 32; o; o >>= 1) L += __shfl_xor(L, o);
+    for (int e0 = 0; e0 < n; e0 += 8) {
+      if (e0) load(e0);
 #pragma unroll
       for (int k = 0; k < 8; k++) {
         const int e = e0 + k;
-        const float w = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, e < 64 ? a[0] : a[1]), e & 63));
+        const float from = e < plan.pre ? ap : ao;
+        const float w = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, from), (e < plan.pre ? e : e - plan.pre) & 63));
         if (e < n && w != 0.f) acc += w * x[k];
       }
     }
@@ -1094,7 +1118,12 @@ __global__ __launch_bounds__(256) void attn_paged_join_kernel(Ragged r, int max_
 // Tokens that are computed for the batch: whole pairs of groups.
 int cut_of(int B, int shared) { return B > 1 ? shared / 64 * 64 : 0; }
 
-constexpr int kFew = 64;  // columns of a sequence that the form for few takes
+// Columns of a sequence that the form for few takes: of any, and (where max_new allows
+// no more, for the launch has to hold the tiles of all) of one of at most kShort keys.
+// 8 prompts of up to 150 rows over their own 160 keys, 12 heads of 64: 8.4 us by the
+// form for few, 16.9 with the form for many, whose 12 to 24 busy workgroups wait for
+// one another's loads; 3001 rows over 4001 keys are read 47 times as often by it.
+constexpr int kFew = 64, kFewShort = 512;
 constexpr int kLeast = 512;
 
 // Workgroups for the tiles of many columns of one head and split: as many tiles of
@@ -1111,19 +1140,30 @@ Tiles tiles_of(int n, int G, int B, int64_t cols) {
 }
 
 AttnPlan plan_of(int n, int B, int Hq, int Hkv, int hd, int max_new, int tokens, int shared, void* ws, int64_t* bytes) {
-  const int64_t cols = (int64_t)max_new * (Hq / Hkv);
+  // the rules count max_new as it was given, not the batch, for the bits of a sequence
+  // are not to depend on the rows of others; sizes count no more than n rows
+  const int64_t rule = (int64_t)max_new * (Hq / Hkv), cols = std::min<int64_t>(max_new, n) * (Hq / Hkv);
   AttnPlan p{};
   p.few = kFew;
-  p.columns = (int)std::min<int64_t>(cols, kFew);
+  p.few_short = rule <= kFewShort ? kFewShort : kFew;
+  p.cols = cols;
+  p.columns = (int)std::min<int64_t>(cols, p.few_short);
   p.cut = std::min(cut_of(B, shared), tokens);
   const int least = 256 * 128 / hd * 2;
-  p.split = {std::min(64, (tokens + least - 1) / least), least, kWaves * kGroup};
-  const int64_t groups = (cols + kTileCols - 1) / kTileCols * Hkv;
-  p.prompt = {groups >= 128 ? 1 : (int)std::min<int64_t>({16, 256 / groups, (tokens + kLeast - 1) / kLeast}), kLeast, kStep};
-  p.pre_chunk = (std::max(kLeast, (p.cut + 63) / 64) + kStep * 4 - 1) / (kStep * 4) * (kStep * 4);
+  const int own_tokens = std::max(1, tokens - p.cut);
+  p.split = {std::min(64, (own_tokens + least - 1) / least), least, kWaves * kGroup};
+  p.short_splits = std::min(p.split.most, (kShort + least - 1) / least);
+  const int64_t groups = (rule + kTileCols - 1) / kTileCols * Hkv;
+  p.prompt = {groups >= 128 ? 1 : (int)std::min<int64_t>({16, 256 / groups, (own_tokens + kLeast - 1) / kLeast}), kLeast, kStep};
+  // the prefix in parts that fill the chip, half of kLeast or more each
+  const int64_t pre_groups = ((int64_t)n * (Hq / Hkv) + kTileCols - 1) / kTileCols * Hkv;
+  const int parts = (int)std::max<int64_t>(1, std::min<int64_t>(64, 256 / pre_groups));
+  p.pre_chunk = (std::max(kLeast / 2, (p.cut + parts - 1) / parts) + kStep * 2 - 1) / (kStep * 2) * (kStep * 2);
   p.pre = (p.cut + p.pre_chunk - 1) / p.pre_chunk;
   const int64_t own = p.cut || p.split.most > 1 ? (int64_t)B * Hkv * p.columns * p.split.most : 0;
-  const int64_t many = cols > kFew && (p.cut || p.prompt.most > 1) ? (int64_t)n * Hq * p.prompt.most : 0;
+  p.many = cols > kFew && !(rule <= kFewShort && own_tokens <= kShort);
+  p.joined = p.many && (p.cut || p.prompt.most > 1);
+  const int64_t many = p.joined ? (int64_t)n * Hq * p.prompt.most : 0;
   const int64_t pre = (int64_t)n * Hq * p.pre;
   p.po = (float*)ws;
   p.prompt_o = p.po + own * hd;
@@ -1145,7 +1185,7 @@ int64_t paged_workspace_bytes(int n, int B, int Hq, int Hkv, int hd, int max_new
 
 int64_t paged_workgroups(int n, int B, int Hq, int Hkv, int hd, int max_new, int tokens, int shared) {
   const AttnPlan p = plan_of(n, B, Hq, Hkv, hd, max_new, tokens, shared, nullptr, nullptr);
-  return tiles_of(n, Hq / Hkv, B, (int64_t)max_new * (Hq / Hkv)).count * Hkv * std::max(p.prompt.most, p.pre);
+  return tiles_of(n, Hq / Hkv, B, p.cols).count * Hkv * std::max(p.prompt.most, p.pre);
 }
 
 hipError_t launch_paged_append(const AppendArgs& a, hipStream_t s) {
@@ -1177,9 +1217,8 @@ hipError_t launch_attention_paged(const PagedAttnArgs& a, hipStream_t s) {
   const float sl2 = (float)(1.4426950408889634 * (double)a.scale);
   auto go = [&](auto h) {
     constexpr int HD = decltype(h)::value;
-    const int64_t cols = (int64_t)a.max_new * G;
-    auto split = [&](auto prefix, dim3 grid) {
-      hipLaunchKernelGGL((attn_paged_split_kernel<HD, 1, decltype(prefix)::value>), grid, kWaves * 64, 0, s, a.q, a.ldq, a.kc, a.vc, r,
+    auto split = [&](auto prefix, int64_t blocks, int seqs) {
+      hipLaunchKernelGGL((attn_paged_split_kernel<HD, 1, decltype(prefix)::value>), dim3((unsigned)blocks, a.Hkv, seqs), kWaves * 64, 0, s, a.q, a.ldq, a.kc, a.vc, r,
                          a.max_new, a.Hkv, G, plan, mask, sl2, a.out);
     };
     auto prompt = [&](auto prefix, int64_t slots, int by_turns, int splits) {
@@ -1188,20 +1227,21 @@ hipError_t launch_attention_paged(const PagedAttnArgs& a, hipStream_t s) {
     };
     if (plan.cut) {
       const int64_t all = (int64_t)r.n * G;
-      if (all <= kFew) split(std::true_type{}, dim3(plan.pre, (unsigned)((all + 15) / 16 * a.Hkv)));
+      if (all <= kFew) split(std::true_type{}, (all + 15) / 16 * plan.pre, 1);
       else prompt(std::true_type{}, (all + kTileCols - 1) / kTileCols, 0, plan.pre);
     }
-    split(std::false_type{}, dim3(plan.split.most, (unsigned)((plan.columns + 15) / 16 * a.Hkv), r.B));
-    if (cols > kFew) {
-      const Tiles t = tiles_of(r.n, G, r.B, cols);
+    const int tiles = (plan.columns + 15) / 16, of_any = std::min(tiles, kFew / 16);
+    split(std::false_type{}, of_any * plan.split.most + (tiles - of_any) * plan.short_splits, r.B);
+    if (plan.many) {
+      const Tiles t = tiles_of(r.n, G, r.B, plan.cols);
       prompt(std::false_type{}, t.count, t.by_turns, plan.prompt.most);
     }
     auto join = [&](auto rows, int64_t count) {
       hipLaunchKernelGGL((attn_paged_join_kernel<HD, decltype(rows)::value>), (unsigned)std::min<int64_t>((count + 3) / 4, 1 << 20), 256, 0, s,
                          r, a.max_new, a.Hkv, G, plan, mask, a.out);
     };
-    if (plan.cut || (cols > kFew && plan.prompt.most > 1)) join(std::true_type{}, (int64_t)r.n * a.Hq);
-    if (!plan.cut && plan.split.most > 1) join(std::false_type{}, (int64_t)r.B * a.Hkv * plan.columns);
+    if (plan.cut || plan.joined) join(std::true_type{}, (int64_t)r.n * a.Hq);
+    else if (plan.split.most > 1) join(std::false_type{}, (int64_t)r.B * a.Hkv * plan.columns);
   };
   if (a.hd == 64) go(std::integral_constant<int, 64>{});
   else go(std::integral_constant<int, 128>{});

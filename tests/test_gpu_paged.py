@@ -299,6 +299,36 @@ def test_attention_does_not_depend_on_the_batch():
             assert torch.equal(_attend(one, q[sl].contiguous(), max_new=s.max_new), whole[sl]), b
 
 
+def test_attention_splits_do_not_follow_the_number_of_rows():
+    """max_new decides how a long sequence is split, not the rows that a batch has."""
+    torch = _torch()
+    for new in (1, 30):
+        s = Setup([(new, 3000), (2000, 5)], 64, 2, 64, 8)
+        q = s.rows(8)
+        for most in (2000, 9000):
+            whole = _attend(s, q, max_new=most)
+            one = Setup([(new, 3000)], 64, 2, 64)
+            one.cache, one.n_pages = s.cache, s.n_pages
+            one.set(s.pages_h[:1], [0, new], s.lens_h[:1])
+            assert torch.equal(_attend(one, q[:new].contiguous(), max_new=most), whole[:new]), (new, most)
+
+
+# Around the borders between the forms: 64 columns of any sequence, 512 of one of at
+# most 1024 keys where max_new allows no more.
+@pytest.mark.parametrize("new,old", [(16, 100), (17, 100), (17, 1007), (17, 1008), (128, 896), (128, 897), (127, 0), (129, 100), (128, 2000)])
+@pytest.mark.parametrize("hd", [64, 128])
+def test_attention_borders_of_the_forms(new, old, hd):
+    s = Setup([(new, old), (1, 2000), (3, 0)], 64, 2, hd, new)
+    _attend_check(s, s.rows(8))
+    _attend_check(s, s.rows(8), window=200, sinks=3)
+
+
+@pytest.mark.parametrize("new,old", [(16, 1200), (17, 1200), (17, 1900), (128, 1200), (128, 1900), (129, 1200), (300, 1200)])
+def test_attention_shared_borders_of_the_forms(new, old):
+    s = Setup([(new, old), (1, 1500), (3, 1155)], 64, 2, 64, new, shared=1152)
+    _attend_check(s, s.rows(8), shared=1152)
+
+
 # ------------------------------------------------------------------- shared
 @pytest.mark.parametrize("hd,page,Hkv,G", [(64, 32, 2, 1), (64, 64, 1, 8), (128, 128, 2, 4), (128, 64, 2, 2)])
 @pytest.mark.parametrize("shared,seqs", [
