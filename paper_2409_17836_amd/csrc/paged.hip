@@ -79,7 +79,7 @@ __device__ inline int64_t group_at(const Ragged& r, int page, int Hkv, int h, in
 }
 
 // ------------------------------------------------------------------ append
-// Grid: (places, Hkv), 256 threads: a group of 32 tokens of one sequence's cache
+// Grid: (Hkv, places), 256 threads: a group of 32 tokens of one sequence's cache
 // and one key/value head, with the query heads that read it.  Place starts[b] /
 // 32 + 2 b + i is group i of sequence b's new tokens (so no sequence's places
 // run into the next one's, wherever its groups begin).
@@ -119,6 +119,8 @@ __device__ inline u32x4 pack8(const float* y) {
   return w;
 }
 
+constexpr int kPlaces = 32768;  // in one plane of the grid
+
 // FAST: rot a multiple of 16 and every run of 8 dims aligned to 16 bytes.
 template <class T, int HD, bool FAST>
 __global__ __launch_bounds__(256) void paged_append_kernel(AppendArgs a) {
@@ -126,15 +128,16 @@ __global__ __launch_bounds__(256) void paged_append_kernel(AppendArgs a) {
   constexpr int NH = 256 / (32 * U);  // heads side by side
   __shared__ u32x4 sv[HD * 4];        // a group of values
   const Ragged& r = a.r;
-  const int b = last_at_most(r.B, blockIdx.x, [&](int i) { return (int64_t)r.starts[i] / kGroup + 2 * (int64_t)i; });
+  const int64_t at_place = (int64_t)blockIdx.z * kPlaces + blockIdx.y;
+  const int b = last_at_most(r.B, at_place, [&](int i) { return (int64_t)r.starts[i] / kGroup + 2 * (int64_t)i; });
   Seq q = sequence(r, b, INT32_MAX);
   if (a.table) q.T = (int)min((int64_t)q.T, max((int64_t)0, a.n_pos - q.len));
   if (q.T <= 0) return;
-  const int64_t place = (int64_t)blockIdx.x - (q.row / kGroup + 2 * (int64_t)b);
+  const int64_t place = at_place - (q.row / kGroup + 2 * (int64_t)b);
   if (place < 0) return;
   const int64_t t0 = q.len / kGroup * (int64_t)kGroup + place * kGroup;  // the group's first token
   if (t0 >= q.len + (int64_t)q.T) return;
-  const int kvh = blockIdx.y, G = a.q ? a.Hq / a.Hkv : 0, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int kvh = blockIdx.x, G = a.q ? a.Hq / a.Hkv : 0, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int lo = (int)max((int64_t)0, q.len - t0), hi = (int)min((int64_t)kGroup, q.len + (int64_t)q.T - t0);
   const int page = r.pages[(int64_t)b * r.max_pages + (t0 >> __builtin_ctz(r.page))];
   const bool there = page >= 0 && page < r.n_pages;
@@ -1193,7 +1196,8 @@ hipError_t launch_paged_append(const AppendArgs& a, hipStream_t s) {
   auto whole = [&](const void* p, int64_t ld, int n) { return ld % n == 0 && ((uintptr_t)p & 15) == 0; };
   const bool fast = a.rot % 16 == 0 && whole(a.k, a.ldk, run) && whole(a.v, a.ldv, run) &&
                     (!a.q || (whole(a.q, a.ldq, run) && whole(a.q_out, a.ldqo, 8)));
-  const dim3 grid((unsigned)(a.r.n / kGroup + 2 * (int64_t)a.r.B), a.Hkv);
+  const int places = a.r.n / kGroup + 2 * a.r.B;
+  const dim3 grid(a.Hkv, std::min(places, kPlaces), (places + kPlaces - 1) / kPlaces);
   auto go = [&](auto t, auto h) {
     using T = decltype(t);
     constexpr int HD = decltype(h)::value;

@@ -16,18 +16,33 @@ typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 
 // ------------------------------------------------------------------- table
 // table[p, i] = mscale (cos, sin)(p freqs[i]), angles and functions in float64:
-// at position 2^17 a float32 angle is off by 2^-7.
+// at position 2^17 a float32 angle is off by 2^-7.  A thread has kPositions
+// positions of a frequency, from a multiple of kPositions on: it turns the first
+// one's (cos, sin) by the frequency, in float64, for the next ones.  A step adds
+// two roundings, so the last is off by 2^-49, of float32's 2^-24.
 struct Freqs {
   double f[kMaxRot / 2];
 };
+constexpr int kPositions = 8;
 
-__global__ __launch_bounds__(256) void rope_table_kernel(Freqs freqs, int half, double mscale, int64_t n, float2* __restrict__ table) {
-  const int64_t step = (int64_t)gridDim.x * 256;
-  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < n; i += step) {
-    const int64_t p = i / half;
-    double s, c;
-    sincos((double)p * freqs.f[i - p * half], &s, &c);
-    table[i] = make_float2((float)(c * mscale), (float)(s * mscale));
+__global__ __launch_bounds__(256) void rope_table_kernel(Freqs freqs, int half, double mscale, int n_pos, float2* __restrict__ table) {
+  // thread number / half, of which the block's first is the same for all lanes
+  const int64_t first = (int64_t)blockIdx.x * 256;
+  const int64_t p0 = first / half;
+  const int rest = (int)(first - p0 * half) + threadIdx.x, more = rest / half, i = rest - more * half;
+  const int64_t p = (p0 + more) * kPositions;
+  if (p >= n_pos) return;
+  const double f = freqs.f[i];
+  double s, c, ds, dc;
+  sincos((double)p * f, &s, &c);
+  sincos(f, &ds, &dc);
+  float2* o = table + p * half + i;
+  const int n = (int)min((int64_t)kPositions, n_pos - p);
+  for (int k = 0; k < n; k++) {
+    o[(int64_t)k * half] = make_float2((float)(c * mscale), (float)(s * mscale));
+    const double t = c * dc - s * ds;
+    s = s * dc + c * ds;
+    c = t;
   }
 }
 
@@ -59,17 +74,20 @@ __device__ inline float load1(const uint16_t* p) { return bf16_to_f32(*p); }
 __device__ inline void store1(float* p, float x) { *p = x; }
 __device__ inline void store1(uint16_t* p, float x) { *p = f32_to_bf16(x); }
 
-// Grid: (blocks of rows, heads / kHeads), 256 threads: np places of a row side
+// Grid: (heads / kHeads, blocks of rows), 256 threads: np places of a row side
 // by side.  FAST: rot a multiple of two runs, hd of a run, everything 16-byte
 // aligned.
+constexpr int kRowBlocks = 32768;  // in one plane of the grid
+
 template <class T, bool FAST>
 __global__ __launch_bounds__(256) void rope_kernel(RopeArgs a, int np, int rows, int per) {
   constexpr int R = Run<T>::n;
-  const int place = threadIdx.x % np, row = blockIdx.x * rows + threadIdx.x / np;
+  const int place = threadIdx.x % np;
+  const int64_t row = ((int64_t)blockIdx.z * kRowBlocks + blockIdx.y) * rows + threadIdx.x / np;
   if ((int)threadIdx.x >= rows * np || row >= a.n) return;
   const int64_t pos = a.pos[row];
   if (pos < 0 || pos >= a.n_pos) return;
-  const int half = a.rot / 2, h0 = blockIdx.y * per, h1 = min(a.heads, h0 + per);
+  const int half = a.rot / 2, h0 = blockIdx.x * per, h1 = min(a.heads, h0 + per);
   const float2* tab = reinterpret_cast<const float2*>(a.table) + pos * half;
   const T* x = static_cast<const T*>(a.x) + row * a.ldx;
   T* o = static_cast<T*>(a.out) + row * a.ldo;
@@ -84,10 +102,17 @@ __global__ __launch_bounds__(256) void rope_kernel(RopeArgs a, int np, int rows,
         const f32x4 w = *reinterpret_cast<const f32x4*>(tab + place * R + i);
         c[i] = w[0], s[i] = a.backward ? -w[1] : w[1], c[i + 1] = w[2], s[i + 1] = a.backward ? -w[3] : w[3];
       }
+      // (the next head's numbers are asked for before this one's are used)
+      Run<T> un, vn;
+      auto load = [&](int h) __attribute__((always_inline)) {
+        un.v = *reinterpret_cast<const decltype(un.v)*>(x + h * a.ldhx + d0);
+        vn.v = *reinterpret_cast<const decltype(un.v)*>(x + h * a.ldhx + d1);
+      };
+      load(h0);
       for (int h = h0; h < h1; h++) {
-        Run<T> u, v, y, z;
-        u.v = *reinterpret_cast<const decltype(u.v)*>(x + h * a.ldhx + d0);
-        v.v = *reinterpret_cast<const decltype(u.v)*>(x + h * a.ldhx + d1);
+        const Run<T> u = un, v = vn;
+        Run<T> y, z;
+        if (h + 1 < h1) load(h + 1);
         y.v = {};
         z.v = {};
         if (a.layout == LMGC_ROPE_HALF) {
@@ -143,8 +168,8 @@ __global__ __launch_bounds__(256) void rope_kernel(RopeArgs a, int np, int rows,
 hipError_t launch_rope_table(const double* freqs, int rot, double mscale, int64_t n_pos, float* table, hipStream_t s) {
   Freqs f{};
   for (int i = 0; i < rot / 2; i++) f.f[i] = freqs[i];
-  const int64_t n = n_pos * (rot / 2);
-  rope_table_kernel<<<(unsigned)std::min<int64_t>((n + 255) / 256, 1 << 20), 256, 0, s>>>(f, rot / 2, mscale, n, (float2*)table);
+  const int64_t n = (n_pos + kPositions - 1) / kPositions * (rot / 2);
+  rope_table_kernel<<<(unsigned)((n + 255) / 256), 256, 0, s>>>(f, rot / 2, mscale, (int)n_pos, (float2*)table);
   return hipGetLastError();
 }
 
@@ -158,9 +183,8 @@ hipError_t launch_rope(const RopeArgs& a, hipStream_t s) {
     const int np = fast ? a.rot / 2 / R + (a.hd - a.rot + 2 * R - 1) / (2 * R) : std::min((a.hd + 1) / 2, 64);
     const int rows = 256 / np;
     const int64_t blocks = ((int64_t)a.n + rows - 1) / rows;
-    int per = blocks * a.heads >= 4096 ? 4 : 1;
-    per = std::max(per, (a.heads + 65534) / 65535);
-    const dim3 grid((unsigned)blocks, (a.heads + per - 1) / per);
+    const int per = blocks * a.heads >= 4096 ? 4 : 1;
+    const dim3 grid((a.heads + per - 1) / per, std::min<int64_t>(blocks, kRowBlocks), (blocks + kRowBlocks - 1) / kRowBlocks);
     if (fast) rope_kernel<T, true><<<grid, 256, 0, s>>>(a, np, rows, per);
     else rope_kernel<T, false><<<grid, 256, 0, s>>>(a, np, rows, per);
   };
