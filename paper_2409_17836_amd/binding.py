@@ -5,6 +5,7 @@ LM-GC hot path runs in the library.  If liblmgc.so is missing the import of
 this module still works, but every call raises: there is no fallback path.
 """
 import ctypes
+import math
 import os
 from typing import List, Optional, Sequence, Tuple
 
@@ -822,9 +823,13 @@ ROPE_SCALINGS = {"none": 0, "linear": 1, "ntk": 2, "yarn": 3}
 def rope_frequencies(rot: int, theta: float = 10000.0, scaling: str = "none", factor: float = 1.0, orig: float = 4096,
                      slow: float = 1.0, fast: float = 32.0) -> np.ndarray:
     """float64 [rot / 2]: the frequencies of lmgc_rope_frequencies."""
-    out = np.zeros(max(int(rot) // 2, 1), np.float64)
+    return np.array(_frequencies(rot, theta, scaling, factor, orig, slow, fast))
+
+
+def _frequencies(rot, theta, scaling, factor, orig, slow, fast):
+    out = (ctypes.c_double * max(int(rot) // 2, 1))()
     _check(lib().lmgc_rope_frequencies(float(theta), rot, ROPE_SCALINGS[scaling], float(factor), float(orig), float(slow),
-                                       float(fast), out.ctypes.data_as(ctypes.POINTER(ctypes.c_double))))
+                                       float(fast), out))
     return out
 
 
@@ -834,9 +839,9 @@ def rope_table(n_pos: int, rot: int, theta: float = 10000.0, scaling: str = "non
     2].  mscale multiplies both; YaRN's 0.1 ln(factor) + 1 with that scaling
     unless given, else 1."""
     import torch
-    f = rope_frequencies(rot, theta, scaling, factor, orig, slow, fast)
+    f = _frequencies(rot, theta, scaling, factor, orig, slow, fast)
     if mscale is None:
-        mscale = 0.1 * float(np.log(factor)) + 1.0 if scaling == "yarn" else 1.0
+        mscale = 0.1 * math.log(factor) + 1.0 if scaling == "yarn" else 1.0
     shape = (n_pos, rot // 2, 2)
     if out is None:
         if stream is None:
@@ -847,7 +852,7 @@ def rope_table(n_pos: int, rot: int, theta: float = 10000.0, scaling: str = "non
     else:
         assert out.dtype == torch.float32 and out.is_contiguous() and out.shape == shape
     st, (po,) = _on(stream, out)
-    _check(lib().lmgc_op_rope_table(f.ctypes.data_as(ctypes.POINTER(ctypes.c_double)), rot, float(mscale), n_pos, po, st))
+    _check(lib().lmgc_op_rope_table(f, rot, float(mscale), n_pos, po, st))
     return out
 
 
@@ -875,8 +880,9 @@ def op_rope(x, positions, table, layout: str = "half", backward: bool = False, o
     dt = _dtype(x)
 
     def strides(t):  # of a single row or head: what a contiguous tensor has
-        h = t.stride(1) if heads > 1 else hd
-        return (t.stride(0) if n > 1 else heads * h), h
+        rows, h, _ = t.stride()
+        h = h if heads > 1 else hd
+        return (rows if n > 1 else heads * h), h
     st, (px, pp, pt, po) = _on(stream, x, positions, table, out)
     _check(lib().lmgc_op_rope(px, dt, n, heads, hd, *strides(x), pp, pt, n_pos, rot, ROPE_LAYOUTS[layout],
                               int(backward), po, *strides(out), st))
@@ -894,19 +900,22 @@ def _paged_check(cache, pages, starts, lens, Hkv, hd):
     """(n_pages, page, B, max_pages) of a cache and a batch, their tensors checked."""
     import torch
     kc, vc = cache
-    assert kc.dtype == vc.dtype == torch.bfloat16 and kc.shape == vc.shape and kc.is_contiguous() and vc.is_contiguous()
-    assert kc.dim() == 4 and kc.shape[1] == Hkv and kc.shape[3] == hd, (tuple(kc.shape), Hkv, hd)
+    shape, i32 = kc.shape, torch.int32
+    assert kc.dtype == vc.dtype == torch.bfloat16 and shape == vc.shape and kc.is_contiguous() and vc.is_contiguous()
+    assert len(shape) == 4 and shape[1] == Hkv and shape[3] == hd, (tuple(shape), Hkv, hd)
     B, most = pages.shape
-    for t, n in ((pages, B * most), (starts, B + 1), (lens, B)):
-        assert t.dtype == torch.int32 and t.is_contiguous() and t.numel() == n
-    return kc.shape[0], kc.shape[2], B, most
+    assert pages.dtype == i32 and pages.is_contiguous()
+    assert starts.dtype == i32 and starts.is_contiguous() and starts.numel() == B + 1
+    assert lens.dtype == i32 and lens.is_contiguous() and lens.numel() == B
+    return shape[0], shape[2], B, most
 
 
 def _row_stride(t):
     """Numbers between rows of t [n, heads, hd], whose heads lie side by side."""
     n, heads, hd = t.shape
-    assert t.stride(2) == 1 and (heads == 1 or t.stride(1) == hd), t.stride()
-    return t.stride(0) if n > 1 else heads * hd
+    rows, of_heads, dims = t.stride()
+    assert dims == 1 and (heads == 1 or of_heads == hd), t.stride()
+    return rows if n > 1 else heads * hd
 
 
 def op_paged_append(cache, k, v, pages, starts, lens, rope=None, layout: str = "half", q=None, q_out=None, stream=None):
@@ -957,14 +966,16 @@ def op_attention_paged(q, cache, pages, starts, lens, max_new: int, window: int 
     else:
         assert out.dtype == torch.bfloat16 and out.is_contiguous() and out.numel() == q.numel()
     # (ctypes would keep the low 32 bits of a larger one)
-    max_new, window, sinks, shared = (max(-1, min(int(x), 2 ** 31 - 1)) for x in (max_new, window, sinks, shared))
+    if not (0 <= max_new <= 1 << 24 and 0 <= window < 1 << 31 and 0 <= sinks < 1 << 31 and 0 <= shared < 1 << 31):
+        max_new, window, sinks, shared = (max(-1, min(int(x), 2 ** 31 - 1)) for x in (max_new, window, sinks, shared))
+        max_new = min(max_new, 1 << 24)
     if ws is None:
-        ws = _empty(paged_workspace(n, B, Hq, Hkv, hd, min(max_new, 1 << 24), most * page, shared), torch.uint8, q, stream)
+        ws = _empty(paged_workspace(n, B, Hq, Hkv, hd, max_new, most * page, shared), torch.uint8, q, stream)
     else:
         assert ws.is_contiguous()  # its bytes lie one behind the other
     st, (pq, pkc, pvc, pp, ps, pl, po, pw) = _on(stream, q, *cache, pages, starts, lens, out, ws)
     _check(lib().lmgc_op_attention_paged(pq, ldq, n, B, Hq, Hkv, hd, pkc, pvc, n_pages, page, pp, most, ps, pl,
-                                         min(max_new, 1 << 24), window, sinks, shared,
+                                         max_new, window, sinks, shared,
                                          hd ** -0.5 if scale is None else float(scale), po, pw,
                                          ws.numel() * ws.element_size(), st))
     return out
