@@ -58,17 +58,27 @@ __device__ inline Seq sequence(const Ragged& r, int b, int limit) {
   return {r0, ok ? min(min(r1 - r0, limit), tokens - len) : 0, len};
 }
 
-// A row's position; -1 if it is no token.
-__device__ inline int position_of(const Ragged& r, int row, int limit) {
-  // the last sequence that begins at or before the row
-  int lo = 0, n = r.B;
-  while (n > 1) {
+// The last sequence that begins at or before a row, for each lane of a wave and its
+// own row: the lanes hold 64 of the first rows and look them up in one another's
+// registers, for look-ups in memory would wait one for the other.
+__device__ inline int sequence_of(const Ragged& r, int row) {
+  const int lane = threadIdx.x & 63, step = (r.B + 63) / 64;
+  const int first = lane * step < r.B ? r.starts[lane * step] : INT32_MAX;
+  int b = 0;
+  for (int h = 32; h; h >>= 1) b += __shfl(first, b + h) <= row ? h : 0;
+  b *= step;
+  for (int n = min(step, r.B - b); n > 1;) {
     const int h = n / 2;
-    const bool right = r.starts[lo + h] <= row;
-    lo += right ? h : 0;
+    const bool right = r.starts[b + h] <= row;
+    b += right ? h : 0;
     n = right ? n - h : h;
   }
-  const Seq s = sequence(r, lo, limit);
+  return b;
+}
+
+// A lane's row's position; -1 if it is no token.
+__device__ inline int position_of(const Ragged& r, int row, int limit) {
+  const Seq s = sequence(r, sequence_of(r, row), limit);
   const int t = row - s.row;
   return t >= 0 && t < s.T ? s.len + t : -1;
 }
@@ -552,7 +562,7 @@ constexpr int kShort = 1024;
 __device__ inline bool is_few(const AttnPlan& p, int cols, int total) { return cols <= p.few || (cols <= p.few_short && total <= kShort); }
 
 template <int HD, int NT, bool PREFIX>
-__global__ __launch_bounds__(kWaves * 64, HD == 64 ? 4 : 3) void attn_paged_split_kernel(
+__global__ __launch_bounds__(kWaves * 64, NT > 1 ? 2 : HD == 64 ? 4 : 3) void attn_paged_split_kernel(
     const uint16_t* __restrict__ q, int64_t ldq, const uint16_t* __restrict__ kc, const uint16_t* __restrict__ vc, Ragged r, int max_new,
     int Hkv, int G, AttnPlan plan, Mask mask, float sl2, uint16_t* __restrict__ out) {
   constexpr int KQ = HD / 32, ND = HD / 16, NW = kWaves, TILE = 16 * NT;
@@ -1041,80 +1051,84 @@ __global__ __launch_bounds__(512, 2) void attn_paged_prompt_kernel(
 // weight), then HD / 64 dims to a lane.
 //
 // ROWS: all rows; else the columns of sequences with few of them, where the others
-// are in one part.
+// are in one part.  A lane has 4 dims of a row and takes the parts 8 at a time, whose
+// statistics and numbers are asked for together.
 template <int HD, bool ROWS>
 __global__ __launch_bounds__(256) void attn_paged_join_kernel(Ragged r, int max_new, int Hkv, int G, AttnPlan plan, Mask mask,
                                                               uint16_t* __restrict__ out) {
-  const int lane = threadIdx.x & 63, Hq = Hkv * G;
+  constexpr int LANES = HD / 4, NR = 256 / LANES;
+  const int own_row = threadIdx.x / LANES, d = threadIdx.x % LANES * 4, Hq = Hkv * G;
+  const int per = ROWS ? Hq : plan.columns;
   const int64_t count = ROWS ? (int64_t)r.n * Hq : (int64_t)r.B * Hkv * plan.columns;
-  const float2 none = make_float2(-INFINITY, 0.f);
-  for (int64_t i = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6); i < count; i += (int64_t)gridDim.x * 4) {
+  for (int64_t i0 = (int64_t)blockIdx.x * NR; i0 < count; i0 += (int64_t)gridDim.x * NR) {
+    // i = i0 + own_row, divided by what is the same for a block and by few
+    const int64_t unit0 = i0 / per;
+    const int rest = (int)(i0 - unit0 * per) + own_row, more = rest / per, i = rest - more * per;
     int b, t, hq;
     Seq q;
-    // (what does not need the sequence is asked for before it is looked up)
-    float2 pre_ml = none, own_ml = none;
     if (ROWS) {
-      if (lane < plan.pre) pre_ml = plan.pre_ml[i * plan.pre + lane];
-      if (plan.joined && lane < plan.prompt.most) own_ml = plan.prompt_ml[i * plan.prompt.most + lane];
-      const int row = (int)(i / Hq);
-      hq = (int)(i - (int64_t)row * Hq);
-      b = last_at_most(r.B, row, [&](int k) { return (int64_t)r.starts[k]; });
+      const int row = (int)min(unit0 + more, (int64_t)r.n - 1);
+      b = sequence_of(r, row);
       q = sequence(r, b, max_new);
       t = row - q.row;
+      hq = i;
     } else {
-      const int64_t head = i / plan.columns;
-      const int c = (int)(i - head * plan.columns);
-      b = (int)(head / Hkv);
+      const uint32_t unit = (uint32_t)min(unit0 + more, (int64_t)r.B * Hkv - 1);
+      b = unit / Hkv;
       q = sequence(r, b, max_new);
-      t = c / G;
-      hq = (int)(head - (int64_t)b * Hkv) * G + c - t * G;
+      t = i / G;
+      hq = (int)(unit - (uint32_t)b * Hkv) * G + i - t * G;
     }
-    if (t < 0 || t >= q.T) continue;
+    if (i0 + own_row >= count || t < 0 || t >= q.T) continue;
     const Span span = span_of(q, mask, plan.cut);
     const bool few = is_few(plan, q.T * G, span.total);
     if (!ROWS && !few) continue;
     const int kvh = hq / G, chunk = (few ? plan.split : plan.prompt).chunk(span.total), nown = (span.total + chunk - 1) / chunk;
     if (plan.cut == 0 && nown <= 1) continue;  // written by the only split
-    const int64_t at = ((int64_t)q.row + t) * Hq + hq;
+    const int64_t at = ((int64_t)q.row + t) * Hq + hq, pre = at * plan.pre;
     const int64_t own = few ? (((int64_t)b * Hkv + kvh) * plan.columns + t * G + (hq - kvh * G)) * plan.split.most : at * plan.prompt.most;
-    const float* own_o = (few ? plan.po : plan.prompt_o) + own * HD;
-    const float* pre_o = plan.pre_o + at * plan.pre * HD;
-    if (few && lane < nown) own_ml = plan.pml[own + lane];
-    if (lane >= nown) own_ml = none;
-    // parts: those of the prefix, then the sequence's own, 8 at a time, so that their
-    // loads are under way together
+    const float* own_o = few ? plan.po : plan.prompt_o;
+    const float2* own_ml = few ? plan.pml : plan.prompt_ml;
+    // parts: those of the prefix, then the sequence's own
     const int n = plan.pre + nown;
-    typedef float f32xd __attribute__((ext_vector_type(HD / 64)));
-    f32xd x[8], acc = {};
-    auto load = [&](int e0) __attribute__((always_inline)) {
+    float M = -INFINITY, L = 0.f;
+    f32x4 acc = {};
+    for (int e0 = 0; e0 < n; e0 += 8) {
+      float2 ml[8];
+      f32x4 x[8];
 #pragma unroll
       for (int k = 0; k < 8; k++) {
         const int e = min(e0 + k, n - 1);
-        x[k] = reinterpret_cast<const f32xd*>(e < plan.pre ? pre_o + (int64_t)e * HD : own_o + (int64_t)(e - plan.pre) * HD)[lane];
+        const bool shared = e < plan.pre;
+        const int64_t part = shared ? pre + e : own + (e - plan.pre);
+        ml[k] = (shared ? plan.pre_ml : own_ml)[part];
+        x[k] = *reinterpret_cast<const f32x4*>((shared ? plan.pre_o : own_o) + part * HD + d);
+        if (e0 + k >= n) ml[k] = make_float2(-INFINITY, 0.f);
       }
-    };
-    load(0);
-    float M = fmaxf(pre_ml.x, own_ml.x);
-    for (int o = 32; o; o >>= 1) M = fmaxf(M, __shfl_xor(M, o));
-    // parts without a token that the query sees (m = -inf, l = 0) count for nothing
-    const float ap = pre_ml.x == -INFINITY && pre_ml.y == 0.f ? 0.f : __builtin_amdgcn_exp2f(pre_ml.x - M);
-    const float ao = own_ml.x == -INFINITY && own_ml.y == 0.f ? 0.f : __builtin_amdgcn_exp2f(own_ml.x - M);
-    float L = ap * pre_ml.y + ao * own_ml.y;
-    for (int o = 32; o; o >>= 1) L += __shfl_xor(L, o);
-    for (int e0 = 0; e0 < n; e0 += 8) {
-      if (e0) load(e0);
+      float top = M;
+#pragma unroll
+      for (int k = 0; k < 8; k++) top = fmaxf(top, ml[k].x);
+      if (top > M) {
+        // (a sum of none but scores of -inf is no number; behind a greater one it is nothing)
+        const float a = __builtin_amdgcn_exp2f(M - top);
+        L = M == -INFINITY ? 0.f : L * a;
+        acc = M == -INFINITY ? f32x4{} : acc * a;
+        M = top;
+      }
 #pragma unroll
       for (int k = 0; k < 8; k++) {
-        const int e = e0 + k;
-        const float from = e < plan.pre ? ap : ao;
-        const float w = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, from), (e < plan.pre ? e : e - plan.pre) & 63));
-        if (e < n && w != 0.f) acc += w * x[k];
+        // parts without a token that the query sees (m = -inf, l = 0) count for nothing
+        const float w = ml[k].x == -INFINITY && ml[k].y == 0.f ? 0.f : __builtin_amdgcn_exp2f(ml[k].x - M);
+        L += w * ml[k].y;
+        if (w != 0.f) acc += w * x[k];
       }
     }
     const float inv = L == 0.f ? 0.f : 1.0f / L;
-    uint16_t* op = out + at * HD + lane * (HD / 64);
+    typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+    u32x2 y;
 #pragma unroll
-    for (int e = 0; e < HD / 64; e++) op[e] = f32_to_bf16(acc[e] * inv);
+    for (int e = 0; e < 2; e++) y[e] = f32_to_bf16(acc[2 * e] * inv) | (uint32_t)f32_to_bf16(acc[2 * e + 1] * inv) << 16;
+    *reinterpret_cast<u32x2*>(out + at * HD + d) = y;
   }
 }
 
@@ -1128,6 +1142,13 @@ int cut_of(int B, int shared) { return B > 1 ? shared / 64 * 64 : 0; }
 // one another's loads; 3001 rows over 4001 keys are read 47 times as often by it.
 constexpr int kFew = 64, kFewShort = 512;
 constexpr int kLeast = 512;
+
+// Columns of the batch up to which a shared prefix goes to the form for few, with 32
+// columns to a workgroup: its four waves wait for less than the eight of the form for
+// many, of which each has its own 32 columns.  A step behind 8192 shared tokens, 8
+// heads of 128: 32.7 us for 36.6 with 128 columns, 43.0 for 48.5 with 256, 66.5 for
+// 64.6 with 512; 12 heads of 64: 30.7 for 33.4 with 64 columns, 46.8 for 44.4 with 128.
+constexpr int kFewPre = 256, kPreTile = 32;
 
 // Workgroups for the tiles of many columns of one head and split: as many tiles of
 // every sequence as the longest may have, by turns, so that the longest tiles run
@@ -1162,9 +1183,12 @@ AttnPlan plan_of(int n, int B, int Hq, int Hkv, int hd, int max_new, int tokens,
   p.short_splits = std::min(p.split.most, (kShort + least - 1) / least);
   const int64_t groups = (rule + kTileCols - 1) / kTileCols * Hkv;
   p.prompt = {groups >= 128 ? 1 : (int)std::min<int64_t>({16, 256 / groups, (own_tokens + kLeast - 1) / kLeast}), kLeast, kStep};
-  // the prefix in parts that fill the chip, half of kLeast or more each
-  const int64_t pre_groups = ((int64_t)n * (Hq / Hkv) + kTileCols - 1) / kTileCols * Hkv;
-  const int parts = (int)std::max<int64_t>(1, std::min<int64_t>(64, 256 / pre_groups));
+  // the prefix in parts that fill the chip (two workgroups of few columns to a CU, one
+  // of many), half of kLeast or more each: with 128 columns behind 8192 tokens 17.5 us
+  // in 16 parts, 18.4 in 8, 25 in 32
+  const int64_t pre_cols = (int64_t)n * (Hq / Hkv), pre_tile = pre_cols <= kFewPre ? kPreTile : kTileCols;
+  const int64_t pre_groups = (pre_cols + pre_tile - 1) / pre_tile * Hkv;
+  const int parts = (int)std::max<int64_t>(1, std::min<int64_t>(64, (pre_cols <= kFewPre ? 512 : 256) / pre_groups));
   p.pre_chunk = (std::max(kLeast / 2, (p.cut + parts - 1) / parts) + kStep * 2 - 1) / (kStep * 2) * (kStep * 2);
   p.pre = (p.cut + p.pre_chunk - 1) / p.pre_chunk;
   const int64_t own = p.cut || p.split.most > 1 ? (int64_t)B * Hkv * p.columns * p.split.most : 0;
@@ -1225,8 +1249,8 @@ hipError_t launch_attention_paged(const PagedAttnArgs& a, hipStream_t s) {
   const float sl2 = (float)(1.4426950408889634 * (double)a.scale);
   auto go = [&](auto h) {
     constexpr int HD = decltype(h)::value;
-    auto split = [&](auto prefix, int64_t blocks, int seqs) {
-      hipLaunchKernelGGL((attn_paged_split_kernel<HD, 1, decltype(prefix)::value>), dim3((unsigned)blocks, a.Hkv, seqs), kWaves * 64, 0, s, a.q, a.ldq, a.kc, a.vc, r,
+    auto split = [&](auto prefix, auto nt, int64_t blocks, int seqs) {
+      hipLaunchKernelGGL((attn_paged_split_kernel<HD, decltype(nt)::value, decltype(prefix)::value>), dim3((unsigned)blocks, a.Hkv, seqs), kWaves * 64, 0, s, a.q, a.ldq, a.kc, a.vc, r,
                          a.max_new, a.Hkv, G, plan, mask, sl2, a.out);
     };
     auto prompt = [&](auto prefix, int64_t slots, int by_turns, int splits) {
@@ -1235,18 +1259,18 @@ hipError_t launch_attention_paged(const PagedAttnArgs& a, hipStream_t s) {
     };
     if (plan.cut) {
       const int64_t all = (int64_t)r.n * G;
-      if (all <= kFew) split(std::true_type{}, (all + 15) / 16 * plan.pre, 1);
+      if (all <= kFewPre) split(std::true_type{}, std::integral_constant<int, kPreTile / 16>{}, (all + kPreTile - 1) / kPreTile * plan.pre, 1);
       else prompt(std::true_type{}, (all + kTileCols - 1) / kTileCols, 0, plan.pre);
     }
     const int tiles = (plan.columns + 15) / 16, of_any = std::min(tiles, kFew / 16);
-    split(std::false_type{}, of_any * plan.split.most + (tiles - of_any) * plan.short_splits, r.B);
+    split(std::false_type{}, std::integral_constant<int, 1>{}, of_any * plan.split.most + (tiles - of_any) * plan.short_splits, r.B);
     if (plan.many) {
       const Tiles t = tiles_of(r.n, G, r.B, plan.cols);
       prompt(std::false_type{}, t.count, t.by_turns, plan.prompt.most);
     }
     auto join = [&](auto rows, int64_t count) {
-      hipLaunchKernelGGL((attn_paged_join_kernel<HD, decltype(rows)::value>), (unsigned)std::min<int64_t>((count + 3) / 4, 1 << 20), 256, 0, s,
-                         r, a.max_new, a.Hkv, G, plan, mask, a.out);
+      hipLaunchKernelGGL((attn_paged_join_kernel<HD, decltype(rows)::value>), (unsigned)std::min<int64_t>((count + 1024 / HD - 1) / (1024 / HD), 1 << 20), 256, 0,
+                         s, r, a.max_new, a.Hkv, G, plan, mask, a.out);
     };
     if (plan.cut || plan.joined) join(std::true_type{}, (int64_t)r.n * a.Hq);
     else if (plan.split.most > 1) join(std::false_type{}, (int64_t)r.B * a.Hkv * plan.columns);
