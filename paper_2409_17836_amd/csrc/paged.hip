@@ -152,9 +152,9 @@ __global__ __launch_bounds__(256) void paged_append_kernel(AppendArgs a) {
   const int page = r.pages[(int64_t)b * r.max_pages + (t0 >> __builtin_ctz(r.page))];
   const bool there = page >= 0 && page < r.n_pages;
   const int64_t at = there ? group_at(r, page, a.Hkv, kvh, (int)t0, HD) : 0;
-  // token and place of the thread: 16 tokens x 4 places to a wave
-  const int t = 16 * (wave & 1) + (lane & 15), g = lane >> 4, x = U == 8 ? wave >> 1 : 0, h0 = U == 8 ? 0 : wave >> 1;
-  const int unit = 4 * x + g;
+  // token and place of the thread: the places of a token side by side, so that a load
+  // has whole lines of a row
+  const int t = U == 8 ? 8 * wave + (lane >> 3) : 16 * (wave & 1) + (lane >> 2), unit = lane % U, h0 = U == 8 ? 0 : wave >> 1;
   const bool mine = t >= lo && t < hi;
   const int64_t row = q.row + (t0 - q.len) + t;  // (only where it is mine)
   const int half = a.rot / 2, nrot = a.table ? a.rot / 16 : 0;
@@ -223,8 +223,8 @@ __global__ __launch_bounds__(256) void paged_append_kernel(AppendArgs a) {
   const T* vrow = static_cast<const T*>(a.v) + row * a.ldv + kvh * HD;
   const T* qrow = static_cast<const T*>(a.q) + row * a.ldq + (int64_t)kvh * G * HD;
   const bool keys = mine && h0 == 0;  // (with heads side by side the first of them has the keys and values)
-  // values: 8 dims of each half (or of neighbouring pieces), 64 bytes of a row to the four lanes of a token
-  const int dv0 = 32 * x + 8 * g, dv1 = dv0 + 32 * (U / 4);
+  // values: 8 dims of each half
+  const int dv0 = 8 * unit, dv1 = dv0 + HD / 2;
   // everything that is there from the start is asked for before anything is used
   Pair kw{}, qw{};
   Eight<T> v0{}, v1{};
@@ -247,7 +247,7 @@ __global__ __launch_bounds__(256) void paged_append_kernel(AppendArgs a) {
     put(d1, y1);
   }
   // values: slot (d, 4 tokens) holds tokens 4 k .. + 3 of both halves
-  auto slot = [](int s) __attribute__((always_inline)) { return s ^ ((s >> 4 & 3) | (s >> 6 & 1) << 2); };
+  auto slot = [](int s) __attribute__((always_inline)) { return s ^ ((s >> 4 & 3) ^ (s >> 7 & 1) << 1 | (s >> 6 & 1) << 2); };
   if (keys && there) {
     uint16_t* words = reinterpret_cast<uint16_t*>(sv);
 #pragma unroll

@@ -77,6 +77,7 @@ __device__ inline void store1(uint16_t* p, float x) { *p = f32_to_bf16(x); }
 // Grid: (heads / kHeads, blocks of rows), 256 threads: np places of a row side
 // by side.  FAST: rot a multiple of two runs, hd of a run, everything 16-byte
 // aligned.
+constexpr int kHeads = 4;
 constexpr int kRowBlocks = 32768;  // in one plane of the grid
 
 template <class T, bool FAST>
@@ -102,42 +103,47 @@ __global__ __launch_bounds__(256) void rope_kernel(RopeArgs a, int np, int rows,
         const f32x4 w = *reinterpret_cast<const f32x4*>(tab + place * R + i);
         c[i] = w[0], s[i] = a.backward ? -w[1] : w[1], c[i + 1] = w[2], s[i + 1] = a.backward ? -w[3] : w[3];
       }
-      // (the next head's numbers are asked for before this one's are used)
-      Run<T> un, vn;
-      auto load = [&](int h) __attribute__((always_inline)) {
-        un.v = *reinterpret_cast<const decltype(un.v)*>(x + h * a.ldhx + d0);
-        vn.v = *reinterpret_cast<const decltype(un.v)*>(x + h * a.ldhx + d1);
-      };
-      load(h0);
-      for (int h = h0; h < h1; h++) {
-        const Run<T> u = un, v = vn;
-        Run<T> y, z;
-        if (h + 1 < h1) load(h + 1);
-        y.v = {};
-        z.v = {};
-        if (a.layout == LMGC_ROPE_HALF) {
+      // the numbers of kHeads heads are asked for at once
+      for (int g0 = h0; g0 < h1; g0 += kHeads) {
+        Run<T> us[kHeads], vs[kHeads];
 #pragma unroll
-          for (int i = 0; i < R; i++) {
-            const float p = u.get(i), q = v.get(i);
-            y.set(i, turn_first(p, q, c[i], s[i]));
-            z.set(i, turn_second(p, q, c[i], s[i]));
-          }
-        } else {
+        for (int k = 0; k < kHeads; k++) {
+          const int h = min(g0 + k, h1 - 1);
+          us[k].v = *reinterpret_cast<const decltype(us[k].v)*>(x + h * a.ldhx + d0);
+          vs[k].v = *reinterpret_cast<const decltype(us[k].v)*>(x + h * a.ldhx + d1);
+        }
 #pragma unroll
-          for (int i = 0; i < R; i++) {
-            const float p = i < R / 2 ? u.get(2 * i) : v.get(2 * i - R), q = i < R / 2 ? u.get(2 * i + 1) : v.get(2 * i + 1 - R);
-            const float e = turn_first(p, q, c[i], s[i]), f = turn_second(p, q, c[i], s[i]);
-            if (i < R / 2) {
-              y.set(2 * i, e);
-              y.set(2 * i + 1, f);
-            } else {
-              z.set(2 * i - R, e);
-              z.set(2 * i + 1 - R, f);
+        for (int k = 0; k < kHeads; k++) {
+          const int h = g0 + k;
+          if (h >= h1) break;
+          const Run<T> u = us[k], v = vs[k];
+          Run<T> y, z;
+          y.v = {};
+          z.v = {};
+          if (a.layout == LMGC_ROPE_HALF) {
+#pragma unroll
+            for (int i = 0; i < R; i++) {
+              const float p = u.get(i), q = v.get(i);
+              y.set(i, turn_first(p, q, c[i], s[i]));
+              z.set(i, turn_second(p, q, c[i], s[i]));
+            }
+          } else {
+#pragma unroll
+            for (int i = 0; i < R; i++) {
+              const float p = i < R / 2 ? u.get(2 * i) : v.get(2 * i - R), q = i < R / 2 ? u.get(2 * i + 1) : v.get(2 * i + 1 - R);
+              const float e = turn_first(p, q, c[i], s[i]), f = turn_second(p, q, c[i], s[i]);
+              if (i < R / 2) {
+                y.set(2 * i, e);
+                y.set(2 * i + 1, f);
+              } else {
+                z.set(2 * i - R, e);
+                z.set(2 * i + 1 - R, f);
+              }
             }
           }
+          *reinterpret_cast<decltype(y.v)*>(o + h * a.ldho + d0) = y.v;
+          *reinterpret_cast<decltype(y.v)*>(o + h * a.ldho + d1) = z.v;
         }
-        *reinterpret_cast<decltype(u.v)*>(o + h * a.ldho + d0) = y.v;
-        *reinterpret_cast<decltype(u.v)*>(o + h * a.ldho + d1) = z.v;
       }
     } else if (copy) {
       const int d0 = a.rot + (place - nrot) * 2 * R;
