@@ -545,9 +545,9 @@ constexpr int kWaves = 4;
 
 struct AttnPlan {
   int64_t cols;          // of the longest sequence, at most
-  int few, few_short;    // columns of a sequence that the form for few takes, and of one of at most kShort keys
+  int few, few_short;    // columns of a sequence that the form for few takes, and of one whose keys are one part
   int columns;           // how many of them there are at most
-  int short_splits;      // parts of a short one, at most
+  int places;            // partial results of a sequence's columns in one head, at most
   Splits split;          // of the form for few columns
   Splits prompt;         // of the form for many
   int many, joined;      // whether the form for many is needed; whether it leaves partial results
@@ -555,11 +555,11 @@ struct AttnPlan {
   int pre, pre_chunk;    // splits of these
   float *po, *prompt_o, *pre_o;      // partial results, and maxima and sums
   float2 *pml, *prompt_ml, *pre_ml;
+  // Places of a column of a sequence with so many keys.
+  __device__ inline int parts(int total) const { return total <= split.least ? 1 : split.most; }
+  // Whether a sequence of so many columns and keys has few.
+  __device__ inline bool is_few(int cols, int total) const { return cols <= few || (cols <= few_short && total <= split.least); }
 };
-
-constexpr int kShort = 1024;
-// Whether a sequence of so many columns and keys has few.
-__device__ inline bool is_few(const AttnPlan& p, int cols, int total) { return cols <= p.few || (cols <= p.few_short && total <= kShort); }
 
 template <int HD, int NT, bool PREFIX>
 __global__ __launch_bounds__(kWaves * 64, NT > 1 ? 2 : HD == 64 ? 4 : 3) void attn_paged_split_kernel(
@@ -571,16 +571,15 @@ __global__ __launch_bounds__(kWaves * 64, NT > 1 ? 2 : HD == 64 ? 4 : 3) void at
   const int tid = threadIdx.x, lane = tid & 63, col = lane & 15, g = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int kvh = blockIdx.y, b = PREFIX ? 0 : blockIdx.z;
-  // the tiles that a sequence of any length may have, all their splits; then those of short ones, with theirs
+  // the tiles that a sequence of any length may have, all their splits; then those of sequences in one part
   const int all = PREFIX ? plan.pre : plan.split.most, of_any = PREFIX ? INT32_MAX : plan.few / TILE * all, bx = blockIdx.x;
-  const int tile = bx < of_any ? bx / all : plan.few / TILE + (bx - of_any) / plan.short_splits;
-  const int split = bx < of_any ? bx % all : (bx - of_any) % plan.short_splits, c0 = tile * TILE;
+  const int tile = bx < of_any ? bx / all : plan.few / TILE + bx - of_any, split = bx < of_any ? bx % all : 0, c0 = tile * TILE;
   Seq sq{0, r.n, 0};
   if (!PREFIX) sq = sequence(r, b, max_new);
   const int cols = sq.T * G, ncol = min(TILE, cols - c0);
   if (ncol <= 0) return;
   const Span span = PREFIX ? Span{0, 0, 0, plan.cut} : span_of(sq, mask, plan.cut);
-  if (!PREFIX && !is_few(plan, cols, span.total)) return;
+  if (!PREFIX && !plan.is_few(cols, span.total)) return;
   // the lane's columns (past the last: the last one's again), their positions
   int pos[NT], p0, p1;
   if (PREFIX) {
@@ -656,7 +655,7 @@ __global__ __launch_bounds__(kWaves * 64, NT > 1 ? 2 : HD == 64 ? 4 : 3) void at
         op[e] = __builtin_bit_cast(uint32_t, bf16x2{(__bf16)(acc[2 * e] * inv), (__bf16)(acc[2 * e + 1] * inv)});
     } else {
       const int64_t at = PREFIX ? ((int64_t)t * Hkv * G + hq) * plan.pre + split
-                                : (((int64_t)b * Hkv + kvh) * plan.columns + c) * plan.split.most + split;
+                                : ((int64_t)b * Hkv + kvh) * plan.places + c * plan.parts(span.total) + split;
       *reinterpret_cast<f32xd*>((PREFIX ? plan.pre_o : plan.po) + at * HD + d0) = acc;
       if (d0 == 0) (PREFIX ? plan.pre_ml : plan.pml)[at] = make_float2(M, L);
     }
@@ -720,7 +719,7 @@ __global__ __launch_bounds__(512, 2) void attn_paged_prompt_kernel(
   const int ncol = min(kTileCols, sq.T * G - c0);
   if (ncol <= 0) return;
   const Span span = PREFIX ? Span{0, min(plan.cut, (min(mask.sinks, plan.cut) + kGroup - 1) & ~(kGroup - 1)), 0, plan.cut} : span_of(sq, mask, plan.cut);
-  if (!PREFIX && is_few(plan, sq.T * G, span.total)) return;
+  if (!PREFIX && plan.is_few(sq.T * G, span.total)) return;
   // the wave's columns (past the last: the last one's again), their positions
   const int w0 = min(c0 + wave * 32, c0 + ncol - 1), w1 = min(c0 + wave * 32 + 31, c0 + ncol - 1);
   const bool works = wave * 32 < ncol;
@@ -1081,12 +1080,12 @@ __global__ __launch_bounds__(256) void attn_paged_join_kernel(Ragged r, int max_
     }
     if (i0 + own_row >= count || t < 0 || t >= q.T) continue;
     const Span span = span_of(q, mask, plan.cut);
-    const bool few = is_few(plan, q.T * G, span.total);
+    const bool few = plan.is_few(q.T * G, span.total);
     if (!ROWS && !few) continue;
     const int kvh = hq / G, chunk = (few ? plan.split : plan.prompt).chunk(span.total), nown = (span.total + chunk - 1) / chunk;
     if (plan.cut == 0 && nown <= 1) continue;  // written by the only split
     const int64_t at = ((int64_t)q.row + t) * Hq + hq, pre = at * plan.pre;
-    const int64_t own = few ? (((int64_t)b * Hkv + kvh) * plan.columns + t * G + (hq - kvh * G)) * plan.split.most : at * plan.prompt.most;
+    const int64_t own = few ? ((int64_t)b * Hkv + kvh) * plan.places + (t * G + hq - kvh * G) * plan.parts(span.total) : at * plan.prompt.most;
     const float* own_o = few ? plan.po : plan.prompt_o;
     const float2* own_ml = few ? plan.pml : plan.prompt_ml;
     // parts: those of the prefix, then the sequence's own
@@ -1136,11 +1135,18 @@ __global__ __launch_bounds__(256) void attn_paged_join_kernel(Ragged r, int max_
 int cut_of(int B, int shared) { return B > 1 ? shared / 64 * 64 : 0; }
 
 // Columns of a sequence that the form for few takes: of any, and (where max_new allows
-// no more, for the launch has to hold the tiles of all) of one of at most kShort keys.
-// 8 prompts of up to 150 rows over their own 160 keys, 12 heads of 64: 8.4 us by the
-// form for few, 16.9 with the form for many, whose 12 to 24 busy workgroups wait for
-// one another's loads; 3001 rows over 4001 keys are read 47 times as often by it.
+// no more, for the launch has to hold the tiles of all) of one whose keys are one part.
+// Every 16 columns read all keys, so it is the faster the fewer of either there are,
+// and for a sequence by itself: of 8 heads of 128, G = 4, 96 columns over 4000 keys
+// take 13.9 us by it and 22.6 by the form for many, those of 8 sequences 48.5 and
+// 48.8, 128 columns of 8 sequences 61.0 and 51.9; over 200 keys 256 columns of 8
+// sequences 17.0 and 20.1, over 380 22.7 and 22.2, 96 columns over 1000 40.0 and 25.6;
+// of 12 heads of 64, 512 columns of 8 sequences over 712 keys 32 and 48.
 constexpr int kFew = 64, kFewShort = 512;
+
+// Keys of a part, at least, in the form for many (fewer fill the chip with one prompt,
+// more leave less to join with several: 128 rows over 1000 keys take 29.5 us, 26.8
+// with 256, 38.1 with 1024; 8 prompts of them over 4000 keys 152, 204 and 123).
 constexpr int kLeast = 512;
 
 // Columns of the batch up to which a shared prefix goes to the form for few, with 32
@@ -1180,7 +1186,6 @@ AttnPlan plan_of(int n, int B, int Hq, int Hkv, int hd, int max_new, int tokens,
   int own_tokens = std::max(1, tokens - p.cut);
   if (mask.window) own_tokens = (int)std::min<int64_t>(own_tokens, (int64_t)mask.window + mask.sinks + max_new + 2 * kGroup);
   p.split = {std::min(64, (own_tokens + least - 1) / least), least, kWaves * kGroup};
-  p.short_splits = std::min(p.split.most, (kShort + least - 1) / least);
   const int64_t groups = (rule + kTileCols - 1) / kTileCols * Hkv;
   p.prompt = {groups >= 128 ? 1 : (int)std::min<int64_t>({16, 256 / groups, (own_tokens + kLeast - 1) / kLeast}), kLeast, kStep};
   // the prefix in parts that fill the chip (two workgroups of few columns to a CU, one
@@ -1191,8 +1196,9 @@ AttnPlan plan_of(int n, int B, int Hq, int Hkv, int hd, int max_new, int tokens,
   const int parts = (int)std::max<int64_t>(1, std::min<int64_t>(64, (pre_cols <= kFewPre ? 512 : 256) / pre_groups));
   p.pre_chunk = (std::max(kLeast / 2, (p.cut + parts - 1) / parts) + kStep * 2 - 1) / (kStep * 2) * (kStep * 2);
   p.pre = (p.cut + p.pre_chunk - 1) / p.pre_chunk;
-  const int64_t own = p.cut || p.split.most > 1 ? (int64_t)B * Hkv * p.columns * p.split.most : 0;
-  p.many = cols > kFew && !(rule <= kFewShort && own_tokens <= kShort);
+  p.places = std::max(std::min(p.columns, kFew) * p.split.most, p.columns);
+  const int64_t own = p.cut || p.split.most > 1 ? (int64_t)B * Hkv * p.places : 0;
+  p.many = cols > kFew && !(rule <= kFewShort && own_tokens <= least);
   p.joined = p.many && (p.cut || p.prompt.most > 1);
   const int64_t many = p.joined ? (int64_t)n * Hq * p.prompt.most : 0;
   const int64_t pre = (int64_t)n * Hq * p.pre;
@@ -1263,7 +1269,7 @@ hipError_t launch_attention_paged(const PagedAttnArgs& a, hipStream_t s) {
       else prompt(std::true_type{}, (all + kTileCols - 1) / kTileCols, 0, plan.pre);
     }
     const int tiles = (plan.columns + 15) / 16, of_any = std::min(tiles, kFew / 16);
-    split(std::false_type{}, std::integral_constant<int, 1>{}, of_any * plan.split.most + (tiles - of_any) * plan.short_splits, r.B);
+    split(std::false_type{}, std::integral_constant<int, 1>{}, of_any * plan.split.most + tiles - of_any, r.B);
     if (plan.many) {
       const Tiles t = tiles_of(r.n, G, r.B, plan.cols);
       prompt(std::false_type{}, t.count, t.by_turns, plan.prompt.most);

@@ -314,8 +314,9 @@ def test_attention_splits_do_not_follow_the_number_of_rows():
 
 
 # Around the borders between the forms: 64 columns of any sequence, 512 of one of at
-# most 1024 keys where max_new allows no more.
-@pytest.mark.parametrize("new,old", [(16, 100), (17, 100), (17, 1007), (17, 1008), (128, 896), (128, 897), (127, 0), (129, 100), (128, 2000)])
+# most 512 keys of 128 (1024 of 64) where max_new allows no more.
+@pytest.mark.parametrize("new,old", [(16, 100), (17, 100), (17, 495), (17, 496), (128, 384), (128, 385), (17, 1007), (17, 1008), (128, 896),
+                                     (128, 897), (127, 0), (129, 100), (128, 2000)])
 @pytest.mark.parametrize("hd", [64, 128])
 def test_attention_borders_of_the_forms(new, old, hd):
     s = Setup([(new, old), (1, 2000), (3, 0)], 64, 2, hd, new)
