@@ -98,6 +98,11 @@ __device__ inline int64_t group_at(const Ragged& r, int page, int Hkv, int h, in
 // sin are read once for the key and the queries.  Keys go out as they are in a
 // group, 16 bytes a lane; values meet in LDS, whose 16-byte slots are permuted so
 // that the 64 halves of a store fall on all banks.
+//
+// It is bound by memory: 4 x 4096 rows of 32 and 8 heads of 128, bf16, 790 MB, take
+// 159 us (4.97 TB/s; a copy 5.15).  With 4 places of 16 tokens to a wave, so half
+// lines to a load, it was 180, with the heads in the grid's slower dimension 206,
+// with non-temporal loads 207.
 template <class T>
 struct Eight;  // 8 dims of a row
 template <>
@@ -537,10 +542,15 @@ struct Columns {
 // Columns: column c = t G + i of a (sequence, key/value head) is query head
 // kvh G + i of its new token t; for the prefix, of row t of the batch.
 //
-// Grid: (splits x tiles of 16 NT columns, Hkv, B), 256 threads.  Wave w takes
+// Grid: (tiles of 16 NT columns x splits, Hkv, B), 256 threads.  Wave w takes
 // groups w, w + 4, .. of its split: S^T = K Q^T, so lane (col, g) holds the
 // scores of its column and tokens 16 i + 4 g + r of a group, an online softmax,
 // O^T += V^T P^T.  The waves' parts meet in LDS.
+//
+// For single tokens it is bound by the cache's bytes: 8 sequences of 4095, 32 heads of
+// 128, 537 MB, in 88 us (6.1 TB/s), and 5 for the join.  Twelve waves a CU, each
+// with a group of 16 KB under way, hide the loads' way; parts of 64 KB a wave keep
+// what is left for the join small.
 constexpr int kWaves = 4;
 
 struct AttnPlan {
@@ -678,6 +688,11 @@ __global__ __launch_bounds__(kWaves * 64, NT > 1 ? 2 : HD == 64 ? 4 : 3) void at
 // (bundle t) and those before them.  A bundle's place in the ring is free again two
 // stretches behind its own, so bundle t + kRing - 2 is asked for in stretch t; and
 // before a barrier each wave waits for its own part of the bundle that is read next.
+//
+// Two prompts of 3001 rows behind 1000 tokens, 32 on 8 heads of 128: 226 us (1.06
+// PFLOP/s; another card 244), where the products alone take 203 and all but them
+// 171.  With two barriers a step and all waves in one phase 242, 32 x 32 x 16
+// products 260, loads beside the products instead of the exponentials 264 (249).
 constexpr int kTileCols = 256;
 constexpr int kStep = 2 * kGroup;
 constexpr int kRing = 4, kAhead = kRing - 2;
@@ -1051,7 +1066,8 @@ __global__ __launch_bounds__(512, 2) void attn_paged_prompt_kernel(
 //
 // ROWS: all rows; else the columns of sequences with few of them, where the others
 // are in one part.  A lane has 4 dims of a row and takes the parts 8 at a time, whose
-// statistics and numbers are asked for together.
+// statistics and numbers are asked for together.  14400 rows of 64 dims in 5 parts
+// take 6.9 us (with a wave to a row 13.5), mostly the way to a row's sequence and back.
 template <int HD, bool ROWS>
 __global__ __launch_bounds__(256) void attn_paged_join_kernel(Ragged r, int max_new, int Hkv, int G, AttnPlan plan, Mask mask,
                                                               uint16_t* __restrict__ out) {
@@ -1131,8 +1147,8 @@ __global__ __launch_bounds__(256) void attn_paged_join_kernel(Ragged r, int max_
   }
 }
 
-// Tokens that are computed for the batch: whole pairs of groups.
-int cut_of(int B, int shared) { return B > 1 ? shared / 64 * 64 : 0; }
+// Tokens that are computed for the batch: whole steps of the form for many.
+int cut_of(int B, int shared) { return B > 1 ? shared / kStep * kStep : 0; }
 
 // Columns of a sequence that the form for few takes: of any, and (where max_new allows
 // no more, for the launch has to hold the tiles of all) of one whose keys are one part.
@@ -1158,8 +1174,8 @@ constexpr int kFewPre = 256, kPreTile = 32;
 
 // Workgroups for the tiles of many columns of one head and split: as many tiles of
 // every sequence as the longest may have, by turns, so that the longest tiles run
-// first; where that were many more than there are, the places that the rows take at
-// most (two prompts of 3001 rows: the last workgroups end 15 % later).
+// first (of two prompts of 3001 rows the last workgroups end 15 % later the other way
+// round); where that were many more than there are, as many as the rows can fill.
 struct Tiles {
   int64_t count;
   int by_turns;
@@ -1179,7 +1195,7 @@ AttnPlan plan_of(int n, int B, int Hq, int Hkv, int hd, int max_new, int tokens,
   p.cols = cols;
   p.columns = (int)std::min<int64_t>(cols, p.few_short);
   p.cut = std::min(cut_of(B, shared), tokens);
-  const int least = 256 * 128 / hd * 2;
+  const int least = 512 * 128 / hd;  // keys of a part in the form for few, at least
   // most tokens of a sequence's own part: those of its pages, or, with a window, of
   // whole groups around it, its new tokens and the first ones (a step in a window of
   // 512 needs one part, no join and 2.7 us less)
@@ -1187,6 +1203,7 @@ AttnPlan plan_of(int n, int B, int Hq, int Hkv, int hd, int max_new, int tokens,
   if (mask.window) own_tokens = (int)std::min<int64_t>(own_tokens, (int64_t)mask.window + mask.sinks + max_new + 2 * kGroup);
   p.split = {std::min(64, (own_tokens + least - 1) / least), least, kWaves * kGroup};
   const int64_t groups = (rule + kTileCols - 1) / kTileCols * Hkv;
+  // (split where the tiles of the longest sequence fill less than half of the chip)
   p.prompt = {groups >= 128 ? 1 : (int)std::min<int64_t>({16, 256 / groups, (own_tokens + kLeast - 1) / kLeast}), kLeast, kStep};
   // the prefix in parts that fill the chip (two workgroups of few columns to a CU, one
   // of many), half of kLeast or more each: with 128 columns behind 8192 tokens 17.5 us

@@ -12,6 +12,7 @@ namespace {
 
 typedef float f32x2 __attribute__((ext_vector_type(2)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 
 // ------------------------------------------------------------------- table
@@ -20,6 +21,8 @@ typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 // positions of a frequency, from a multiple of kPositions on: it turns the first
 // one's (cos, sin) by the frequency, in float64, for the next ones.  A step adds
 // two roundings, so the last is off by 2^-49, of float32's 2^-24.
+// 131072 positions of 64 frequencies, 67 MB, take 12.5 us (5.35 TB/s), bound by the
+// stores; 31 with a sine and a cosine for each.
 struct Freqs {
   double f[kMaxRot / 2];
 };
@@ -49,6 +52,8 @@ __global__ __launch_bounds__(256) void rope_table_kernel(Freqs freqs, int half, 
 // ---------------------------------------------------------------- rotation
 // 16 bytes of a row to a run; a thread has the two runs of as many pairs, of
 // the same place in kHeads heads, so a pair's cos and sin are read once for them.
+// Bound by memory: 8191 rows of 36 heads of 64, float32, 151 MB, take 35.0 us (4.35
+// TB/s; a copy 5.15); 37.4 with one head's loads at a time.
 template <class T>
 struct Run;
 template <>
@@ -56,16 +61,16 @@ struct Run<float> {
   static constexpr int n = 4;
   f32x4 v;
   __device__ inline float get(int i) const { return v[i]; }
-  __device__ inline void set(int i, float x) { v[i] = x; }
+  __device__ inline void set(const float* y) { v = f32x4{y[0], y[1], y[2], y[3]}; }
 };
 template <>
 struct Run<uint16_t> {
   static constexpr int n = 8;
   u32x4 v;
   __device__ inline float get(int i) const { return __builtin_bit_cast(float, i & 1 ? v[i >> 1] & 0xffff0000u : v[i >> 1] << 16); }
-  __device__ inline void set(int i, float x) {
-    const uint32_t b = f32_to_bf16(x);
-    v[i >> 1] = i & 1 ? (v[i >> 1] & 0xffffu) | b << 16 : (v[i >> 1] & 0xffff0000u) | b;
+  __device__ inline void set(const float* y) {
+#pragma unroll
+    for (int i = 0; i < 4; i++) v[i] = __builtin_bit_cast(uint32_t, bf16x2{(__bf16)y[2 * i], (__bf16)y[2 * i + 1]});
   }
 };
 
@@ -77,7 +82,7 @@ __device__ inline void store1(uint16_t* p, float x) { *p = f32_to_bf16(x); }
 // Grid: (heads / kHeads, blocks of rows), 256 threads: np places of a row side
 // by side.  FAST: rot a multiple of two runs, hd of a run, everything 16-byte
 // aligned.
-constexpr int kHeads = 4;
+constexpr int kHeads = 2;
 constexpr int kRowBlocks = 32768;  // in one plane of the grid
 
 template <class T, bool FAST>
@@ -117,32 +122,27 @@ __global__ __launch_bounds__(256) void rope_kernel(RopeArgs a, int np, int rows,
           const int h = g0 + k;
           if (h >= h1) break;
           const Run<T> u = us[k], v = vs[k];
-          Run<T> y, z;
-          y.v = {};
-          z.v = {};
+          float y[R], z[R];
           if (a.layout == LMGC_ROPE_HALF) {
 #pragma unroll
             for (int i = 0; i < R; i++) {
               const float p = u.get(i), q = v.get(i);
-              y.set(i, turn_first(p, q, c[i], s[i]));
-              z.set(i, turn_second(p, q, c[i], s[i]));
+              y[i] = turn_first(p, q, c[i], s[i]);
+              z[i] = turn_second(p, q, c[i], s[i]);
             }
           } else {
 #pragma unroll
             for (int i = 0; i < R; i++) {
               const float p = i < R / 2 ? u.get(2 * i) : v.get(2 * i - R), q = i < R / 2 ? u.get(2 * i + 1) : v.get(2 * i + 1 - R);
-              const float e = turn_first(p, q, c[i], s[i]), f = turn_second(p, q, c[i], s[i]);
-              if (i < R / 2) {
-                y.set(2 * i, e);
-                y.set(2 * i + 1, f);
-              } else {
-                z.set(2 * i - R, e);
-                z.set(2 * i + 1 - R, f);
-              }
+              (i < R / 2 ? y[2 * i] : z[2 * i - R]) = turn_first(p, q, c[i], s[i]);
+              (i < R / 2 ? y[2 * i + 1] : z[2 * i + 1 - R]) = turn_second(p, q, c[i], s[i]);
             }
           }
-          *reinterpret_cast<decltype(y.v)*>(o + h * a.ldho + d0) = y.v;
-          *reinterpret_cast<decltype(y.v)*>(o + h * a.ldho + d1) = z.v;
+          Run<T> out;
+          out.set(y);
+          *reinterpret_cast<decltype(out.v)*>(o + h * a.ldho + d0) = out.v;
+          out.set(z);
+          *reinterpret_cast<decltype(out.v)*>(o + h * a.ldho + d1) = out.v;
         }
       }
     } else if (copy) {
@@ -189,7 +189,10 @@ hipError_t launch_rope(const RopeArgs& a, hipStream_t s) {
     const int np = fast ? a.rot / 2 / R + (a.hd - a.rot + 2 * R - 1) / (2 * R) : std::min((a.hd + 1) / 2, 64);
     const int rows = 256 / np;
     const int64_t blocks = ((int64_t)a.n + rows - 1) / rows;
-    const int per = blocks * a.heads >= 4096 ? 4 : 1;
+    // two heads to a thread where one fills the chip: 8 rows of 64 heads of 128 take 2.17
+    // us with one and 2.30 with two, 512 rows 4.47 and 3.98 (four: 3.97), 8192 47.0 and 45.6
+    // (47.2)
+    const int per = blocks * a.heads >= 512 ? kHeads : 1;
     const dim3 grid((a.heads + per - 1) / per, std::min<int64_t>(blocks, kRowBlocks), (blocks + kRowBlocks - 1) / kRowBlocks);
     if (fast) rope_kernel<T, true><<<grid, 256, 0, s>>>(a, np, rows, per);
     else rope_kernel<T, false><<<grid, 256, 0, s>>>(a, np, rows, per);
