@@ -1239,7 +1239,8 @@ int64_t paged_workspace_bytes(int n, int B, int Hq, int Hkv, int hd, int max_new
 
 int64_t paged_workgroups(int n, int B, int Hq, int Hkv, int hd, int max_new, int tokens, int shared) {
   const AttnPlan p = plan_of(n, B, Hq, Hkv, hd, max_new, tokens, shared, Mask{0, 0}, nullptr, nullptr);
-  return tiles_of(n, Hq / Hkv, B, p.cols).count * Hkv * std::max(p.prompt.most, p.pre);
+  const int64_t pre = p.cut ? ((int64_t)n * (Hq / Hkv) + kTileCols - 1) / kTileCols * p.pre : 0;
+  return std::max(tiles_of(n, Hq / Hkv, B, p.cols).count * p.prompt.most, pre) * Hkv;
 }
 
 hipError_t launch_paged_append(const AppendArgs& a, hipStream_t s) {

@@ -220,7 +220,7 @@ static void run(const Case& c, int id) {
   std::copy(gq, gq + q.size(), wq.begin());
   uint16_t* out = (uint16_t*)guarded(q.size() * 2);
   std::fill(out, out + q.size(), (uint16_t)0x1234);
-  const int max_new = std::min(c.max_new, c.n);
+  const int max_new = c.max_new;
   const int64_t bytes = paged_workspace_bytes(c.n, B, Hq, c.Hkv, hd, max_new, tokens, c.shared);
   char* ws = guarded(bytes);
   memset(ws, 0xff, bytes);
@@ -270,7 +270,7 @@ static void run(const Case& c, int id) {
 
 int main() {
   const int big = 1 << 30;
-  const std::vector<Case> cases = {
+  std::vector<Case> cases = {
       // a whole batch, lengths on every side of groups and pages, rows behind the last
       {64, 32, 2, 2, 0, 0, 0, 99, 64, LMGC_ROPE_HALF, {0, 1, 36, 36, 37}, {40, 0, 5, 31}, {3, 4, 7, 0, 1, 2, 5, 6, 7, 8, 9, 10}, 40, 12},
       // pages outside the pool, lengths and rows outside theirs
@@ -293,7 +293,22 @@ int main() {
       // many columns behind a prefix, rows of no token among them
       {64, 32, 1, 4, 0, 0, 64, 999, 64, LMGC_ROPE_HALF, {2, 40, 41, 61}, {64, 80, 70}, {0, 1, 2, 3, 0, 1, 4, 5, 0, 1, 6, 7}, 63, 8},
       {64, 32, 1, 4, 50, 3, 64, 999, 64, LMGC_ROPE_HALF, {0, 40, 60}, {64, 90}, {0, 1, 2, 3, 0, 1, 4, 5}, 60, 8},
+      // more rows than max_new, which has many columns; and few of one part, beside others
+      {64, 32, 1, 16, 0, 0, 0, 40, 64, LMGC_ROPE_HALF, {0, 50, 52}, {20, 70}, {0, 1, 2, 3, 4, 5}, 53, 6},
+      {64, 32, 1, 8, 0, 0, 0, 60, 64, LMGC_ROPE_HALF, {0, 30, 33, 93}, {20, 70, 10}, {0, 1, 2, 3, 4, 5, 6, 7, 8}, 94, 9},
+      {128, 32, 1, 8, 40, 2, 64, 60, 64, LMGC_ROPE_HALF, {0, 30, 33}, {64, 70}, {0, 1, 2, 3, 0, 1, 4, 5}, 34, 6},
+      {128, 64, 1, 4, 0, 0, 0, 20, 128, LMGC_ROPE_HALF, {0, 17, 20}, {500, 40}, {8, 7, 6, 5, 4, 3, 2, 1, 0, 9, 10, 11, 12, 13, 14, 15, 16, 17}, 20, 18},
   };
+  // more sequences than a wave has lanes, some without rows, behind a prefix: 140 columns, 280, more than 512
+  for (int G : {2, 4, 8}) {
+    Case c{64, 32, 1, G, 0, 0, 64, 999, 64, LMGC_ROPE_HALF, {1}, {}, {}, 73, 72};
+    for (int b = 0; b < 70; b++) {
+      c.starts.push_back(c.starts[b] + (b % 9 == 4 ? 0 : b % 9 == 5 ? 2 : 1));
+      c.lens.push_back(64 + b % 30);
+      c.pages.insert(c.pages.end(), {0, 1, 2 + b});
+    }
+    cases.push_back(c);
+  }
   for (int late = 0; late < 2; late++) {
     g_late = late;
     for (size_t i = 0; i < cases.size(); i++) run(cases[i], (int)i);

@@ -359,6 +359,16 @@ def test_shared_tokens_inside_the_prefix():
     _attend_check(s, s.rows(4), shared=256, window=40, sinks=70)
 
 
+@pytest.mark.parametrize("G", [1, 2, 4])
+@pytest.mark.parametrize("B_", [65, 150])
+def test_shared_by_more_sequences_than_lanes(B_, G):
+    """(some of them without rows)"""
+    s = Setup([(0 if b % 9 == 4 else 2 if b % 9 == 5 else 1, 128 + b % 70) for b in range(B_)], 64, 1, 64, B_, pad=2, shared=128)
+    q = s.rows(G)
+    _attend_check(s, q, shared=128)
+    _attend_check(s, q, shared=128, window=90, sinks=3)
+
+
 def test_shared_of_one_sequence_and_of_none():
     torch = _torch()
     s = Setup([(2, 300)], 64, 2, 64, 3)

@@ -135,6 +135,14 @@ def test_attention_unsupported(kw):
     assert _attention(**kw) == EUNSUPPORTED
 
 
+def test_attention_of_more_columns_than_a_launch_has():
+    """(of the batch, behind a prefix: rows of no token count too)"""
+    rows = dict(n=1 << 24, Hq=1024, Hkv=64, ldq=1 << 16, max_new=1, n_pages=1, page=64, bytes=1 << 62, ws=1 << 58, q=1 << 55, out=1 << 56)
+    assert _attention(**rows, shared=64) == EUNSUPPORTED
+    rows["max_new"] = 1 << 24
+    assert _attention(**rows) == EUNSUPPORTED
+
+
 def test_attention_of_no_rows_is_fine():
     assert _attention(n=0, q=None, out=None, ws=None, bytes=0) == 0
 
