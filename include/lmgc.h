@@ -743,7 +743,8 @@ int lmgc_op_paged_append(const void* d_k, const void* d_v, int32_t dtype, int64_
  *   aligned, its contents free; calls that may run at the same time need one each.
  * Masked keys count for nothing, whatever they and their values hold (NaN and
  * infinities too); visible ones that are not finite do as in the formula.  A
- * query that sees no key (its pages are outside the pool) gets zeros.
+ * query that sees no key (its pages are outside the pool), or whose scores are all
+ * -infinity, gets zeros.
  * Probabilities are rounded to bf16 (2^-8 of each at most) for their product with the
  * values and divided by the sum of the rounded ones; scores, maxima and sums are
  * float32.  A query's result depends on its own sequence (length and number of

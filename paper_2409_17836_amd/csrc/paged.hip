@@ -1124,10 +1124,9 @@ __global__ __launch_bounds__(256) void attn_paged_join_kernel(Ragged r, int max_
 #pragma unroll
       for (int k = 0; k < 8; k++) top = fmaxf(top, ml[k].x);
       if (top > M) {
-        // (a sum of none but scores of -inf is no number; behind a greater one it is nothing)
-        const float a = __builtin_amdgcn_exp2f(M - top);
-        L = M == -INFINITY ? 0.f : L * a;
-        acc = M == -INFINITY ? f32x4{} : acc * a;
+        const float a = __builtin_amdgcn_exp2f(M - top);  // (0 times what came of a NaN stays one)
+        L *= a;
+        acc *= a;
         M = top;
       }
 #pragma unroll

@@ -247,6 +247,42 @@ def test_attention_visible_infinities_of_values(T):
     _attend_check(s, s.rows(2))
 
 
+def _set_keys(s, tokens, value, dim=slice(None)):
+    """The keys of the first sequence's tokens, or one dim of them."""
+    torch = _torch()
+    plain = R.in_pool(np.arange(s.cache[0].numel()).reshape(s.cache[0].shape), False)
+    for j in tokens:
+        at = np.atleast_1d(plain[s.pages_h[0, j // s.page], :, j % s.page, dim]).reshape(-1)
+        s.cache[0].view(-1)[torch.from_numpy(at).cuda()] = value
+
+
+@pytest.mark.parametrize("T", [1, 30])
+@pytest.mark.parametrize("tokens", [range(3), range(4500), range(5000)])
+def test_attention_keys_that_are_no_numbers(T, tokens):
+    """A NaN among the keys that a query sees is one in its result, in whichever of its parts."""
+    s = Setup([(T, 5000), (1, 40)], 64, 1, 128, 3)
+    _set_keys(s, tokens, float("nan"))
+    out = _attend_check(s, s.rows(4))
+    assert bool(out[:T].isnan().all()) and bool(out[T:].isfinite().all())
+
+
+@pytest.mark.parametrize("T", [1, 30])
+def test_attention_scores_of_minus_infinity(T):
+    """They weigh nothing beside others; where there are no others the result is zeros."""
+    s = Setup([(T, 5000), (1, 40)], 64, 1, 128, 3)
+    q = s.rows(4)
+    q[:, :, 0] = 1.0
+    older = 4700
+    _set_keys(s, range(older), 0.0)
+    want, tol, _ = R.attention(_np(q)[T - 1:T], *s.plain(), R.Batch(s.pages_h[:1], np.array([0, 1]), np.array([5000 + T - 1]), 1, s.n_pages, s.page), 1,
+                               window=5000 + T - older)
+    _set_keys(s, range(older), float("-inf"), 0)
+    got = _np(_attend(s, q)).reshape(s.n, 4, 128)
+    assert (abs(got[T - 1] - want[0]) <= tol[0]).all()
+    _set_keys(s, range(older, 5000 + T), float("-inf"), 0)
+    assert (_np(_attend(s, q))[:T] == 0).all()
+
+
 def test_attention_pages_outside_the_pool():
     """Their tokens count as masked; a query that sees no other gets zeros."""
     s = Setup([(40, 100), (1, 20), (2, 90), (1, 64)], 32, 2, 64, 4, stale=float("nan"))
