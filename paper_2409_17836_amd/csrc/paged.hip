@@ -252,7 +252,7 @@ __global__ __launch_bounds__(256) void paged_append_kernel(AppendArgs a) {
     put(d1, y1);
   }
   // values: slot (d, 4 tokens) holds tokens 4 k .. + 3 of both halves
-  auto slot = [](int s) __attribute__((always_inline)) { return s ^ ((s >> 4 & 3) ^ (s >> 7 & 1) << 1 | (s >> 6 & 1) << 2); };
+  auto slot = [](int s) __attribute__((always_inline)) { return s ^ (((s >> 4 & 3) ^ (s >> 7 & 1) << 1) | (s >> 6 & 1) << 2); };
   if (keys && there) {
     uint16_t* words = reinterpret_cast<uint16_t*>(sv);
 #pragma unroll

@@ -52,7 +52,7 @@ __global__ __launch_bounds__(256) void rope_table_kernel(Freqs freqs, int half, 
 // ---------------------------------------------------------------- rotation
 // 16 bytes of a row to a run; a thread has the two runs of as many pairs, of
 // the same place in kHeads heads, so a pair's cos and sin are read once for them.
-// Bound by memory: 8191 rows of 36 heads of 64, float32, 151 MB, take 35.0 us (4.35
+// Bound by memory: 8191 rows of 36 heads of 64, float32, 151 MB, take 35.6 us (4.27
 // TB/s; a copy 5.15); 37.4 with one head's loads at a time.
 template <class T>
 struct Run;
