@@ -742,9 +742,10 @@ int lmgc_op_paged_append(const void* d_k, const void* d_v, int32_t dtype, int64_
  *   d_ws: lmgc_paged_workspace bytes (with tokens = max_pages page), 16-byte
  *   aligned, its contents free; calls that may run at the same time need one each.
  * Masked keys count for nothing, whatever they and their values hold (NaN and
- * infinities too); visible ones that are not finite do as in the formula.  A
- * query that sees no key (its pages are outside the pool), or whose scores are all
- * -infinity, gets zeros.
+ * infinities too); visible ones that are not finite do as in the formula, where
+ * a probability below 2^-90 of the largest may be zero (and so make an infinite
+ * value NaN).  A query that sees no key (its pages are outside the pool), or whose
+ * scores are all -infinity, gets zeros.
  * Probabilities are rounded to bf16 (2^-8 of each at most) for their product with the
  * values and divided by the sum of the rounded ones; scores, maxima and sums are
  * float32.  A query's result depends on its own sequence (length and number of

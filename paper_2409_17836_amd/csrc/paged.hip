@@ -1118,7 +1118,10 @@ __global__ __launch_bounds__(256) void attn_paged_join_kernel(Ragged r, int max_
         const int64_t part = shared ? pre + e : own + (e - plan.pre);
         ml[k] = (shared ? plan.pre_ml : own_ml)[part];
         x[k] = *reinterpret_cast<const f32x4*>((shared ? plan.pre_o : own_o) + part * HD + d);
-        if (e0 + k >= n) ml[k] = make_float2(-INFINITY, 0.f);
+        if (e0 + k >= n) {
+          ml[k] = make_float2(-INFINITY, 0.f);
+          x[k] = f32x4{};
+        }
       }
       float top = M;
 #pragma unroll
@@ -1134,7 +1137,7 @@ __global__ __launch_bounds__(256) void attn_paged_join_kernel(Ragged r, int max_
         // parts without a token that the query sees (m = -inf, l = 0) count for nothing
         const float w = ml[k].x == -INFINITY && ml[k].y == 0.f ? 0.f : __builtin_amdgcn_exp2f(ml[k].x - M);
         L += w * ml[k].y;
-        if (w != 0.f) acc += w * x[k];
+        acc += w * x[k];  // (of no weight too: what is no number there stays none)
       }
     }
     const float inv = L == 0.f ? 0.f : 1.0f / L;

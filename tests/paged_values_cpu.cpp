@@ -1,0 +1,154 @@
+// Attention over the paged cache on the CPU (tests/cpu_hip) beside plain loops in
+// float64, for values at which the way to a result shows: no numbers in one part of
+// the keys, scores far apart.  Prints "ok".
+#define main paged_cpu_main
+#include "paged_cpu.cpp"
+#undef main
+
+struct Problem {
+  int hd, page, Hkv, G, window, sinks, shared, max_new;
+  std::vector<int> T, len;  // new tokens of each sequence, tokens before them
+  int pad;                  // rows of no token behind them
+};
+
+// A batch whose numbers are set one by one.  The first `shared` tokens of all
+// sequences are those of the first.
+struct Attention {
+  Problem p;
+  int B, most, n, Hq;
+  std::vector<int> starts;
+  std::vector<float> q, kv[2];  // [n, Hq, hd]; [B, most page, Hkv, hd]
+  static constexpr float scale = 0.125f;
+  Attention(const Problem& p, int seed) : p(p), B((int)p.T.size()), most(0), Hq(p.Hkv * p.G), starts{0} {
+    for (int b = 0; b < B; b++) {
+      starts.push_back(starts[b] + p.T[b]);
+      most = std::max(most, (p.len[b] + p.T[b] + p.page - 1) / p.page);
+    }
+    n = starts[B] + p.pad;
+    std::mt19937 rng(seed);
+    std::normal_distribution<float> normal;
+    q.resize((size_t)n * Hq * p.hd);
+    for (auto& x : kv) x.resize((size_t)B * most * p.page * p.Hkv * p.hd);
+    for (auto* x : {&q, &kv[0], &kv[1]})
+      for (auto& e : *x) e = normal(rng);
+  }
+  float& query(int row, int h, int d) { return q[((size_t)row * Hq + h) * p.hd + d]; }
+  float& token(int i, int b, int t, int h, int d) { return kv[i][((((size_t)(t < p.shared ? 0 : b) * most * p.page) + t) * p.Hkv + h) * p.hd + d]; }
+  float& key(int b, int t, int h, int d) { return token(0, b, t, h, d); }
+  float& value(int b, int t, int h, int d) { return token(1, b, t, h, d); }
+
+  std::vector<uint16_t> run() {
+    const int hd = p.hd, lead = p.shared / p.page, n_pages = lead + B * (most - lead), tokens = most * p.page;
+    check(p.shared % p.page == 0, "whole pages", p.shared);
+    std::vector<int> pages(B * most);
+    for (int b = 0; b < B; b++)
+      for (int i = 0; i < most; i++) pages[b * most + i] = i < lead ? i : lead + b * (most - lead) + i - lead;
+    std::vector<uint16_t> pool[2], wq(q.size());
+    for (auto& x : pool) x.assign((size_t)n_pages * p.Hkv * p.page * hd, 0x7fc1);
+    for (int i = 0; i < 2; i++)
+      for (int b = 0; b < B; b++)
+        for (int t = 0; t < p.len[b] + p.T[b]; t++)
+          for (int h = 0; h < p.Hkv; h++)
+            for (int d = 0; d < hd; d++)
+              pool[i][(((size_t)pages[b * most + t / p.page] * p.Hkv + h) * p.page + t % p.page / 32 * 32) * hd + (i ? at_value(t % 32, d) : at_key(t % 32, d, hd))] =
+                  f32_to_bf16(token(i, b, t, h, d));
+    for (size_t i = 0; i < q.size(); i++) wq[i] = f32_to_bf16(q[i]);
+    uint16_t* out = (uint16_t*)guarded(q.size() * 2);
+    std::fill(out, out + q.size(), (uint16_t)0x1234);
+    const int64_t bytes = paged_workspace_bytes(n, B, Hq, p.Hkv, hd, p.max_new, tokens, p.shared);
+    char* ws = guarded(bytes);
+    memset(ws, 0xff, bytes);
+    const Ragged r{copy(pages), copy(starts), copy(p.len), B, n, most, p.page, n_pages};
+    const PagedAttnArgs a{copy(wq), copy(pool[0]), copy(pool[1]), Hq * hd, Hq, p.Hkv, hd, p.max_new, p.window, p.sinks, p.shared, scale, out, ws, r};
+    launch_attention_paged(a, nullptr);
+    for (auto& l : g_loads) check(l.empty(), "a load outlives its kernel", 0);
+    return std::vector<uint16_t>(out, out + q.size());
+  }
+
+  // Against softmax(scale q.k) v: probabilities rounded to bf16 (2^-8 of each) as the
+  // result is, scores in float32 (2^-24 (hd + 8) of the sum of their terms' sizes).
+  // A probability below 2^-126 of the largest is zero.
+  void compare(const char* what, int id) {
+    g_late = id % 2;
+    const std::vector<uint16_t> got = run();
+    auto bf16 = [](float x) { return (double)bf16_to_f32(f32_to_bf16(x)); };
+    for (int b = 0; b < B; b++)
+      for (int t = 0; t < std::min(p.T[b], p.max_new); t++)
+        for (int h = 0; h < Hq; h++) {
+          const int row = starts[b] + t, pos = p.len[b] + t, kvh = h / p.G;
+          std::vector<int> seen;
+          std::vector<double> s;
+          double top = -INFINITY, size = 0, sum = 0;
+          for (int j = 0; j <= pos; j++) {
+            if (p.window && j <= pos - p.window && j >= p.sinks) continue;
+            double x = 0, terms = 0;
+            for (int d = 0; d < p.hd; d++) {
+              const double y = scale * bf16(query(row, h, d)) * bf16(key(b, j, kvh, d));
+              x += y;
+              terms += fabs(y);
+            }
+            seen.push_back(j);
+            s.push_back(x);
+            if (x > top) top = x;
+            if (std::isfinite(terms)) size = std::max(size, terms);
+          }
+          for (double& x : s) {
+            x = top == -INFINITY && x == x ? 0 : exp(x - top);
+            if (x < 0x1p-126) x = 0;
+            sum += x;
+          }
+          for (int d = 0; d < p.hd; d++) {
+            double w = 0, dev = 0;
+            for (size_t i = 0; i < seen.size() && sum != 0; i++) {
+              const double x = s[i] / sum * bf16(value(b, seen[i], kvh, d));
+              w += x;
+              dev += fabs(x);
+            }
+            dev += fabs(w);
+            const double g = bf16_to_f32(got[((size_t)row * Hq + h) * p.hd + d]);
+            const double tol = (0x1p-8 + 0x1p-22 + 0x1p-24 * (p.hd + 8) * size) * dev * (1 + 0x1p-6) + 0x1p-8 * fabs(w) + 1e-37;
+            if (g != g ? w == w : std::isfinite(w) ? !(fabs(g - w) <= tol) : g != w) {
+              printf("%s %d, row %d head %d dim %d: %g, not %g\n", what, id, row, h, d, g, w);
+              exit(1);
+            }
+          }
+        }
+    for (size_t i = (size_t)starts[B] * Hq * p.hd; i < got.size(); i++) check(got[i] == 0x1234, "a row of no token", (int)i);
+  }
+};
+
+// Keys of two sizes along the first dim: scores of -160 for tokens before `half` and of
+// 160 from there on, so that the former's probabilities are zero.
+static void far_apart(Attention& a, int half) {
+  for (auto* x : {&a.q, &a.kv[0]}) std::fill(x->begin(), x->end(), 0.f);
+  for (int row = 0; row < a.n; row++)
+    for (int h = 0; h < a.Hq; h++) a.query(row, h, 0) = 1;
+  for (int b = 0; b < a.B; b++)
+    for (int t = 0; t < a.p.len[b] + a.p.T[b]; t++)
+      for (int h = 0; h < a.p.Hkv; h++) a.key(b, t, h, 0) = t < half ? -1280 : 1280;
+}
+
+// A visible value that is no number is one in the result, whichever part of the keys it is
+// in and however little that part weighs.
+static void no_numbers_in_a_part() {
+  const std::vector<Problem> problems = {
+      {128, 64, 1, 1, 0, 0, 0, 1, {1}, {1100}, 0},             // three parts of few columns
+      {128, 64, 1, 1, 0, 0, 0, 70, {70}, {1100}, 0},           // of many
+      {64, 64, 1, 2, 0, 0, 1024, 1, {1, 1}, {1100, 1040}, 1},  // four of a prefix, few columns, and the sequences' own
+      {64, 64, 1, 8, 0, 0, 1024, 20, {20, 17}, {1024, 1040}, 0},  // many
+  };
+  int id = 0;
+  for (const Problem& p : problems)
+    for (float odd : {(float)NAN, (float)INFINITY, (float)-INFINITY})
+      for (int at : {3, 600, 1030}) {
+        Attention a(p, id);
+        far_apart(a, 512);
+        a.value(0, at, 0, 5) = odd;
+        a.compare("no number in a part", id++);
+      }
+}
+
+int main() {
+  no_numbers_in_a_part();
+  printf("ok\n");
+}

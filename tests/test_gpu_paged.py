@@ -536,3 +536,35 @@ def test_whole_windows_as_the_dense_attention():
         assert torch.equal(q1, qr[rows])
         got = _attend(one, q1)
         assert (abs(got.float() - out[rows].float()) <= 2 * 5 * 2.0 ** -8 + 2.0 ** -7 * abs(out[rows].float())).all()
+
+
+# ----------------------------------------------------- values that are no numbers
+def _places(s, i, b, tokens, dims):
+    """Where the numbers of a sequence's tokens lie in the pool of keys (i = 0) or values."""
+    plain = R.in_pool(np.arange(s.cache[i].numel()).reshape(s.cache[i].shape), bool(i))
+    j = np.asarray(list(tokens))
+    return _torch().from_numpy(plain[s.pages_h[b, j // s.page], :, j % s.page][..., dims].reshape(-1)).cuda()
+
+
+def _set(s, i, b, tokens, dims, value):
+    s.cache[i].view(-1)[_places(s, i, b, tokens, dims)] = value
+
+
+@pytest.mark.parametrize("at", [3, 600, 1030])
+@pytest.mark.parametrize("seqs,G,hd,shared", [([(1, 1100)], 1, 128, 0), ([(70, 1100)], 1, 128, 0), ([(1, 1100), (1, 1040)], 2, 64, 1024),
+                                              ([(20, 1024), (17, 1040)], 8, 64, 1024)])
+def test_attention_visible_nan_in_a_part_of_no_weight(seqs, G, hd, shared, at):
+    """A NaN among visible values is one in the result, whichever part of the keys holds it,
+    and if all probabilities of that part are zero."""
+    s = Setup(seqs, 64, 1, hd, 3, shared=shared)
+    q = s.rows(G)
+    q.zero_()
+    q[:, :, 0] = hd ** 0.5
+    for b, (T, n) in enumerate(seqs):
+        _set(s, 0, b, range(T + n), slice(None), 0.0)
+        _set(s, 0, b, range(512), [0], -160.0)
+        _set(s, 0, b, range(512, T + n), [0], 160.0)
+    _set(s, 1, 0, [at], [5], float("nan"))
+    out = _attend_check(s, q, shared=shared).view(s.n, G, hd)
+    sees = [row for b, row, pos in s.batch.rows() if pos >= at and (b == 0 or at < shared)]
+    assert sees and bool(out[sees][:, :, 5].isnan().all())

@@ -18,3 +18,13 @@ def test_batches_out_of_range_stay_in_bounds(tmp_path):
     assert r.returncode == 0, r.stderr[-2000:]
     r = subprocess.run([exe], capture_output=True, text=True, timeout=300)
     assert r.returncode == 0 and r.stdout.strip() == "ok", (r.returncode, r.stdout[-500:])
+
+
+@pytest.mark.skipif(not os.path.exists(CLANG), reason="needs clang++")
+def test_values_at_which_the_way_to_a_result_shows(tmp_path):
+    exe = str(tmp_path / "paged_values_cpu")
+    r = subprocess.run([CLANG, "-std=c++17", "-O2", "-w", "-I", os.path.join(HERE, "cpu_hip"),
+                        os.path.join(HERE, "paged_values_cpu.cpp"), "-o", exe], capture_output=True, text=True)
+    assert r.returncode == 0, r.stderr[-2000:]
+    r = subprocess.run([exe], capture_output=True, text=True, timeout=300)
+    assert r.returncode == 0 and r.stdout.strip() == "ok", (r.returncode, r.stdout[-500:])
