@@ -658,7 +658,8 @@ __global__ __launch_bounds__(kWaves * 64, NT > 1 ? 2 : HD == 64 ? 4 : 3) void at
     }
     const int t = c / G, hq = kvh * G + c - t * G;
     if (only) {
-      const float inv = L == 0.f ? 0.f : 1.0f / L;  // (no visible key: zeros)
+      const float inv = 1.0f / (L == 0.f ? 1.0f : L);
+      if (L == 0.f) acc = f32xd{};  // no weight, nothing of the values
       uint32_t* op = reinterpret_cast<uint32_t*>(out + ((int64_t)(sq.row + t) * Hkv * G + hq) * HD + d0);
 #pragma unroll
       for (int e = 0; e < DT / 2; e++)
@@ -1043,7 +1044,11 @@ __global__ __launch_bounds__(512, 2) void attn_paged_prompt_kernel(
     if (c > w1) continue;
     const int64_t row = ((int64_t)sq.row + t) * Hkv * G + (int64_t)kvh * G + c - t * G;
     if (only) {
-      const float inv = L == 0.f ? 0.f : 1.0f / L;  // (no visible key: zeros)
+      const float inv = 1.0f / (L == 0.f ? 1.0f : L);
+      if (L == 0.f) {  // no weight, nothing of the values
+#pragma unroll
+        for (int i = 0; i < ND; i++) acc[y][i] = f32x4{};
+      }
       uint16_t* op = out + row * HD + 4 * g;
 #pragma unroll
       for (int i = 0; i < ND; i++) {
@@ -1140,7 +1145,8 @@ __global__ __launch_bounds__(256) void attn_paged_join_kernel(Ragged r, int max_
         acc += w * x[k];  // (of no weight too: what is no number there stays none)
       }
     }
-    const float inv = L == 0.f ? 0.f : 1.0f / L;
+    const float inv = 1.0f / (L == 0.f ? 1.0f : L);
+    if (L == 0.f) acc = f32x4{};  // no weight, nothing of the values
     typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
     u32x2 y;
 #pragma unroll

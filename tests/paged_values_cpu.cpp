@@ -148,7 +148,31 @@ static void no_numbers_in_a_part() {
       }
 }
 
+// A query whose scores are all -infinity gets zeros, whatever the values are.
+static void no_weight_at_all() {
+  const std::vector<Problem> problems = {
+      {64, 32, 1, 1, 0, 0, 0, 1, {1}, {40}, 0},             // one part of few columns
+      {64, 32, 1, 2, 0, 0, 0, 1, {1}, {1100}, 0},           // two
+      {64, 32, 1, 4, 0, 0, 0, 1000, {20}, {70}, 0},         // one of many
+      {64, 32, 1, 4, 0, 0, 0, 20, {20}, {1100}, 0},         // three
+      {64, 32, 1, 1, 0, 0, 64, 2, {1, 2}, {70, 70}, 0},     // a prefix, few columns
+      {64, 32, 1, 8, 0, 0, 64, 20, {20, 18}, {70, 70}, 0},  // many
+  };
+  int id = 0;
+  for (const Problem& p : problems)
+    for (float odd : {(float)NAN, (float)INFINITY}) {
+      Attention a(p, id);
+      for (int row = 0; row < a.n; row++)
+        for (int h = 0; h < a.Hq; h++) a.query(row, h, 0) = 1;
+      for (int b = 0; b < a.B; b++)
+        for (int t = 0; t < p.len[b] + p.T[b]; t++) a.key(b, t, 0, 0) = -INFINITY;
+      a.value(0, 3, 0, 5) = a.value(0, p.len[0], 0, 6) = odd;
+      a.compare("no weight at all", id++);
+    }
+}
+
 int main() {
+  no_weight_at_all();
   no_numbers_in_a_part();
   printf("ok\n");
 }

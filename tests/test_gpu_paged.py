@@ -568,3 +568,16 @@ def test_attention_visible_nan_in_a_part_of_no_weight(seqs, G, hd, shared, at):
     out = _attend_check(s, q, shared=shared).view(s.n, G, hd)
     sees = [row for b, row, pos in s.batch.rows() if pos >= at and (b == 0 or at < shared)]
     assert sees and bool(out[sees][:, :, 5].isnan().all())
+
+
+@pytest.mark.parametrize("seqs,G,shared,most", [([(1, 40)], 1, 0, 1), ([(1, 1100)], 2, 0, 1), ([(20, 70)], 4, 0, 1000), ([(20, 1100)], 4, 0, 20),
+                                                ([(1, 70), (2, 70)], 1, 64, 2), ([(20, 70), (18, 70)], 8, 64, 20)])
+def test_attention_scores_of_minus_infinity_beside_nan(seqs, G, shared, most):
+    """Queries whose scores are all -infinity get zeros, whatever the values are."""
+    s = Setup(seqs, 32, 1, 64, 3, shared=shared)
+    q = s.rows(G)
+    q[:, :, 0] = 1.0
+    for b, (T, n) in enumerate(seqs):
+        _set(s, 0, b, range(T + n), [0], float("-inf"))
+        _set(s, 1, b, [3, n], [5, 6], float("nan"))
+    assert (_np(_attend(s, q, shared=shared, max_new=most)) == 0).all()
