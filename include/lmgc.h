@@ -748,7 +748,8 @@ int lmgc_op_paged_append(const void* d_k, const void* d_v, int32_t dtype, int64_
  * scores are all -infinity, gets zeros.
  * Probabilities are rounded to bf16 (2^-8 of each at most) for their product with the
  * values and divided by the sum of the rounded ones; scores, maxima and sums are
- * float32.  A query's result depends on its own sequence (length and number of
+ * float32, where a sum of finite values never passes its range but a score may (and is
+ * infinite then).  A query's result depends on its own sequence (length and number of
  * new tokens), max_new, Hq and Hkv, not on the other sequences; with shared > 0
  * on n and B, too, which say how the shared part is split.
  * GPU, async.  Errors: EINVAL, ESIZE, EUNSUPPORTED (hd, page, more than 2^32

@@ -430,6 +430,13 @@ __device__ inline void add_masked_values(Value value, const bf16x8 (&pf)[NT], f3
   }
 }
 
+// Sums of values near bf16's largest pass float32 where their mean does not.  So the
+// columns whose results are no numbers the second time either get a third one, with
+// their references kLift above the largest score: 2^24 probabilities of 2^8 / 2^kLift
+// each are less than one.  Joins weigh parts against kJoinLift above the largest
+// reference, for up to 128 parts of large sums.
+constexpr float kLift = 34.f, kJoinLift = 8.f;
+
 // The running softmax of a wave's 16 NT columns.
 template <int HD, int NT>
 struct Columns {
@@ -437,11 +444,12 @@ struct Columns {
   float m[NT];
   f32x4 l[NT], o[NT][ND];  // row sums (four times), O^T: 4 dims of 16 each
   // Groups v, v + step, .. of the span up to v1: S^T = K Q^T, an online softmax,
-  // O^T += V^T P^T.  EXACT: where masked values may be no numbers.
+  // O^T += V^T P^T.  EXACT: where masked values may be no numbers; the references lie
+  // `lift` above the largest scores.
   template <bool EXACT>
   __device__ inline void walk(const bf16x8 (&qf)[NT][KQ], const uint16_t* kc, const uint16_t* vc, const Ragged& r, const int32_t* pages, int Hkv,
                               int kvh, const Span& span, int v, int v1, int step, int p0, int p1, const int (&pos)[NT], const Mask& mask,
-                              float sl2) {
+                              float sl2, const float (&lift)[NT]) {
     const int lane = threadIdx.x & 63, g = lane >> 4;
 #pragma unroll
     for (int y = 0; y < NT; y++) {
@@ -492,6 +500,7 @@ struct Columns {
           for (int e = 0; e < 4; e++) mx = fmaxf(mx, s[i][e]);  // (drops a NaN; it comes back through the exponential)
         mx = fmaxf(mx, __shfl_xor(mx, 16));
         mx = fmaxf(mx, __shfl_xor(mx, 32)) * sl2;
+        if (EXACT) mx += lift[y];
         if (mx > m[y]) {
           const float a = __builtin_amdgcn_exp2f(m[y] - mx);
           l[y] *= a;
@@ -524,17 +533,26 @@ struct Columns {
       }
     }
   }
-  // Whether some number of any column's result is none: then what a masked value
-  // was may have come in.
-  __device__ inline bool odd() const {
+  // The lanes that have a number of a column's result that is none: then what a
+  // masked value was may have come in, or a sum have passed float32.
+  __device__ inline uint64_t odd(int y) const {
     float x = 0.f;
 #pragma unroll
-    for (int y = 0; y < NT; y++)
+    for (int i = 0; i < ND; i++)
 #pragma unroll
-      for (int i = 0; i < ND; i++)
+      for (int e = 0; e < 4; e++) x = fmaf(o[y][i][e], 0.f, x);
+    return __ballot(!(x == 0.f));
+  }
+  // Whether there are any; lift: what their columns' references are to be raised by.
+  __device__ inline bool odd(float (&lift)[NT], float by) const {
+    uint64_t any = 0;
 #pragma unroll
-        for (int e = 0; e < 4; e++) x = fmaf(o[y][i][e], 0.f, x);
-    return __ballot(!(x == 0.f)) != 0;
+    for (int y = 0; y < NT; y++) {
+      const uint64_t lanes = odd(y);
+      lift[y] = lanes >> (threadIdx.x & 15) & 0x1000100010001 ? by : 0.f;
+      any |= lanes;
+    }
+    return any != 0;
   }
 };
 
@@ -627,8 +645,10 @@ __global__ __launch_bounds__(kWaves * 64, NT > 1 ? 2 : HD == 64 ? 4 : 3) void at
   }
   Columns<HD, NT> x;
   const int32_t* pages = r.pages + (int64_t)b * r.max_pages;
-  x.template walk<false>(qf, kc, vc, r, pages, Hkv, kvh, span, v0 + wave * kGroup, v1, NW * kGroup, p0, p1, pos, mask, sl2);
-  if (x.odd()) x.template walk<true>(qf, kc, vc, r, pages, Hkv, kvh, span, v0 + wave * kGroup, v1, NW * kGroup, p0, p1, pos, mask, sl2);
+  float lift[NT] = {};
+  x.template walk<false>(qf, kc, vc, r, pages, Hkv, kvh, span, v0 + wave * kGroup, v1, NW * kGroup, p0, p1, pos, mask, sl2, lift);
+  for (int again = 0; again < 2 && x.odd(lift, again ? kLift : 0.f); again++)
+    x.template walk<true>(qf, kc, vc, r, pages, Hkv, kvh, span, v0 + wave * kGroup, v1, NW * kGroup, p0, p1, pos, mask, sl2, lift);
   // HD / (4 NW) dims of a column to a thread
   constexpr int DT = HD / (4 * NW);
   typedef float f32xd __attribute__((ext_vector_type(DT)));
@@ -647,6 +667,7 @@ __global__ __launch_bounds__(kWaves * 64, NT > 1 ? 2 : HD == 64 ? 4 : 3) void at
     float M = sm[0][oc];
 #pragma unroll
     for (int w = 1; w < NW; w++) M = fmaxf(M, sm[w][oc]);
+    M += kJoinLift;
     float L = 0.f;
     f32xd acc = {};
 #pragma unroll
@@ -903,8 +924,9 @@ __global__ __launch_bounds__(512, 2) void attn_paged_prompt_kernel(
       v[(wave + 8 * i) * 64 + lane] &= words_of(seen, g);
     }
   };
-  // scores to probabilities
-  auto soften = [&](int k) __attribute__((always_inline)) {
+  // scores to probabilities (lifted: with references `lift` above the scores)
+  float lift[2] = {};
+  auto soften = [&](int k, auto lifted) __attribute__((always_inline)) {
     if (!(whole >> (k - first) & 1)) {
 #pragma unroll
       for (int y = 0; y < 2; y++)
@@ -926,6 +948,7 @@ __global__ __launch_bounds__(512, 2) void attn_paged_prompt_kernel(
 #pragma unroll
         for (int e = 0; e < 4; e++) x = fmaxf(x, sc[i][y][e]);
       mx[y] = x * sl2;
+      if (decltype(lifted)::value) mx[y] += lift[y];
     }
     // a column's reference moves only when a score passes it by 2^8
     if (__ballot(mx[0] > m[0] + 8.0f || mx[1] > m[1] + 8.0f)) {
@@ -984,7 +1007,7 @@ __global__ __launch_bounds__(512, 2) void attn_paged_prompt_kernel(
     const int ring = k & (kRing - 1), up = (k + 1) & (kRing - 1);  // of the step's values; of the next step's keys
     __builtin_amdgcn_sched_barrier(0);
     if (works) {
-      soften(k);
+      soften(k, std::false_type{});
       // (kept here: the compiler would move the exponentials to their use)
       keep(pf[0]);
       keep(pf[1]);
@@ -1014,7 +1037,7 @@ __global__ __launch_bounds__(512, 2) void attn_paged_prompt_kernel(
   }
   wait_loads<0>();  // no load to LDS outlives the workgroup
   if (!works) return;
-  if (cs.odd()) {
+  for (int again = 0; again < 2 && cs.odd(lift, again ? kLift : 0.f); again++) {
     // once more, by itself and in the same order
     cs = Columns<HD, 2>{};
     m[0] = m[1] = -INFINITY;
@@ -1026,7 +1049,7 @@ __global__ __launch_bounds__(512, 2) void attn_paged_prompt_kernel(
       };
       const u32x4* keys[2] = {group(kc, 0), group(kc, 1)};
       scores([&](int i, int x) __attribute__((always_inline)) { return keys[i >> 1][((i & 1) * KQ + x) * 64]; });
-      soften(k);
+      soften(k, std::true_type{});
       sums();
 #pragma unroll
       for (int x = 0; x < 2; x++) {
@@ -1109,7 +1132,7 @@ __global__ __launch_bounds__(256) void attn_paged_join_kernel(Ragged r, int max_
     const int64_t own = few ? ((int64_t)b * Hkv + kvh) * plan.places + (t * G + hq - kvh * G) * plan.parts(span.total) : at * plan.prompt.most;
     const float* own_o = few ? plan.po : plan.prompt_o;
     const float2* own_ml = few ? plan.pml : plan.prompt_ml;
-    // parts: those of the prefix, then the sequence's own
+    // parts: those of the prefix, then the sequence's own; M is kJoinLift above their largest
     const int n = plan.pre + nown;
     float M = -INFINITY, L = 0.f;
     f32x4 acc = {};
@@ -1128,9 +1151,10 @@ __global__ __launch_bounds__(256) void attn_paged_join_kernel(Ragged r, int max_
           x[k] = f32x4{};
         }
       }
-      float top = M;
+      float top = ml[0].x;
 #pragma unroll
-      for (int k = 0; k < 8; k++) top = fmaxf(top, ml[k].x);
+      for (int k = 1; k < 8; k++) top = fmaxf(top, ml[k].x);
+      top += kJoinLift;
       if (top > M) {
         const float a = __builtin_amdgcn_exp2f(M - top);  // (0 times what came of a NaN stays one)
         L *= a;

@@ -171,7 +171,35 @@ static void no_weight_at_all() {
     }
 }
 
+// Values near bf16's largest: their mean is a number, their sum is none.
+static void large_values() {
+  const std::vector<Problem> problems = {
+      {64, 32, 1, 1, 0, 0, 0, 1, {1}, {40}, 0},             // one part of few columns
+      {128, 32, 1, 2, 0, 0, 0, 1, {1}, {1500}, 0},          // three
+      {64, 32, 1, 4, 0, 0, 0, 1000, {20}, {170}, 0},        // one of many
+      {64, 32, 1, 4, 60, 3, 0, 1000, {20}, {170}, 0},       // behind a window
+      {128, 32, 1, 4, 0, 0, 0, 20, {20}, {1100}, 0},        // three
+      {64, 32, 1, 1, 0, 0, 640, 2, {1, 2}, {700, 650}, 0},  // a prefix, few columns
+      {64, 32, 1, 8, 0, 0, 640, 20, {20, 18}, {700, 650}, 1},  // many
+  };
+  int id = 0;
+  for (const Problem& p : problems)
+    for (int rising : {0, 1}) {
+      Attention a(p, id);
+      // scores around zero, or 7 (in powers of two) larger with every 30 keys
+      for (int row = 0; row < a.n && rising; row++)
+        for (int h = 0; h < a.Hq; h++) a.query(row, h, 0) = 1;
+      for (int b = 0; b < a.B; b++)
+        for (int t = 0; t < p.len[b] + p.T[b]; t++) {
+          if (rising) a.key(b, t, 0, 0) = 8 * 0.23f * 0.693f * (t % 1024);
+          for (int d = 0; d < p.hd; d++) a.value(b, t, 0, d) = (d % 2 ? -1 : 1) * (3.3e38f - 1e37f * (t % 7));
+        }
+      a.compare("large values", id++);
+    }
+}
+
 int main() {
+  large_values();
   no_weight_at_all();
   no_numbers_in_a_part();
   printf("ok\n");

@@ -581,3 +581,23 @@ def test_attention_scores_of_minus_infinity_beside_nan(seqs, G, shared, most):
         _set(s, 0, b, range(T + n), [0], float("-inf"))
         _set(s, 1, b, [3, n], [5, 6], float("nan"))
     assert (_np(_attend(s, q, shared=shared, max_new=most)) == 0).all()
+
+
+@pytest.mark.parametrize("rising", [0.0, 0.2])
+@pytest.mark.parametrize("seqs,G,hd,shared,kw", [
+    ([(1, 40)], 1, 64, 0, {}), ([(1, 1500)], 2, 128, 0, {}), ([(20, 170)], 4, 64, 0, dict(max_new=1000)),
+    ([(20, 170)], 4, 64, 0, dict(max_new=1000, window=60, sinks=3)), ([(20, 1100), (1, 5000)], 4, 128, 0, {}),
+    ([(1, 700), (2, 650)], 1, 64, 640, {}), ([(20, 700), (18, 650)], 8, 64, 640, {})])
+def test_attention_values_near_the_largest(seqs, G, hd, shared, kw, rising):
+    """Their mean is a number where their sum is none; with scores around zero and with such
+    that rise from key to key."""
+    torch = _torch()
+    s = Setup(seqs, 64, 1, hd, 3, shared=shared)
+    q = s.rows(G)
+    v = torch.full((s.n_pages, 1, 64, hd), 3.3e38, device="cuda") - 1e37 * torch.randint(0, 7, (s.n_pages, 1, 64, hd), device="cuda")
+    s.cache[1].copy_(v.to(torch.bfloat16))
+    if rising:
+        q[:, :, 0] = 1.0
+        for b, (T, n) in enumerate(seqs):
+            _set(s, 0, b, range(T + n), [0], rising * hd ** 0.5 * (torch.arange(T + n, device="cuda") % 1024).to(torch.bfloat16))
+    _attend_check(s, q, shared=shared, **kw)
