@@ -576,6 +576,7 @@ struct AttnPlan {
   int few, few_short;    // columns of a sequence that the form for few takes, and of one whose keys are one part
   int columns;           // how many of them there are at most
   int places;            // partial results of a sequence's columns in one head, at most
+  int by_row;            // whether these lie row by row or, where that is less, sequence by sequence
   Splits split;          // of the form for few columns
   Splits prompt;         // of the form for many
   int many, joined;      // whether the form for many is needed; whether it leaves partial results
@@ -583,8 +584,11 @@ struct AttnPlan {
   int pre, pre_chunk;    // splits of these
   float *po, *prompt_o, *pre_o;      // partial results, and maxima and sums
   float2 *pml, *prompt_ml, *pre_ml;
-  // Places of a column of a sequence with so many keys.
-  __device__ inline int parts(int total) const { return total <= split.least ? 1 : split.most; }
+  // The first partial result of column c of sequence b and a head of so many with so many
+  // keys; at: its row and query head.
+  __device__ inline int64_t own(int b, int Hkv, int kvh, int c, int total, int64_t at) const {
+    return by_row ? at * split.most : ((int64_t)b * Hkv + kvh) * places + c * (total <= split.least ? 1 : split.most);
+  }
   // Whether a sequence of so many columns and keys has few.
   __device__ inline bool is_few(int cols, int total) const { return cols <= few || (cols <= few_short && total <= split.least); }
 };
@@ -686,8 +690,7 @@ __global__ __launch_bounds__(kWaves * 64, NT > 1 ? 2 : HD == 64 ? 4 : 3) void at
       for (int e = 0; e < DT / 2; e++)
         op[e] = __builtin_bit_cast(uint32_t, bf16x2{(__bf16)(acc[2 * e] * inv), (__bf16)(acc[2 * e + 1] * inv)});
     } else {
-      const int64_t at = PREFIX ? ((int64_t)t * Hkv * G + hq) * plan.pre + split
-                                : ((int64_t)b * Hkv + kvh) * plan.places + c * plan.parts(span.total) + split;
+      const int64_t row = (int64_t)(sq.row + t) * Hkv * G + hq, at = (PREFIX ? row * plan.pre : plan.own(b, Hkv, kvh, c, span.total, row)) + split;
       *reinterpret_cast<f32xd*>((PREFIX ? plan.pre_o : plan.po) + at * HD + d0) = acc;
       if (d0 == 0) (PREFIX ? plan.pre_ml : plan.pml)[at] = make_float2(M, L);
     }
@@ -1129,7 +1132,7 @@ __global__ __launch_bounds__(256) void attn_paged_join_kernel(Ragged r, int max_
     const int kvh = hq / G, chunk = (few ? plan.split : plan.prompt).chunk(span.total), nown = (span.total + chunk - 1) / chunk;
     if (plan.cut == 0 && nown <= 1) continue;  // written by the only split
     const int64_t at = ((int64_t)q.row + t) * Hq + hq, pre = at * plan.pre;
-    const int64_t own = few ? ((int64_t)b * Hkv + kvh) * plan.places + (t * G + hq - kvh * G) * plan.parts(span.total) : at * plan.prompt.most;
+    const int64_t own = few ? plan.own(b, Hkv, kvh, t * G + hq - kvh * G, span.total, at) : at * plan.prompt.most;
     const float* own_o = few ? plan.po : plan.prompt_o;
     const float2* own_ml = few ? plan.pml : plan.prompt_ml;
     // parts: those of the prefix, then the sequence's own; M is kJoinLift above their largest
@@ -1246,7 +1249,11 @@ AttnPlan plan_of(int n, int B, int Hq, int Hkv, int hd, int max_new, int tokens,
   p.pre_chunk = (std::max(kLeast / 2, (p.cut + parts - 1) / parts) + kStep * 2 - 1) / (kStep * 2) * (kStep * 2);
   p.pre = (p.cut + p.pre_chunk - 1) / p.pre_chunk;
   p.places = std::max(std::min(p.columns, kFew) * p.split.most, p.columns);
-  const int64_t own = p.cut || p.split.most > 1 ? (int64_t)B * Hkv * p.places : 0;
+  // (one chunk of 64 rows beside 63 single tokens, 32 heads of 128, 64 parts: 135 MB by
+  // rows, 4.3 GB by sequences; 2 prompts of 3000 rows 6.4 GB and 136 MB)
+  const int64_t by_row = (int64_t)n * Hq * p.split.most, by_seq = (int64_t)B * Hkv * p.places;
+  p.by_row = by_row < by_seq;
+  const int64_t own = p.cut || p.split.most > 1 ? std::min(by_row, by_seq) : 0;
   p.many = cols > kFew && !(rule <= kFewShort && own_tokens <= least);
   p.joined = p.many && (p.cut || p.prompt.most > 1);
   const int64_t many = p.joined ? (int64_t)n * Hq * p.prompt.most : 0;

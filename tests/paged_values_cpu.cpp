@@ -198,7 +198,22 @@ static void large_values() {
     }
 }
 
+// A chunk beside single tokens, so that partial results lie row by row, and single tokens
+// beside sequences without rows, so that they lie sequence by sequence.
+static void places_of_parts() {
+  const std::vector<Problem> problems = {
+      {128, 64, 2, 2, 0, 0, 0, 8, {1, 8, 1, 0, 1, 2}, {1100, 700, 3, 9, 600, 1030}, 2},
+      {64, 64, 1, 4, 0, 0, 64, 8, {1, 8, 1, 0, 1, 2}, {1100, 700, 66, 70, 600, 1300}, 2},
+      {64, 64, 2, 4, 700, 5, 0, 8, {1, 8, 1, 0, 1, 2}, {1100, 700, 66, 70, 600, 1300}, 0},
+      {128, 64, 2, 2, 0, 0, 0, 1, {1, 0, 0, 1}, {1100, 9, 4, 600}, 0},
+      {128, 64, 1, 8, 0, 0, 0, 60, {1, 60, 1}, {1100, 400, 600}, 3},
+  };
+  int id = 0;
+  for (const Problem& p : problems) Attention(p, id).compare("places of parts", id), id++;
+}
+
 int main() {
+  places_of_parts();
   large_values();
   no_weight_at_all();
   no_numbers_in_a_part();

@@ -164,6 +164,21 @@ def test_attention_workspace():
             B.paged_workspace(*bad)
 
 
+def test_attention_workspace_is_what_rows_fill():
+    """A chunk beside single tokens: the partial results of its rows, not those of a chunk for
+    each sequence."""
+    part = (128 + 2) * 4  # bytes of a partial result
+    for singles in (63, 255):
+        rows = 64 + singles
+        # 64 parts of 512 tokens for each row and head
+        assert B.paged_workspace(rows, singles + 1, 32, 32, 128, 64, 32768) <= rows * 32 * 64 * part
+        assert B.paged_workspace(rows, singles + 1, 32, 8, 128, 16, 32768) <= rows * 32 * 64 * part
+    # nor those of each row of a long prompt, where few sequences have few columns
+    assert B.paged_workspace(6000, 2, 32, 32, 128, 6000, 32768) <= 2 * 32 * 64 * 64 * part
+    # single tokens: a column of each
+    assert B.paged_workspace(64, 64, 32, 8, 128, 1, 32768) == 64 * 32 * 64 * part
+
+
 # ------------------------------------------------------------------- binding
 def _batch(n=4, Bn=2, most=2):
     import torch
