@@ -753,7 +753,7 @@ int lmgc_op_paged_append(const void* d_k, const void* d_v, int32_t dtype, int64_
  * new tokens), max_new, Hq and Hkv, not on the other sequences; with shared > 0
  * on n and B, too, which say how the shared part is split.
  * GPU, async.  Errors: EINVAL, ESIZE, EUNSUPPORTED (hd, page, more than 2^32
- * threads).
+ * threads in a dimension of a launch).
  */
 int64_t lmgc_paged_workspace(int32_t n, int32_t B, int32_t Hq, int32_t Hkv, int32_t hd,
                              int32_t max_new, int32_t tokens, int32_t shared);

@@ -220,7 +220,7 @@ int lmgc_op_attention_paged(const uint16_t* d_q, int64_t ldq, int32_t n, int32_t
   if (!aligned(d_q, 16) || ldq % 8 || !aligned(d_out, 16) || !aligned(d_ws, 16))
     return set_error(LMGC_EINVAL, "pointers must be 16-byte aligned and ldq a multiple of 8");
   const int tokens = max_pages * page;
-  if (paged_workgroups(n, B, Hq, Hkv, hd, max_new, tokens, shared) >= 1 << 23)  // 2^32 threads
+  if (paged_workgroups(n, B, Hq, Hkv, hd, max_new, tokens, shared, window, sinks) >= 1 << 23)  // 2^32 threads
     return set_error(LMGC_EUNSUPPORTED, "too many columns for one launch");
   const int64_t need = paged_workspace_bytes(n, B, Hq, Hkv, hd, max_new, tokens, shared), no = (int64_t)n * Hq * hd * 2;
   if (need > 0 && (!d_ws || ws_bytes < (size_t)need))

@@ -58,8 +58,9 @@ struct PagedAttnArgs {
   Ragged r;
 };
 int64_t paged_workspace_bytes(int n, int B, int Hq, int Hkv, int hd, int max_new, int tokens, int shared);
-// Workgroups of the largest launch.
-int64_t paged_workgroups(int n, int B, int Hq, int Hkv, int hd, int max_new, int tokens, int shared);
+// Workgroups of the largest launch in one dimension (other launches have heads and
+// sequences in two of their own).
+int64_t paged_workgroups(int n, int B, int Hq, int Hkv, int hd, int max_new, int tokens, int shared, int window, int sinks);
 hipError_t launch_attention_paged(const PagedAttnArgs& a, hipStream_t s);
 
 }  // namespace lmgc

@@ -1276,10 +1276,11 @@ int64_t paged_workspace_bytes(int n, int B, int Hq, int Hkv, int hd, int max_new
   return bytes;
 }
 
-int64_t paged_workgroups(int n, int B, int Hq, int Hkv, int hd, int max_new, int tokens, int shared) {
-  const AttnPlan p = plan_of(n, B, Hq, Hkv, hd, max_new, tokens, shared, Mask{0, 0}, nullptr, nullptr);
+int64_t paged_workgroups(int n, int B, int Hq, int Hkv, int hd, int max_new, int tokens, int shared, int window, int sinks) {
+  const AttnPlan p = plan_of(n, B, Hq, Hkv, hd, max_new, tokens, shared, Mask{window, sinks}, nullptr, nullptr);
   const int64_t pre = p.cut ? ((int64_t)n * (Hq / Hkv) + kTileCols - 1) / kTileCols * p.pre : 0;
-  return std::max(tiles_of(n, Hq / Hkv, B, p.cols).count * p.prompt.most, pre) * Hkv;
+  const int64_t own = p.many ? tiles_of(n, Hq / Hkv, B, p.cols).count * p.prompt.most : 0;
+  return std::max(own, pre) * Hkv;
 }
 
 hipError_t launch_paged_append(const AppendArgs& a, hipStream_t s) {

@@ -601,3 +601,22 @@ def test_attention_values_near_the_largest(seqs, G, hd, shared, kw, rising):
         for b, (T, n) in enumerate(seqs):
             _set(s, 0, b, range(T + n), [0], rising * hd ** 0.5 * (torch.arange(T + n, device="cuda") % 1024).to(torch.bfloat16))
     _attend_check(s, q, shared=shared, **kw)
+
+
+def test_attention_of_single_tokens_of_as_many_sequences_as_there_may_be():
+    """65535 on 32 heads: some of them beside float64, all of them by a smaller call's bits."""
+    torch = _torch()
+    s = Setup([(1, 63)], 64, 32, 64, 3)
+    some, n = 40, 65535
+    lens = np.arange(n) % 64
+    s.n = n
+    q = s.rows(32)
+    pages = np.repeat(s.pages_h, n, 0)
+    whole = B.op_attention_paged(q, s.cache, _ints(pages), _ints(np.arange(n + 1)), _ints(lens), 1)
+    s.n = some
+    s.set(pages[:some], np.arange(some + 1), lens[:some])
+    assert torch.equal(_attend_check(s, q[:some], max_new=1), whole[:some])
+    for first in range(some, n, 16384):
+        s.n = min(16384, n - first)
+        s.set(pages[:s.n], np.arange(s.n + 1), lens[first:first + s.n])
+        assert torch.equal(_attend(s, q[first:first + s.n], max_new=1), whole[first:first + s.n])

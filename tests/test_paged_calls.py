@@ -143,6 +143,17 @@ def test_attention_of_more_columns_than_a_launch_has():
     assert _attention(**rows) == EUNSUPPORTED
 
 
+def test_attention_counts_only_what_it_launches():
+    """65535 sequences of few columns have no use for the form for many, nor have longer ones
+    behind a window that is one part of keys: such calls come as far as the workspace."""
+    rows = dict(n=65535, B=65535, Hq=32, Hkv=32, ldq=32 * 64, most=512, max_new=1, n_pages=1, page=64, bytes=0, ws=None, q=1 << 55, out=1 << 56)
+    assert _attention(**rows) == ESIZE
+    rows.update(n=65535 * 16, Hq=128, ldq=128 * 64, max_new=16)
+    assert _attention(**rows) == ESIZE
+    rows.update(max_new=17)  # 68 columns
+    assert _attention(**rows) == EUNSUPPORTED and _attention(**rows, window=64) == ESIZE
+
+
 def test_attention_of_no_rows_is_fine():
     assert _attention(n=0, q=None, out=None, ws=None, bytes=0) == 0
 
