@@ -437,6 +437,17 @@ __device__ inline void add_masked_values(Value value, const bf16x8 (&pf)[NT], f3
 // reference, for up to 128 parts of large sums.
 constexpr float kLift = 34.f, kJoinLift = 8.f;
 
+// Zeros for the queries of columns that are no token's, which may hold anything: no
+// number there would have the wave do all its columns again.
+template <int NT, int KQ>
+__device__ inline void clear_no_tokens(bf16x8 (&qf)[NT][KQ], const int (&pos)[NT]) {
+#pragma unroll
+  for (int y = 0; y < NT; y++)
+#pragma unroll
+    for (int x = 0; x < KQ; x++)
+      if (pos[y] < 0) qf[y][x] = bf16x8{};
+}
+
 // The running softmax of a wave's 16 NT columns.
 template <int HD, int NT>
 struct Columns {
@@ -647,6 +658,7 @@ __global__ __launch_bounds__(kWaves * 64, NT > 1 ? 2 : HD == 64 ? 4 : 3) void at
 #pragma unroll
     for (int x = 0; x < KQ; x++) qf[y][x] = *reinterpret_cast<const bf16x8*>(qrow + t * ldq + (c - t * G) * HD + 32 * x);
   }
+  if (PREFIX) clear_no_tokens(qf, pos);
   Columns<HD, NT> x;
   const int32_t* pages = r.pages + (int64_t)b * r.max_pages;
   float lift[NT] = {};
@@ -813,6 +825,7 @@ __global__ __launch_bounds__(512, 2) void attn_paged_prompt_kernel(
 #pragma unroll
     for (int x = 0; x < KQ; x++) qf[y][x] = *reinterpret_cast<const bf16x8*>(qp + 32 * x);
   }
+  if (PREFIX) clear_no_tokens(qf, pos);
   keep(qf[0]);
   keep(qf[1]);  // (arrived: a wait for them further on would be one for all loads)
   // Step k is place v0 + 64 k of the span, and `jump` more from step `hole` on:

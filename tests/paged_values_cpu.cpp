@@ -1,6 +1,10 @@
 // Attention over the paged cache on the CPU (tests/cpu_hip) beside plain loops in
 // float64, for values at which the way to a result shows: no numbers in one part of
 // the keys, scores far apart.  Prints "ok".
+#include <hip/hip_runtime.h>
+
+static long g_products;  // terms of matrix products, the instruction's for the most part
+#define fmaf(a, b, c) (g_products++, (fmaf)(a, b, c))
 #define main paged_cpu_main
 #include "paged_cpu.cpp"
 #undef main
@@ -212,7 +216,26 @@ static void places_of_parts() {
   for (const Problem& p : problems) Attention(p, id).compare("places of parts", id), id++;
 }
 
+// What rows of no token hold costs nothing: they are in the prefix's columns, whose results
+// nobody takes.
+static void rows_of_no_token() {
+  for (int G : {1, 8}) {  // few columns of a prefix, many
+    long products[2];
+    for (int odd = 0; odd < 2; odd++) {
+      Attention a({64, 64, 1, G, 0, 0, 640, 40, {3, 40}, {640, 700}, 30}, G);
+      for (int row = a.starts[2]; row < a.n; row++)
+        for (int h = 0; h < G; h++) a.query(row, h, 7) = odd ? row % 2 ? NAN : INFINITY : 1;
+      g_products = 0;
+      a.run();
+      products[odd] = g_products;
+      a.compare("rows of no token", G);
+    }
+    check(products[0] == products[1], "more products for rows of no token", G);
+  }
+}
+
 int main() {
+  rows_of_no_token();
   places_of_parts();
   large_values();
   no_weight_at_all();

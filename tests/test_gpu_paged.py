@@ -620,3 +620,14 @@ def test_attention_of_single_tokens_of_as_many_sequences_as_there_may_be():
         s.n = min(16384, n - first)
         s.set(pages[:s.n], np.arange(s.n + 1), lens[first:first + s.n])
         assert torch.equal(_attend(s, q[first:first + s.n], max_new=1), whole[first:first + s.n])
+
+
+@pytest.mark.parametrize("G", [1, 8])
+def test_shared_rows_of_no_token_may_hold_anything(G):
+    torch = _torch()
+    s = Setup([(3, 640), (40, 700)], 64, 1, 64, 3, shared=640, pad=30)
+    q = s.rows(G)
+    clean = _attend_check(s, q, shared=640)
+    q[43:, :, ::9] = float("nan")
+    q[50:60] = float("inf")
+    assert torch.equal(_attend(s, q, shared=640), clean)
