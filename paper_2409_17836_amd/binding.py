@@ -820,6 +820,12 @@ ROPE_LAYOUTS = {"half": 0, "interleaved": 1}
 ROPE_SCALINGS = {"none": 0, "linear": 1, "ntk": 2, "yarn": 3}
 
 
+def _int32(x):
+    """A size for the library: the nearest of [-1, 2^31) (ctypes would keep the low 32
+    bits of another), and it refuses what it does not take."""
+    return max(-1, min(int(x), 2 ** 31 - 1))
+
+
 def rope_frequencies(rot: int, theta: float = 10000.0, scaling: str = "none", factor: float = 1.0, orig: float = 4096,
                      slow: float = 1.0, fast: float = 32.0) -> np.ndarray:
     """float64 [rot / 2]: the frequencies of lmgc_rope_frequencies."""
@@ -827,7 +833,8 @@ def rope_frequencies(rot: int, theta: float = 10000.0, scaling: str = "none", fa
 
 
 def _frequencies(rot, theta, scaling, factor, orig, slow, fast):
-    out = (ctypes.c_double * max(int(rot) // 2, 1))()
+    rot = _int32(rot)
+    out = (ctypes.c_double * max(min(rot, 512) // 2, 1))()  # (no rot past 512 is taken)
     _check(lib().lmgc_rope_frequencies(float(theta), rot, ROPE_SCALINGS[scaling], float(factor), float(orig), float(slow),
                                        float(fast), out))
     return out
@@ -946,7 +953,7 @@ def op_paged_append(cache, k, v, pages, starts, lens, rope=None, layout: str = "
 
 
 def paged_workspace(n: int, B: int, Hq: int, Hkv: int, hd: int, max_new: int, tokens: int, shared: int = 0) -> int:
-    return _size(lib().lmgc_paged_workspace(n, B, Hq, Hkv, hd, max_new, tokens, shared))
+    return _size(lib().lmgc_paged_workspace(*map(_int32, (n, B, Hq, Hkv, hd, max_new, tokens, shared))))
 
 
 def op_attention_paged(q, cache, pages, starts, lens, max_new: int, window: int = 0, sinks: int = 0, shared: int = 0,
@@ -965,9 +972,8 @@ def op_attention_paged(q, cache, pages, starts, lens, max_new: int, window: int 
         out = _empty((n, Hq * hd), torch.bfloat16, q, stream)
     else:
         assert out.dtype == torch.bfloat16 and out.is_contiguous() and out.numel() == q.numel()
-    # (ctypes would keep the low 32 bits of a larger one)
     if not (0 <= max_new <= 1 << 24 and 0 <= window < 1 << 31 and 0 <= sinks < 1 << 31 and 0 <= shared < 1 << 31):
-        max_new, window, sinks, shared = (max(-1, min(int(x), 2 ** 31 - 1)) for x in (max_new, window, sinks, shared))
+        max_new, window, sinks, shared = map(_int32, (max_new, window, sinks, shared))
         max_new = min(max_new, 1 << 24)
     if ws is None:
         ws = _empty(paged_workspace(n, B, Hq, Hkv, hd, max_new, most * page, shared), torch.uint8, q, stream)

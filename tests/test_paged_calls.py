@@ -252,3 +252,20 @@ def test_windows_past_32_bits(monkeypatch, given, taken):
         B.op_attention_paged(*args, ws=ws, **{name: given})
         assert fake.args[-8 + i] == taken
     assert fake.args[-2] == 4 * (1 << 12)  # bytes of the workspace
+
+
+@pytest.mark.parametrize("at", range(8))
+@pytest.mark.parametrize("past", [1 << 32, -(1 << 32)])
+def test_sizes_past_32_bits(at, past):
+    """They are refused, not taken for what their low 32 bits hold."""
+    sizes = [8, 2, 4, 2, 64, 8, 4096, 0]
+    assert B.paged_workspace(*sizes) > 0
+    if at == 7 and past > 0:  # (more in common than there is: all of it)
+        assert B.paged_workspace(*sizes[:7], past) == B.paged_workspace(*sizes[:7], 4096)
+        return
+    sizes[at] += past
+    with pytest.raises(B.LMGCError):
+        B.paged_workspace(*sizes)
+    with pytest.raises(B.LMGCError) as e:
+        B.rope_frequencies(64 + past)
+    assert e.value.code == EINVAL
