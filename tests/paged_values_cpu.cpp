@@ -234,7 +234,26 @@ static void rows_of_no_token() {
   }
 }
 
+// NaN and infinities in a shared prefix, among keys and values that a window hides from
+// some of the columns of a wave and not from others (and from all of some waves): in
+// both forms, whole and behind the sinks.
+static void no_numbers_in_a_prefix() {
+  int id = 0;
+  for (int G : {2, 12})
+    for (int hd : {64, 128})
+      for (int sinks : {0, 3})
+        for (int at : {1, 95, 100, 105, 119, 150}) {
+          // 48 columns, or 288, whose windows begin at 92 to 111, 120 and behind the prefix
+          Attention a({hd, 64, 1, G, 101, sinks, 192, 12, {12, 1, 9, 1}, {200, 220, 192, 300}, 1}, id);
+          const float odd[] = {NAN, INFINITY, -INFINITY};
+          a.value(0, at, 0, 5) = odd[id % 3];
+          if (id % 2) a.key(0, at, 0, 7) = odd[(id + 1) % 3];
+          a.compare("no numbers in a prefix", id++);
+        }
+}
+
 int main() {
+  no_numbers_in_a_prefix();
   rows_of_no_token();
   places_of_parts();
   large_values();

@@ -631,3 +631,22 @@ def test_shared_rows_of_no_token_may_hold_anything(G):
     q[43:, :, ::9] = float("nan")
     q[50:60] = float("inf")
     assert torch.equal(_attend(s, q, shared=640), clean)
+
+
+@pytest.mark.parametrize("at", [1, 95, 100, 105, 119, 150])
+@pytest.mark.parametrize("keys,value", [(False, float("nan")), (False, float("-inf")), (True, float("nan")), (True, float("inf"))])
+@pytest.mark.parametrize("G,hd,sinks", [(2, 64, 0), (2, 128, 3), (12, 64, 3), (12, 128, 0)])
+def test_shared_masked_numbers_count_for_nothing(G, hd, sinks, keys, value, at):
+    """NaN and infinities on a prefix that a window hides from some columns of a wave and not
+    from others, 46 columns or 276: who does not see them is as without, to the bit."""
+    torch = _torch()
+    s = Setup([(12, 200), (1, 220), (9, 192), (1, 300)], 64, 1, hd, 3, shared=192)
+    q = s.rows(G)
+    clean = _attend_check(s, q, shared=192, window=101, sinks=sinks)
+    _set(s, 0 if keys else 1, 0, [at], [5], value)
+    out = _attend_check(s, q, shared=192, window=101, sinks=sinks)
+    blind = [row for b, row, pos in s.batch.rows() if at <= pos - 101 and at >= sinks]
+    assert blind and torch.equal(out[blind], clean[blind]) if at >= sinks else not blind
+    sees = [row for row in range(s.n) if row not in blind]
+    if not keys and sees:
+        assert not bool(out[sees].view(len(sees), G, hd)[:, :, 5].isfinite().any())
