@@ -252,7 +252,61 @@ static void no_numbers_in_a_prefix() {
         }
 }
 
+// Appended keys and values and rotated queries, signs and all, against float64: float32
+// arithmetic (2^-23 of the products' sizes), one rounding to bf16 (2^-8).
+template <class T>
+static void rotation_signs(int hd, int rot, int layout, int skew, int id) {
+  const int Hkv = 2, Hq = 4, n = 9, old = 27, page = 32, ld = (Hkv + Hq) * hd + 8;
+  std::mt19937 rng(id);
+  std::normal_distribution<float> normal;
+  std::vector<T> rows((size_t)n * ld + 1), vrows((size_t)n * Hkv * hd);
+  auto number = [](T x) { return sizeof(T) == 2 ? (double)bf16_to_f32(x) : (double)x; };
+  auto make = [&](float x) { return sizeof(T) == 2 ? (T)f32_to_bf16(x) : (T)x; };
+  for (auto* x : {&rows, &vrows})
+    for (auto& e : *x) e = make(normal(rng));
+  std::vector<float> table((size_t)64 * rot);
+  for (auto& e : table) e = normal(rng);
+  uint16_t *kc = (uint16_t*)guarded(2 * Hkv * page * hd * 2), *vc = (uint16_t*)guarded(2 * Hkv * page * hd * 2), *qo = (uint16_t*)guarded(n * Hq * hd * 2);
+  const T *in = copy(rows) + skew, *vin = copy(vrows);
+  const std::vector<int> pages = {1, 0}, starts = {0, n}, lens = {old};
+  const Ragged r{copy(pages), copy(starts), copy(lens), 1, n, 2, page, 2};
+  const AppendArgs a{in, vin, in + Hkv * hd, ld, Hkv * hd, ld, Hq * hd, sizeof(T) == 2 ? LMGC_DTYPE_BF16 : LMGC_DTYPE_F32, Hq, Hkv, hd, rot, layout,
+                     kc, vc, qo, copy(table), 64, r};
+  launch_paged_append(a, nullptr);
+  for (int t = 0; t < n; t++)
+    for (int h = 0; h < Hkv + Hq; h++)
+      for (int d = 0; d < hd; d++) {
+        const T* x = in + (size_t)t * ld + h * hd;
+        const int pos = old + t, half = rot / 2;
+        double y = number(x[d]), size = 0;
+        if (d < rot) {
+          const bool split = layout == LMGC_ROPE_HALF, second = split ? d >= half : d & 1;
+          const int i = split ? d % half : d / 2, other = split ? (second ? d - half : d + half) : d ^ 1;
+          const double c = table[((size_t)pos * half + i) * 2], s = table[((size_t)pos * half + i) * 2 + 1];
+          const double u = y * c, v = number(x[other]) * s * (second ? 1 : -1);
+          y = u + v;
+          size = fabs(u) + fabs(v);
+        }
+        const size_t at = (((size_t)pages[pos / page] * Hkv + h) * page) * hd;
+        const double got = bf16_to_f32(h < Hkv ? kc[at + at_key(pos % page, d, hd)] : qo[((size_t)t * Hq + h - Hkv) * hd + d]);
+        check(fabs(got - y) <= 0x1p-23 * size + 0x1p-8 * fabs(y) * (1 + 0x1p-8), h < Hkv ? "a key's number" : "a query's number", id);
+        if (h < Hkv) check(vc[at + at_value(pos % page, d)] == f32_to_bf16((float)number(vin[((size_t)t * Hkv + h) * hd + d])), "a value's number", id);
+      }
+}
+
+static void rotations() {
+  int id = 0;
+  for (int layout : {LMGC_ROPE_HALF, LMGC_ROPE_INTERLEAVED})
+    for (int hd : {64, 128})
+      for (int rot : {hd, 32, 6})
+        for (int skew : {0, 1}) {
+          rotation_signs<uint16_t>(hd, rot, layout, skew, id++);
+          rotation_signs<float>(hd, rot, layout, skew, id++);
+        }
+}
+
 int main() {
+  rotations();
   no_numbers_in_a_prefix();
   rows_of_no_token();
   places_of_parts();
