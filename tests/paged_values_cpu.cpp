@@ -305,7 +305,22 @@ static void rotations() {
         }
 }
 
+// Long walks of the form for many: as a max_new of many columns has it, in one part, with
+// more than the 32 steps whose pages are looked up at once; twice where a value that some
+// queries do not see is no number.
+static void long_walks() {
+  int id = 0;
+  for (int hd : {64, 128})
+    for (int window : {0, 2500})
+      for (bool odd : {false, true}) {
+        Attention a({hd, 64, 1, 1, window, window ? 70 : 0, 0, 1 << 20, {70, 1}, {2700, 2300}, 0}, id);
+        if (odd) a.value(0, 2740, 0, 3) = a.value(0, 230, 0, 4) = NAN;
+        a.compare("a long walk", id++);
+      }
+}
+
 int main() {
+  long_walks();
   rotations();
   no_numbers_in_a_prefix();
   rows_of_no_token();

@@ -650,3 +650,32 @@ def test_shared_masked_numbers_count_for_nothing(G, hd, sinks, keys, value, at):
     sees = [row for row in range(s.n) if row not in blind]
     if not keys and sees:
         assert not bool(out[sees].view(len(sees), G, hd)[:, :, 5].isfinite().any())
+
+
+@pytest.mark.parametrize("odd", [False, True])
+@pytest.mark.parametrize("window,sinks", [(0, 0), (2500, 70)])
+@pytest.mark.parametrize("hd,page", [(64, 64), (128, 256)])
+@pytest.mark.parametrize("new,old", [(70, 3000), (300, 4500), (70, 9000)])
+def test_attention_long_prompts_in_one_part(new, old, hd, page, window, sinks, odd):
+    """As a large max_new has it: more steps than the 32 whose pages are looked up at once;
+    walked twice where a value that some queries do not see is no number."""
+    log(f"long prompts {new} {old} {hd} {window} {odd}")
+    s = Setup([(new, old), (1, 2300), (65, 2100)], page, 1, hd, new, stale=float("nan"))
+    if odd:
+        _set(s, 1, 0, [old + new // 2], [3], float("nan"))
+        _set(s, 1, 0, [old - 2470], [4], float("inf"))
+    _attend_check(s, s.rows(1), max_new=1 << 20, window=window, sinks=sinks)
+
+
+@pytest.mark.parametrize("window,sinks", [(0, 0), (2700, 70)])
+@pytest.mark.parametrize("hd", [64, 128])
+def test_shared_long_prefix_in_one_part(hd, window, sinks):
+    """128 heads by two tiles of columns fill the chip, so the prefix is one part of 40 steps; beside
+    float64 for some of the heads."""
+    s = Setup([(150, 2560), (151, 2600)], 64, 128, hd, 3, shared=2560)
+    q = s.rows(128)
+    out = _attend(s, q, shared=2560, window=window, sinks=sinks)
+    heads = [0, 77, 127]
+    want, tol, token = R.attention(_np(q[:, heads]), *(R.in_pool(_np(x[:, heads]), bool(i)) for i, x in enumerate(s.cache)), s.batch, s.max_new,
+                                   window=window, sinks=sinks)
+    assert token.all() and (abs(_np(out).reshape(s.n, 128, hd)[:, heads] - want) <= tol).all()
