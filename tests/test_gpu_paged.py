@@ -679,3 +679,20 @@ def test_shared_long_prefix_in_one_part(hd, window, sinks):
     want, tol, token = R.attention(_np(q[:, heads]), *(R.in_pool(_np(x[:, heads]), bool(i)) for i, x in enumerate(s.cache)), s.batch, s.max_new,
                                    window=window, sinks=sinks)
     assert token.all() and (abs(_np(out).reshape(s.n, 128, hd)[:, heads] - want) <= tol).all()
+
+
+@pytest.mark.parametrize("value", [float("nan"), float("inf"), float("-inf")])
+@pytest.mark.parametrize("keys", [False, True])
+@pytest.mark.parametrize("hd", [64, 128])
+def test_attention_a_row_between_masked_numbers(hd, keys, value):
+    """Of three new tokens the first sees a number that is none before the others' windows, the last
+    one at its own place; the second, in the same wave, is as without them, to the bit."""
+    torch = _torch()
+    s = Setup([(3, 100), (1, 60)], 32, 2, hd, 3)
+    q = s.rows(4)
+    clean = _attend_check(s, q, window=90)
+    _set(s, 0 if keys else 1, 0, [11, 102], [6], value)
+    out = _attend_check(s, q, window=90)
+    assert torch.equal(out[[1, 3]], clean[[1, 3]])
+    if not keys:
+        assert not bool(out[[0, 2]].view(2, 4, hd)[:, :, 6].isfinite().any())
