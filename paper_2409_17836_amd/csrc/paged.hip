@@ -433,9 +433,10 @@ __device__ inline void add_masked_values(Value value, const bf16x8 (&pf)[NT], f3
 // Sums of values near bf16's largest pass float32 where their mean does not.  So the
 // columns whose results are no numbers the second time either get a third one, with
 // their references kLift above the largest score: 2^24 probabilities of 2^8 / 2^kLift
-// each are less than one.  Joins weigh parts against kJoinLift above the largest
-// reference, for up to 128 parts of large sums.
-constexpr float kLift = 34.f, kJoinLift = 8.f;
+// each are less than one.  Joins weigh their large sums, of four waves or up to 128
+// parts, against kWaveLift or kJoinLift above the largest reference (little enough for
+// bf16's smallest normal values to keep 11 bits).
+constexpr float kLift = 34.f, kWaveLift = 3.f, kJoinLift = 8.f;
 
 // Zeros for the queries of columns that are no token's, which may hold anything: no
 // number there would have the wave do all its columns again.
@@ -683,7 +684,7 @@ __global__ __launch_bounds__(kWaves * 64, NT > 1 ? 2 : HD == 64 ? 4 : 3) void at
     float M = sm[0][oc];
 #pragma unroll
     for (int w = 1; w < NW; w++) M = fmaxf(M, sm[w][oc]);
-    M += kJoinLift;
+    M += kWaveLift;
     float L = 0.f;
     f32xd acc = {};
 #pragma unroll

@@ -23,6 +23,7 @@ struct Attention {
   std::vector<int> starts;
   std::vector<float> q, kv[2];  // [n, Hq, hd]; [B, most page, Hkv, hd]
   static constexpr float scale = 0.125f;
+  double absolute = 1e-37;  // what a result may be off by whatever it is
   Attention(const Problem& p, int seed) : p(p), B((int)p.T.size()), most(0), Hq(p.Hkv * p.G), starts{0} {
     for (int b = 0; b < B; b++) {
       starts.push_back(starts[b] + p.T[b]);
@@ -110,7 +111,7 @@ struct Attention {
             }
             dev += fabs(w);
             const double g = bf16_to_f32(got[((size_t)row * Hq + h) * p.hd + d]);
-            const double tol = (0x1p-8 + 0x1p-22 + 0x1p-24 * (p.hd + 8) * size) * dev * (1 + 0x1p-6) + 0x1p-8 * fabs(w) + 1e-37;
+            const double tol = (0x1p-8 + 0x1p-22 + 0x1p-24 * (p.hd + 8) * size) * dev * (1 + 0x1p-6) + 0x1p-8 * fabs(w) + absolute;
             if (g != g ? w == w : std::isfinite(w) ? !(fabs(g - w) <= tol) : g != w) {
               printf("%s %d, row %d head %d dim %d: %g, not %g\n", what, id, row, h, d, g, w);
               exit(1);
@@ -319,7 +320,26 @@ static void long_walks() {
       }
 }
 
+// Values of bf16's smallest normal exponents keep their digits through every join.
+static void small_values() {
+  const std::vector<Problem> problems = {
+      {64, 32, 1, 1, 0, 0, 0, 1, {1}, {40}, 0},                // one part of few columns
+      {128, 32, 1, 2, 0, 0, 0, 1, {1}, {1500}, 0},             // three
+      {128, 32, 1, 4, 0, 0, 0, 20, {20}, {1100}, 0},           // three of many
+      {64, 32, 1, 1, 0, 0, 640, 2, {1, 2}, {700, 650}, 0},     // a prefix, few columns
+      {64, 32, 1, 8, 0, 0, 640, 20, {20, 18}, {700, 650}, 1},  // many
+  };
+  int id = 0;
+  for (const Problem& p : problems) {
+    Attention a(p, id);
+    for (float& e : a.kv[1]) e = (1 + fminf(fabsf(e), 2)) * 0x1p-126f;
+    a.absolute = 0;
+    a.compare("small values", id++);
+  }
+}
+
 int main() {
+  small_values();
   long_walks();
   rotations();
   no_numbers_in_a_prefix();

@@ -696,3 +696,18 @@ def test_attention_a_row_between_masked_numbers(hd, keys, value):
     assert torch.equal(out[[1, 3]], clean[[1, 3]])
     if not keys:
         assert not bool(out[[0, 2]].view(2, 4, hd)[:, :, 6].isfinite().any())
+
+
+@pytest.mark.parametrize("seqs,G,hd,shared", [([(1, 1500)], 2, 128, 0), ([(20, 1100), (1, 5000)], 4, 128, 0), ([(1, 700), (2, 650)], 1, 64, 640),
+                                              ([(20, 700), (18, 650)], 8, 64, 640)])
+def test_attention_small_values_keep_their_digits(seqs, G, hd, shared):
+    """Values 2^115 times smaller give results as much smaller, to a step of bf16."""
+    torch = _torch()
+    s = Setup(seqs, 64, 1, hd, 3, shared=shared)
+    q = s.rows(G)
+    s.cache[1].copy_((1 + s.cache[1].float().abs().clamp(max=2)).to(torch.bfloat16))
+    whole = _attend(s, q, shared=shared)
+    s.cache[1].mul_(2.0 ** -115)
+    small = _attend(s, q, shared=shared)
+    # half a step of bf16 (2^-8) each; float32 sums weighted 2^-11 of values past 2^-115 keep 2^-20
+    assert (abs(small.double() * 2.0 ** 115 - whole.double()) <= 2.0 ** -7 * whole.double()).all()
