@@ -669,7 +669,9 @@ enum { LMGC_ROPE_HALF = 0, LMGC_ROPE_INTERLEAVED = 1 };
  * longer than the `orig` tokens of training: not at all; f / factor; theta
  * factor^(rot / (rot - 2)) in theta's place (NTK-aware, rot >= 4); or by parts
  * (YaRN, arXiv 2309.00071): with r = orig f / 2 pi turns and keep = clamp((r -
- * slow) / (fast - slow), 0, 1), f keep + f / factor (1 - keep). */
+ * slow) / (fast - slow), 0, 1), f keep + f / factor (1 - keep).  (Where keep is a
+ * ramp over i between rounded ends, as some checkpoints have it, the frequencies are
+ * the caller's: lmgc_op_rope_table takes any.) */
 enum { LMGC_ROPE_PLAIN = 0, LMGC_ROPE_LINEAR = 1, LMGC_ROPE_NTK = 2, LMGC_ROPE_YARN = 3 };
 /* freqs: host, rot / 2 numbers.  rot even, in [2, 512].  Host.  Errors: EINVAL. */
 int lmgc_rope_frequencies(double theta, int32_t rot, int32_t scaling, double factor, double orig,
@@ -709,7 +711,7 @@ int lmgc_op_rope(const void* d_x, int32_t dtype, int64_t n, int32_t heads, int32
  * read when the call runs.  Left out, and left as they were: rows that belong to
  * no sequence, rows that pass max_pages page tokens, sequences whose rows are
  * not within [0, n) or whose length is not within [0, max_pages page), and the
- * tokens of pages outside [0, n_pages).  Sequences may have pages in common as
+ * keys and values of pages outside [0, n_pages).  Sequences may have pages in common as
  * long as no call appends to them.
  *
  * Appending stores k and v (dtype, rows of Hkv hd numbers, ldk and ldv apart) as
@@ -750,8 +752,8 @@ int lmgc_op_paged_append(const void* d_k, const void* d_v, int32_t dtype, int64_
  * values and divided by the sum of the rounded ones; scores, maxima and sums are
  * float32, where a sum of finite values never passes its range but a score may (and is
  * infinite then).  A query's result depends on its own sequence (length and number of
- * new tokens), max_new, Hq and Hkv, not on the other sequences; with shared > 0
- * on n and B, too, which say how the shared part is split.
+ * new tokens), max_new, Hq and Hkv, not on the other sequences nor on max_pages; with
+ * shared > 0 on n and B, too, which say how the shared part is split.
  * GPU, async.  Errors: EINVAL, ESIZE, EUNSUPPORTED (hd, page, more than 2^32
  * threads in a dimension of a launch).
  */

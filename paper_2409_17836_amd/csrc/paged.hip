@@ -99,9 +99,10 @@ __device__ inline int64_t group_at(const Ragged& r, int page, int Hkv, int h, in
 // group, 16 bytes a lane; values meet in LDS, whose 16-byte slots are permuted so
 // that the 64 halves of a store fall on all banks.
 //
-// It is bound by memory: 4 x 4096 rows of 32 and 8 heads of 128, bf16, 790 MB, take
-// 159 us (4.97 TB/s; a copy 5.15).  With 4 places of 16 tokens to a wave, so half
-// lines to a load, it was 180, with the heads in the grid's slower dimension 206,
+// It is bound by memory: 4 x 4096 rows of 32 and 32 heads of 128, bf16, 790 MB, take
+// 158 us (5.0 TB/s; a copy 5.15), without the queries 105.  Number by number (not FAST)
+// 786, and 644 where rot is 100.  With 4 places of 16 tokens to a wave, so half lines
+// to a load, it was 180, with the heads in the grid's slower dimension 206,
 // with non-temporal loads 207.
 template <class T>
 struct Eight;  // 8 dims of a row
@@ -577,8 +578,8 @@ struct Columns {
 // scores of its column and tokens 16 i + 4 g + r of a group, an online softmax,
 // O^T += V^T P^T.  The waves' parts meet in LDS.
 //
-// For single tokens it is bound by the cache's bytes: 8 sequences of 4095, 32 heads of
-// 128, 537 MB, in 88 us (6.1 TB/s), and 5 for the join.  Twelve waves a CU, each
+// For single tokens it is bound by the cache's bytes: 8 sequences of up to 4095, 32 heads
+// of 128, 520 MB, in 91 us (5.7 TB/s), and 5 for the join; of 64, 260 MB, 52 in all.  Twelve waves a CU, each
 // with a group of 16 KB under way, hide the loads' way; parts of 64 KB a wave keep
 // what is left for the join small.
 constexpr int kWaves = 4;
@@ -1106,13 +1107,10 @@ __global__ __launch_bounds__(512, 2) void attn_paged_prompt_kernel(
   }
 }
 
-// Joins the parts of a row and head: a wave each, first a lane per part (its
-// weight), then HD / 64 dims to a lane.
-//
-// ROWS: all rows; else the columns of sequences with few of them, where the others
-// are in one part.  A lane has 4 dims of a row and takes the parts 8 at a time, whose
-// statistics and numbers are asked for together.  14400 rows of 64 dims in 5 parts
-// take 6.9 us (with a wave to a row 13.5), mostly the way to a row's sequence and back.
+// Joins the parts of a row and head: HD / 4 lanes each, 4 dims to a lane, which takes
+// the parts 8 at a time with a running maximum.  ROWS: all rows; else the columns of
+// sequences with few of them, where the others are in one part.  A step's statistics and numbers are asked for together.  14400 rows of 64 dims in 5 parts
+// take 6.6 us (with a wave to a row 13.5), mostly the way to a row's sequence and back.
 template <int HD, bool ROWS>
 __global__ __launch_bounds__(256) void attn_paged_join_kernel(Ragged r, int max_new, int Hkv, int G, AttnPlan plan, Mask mask,
                                                               uint16_t* __restrict__ out) {

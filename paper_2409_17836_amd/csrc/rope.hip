@@ -20,8 +20,9 @@ typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 // at position 2^17 a float32 angle is off by 2^-7.  A thread has kPositions
 // positions of a frequency, from a multiple of kPositions on: it turns the first
 // one's (cos, sin) by the frequency, in float64, for the next ones.  A step adds
-// two roundings, so the last is off by 2^-49, of float32's 2^-24.
-// 131072 positions of 64 frequencies, 67 MB, take 12.5 us (5.35 TB/s), bound by the
+// two roundings, 2^-49 to the last of a run; the angle p f itself is rounded, 2^-53 of it
+// (2^-36 at 2^17 and 2^-29 at 2^24 radians, of float32's 2^-24).
+// 131072 positions of 64 frequencies, 67 MB, take 12.7 us (5.3 TB/s), bound by the
 // stores; 31 with a sine and a cosine for each.
 struct Freqs {
   double f[kMaxRot / 2];
@@ -53,7 +54,8 @@ __global__ __launch_bounds__(256) void rope_table_kernel(Freqs freqs, int half, 
 // 16 bytes of a row to a run; a thread has the two runs of as many pairs, of
 // the same place in kHeads heads, so a pair's cos and sin are read once for them.
 // Bound by memory: 8191 rows of 36 heads of 64, float32, 151 MB, take 35.6 us (4.27
-// TB/s; a copy 5.15); 37.4 with one head's loads at a time.
+// TB/s; a copy 5.15); 37.4 with one head's loads at a time.  16384 rows of 64 heads of
+// 128, bf16, take 96 us; number by number (not FAST) 211, and 298 where rot is 100.
 template <class T>
 struct Run;
 template <>
