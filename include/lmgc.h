@@ -736,7 +736,7 @@ int lmgc_op_paged_append(const void* d_k, const void* d_v, int32_t dtype, int64_
  * scale q.k) v over keys j <= position and, if window > 0, j > position - window
  * or j < sinks.  Query head h reads key/value head h Hkv / Hq.
  *   d_q: bf16, rows of Hq hd numbers ldq apart, 16-byte aligned; d_out: bf16 [n,
- *   Hq hd].  scale > 0 (1 / sqrt(hd), as a rule).
+ *   Hq hd].  scale in (0, 2^127] (1 / sqrt(hd), as a rule).
  *   max_new: no sequence has more new tokens (rows behind that are left out).
  *   shared: the first `shared` tokens of all sequences are the same, and each
  *   sequence's pages say so (by pages in common, or by copies); they are read

@@ -212,7 +212,7 @@ int lmgc_op_attention_paged(const uint16_t* d_q, int64_t ldq, int32_t n, int32_t
   if ((rc = check_cache(cache, r))) return rc;
   if (max_new < 1 || max_new > kMaxTokens) return set_error(LMGC_EINVAL, "max_new must be in [1, 2^24]");
   if (window < 0 || sinks < 0 || shared < 0) return set_error(LMGC_EINVAL, "window, sinks and shared must be >= 0");
-  if (!(scale > 0) || !isfinite(scale)) return set_error(LMGC_EINVAL, "scale must be positive");
+  if (!(scale > 0) || !isfinite(scores_scale(scale))) return set_error(LMGC_EINVAL, "scale must be positive and log2(e) of it finite");
   const int64_t eq = extent(n, (int64_t)Hq * hd, ldq, "ldq");
   if (eq < 0) return (int)eq;
   if (n == 0) return LMGC_OK;

@@ -57,6 +57,8 @@ struct PagedAttnArgs {
   void* ws;
   Ragged r;
 };
+// Of scores in powers of two.
+inline float scores_scale(float scale) { return (float)(1.4426950408889634 * (double)scale); }
 int64_t paged_workspace_bytes(int n, int B, int Hq, int Hkv, int hd, int max_new, int tokens, int shared);
 // Workgroups of the largest launch in one dimension (other launches have heads and
 // sequences in two of their own).

@@ -1322,7 +1322,7 @@ hipError_t launch_attention_paged(const PagedAttnArgs& a, hipStream_t s) {
   const int G = a.Hq / a.Hkv;
   const Mask mask{a.window, a.sinks};
   const AttnPlan plan = plan_of(r.n, r.B, a.Hq, a.Hkv, a.hd, a.max_new, r.max_pages * r.page, a.shared, mask, a.ws, nullptr);
-  const float sl2 = (float)(1.4426950408889634 * (double)a.scale);
+  const float sl2 = scores_scale(a.scale);
   auto go = [&](auto h) {
     constexpr int HD = decltype(h)::value;
     auto split = [&](auto prefix, auto nt, int64_t blocks, int seqs) {

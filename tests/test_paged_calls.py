@@ -154,6 +154,12 @@ def test_attention_counts_only_what_it_launches():
     assert _attention(**rows) == EUNSUPPORTED and _attention(**rows, window=64) == ESIZE
 
 
+def test_attention_scale_in_powers_of_two():
+    """log2(e) times the scale, which scores are multiplied by, has to be a number too."""
+    assert _attention(scale=3e38) == EINVAL
+    assert _attention(scale=2.3e38, most=128, page=256, ws=None) == ESIZE  # (as far as the workspace)
+
+
 def test_attention_of_no_rows_is_fine():
     assert _attention(n=0, q=None, out=None, ws=None, bytes=0) == 0
 
